@@ -490,6 +490,84 @@ GAS_API gas_status gas_sgd_step_clipped(void* W, int64_t n, gas_dtype dt, const 
                                 void* stream);
 
 /*
+ * The norms before and after a block of a residual model, with the block's gate and residual scale and the residual stream, in
+ * one pass over the rows (a block: aggregation and transform):
+ *     y = N_post(A[i]) * p + p_bias,   g = sigmoid(T[i]),
+ *     H[i] = h = X[i] + alpha * s * g * y,   U[i] = N_pre(h) * q + q_bias,
+ * H the stream behind the block, U the next block's input.  N of a row z of F values:
+ *     GAS_NORM_NONE z,  GAS_NORM_RMS z / sqrt(mean(z^2) + eps),  GAS_NORM_LAYER (z - mean) / sqrt(mean((z - mean)^2) + eps).
+ * Everything is computed in fp32 and rounded once; U is formed from h before that is rounded.
+ * X, A, H, U: [n_rows, F] of type dt.  A: the block's output; NULL: no block, h = X (the norm of a model's first layer).  T: gate
+ * logits of type dt, [n_rows, F] (gate_cols = F) or one of a row, [n_rows, 1] (gate_cols = 1); NULL: g = 1.  p, p_bias, s, q,
+ * q_bias: fp32[F]; NULL: 1 for a gain or s, 0 for a bias.  H or U may be NULL.  stats: optional fp32[n_rows, 4], what the backward
+ * call needs: mean and 1 / deviation of the row of A, and of h (0 and 1 where a norm has none); 16-byte aligned.
+ * push_idx, push_hist: optional Push, U[i] also to push_hist[push_idx[i]] (int32, distinct; U may be NULL then).
+ * H and U may each be X, A or a full T itself (same address and row stride); other overlaps of outputs are refused.
+ * A row's infinity or NaN stays in its row; squares that leave fp32's range count as infinity.
+ *
+ * gas_residual_norm_bwd, from the gradients GH at H (of the stream; NULL: none) and GU at U (NULL: none): with hn, an the normed rows,
+ *     d = GU * q,   GX = e = GH + r_h (d - [mean d] - hn mean(d hn)),      r = 1 / deviation, [.] for a layer norm only
+ *     dy = e alpha s g,  c = dy p,   GA = r_a (c - [mean c] - an mean(c an)),   GT = dy y (1 - g) (one gate of a row: the row's sum),
+ *     gp = sum dy an, gp_bias = sum dy, gs = sum e alpha g y, gq = sum GU hn, gq_bias = sum GU     over the rows, fp32[F].
+ * H as stored and stats as written by the forward call.  Any output may be NULL; GX may be GH, GA may be A, and so on, as above;
+ * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace: gas_residual_norm_bwd_workspace(n_rows, F) bytes
+ * from a multiple of 16 on.
+ */
+typedef enum { GAS_NORM_NONE = 0, GAS_NORM_RMS = 1, GAS_NORM_LAYER = 2 } gas_norm_kind;
+GAS_API gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t lda, const void* T, int64_t ldt,
+                         int32_t gate_cols, int64_t n_rows, int32_t F, gas_dtype dt, int32_t norm_post, const float* p,
+                         const float* p_bias, const float* s, float alpha, int32_t norm_pre, const float* q, const float* q_bias,
+                         float eps, void* H, int64_t ldh, void* U, int64_t ldu, float* stats, const int32_t* push_idx,
+                         void* push_hist, int64_t n_hist_rows, int64_t ld_push, void* stream);
+GAS_API int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F);
+GAS_API gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, int64_t ldgu, const void* H, int64_t ldh,
+                         const void* A, int64_t lda, const void* T, int64_t ldt, int32_t gate_cols, const float* stats,
+                         int64_t n_rows, int32_t F, gas_dtype dt, int32_t norm_post, const float* p, const float* p_bias,
+                         const float* s, float alpha, int32_t norm_pre, const float* q, void* GX, int64_t ldgx, void* GA, int64_t ldga,
+                         void* GT, int64_t ldgt, float* gp, float* gp_bias, float* gs, float* gq, float* gq_bias, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/*
+ * The squared norm of many tensors: out[0] = sum of x[i][j]^2 over all of them (fp64 accumulation in a fixed order, one fp32
+ * result), x, n: host arrays of `count`.  steps: optional device counter, goes up by one if the result is neither an infinity nor
+ * a NaN: the number of the step that gas_adamw_steps then takes.  workspace: gas_sq_norms_workspace(count, n) bytes from a
+ * multiple of 8 on.
+ */
+GAS_API int64_t gas_sq_norms_workspace(int32_t count, const int64_t* n);
+GAS_API gas_status gas_sq_norms(int32_t count, const float* const* x, const int64_t* n, float* out, int32_t* steps, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+
+/*
+ * AdamW with decoupled weight decay on `count` tensors, which share launches:
+ *     g = c dW,  m <- beta1 m + rate1 g,  v <- beta2 v + rate2 g^2,  beta = 1 - rate,
+ *     W <- W - lr wd W - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
+ * The rates are what is passed: 1 - 0.999 from a float has lost five of its digits.
+ * W, dtypes (a gas_dtype each), n, dW, weight_decay (NULL: none): host arrays of `count`; W[i], dW[i] (fp32): n[i] contiguous
+ * elements.  Tensors that share memory are updated in order; a gradient must not overlap a tensor of the call.
+ * t: `step` >= 1, or, if `steps` is given, what it holds on the device (so a captured step counts on).  c = 1, or with sq_norm (fp32[1],
+ * device: the squared norm of all gradients, gas_sq_norms) min(1, max_norm / (sqrt(sq_norm) + 1e-6)), max_norm > 0, possibly
+ * infinite; if sq_norm is an infinity or a NaN, the call changes nothing.
+ * State: the tensors' elements one tensor after another, each from a multiple of 256 on: gas_adamw_elements(count, n) elements in
+ * all, state_elements of them are there.  Zeros to begin with.
+ *   state_bits 32: m, v fp32.
+ *   state_bits 8:  m int8, v uint8, scales fp32[elements / 256, 2], s_m and s_v of every 256 elements, which are the largest
+ *                  magnitudes there: m stands for s_m k |k| / 127^2, v for s_v (k / 255)^4.  Values between two codes go to one of
+ *                  them at random with the value as expectation, by the step's number and the element's place, so results are
+ *                  the same from run to run; a v > 0 is never 0.  256 elements with an infinity or a NaN read as NaN from then on.
+ * master (optional, fp32 in the state's layout): the values of the GAS_BF16 tensors, which are updated in its place; W is set to them,
+ * rounded.  Without it bf16 tensors are read, updated in fp32 and rounded to nearest.  The places of GAS_F32 tensors are not used.
+ *
+ * gas_adamw_unpack: the values that states of 8 bits stand for, n elements (a multiple of 256) as type dt.
+ */
+GAS_API int64_t gas_adamw_elements(int32_t count, const int64_t* n);
+GAS_API gas_status gas_adamw_steps(int32_t count, void* const* W, const int32_t* dtypes, const int64_t* n, const float* const* dW, void* m,
+                         void* v, float* scales, float* master, int64_t state_elements, int32_t state_bits, float lr, float rate1,
+                         float rate2, float eps, const float* weight_decay, int64_t step, const int32_t* steps, const float* sq_norm,
+                         float max_norm, void* stream);
+GAS_API gas_status gas_adamw_unpack(const void* m, const void* v, const float* scales, int64_t n, gas_dtype dt, void* m_out, void* v_out,
+                         void* stream);
+
+/*
  * PNA's neighbourhood aggregation (operator appendix): for every row v of the
  * batch subgraph, in one pass over the gathered rows,
  *     agg_0 = mean, agg_1 = min, agg_2 = max  over X[col[k], 0:F], k in row v,

@@ -8,4 +8,6 @@ from .binding import (  # noqa: F401
     gas_spmm_linear_layers, gas_spmm_t_relu_linear_layers,
     gas_relu_bwd, gas_linear_bwd_input, gas_linear_bwd_input_add, gas_linear_bwd_weight, gas_linear_bwd_weight_workspace, gas_linear_bwd_weight_static, gas_linear_bwd_weights,
     gas_softmax_xent, gas_sgd_step, gas_sgd_steps, gas_sq_norm, gas_sgd_step_clipped, gas_axpy, gas_row_distance, gas_row_distance_bwd, gas_row_dot,
-    gas_pna_aggregate, gas_gat_aggregate, gas_pna_aggregate_bwd, gas_gat_aggregate_bwd)
+    gas_pna_aggregate, gas_gat_aggregate, gas_pna_aggregate_bwd, gas_gat_aggregate_bwd,
+    NORM_NONE, NORM_RMS, NORM_LAYER, gas_residual_norm, gas_residual_norm_bwd, gas_residual_norm_bwd_workspace,
+    gas_sq_norms, gas_adamw_elements, gas_adamw_steps, gas_adamw_unpack)

@@ -2,6 +2,7 @@
 argument marshalling only.  Tensors are torch tensors on the GPU; every step
 runs in the library's kernels on torch's current stream.  The calls of a pass go
 through csrc/marshal.cpp, the others through ctypes."""
+import array
 import ctypes as C
 import os
 import warnings
@@ -29,9 +30,13 @@ EXPORTS = [
     "gas_gat_aggregate_bwd_heads", "gas_pna_aggregate_bwd_workspace", "gas_gat_aggregate_bwd_workspace",
     "gas_gat_aggregate_bwd_heads_workspace", "gas_linear_in_order", "gas_gat_aggregate_push", "gas_pna_aggregate_own", "gas_pna_aggregate_bwd_bounded",
     "gas_gat_aggregate_bwd_bounded",
+    "gas_residual_norm", "gas_residual_norm_bwd", "gas_residual_norm_bwd_workspace", "gas_sq_norms", "gas_sq_norms_workspace",
+    "gas_adamw_elements", "gas_adamw_steps", "gas_adamw_unpack",
     "gas_disk_open", "gas_disk_close", "gas_disk_pull", "gas_disk_push", "gas_disk_wait", "gas_disk_read_rows",
     "gas_disk_write_rows", "gas_disk_sync",
 ]
+
+_COUNTS = ("_workspace", "_elements")        # calls that return a number, no status
 
 _lib = None
 
@@ -60,8 +65,10 @@ def lib():
         L.gas_pna_aggregate_bwd_workspace.restype = C.c_int64
         L.gas_gat_aggregate_bwd_workspace.restype = C.c_int64
         L.gas_gat_aggregate_bwd_heads_workspace.restype = C.c_int64
+        for name in ("gas_residual_norm_bwd_workspace", "gas_sq_norms_workspace", "gas_adamw_elements"):
+            getattr(L, name).restype = C.c_int64
         for name in EXPORTS:
-            if name not in ("gas_last_error", "gas_version", "gas_plan_destroy") and not name.endswith("_workspace"):
+            if name not in ("gas_last_error", "gas_version", "gas_plan_destroy") and not name.endswith(_COUNTS):
                 getattr(L, name).restype = C.c_int
         _lib = L
     return _lib
@@ -94,6 +101,9 @@ _SIGNATURES = dict(
     gas_row_dot="pqpqqiippp", gas_row_distance_bwd="pqpqqiifpqp", gas_disk_open="pqiiiiqp", gas_disk_close="p",
     gas_disk_pull="ppqqpqpp", gas_disk_push="ppqqpqpp", gas_disk_wait="pq", gas_disk_read_rows="ppqqpq",
     gas_disk_write_rows="ppqqpq", gas_disk_sync="p",
+    gas_residual_norm="pqpqpqiqiiipppfippfpqpqpppqqp", gas_residual_norm_bwd_workspace="qi",
+    gas_residual_norm_bwd="pqpqpqpqpqipqiiipppfippqpqpqppppppqp", gas_sq_norms="ipppppqp", gas_sq_norms_workspace="ip",
+    gas_adamw_elements="ip", gas_adamw_steps="ippppppppqiffffpqppfp", gas_adamw_unpack="pppqippp",
 )
 
 
@@ -126,20 +136,21 @@ class _Calls:
     any ctypes objects, as before."""
 
     def __init__(self):
-        global _mat, _size, _ptr
+        global _mat, _size, _ptr, _tensors
         lib()
         native = _marshalling()
         if native is None:
-            _mat, _size, _ptr = _mat_any, _size_any, _ptr_any
+            _mat, _size, _ptr, _tensors = _mat_any, _size_any, _ptr_any, _tensors_any
         else:
             native.set_slow(_mat_any, _size_any, _ptr_any)
             _mat, _size, _ptr = native.mat, native.size, native.ptr
+            _tensors = lambda ts: native.tensors(ts) or _tensors_any(ts)
         raw = C.CDLL(LIB_PATH)
         types = dict(p=C.c_void_p, q=C.c_int64, i=C.c_int32, f=C.c_float)
         for name, sig in _SIGNATURES.items():
             fn = getattr(raw, name)
             fn.argtypes = [types[c] for c in sig]
-            fn.restype = C.c_int64 if name.endswith("_workspace") else C.c_int
+            fn.restype = C.c_int64 if name.endswith(_COUNTS) else C.c_int
             setattr(self, name, _by_ctypes(fn) if native is None else getattr(native, name, fn))
 
 
@@ -192,7 +203,15 @@ def _ptr_any(t, dtype=None):
     return t.data_ptr()
 
 
-_mat, _size, _ptr = _mat_any, _size_any, _ptr_any        # until the library is loaded (_Calls)
+def _tensors_any(ts):
+    """Of a list of contiguous tensors of the feature types, as host arrays in bytes: addresses (int64), elements (int64) and dtype codes (int32)."""
+    for t in ts:
+        _dt(t)
+    return tuple(array.array(c, v).tobytes() for c, v in (("Q", [_ptr_any(t) for t in ts]), ("q", [t.numel() for t in ts]),
+                                                          ("i", [_dt(t) for t in ts])))
+
+
+_mat, _size, _ptr, _tensors = _mat_any, _size_any, _ptr_any, _tensors_any        # until the library is loaded (_Calls)
 _NONE = (0, 0, 0, 0, None)                               # _size of an argument that is not given
 
 
@@ -714,6 +733,134 @@ def gas_sgd_step_clipped(w, dw, lr, sq_norms, max_norm, weight_decay=0.0):
     _check(_calls().gas_sgd_step_clipped(_ptr(w), w.numel(), _dt(w), _ptr(dw, torch.float32),
                                       lr, weight_decay, _ptr(sq_norms, torch.float32),
                                       sq_norms.numel(), max_norm, _stream()))
+
+
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+
+
+def _vector(v, width, what):
+    """Address of a float32 vector of `width`, 0 for None."""
+    if v is None:
+        return 0
+    if v.numel() != width:
+        raise ValueError(f"{what}: a vector of {v.numel()} for rows of {width}")
+    return _ptr(v, torch.float32)
+
+
+def gas_residual_norm(x, h=None, u=None, a=None, t=None, post=NORM_NONE, p=None, p_bias=None, s=None, alpha=1.0, pre=NORM_NONE, q=None,
+                      q_bias=None, eps=1e-5, stats=None, idx=None, hist=None):
+    """h = x + alpha * s * sigmoid(t) * (N_post(a) * p + p_bias) and u = N_pre(h) * q + q_bias, either of them or both; x, a, h, u: [n, F],
+    t: [n, F] or [n, 1], vectors float32 [F].  stats: float32 [n, 4], kept for the backward call.  idx, hist: u[i] also to hist[idx[i]]."""
+    xp, ldx, n, width, dt = _size(x)
+    rows = (n, width, dt)
+    ap, lda, *like_a = (0, 0, *rows) if a is None else _size(a)
+    hp, ldh, *like_h = (0, 0, *rows) if h is None else _size(h)
+    up, ldu, *like_u = (0, 0, *rows) if u is None else _size(u)
+    tp, ldt, nt, gates, dtt = (0, 0, n, 0, dt) if t is None else _size(t)
+    gp, ldg, n_hist, fg, dtg = (0, 0, 0, width, dt) if hist is None else _size(hist)
+    if not (tuple(like_a) == tuple(like_h) == tuple(like_u) == rows) or nt != n or dtt != dt or dtg != dt or fg != width or \
+            (hist is None) != (idx is None) or (idx is not None and idx.numel() != n) or (stats is not None and stats.shape != (n, 4)):
+        raise ValueError("gas_residual_norm: shapes or dtypes do not match")
+    vec = lambda v: _vector(v, width, "gas_residual_norm")
+    _check(_calls().gas_residual_norm(
+        xp, ldx, ap, lda, tp, ldt, gates, n, width, dt, post, vec(p), vec(p_bias), vec(s), alpha, pre, vec(q), vec(q_bias), eps,
+        hp, ldh, up, ldu, _ptr(stats, torch.float32), _ptr(idx, torch.int32), gp, n_hist, ldg, _stream()))
+
+
+def gas_residual_norm_bwd(gh, gu, h, stats, gx=None, ga=None, gt=None, a=None, t=None, post=NORM_NONE, p=None, p_bias=None, s=None, alpha=1.0,
+                          pre=NORM_NONE, q=None, gp=None, gp_bias=None, gs=None, gq=None, gq_bias=None, workspace=None):
+    """Backward of gas_residual_norm: gh, gu: gradients at h and u (None: none there); h and stats as the forward call left them.  gx, ga, gt:
+    [n, F] (gt as t), gp, gp_bias, gs, gq, gq_bias: float32 [F], each optional.  workspace: a uint8 tensor of at least
+    gas_residual_norm_bwd_workspace(n, F) bytes, allocated here if not given."""
+    like = next((m for m in (gh, gu, gx, ga) if m is not None), None)
+    if like is None:
+        raise ValueError("gas_residual_norm_bwd: no gradient is given")
+    _, _, n, width, dt = _size(like)
+    mats = []
+    for m in (gh, gu, h, a, gx, ga):
+        if m is None:
+            mats.append((0, 0))
+            continue
+        mp, ld, rows, cols, dtm = _size(m)
+        if rows != n or cols != width or dtm != dt:
+            raise ValueError("gas_residual_norm_bwd: shapes or dtypes do not match")
+        mats.append((mp, ld))
+    (ghp, ldgh), (gup, ldgu), (hp, ldh), (ap, lda), (gxp, ldgx), (gap, ldga) = mats
+    tp, ldt, nt, gates, dtt = (0, 0, n, 0, dt) if t is None else _size(t)
+    gtp, ldgt, ngt, fgt, dtgt = (0, 0, n, gates, dt) if gt is None else _size(gt)
+    if nt != n or dtt != dt or ngt != n or fgt != gates or dtgt != dt or (stats is not None and stats.shape != (n, 4)):
+        raise ValueError("gas_residual_norm_bwd: shapes or dtypes do not match")
+    if workspace is None:
+        workspace = torch.empty(_calls().gas_residual_norm_bwd_workspace(n, width), dtype=torch.uint8, device=like.device)
+    vec = lambda v: _vector(v, width, "gas_residual_norm_bwd")
+    _check(_calls().gas_residual_norm_bwd(
+        ghp, ldgh, gup, ldgu, hp, ldh, ap, lda, tp, ldt, gates, _ptr(stats, torch.float32), n, width, dt, post, vec(p), vec(p_bias), vec(s),
+        alpha, pre, vec(q), gxp, ldgx, gap, ldga, gtp, ldgt, vec(gp), vec(gp_bias), vec(gs), vec(gq), vec(gq_bias), _ptr(workspace),
+        workspace.numel() * workspace.element_size(), _stream()))
+
+
+def gas_residual_norm_bwd_workspace(n_rows, width) -> int:
+    return int(_calls().gas_residual_norm_bwd_workspace(n_rows, width))
+
+
+def gas_sq_norms(xs, out, steps=None, workspace=None):
+    """out[0] = sum of the squares of every tensor of a list (float32, contiguous).  steps: int32 counter on the device, goes up by one if
+    the sum is finite.  workspace: a uint8 tensor, allocated here if not given."""
+    calls = _calls()
+    n = len(xs)
+    ptrs, sizes, codes = _tensors(xs)
+    if any(codes):
+        raise TypeError("gas_sq_norms: tensors of float32")
+    if out.numel() < 1 or (steps is not None and steps.numel() < 1):
+        raise ValueError("gas_sq_norms: no place for the result")
+    need = calls.gas_sq_norms_workspace(n, sizes)
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=out.device)
+    _check(calls.gas_sq_norms(n, ptrs, sizes, _ptr(out, torch.float32), _ptr(steps, torch.int32), _ptr(workspace),
+                              workspace.numel() * workspace.element_size(), _stream()))
+
+
+def gas_adamw_elements(sizes) -> int:
+    """Elements of the state of tensors of these sizes: every one begins at a multiple of 256."""
+    return int(_calls().gas_adamw_elements(len(sizes), array.array("q", sizes).tobytes()))
+
+
+def gas_adamw_steps(ws, dws, m, v, lr, step=0, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, scales=None, master=None, steps=None,
+                    sq_norm=None, max_norm=float("inf")):
+    """One AdamW step of every tensor of `ws` (float32 or bfloat16) with the gradients `dws` (float32), in place.  m, v: the state, zeros
+    to begin with, of gas_adamw_elements(sizes) elements: float32, or int8 and uint8 with scales (float32, one pair for 256 elements).
+    master: float32 values of the bfloat16 tensors, in the state's layout.  step: the step's number, from 1 on, or steps: an int32
+    counter on the device that holds it.  weight_decay: a number, or one for each tensor.  sq_norm: the gradients' squared norm
+    (gas_sq_norms), which clips them to max_norm and, if it is not finite, leaves everything as it is."""
+    n, calls = len(ws), _calls()
+    ptrs, sizes, codes = _tensors(ws)
+    grads, grad_sizes, grad_codes = _tensors(dws)
+    if grad_sizes != sizes or any(grad_codes):
+        raise ValueError("gas_adamw_steps: gradients of the tensors' sizes, float32")
+    bits = 32 if m.dtype == torch.float32 else 8
+    room = m.numel()
+    if v.numel() != room or (master is not None and master.numel() != room) or (scales is None) != (bits == 32) or \
+            (scales is not None and scales.numel() < 2 * (room // 256)) or (sq_norm is not None and sq_norm.numel() < 1):
+        raise ValueError("gas_adamw_steps: the parts of the state do not match")
+    if isinstance(weight_decay, (int, float)):
+        decay = (array.array("f", [weight_decay]) * n).tobytes()
+    else:
+        decay = array.array("f", weight_decay).tobytes()
+        if len(decay) != 4 * n:
+            raise ValueError("gas_adamw_steps: one weight decay for each tensor")
+    _check(calls.gas_adamw_steps(
+        n, ptrs, codes, sizes, grads, _ptr(m, torch.float32 if bits == 32 else torch.int8), _ptr(v, torch.float32 if bits == 32 else torch.uint8),
+        _ptr(scales, torch.float32), _ptr(master, torch.float32), room, bits, lr, 1.0 - beta1, 1.0 - beta2, eps, decay, step, _ptr(steps, torch.int32),
+        _ptr(sq_norm, torch.float32), max_norm, _stream()))
+
+
+def gas_adamw_unpack(m, v, scales, m_out, v_out):
+    """The values that states of 8 bits stand for, as float32 or bfloat16."""
+    n = m.numel()
+    if v.numel() != n or m_out.numel() != n or v_out.numel() != n or scales.numel() < 2 * (n // 256) or m_out.dtype != v_out.dtype:
+        raise ValueError("gas_adamw_unpack: shapes or dtypes do not match")
+    _check(_calls().gas_adamw_unpack(_ptr(m, torch.int8), _ptr(v, torch.uint8), _ptr(scales, torch.float32), n, _dt(m_out), _ptr(m_out),
+                                     _ptr(v_out), _stream()))
 
 
 ANY_LENGTH = 0x7FFFFFFF          # of rows and columns: nothing is known

@@ -9,6 +9,7 @@
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstring>
 #include <tuple>
 #include <utility>
 
@@ -90,6 +91,44 @@ PyObject* ptr(PyObject*, PyObject* const* args, Py_ssize_t n) {
     return PyObject_Vectorcall(slow_ptr, args, n, nullptr);
 }
 
+// tensors(list): addresses, elements (int64 each) and dtype codes (int32) of contiguous tensors of the feature types, as bytes; None
+// if any of them is something else, which the Python function decides about
+PyObject* tensors(PyObject*, PyObject* o) {
+    PyObject* list = PySequence_Fast(o, "a list of tensors");
+    if (!list) return nullptr;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    PyObject* at = PyBytes_FromStringAndSize(nullptr, n * 8);
+    PyObject* count = PyBytes_FromStringAndSize(nullptr, n * 8);
+    PyObject* code = PyBytes_FromStringAndSize(nullptr, n * 4);
+    bool ok = at && count && code;
+    Py_ssize_t i = 0;
+    try {
+        for (; ok && i < n; ++i) {
+            const at::Tensor* t = plain(PySequence_Fast_GET_ITEM(list, i));
+            const at::ScalarType s = t ? t->scalar_type() : at::kDouble;
+            if (!t || (s != at::kFloat && s != at::kBFloat16) || !t->is_contiguous()) break;
+            const int64_t address = (int64_t)(uintptr_t)t->data_ptr(), elements = t->numel();
+            const int32_t c = s == at::kFloat ? GAS_F32 : GAS_BF16;
+            memcpy(PyBytes_AS_STRING(at) + 8 * i, &address, 8);
+            memcpy(PyBytes_AS_STRING(count) + 8 * i, &elements, 8);
+            memcpy(PyBytes_AS_STRING(code) + 4 * i, &c, 4);
+        }
+    } catch (...) {
+    }
+    Py_DECREF(list);
+    PyObject* out = nullptr;
+    if (ok && i == n) {
+        out = PyTuple_Pack(3, at, count, code);
+    } else if (ok) {
+        Py_INCREF(Py_None);
+        out = Py_None;
+    }
+    Py_XDECREF(at);
+    Py_XDECREF(count);
+    Py_XDECREF(code);
+    return out;
+}
+
 // ---- calls
 // A pointer argument: an address, None, a ctypes array (its memory) or a ctypes pointer (its value).
 bool get(PyObject* o, uintptr_t* out) {
@@ -169,6 +208,7 @@ PyMethodDef methods[] = {
     {"mat", mat, METH_O, nullptr},
     {"size", size, METH_O, nullptr},
     {"ptr", (PyCFunction)(void (*)())ptr, METH_FASTCALL, nullptr},
+    {"tensors", tensors, METH_O, nullptr},
     {"set_slow", set_slow, METH_VARARGS, nullptr},
     GAS_CALL(gas_pull), GAS_CALL(gas_push), GAS_CALL(gas_pull_host), GAS_CALL(gas_push_host), GAS_CALL(gas_gcn_norm),
     GAS_CALL(gas_spmm), GAS_CALL(gas_spmm_hist), GAS_CALL(gas_spmm_table), GAS_CALL(gas_fuse_sources), GAS_CALL(gas_spmm_t),
@@ -181,6 +221,8 @@ PyMethodDef methods[] = {
     GAS_CALL(gas_pna_aggregate_own), GAS_CALL(gas_pna_aggregate_bwd_bounded), GAS_CALL(gas_pna_aggregate_bwd_workspace),
     GAS_CALL(gas_pna_groups), GAS_CALL(gas_pna_groups_workspace), GAS_CALL(gas_pna_linear), GAS_CALL(gas_pna_linear_workspace),
     GAS_CALL(gas_pna_linear_bwd_input), GAS_CALL(gas_pna_linear_bwd_weight), GAS_CALL(gas_pna_linear_bwd_weight_workspace),
+    GAS_CALL(gas_residual_norm), GAS_CALL(gas_residual_norm_bwd), GAS_CALL(gas_residual_norm_bwd_workspace), GAS_CALL(gas_sq_norms),
+    GAS_CALL(gas_sq_norms_workspace), GAS_CALL(gas_adamw_elements), GAS_CALL(gas_adamw_steps), GAS_CALL(gas_adamw_unpack),
     GAS_CALL(gas_gat_aggregate_push), GAS_CALL(gas_gat_aggregate_bwd_bounded), GAS_CALL(gas_gat_aggregate_bwd_heads_workspace),
     {nullptr, nullptr, 0, nullptr}};
 
