@@ -1,6 +1,8 @@
 // Norms before and after a block, with the block's gate, its residual scale and the residual stream, forward and backward:
 //     y = N_post(a) p + p_bias,   h = x + alpha s sigmoid(t) y,   u = N_pre(h) q + q_bias.
 // One wavefront per row, element by element; statistics, sums and the row itself in 32 bits, each output rounded once.
+#include <type_traits>
+
 #include "common.h"
 #include "wave.h"
 
@@ -80,6 +82,238 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm c) {
         if (c.H) store_one<BF>(c.H, row * c.ldh + f, h);
         if (c.U) store_one<BF>(c.U, row * c.ldu + f, u);
         if (c.hist) store_one<BF>(c.hist, to * c.ld_hist + f, u);
+    }
+}
+
+// ---- rows in registers
+// Sum over aligned groups of G lanes, in every lane of the group, in the same order everywhere: data-parallel moves within 16 lanes,
+// swaps of rows of 16 and of halves beyond.  Through LDS (shuffles) a step takes some 60 cycles, this way some 8.
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));            // quad_perm 1 0 3 2
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));            // quad_perm 2 3 0 1
+    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));           // row_half_mirror
+    if constexpr (G >= 16) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, true));   // row_mirror
+    if constexpr (G >= 32) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return v;
+}
+// The same over the lanes with the same place in their groups of G: what the groups of a wavefront have between them.
+template <int G>
+__device__ __forceinline__ float across_groups(float v) {
+    if constexpr (G <= 8) v += other_half(v);
+    if constexpr (G <= 16) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    if constexpr (G <= 32) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    return v;
+}
+
+// How a row lies in the lanes: W = 1: in a team of G lanes, 64 / G rows to a wavefront, four wavefronts to a workgroup; W > 1: in the W
+// wavefronts of a workgroup (G = 64).  A lane has P pieces of 16 bytes.  MASK: F is no multiple of a piece; the last piece is the
+// row's last 16 bytes then, and what of them the piece before has already is left out of the sums (both store the same values there).
+template <bool BF, int G, int W, int P, bool MASK>
+struct RowLanes {
+    static constexpr int E = Elems<BF>::E, EB = BF ? 2 : 4;
+    static constexpr int kThreads = W == 1 ? 256 : W * 64;
+    static constexpr int kRows = W == 1 ? 4 * (64 / G) : 1;           // of a workgroup at a time
+    static_assert(W == 1 || G == 64, "several wavefronts have all of their lanes");
+    int place, c[P], skip[P];            // place in the row's lanes; a piece's first element, and its elements that another piece has
+    bool on[P];
+    __device__ __forceinline__ RowLanes(int F) {
+        place = W == 1 ? threadIdx.x % G : threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            c[i] = (place + i * G * W) * E;
+            on[i] = c[i] < F;
+            skip[i] = 0;
+            if constexpr (MASK)
+                if (on[i] && c[i] + E > F) {
+                    skip[i] = c[i] + E - F;
+                    c[i] = F - E;
+                }
+        }
+    }
+    // the row that this thread's lanes take in the workgroup's turn that begins with `base`
+    static __device__ __forceinline__ int64_t row(int64_t base) { return W == 1 ? base + threadIdx.x / G : base; }
+    // 16 bytes of any alignment: the same load
+    __device__ __forceinline__ void load(const char* m, int64_t ld, int64_t r, bool live, u32x4 (&v)[P]) const {
+        typedef u32x4 piece __attribute__((aligned(2)));
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            v[i] = u32x4{0u, 0u, 0u, 0u};
+            if (live && on[i]) v[i] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(m + (r * ld + c[i]) * EB));
+        }
+    }
+    __device__ __forceinline__ void store(char* m, int64_t ld, int64_t r, const u32x4 (&v)[P]) const {
+        typedef u32x4 piece __attribute__((aligned(2)));
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + (r * ld + c[i]) * EB));
+    }
+    __device__ __forceinline__ void vector(const float* v, float otherwise, float (&x)[P][E]) const {
+        typedef f32x4 piece __attribute__((aligned(4)));
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                f32x4 w = {otherwise, otherwise, otherwise, otherwise};
+                if (v && on[i]) w = *reinterpret_cast<const piece*>(v + c[i] + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[i][e + j] = w[j];
+            }
+    }
+    // the sum of x over the row's elements of this lane
+    __device__ __forceinline__ float own(const float (&x)[P][E]) const {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) part += MASK && e < skip[i] ? 0.f : x[i][e];
+            sum += on[i] ? part : 0.f;
+        }
+        return sum;
+    }
+    __device__ __forceinline__ float own_dot(const float (&x)[P][E], const float (&y)[P][E]) const {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) part = fmaf(MASK && e < skip[i] ? 0.f : x[i][e], y[i][e], part);
+            sum += on[i] ? part : 0.f;
+        }
+        return sum;
+    }
+};
+
+// N sums over a row at once.  Several wavefronts hand their sums over in LDS, in two places by turns, so one barrier is enough: who writes
+// a place again has passed the barrier behind its last reading.
+template <int G, int W, int N>
+__device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[3][16], int& turn) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = group_sum<G>(v[k]);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) red[turn][k][threadIdx.x >> 6] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float sum = red[turn][k][0];
+#pragma unroll
+            for (int w = 1; w < W; ++w) sum += red[turn][k][w];
+            v[k] = sum;
+        }
+        turn ^= 1;
+    }
+}
+__device__ __forceinline__ float fast_gate(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269504f)); }
+
+// z becomes what it is beyond its mean; returns 1 / deviation.
+template <class L, int G, int W, int P, int E>
+__device__ __forceinline__ float centre(const L& lanes, int kind, int F, float eps, float (&z)[P][E], float* mean, float (*red)[3][16], int& turn) {
+    *mean = 0.f;
+    if (kind == GAS_NORM_NONE) return 1.f;
+    float sum[1];
+    if (kind == GAS_NORM_LAYER) {
+        sum[0] = lanes.own(z);
+        row_sums<G, W>(sum, red, turn);
+        *mean = sum[0] / (float)F;
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) z[i][e] -= *mean;
+    }
+    sum[0] = lanes.own_dot(z, z);
+    row_sums<G, W>(sum, red, turn);
+    return rsqrtf(sum[0] / (float)F + eps);
+}
+
+// One pass over the rows: the next row of a team is on its way while this one is worked on.
+template <bool BF, int G, int W, int P, bool MASK>
+__global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void residual_norm_rows_kernel(ResidualNorm c) {
+    using L = RowLanes<BF, G, W, P, MASK>;
+    constexpr int E = L::E;
+    __shared__ float red[2][3][16];
+    int turn = 0;
+    const L lanes(c.F);
+    const int64_t step = (int64_t)gridDim.x * L::kRows;
+    int64_t base = (int64_t)blockIdx.x * L::kRows + (W == 1 ? (threadIdx.x >> 6) * (64 / G) : 0);      // the wavefront's first row
+    const int64_t team = W == 1 ? (threadIdx.x & 63) / G : 0;
+    u32x4 x[P], a[P], t[P];
+    float t1 = 0.f;
+    int32_t to = 0;
+#pragma unroll
+    for (int i = 0; i < P; ++i) x[i] = a[i] = t[i] = u32x4{0u, 0u, 0u, 0u};
+    auto fetch = [&](int64_t row) {
+        const bool live = row < c.n;
+        lanes.load(c.X, c.ldx, row, live, x);
+        if (c.A) lanes.load(c.A, c.lda, row, live, a);
+        if (c.gate_cols > 1) lanes.load(c.T, c.ldt, row, live, t);
+        if (c.gate_cols == 1 && live) t1 = load_one<BF>(c.T, row * c.ldt);
+        if (c.hist && live) to = c.idx[row];
+    };
+    fetch(base + team);
+    float p[P][E], p_bias[P][E], s[P][E], q[P][E], q_bias[P][E];
+    lanes.vector(c.p, 1.f, p);
+    lanes.vector(c.p_bias, 0.f, p_bias);
+    lanes.vector(c.s, 1.f, s);
+    lanes.vector(c.q, 1.f, q);
+    lanes.vector(c.q_bias, 0.f, q_bias);
+    const bool normed = c.U || c.hist || c.stats;
+    for (; base < c.n; base += step) {
+        const int64_t row = base + team;
+        float h[P][E], y[P][E], g[P][E];
+        const float gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
+        const int64_t place = to;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            unpack<BF>(x[i], h[i]);
+            unpack<BF>(a[i], y[i]);
+            unpack<BF>(t[i], g[i]);
+        }
+        if (base + step < c.n) fetch(row + step);
+        float mean_a = 0.f, r_a = 1.f, mean_h, r_h;
+        if (c.A) {
+            r_a = centre<L, G, W>(lanes, c.post, c.F, c.eps, y, &mean_a, red, turn);
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float k = c.alpha * s[i][e] * (c.gate_cols > 1 ? fast_gate(g[i][e]) : gate);
+                    h[i][e] = fmaf(k, fmaf(y[i][e] * r_a, p[i][e], p_bias[i][e]), h[i][e]);
+                }
+        }
+        u32x4 out[P];
+        if (c.H && row < c.n) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[i] = pack<BF>(h[i]);
+            lanes.store(c.H, c.ldh, row, out);
+        }
+        if (!normed) continue;
+        r_h = centre<L, G, W>(lanes, c.pre, c.F, c.eps, h, &mean_h, red, turn);
+        if (row >= c.n) continue;
+        if (c.stats && lanes.place == 0) reinterpret_cast<f32x4*>(c.stats)[row] = f32x4{mean_a, r_a, mean_h, r_h};
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) h[i][e] = fmaf(h[i][e] * r_h, q[i][e], q_bias[i][e]);
+            out[i] = pack<BF>(h[i]);
+        }
+        if (c.U) lanes.store(c.U, c.ldu, row, out);
+        if (c.hist) lanes.store(c.hist, c.ld_hist, place, out);
     }
 }
 
@@ -178,12 +412,177 @@ __global__ __launch_bounds__(256) void residual_norm_columns_kernel(ResidualNorm
             c.partials[((int64_t)blockIdx.y * 5 + k) * c.F + f] = (part[0][k][lane] + part[1][k][lane]) + (part[2][k][lane] + part[3][k][lane]);
 }
 
-__global__ __launch_bounds__(64) void residual_norm_finish_kernel(ResidualNormBwd c) {
-    const int f = blockIdx.x * 64 + threadIdx.x, k = blockIdx.y;
-    if (f >= c.F || !c.sums[k]) return;
+// The backward pass with the row in registers: every matrix is read once and written once, and a lane keeps the sums of its columns
+// over all rows that it takes.
+template <bool BF, int G, int W, int P, bool MASK>
+__global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void residual_norm_bwd_rows_kernel(ResidualNormBwd c) {
+    using L = RowLanes<BF, G, W, P, MASK>;
+    constexpr int E = L::E;
+    __shared__ float red[2][3][16];
+    __shared__ float columns[W == 1 ? 4 : 1][W == 1 ? G * P * E : 1];
+    int turn = 0;
+    const L lanes(c.F);
+    const int64_t step = (int64_t)gridDim.x * L::kRows;
+    int64_t base = (int64_t)blockIdx.x * L::kRows + (W == 1 ? (threadIdx.x >> 6) * (64 / G) : 0);
+    const int64_t team = W == 1 ? (threadIdx.x & 63) / G : 0;
+    u32x4 gh[P], gu[P], h[P], a[P], t[P];
+    f32x4 st;
+    float t1;
+#pragma unroll
+    for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = a[i] = t[i] = u32x4{0u, 0u, 0u, 0u};
+    auto fetch = [&](int64_t row) {
+        const bool live = row < c.n;
+        if (c.GH) lanes.load(c.GH, c.ldgh, row, live, gh);
+        if (c.GU) {
+            lanes.load(c.GU, c.ldgu, row, live, gu);
+            lanes.load(c.H, c.ldh, row, live, h);
+        }
+        if (c.A) lanes.load(c.A, c.lda, row, live, a);
+        if (c.gate_cols > 1) lanes.load(c.T, c.ldt, row, live, t);
+        t1 = c.gate_cols == 1 && live ? load_one<BF>(c.T, row * c.ldt) : 0.f;
+        st = !live ? f32x4{0.f, 0.f, 0.f, 0.f} : c.stats ? reinterpret_cast<const f32x4*>(c.stats)[row] : f32x4{0.f, 1.f, 0.f, 1.f};
+    };
+    fetch(base + team);
+    float p[P][E], p_bias[P][E], s[P][E], q[P][E];
+    lanes.vector(c.p, 1.f, p);
+    lanes.vector(c.p_bias, 0.f, p_bias);
+    lanes.vector(c.s, 1.f, s);
+    lanes.vector(c.q, 1.f, q);
+    float sum[5][P][E];
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[k][i][e] = 0.f;
+    const float inv_f = 1.f / (float)c.F;
+    for (; base < c.n; base += step) {
+        const int64_t row = base + team;
+        const float mean_a = st[0], r_a = st[1], mean_h = st[2], r_h = st[3];
+        const float gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
+        float e_[P][E], hn[P][E], d[P][E], an[P][E], g[P][E];
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            unpack<BF>(gh[i], e_[i]);
+            unpack<BF>(gu[i], d[i]);
+            unpack<BF>(h[i], hn[i]);
+            unpack<BF>(a[i], an[i]);
+            unpack<BF>(t[i], g[i]);
+        }
+        if (base + step < c.n) fetch(row + step);
+        if (c.GU) {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    hn[i][e] = (hn[i][e] - mean_h) * r_h;
+                    sum[3][i][e] = fmaf(d[i][e], hn[i][e], sum[3][i][e]);
+                    sum[4][i][e] += d[i][e];
+                    d[i][e] *= q[i][e];
+                }
+            float m[2] = {0.f, 0.f};
+            if (c.pre != GAS_NORM_NONE) {
+                m[0] = lanes.own(d);
+                m[1] = lanes.own_dot(d, hn);
+                row_sums<G, W>(m, red, turn);
+                m[0] = c.pre == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
+                m[1] *= inv_f;
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) e_[i][e] = fmaf(r_h, d[i][e] - m[0] - hn[i][e] * m[1], e_[i][e]);
+        }
+        u32x4 out[P];
+        if (c.GX && row < c.n) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[i] = pack<BF>(e_[i]);
+            lanes.store(c.GX, c.ldgx, row, out);
+        }
+        if (!c.A) continue;
+        // from here on: e_ the gradient at the gated branch before s, then c = dy p; hn the gate's gradient; d what is left of y
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                an[i][e] = (an[i][e] - mean_a) * r_a;
+                const float y = fmaf(an[i][e], p[i][e], p_bias[i][e]), ge = c.gate_cols > 1 ? fast_gate(g[i][e]) : gate;
+                const float branch = e_[i][e] * (c.alpha * ge), dy = branch * s[i][e];
+                sum[0][i][e] = fmaf(dy, an[i][e], sum[0][i][e]);
+                sum[1][i][e] += dy;
+                sum[2][i][e] = fmaf(branch, y, sum[2][i][e]);
+                hn[i][e] = dy * y * (1.f - ge);
+                d[i][e] = dy * p[i][e];
+            }
+        float m[3] = {0.f, 0.f, 0.f};
+        if (c.post != GAS_NORM_NONE || c.gate_cols == 1) {
+            m[0] = lanes.own(d);
+            m[1] = lanes.own_dot(d, an);
+            if (c.gate_cols == 1) m[2] = lanes.own(hn);
+            row_sums<G, W>(m, red, turn);
+            m[0] = c.post == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
+            m[1] = c.post != GAS_NORM_NONE ? m[1] * inv_f : 0.f;
+        }
+        if (row >= c.n) continue;
+        if (c.GA) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[i][e] = r_a * (d[i][e] - m[0] - an[i][e] * m[1]);
+                out[i] = pack<BF>(d[i]);
+            }
+            lanes.store(c.GA, c.ldga, row, out);
+        }
+        if (c.GT && c.gate_cols == 1 && lanes.place == 0) store_one<BF>(c.GT, row * c.ldgt, m[2]);
+        if (c.GT && c.gate_cols > 1) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) out[i] = pack<BF>(hn[i]);
+            lanes.store(c.GT, c.ldgt, row, out);
+        }
+    }
+    // the workgroup's sums: across the teams of a wavefront by moves, across its wavefronts in LDS
+    float* to = c.partials + (int64_t)blockIdx.x * 5 * c.F;
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+        if (!c.sums[k]) continue;
+        if constexpr (W > 1) {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+                if (lanes.on[i])
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (!MASK || e >= lanes.skip[i]) to[(int64_t)k * c.F + lanes.c[i] + e] = sum[k][i][e];
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float v = across_groups<G>(sum[k][i][e]);
+                    if ((threadIdx.x & 63) < G && lanes.on[i] && (!MASK || e >= lanes.skip[i])) columns[threadIdx.x >> 6][lanes.c[i] + e] = v;
+                }
+            __syncthreads();
+            for (int f = threadIdx.x; f < c.F; f += 256)
+                to[(int64_t)k * c.F + f] = (columns[0][f] + columns[1][f]) + (columns[2][f] + columns[3][f]);
+            __syncthreads();
+        }
+    }
+}
+
+// Sums over the workgroups' sums: 16 columns to a workgroup, 64 of the partial rows side by side, added up in order.
+__global__ __launch_bounds__(1024) void residual_norm_finish_kernel(ResidualNormBwd c) {
+    __shared__ float part[64][17];
+    const int k = blockIdx.y, column = threadIdx.x & 15, slot = threadIdx.x >> 4, f = blockIdx.x * 16 + column;
+    if (!c.sums[k]) return;
     float sum = 0.f;
-    for (int j = 0; j < c.slabs; ++j) sum += c.partials[((int64_t)j * 5 + k) * c.F + f];
-    c.sums[k][f] = sum;
+    if (f < c.F)
+        for (int j = slot; j < c.slabs; j += 64) sum += c.partials[((int64_t)j * 5 + k) * c.F + f];
+    part[slot][column] = sum;
+    __syncthreads();
+    for (int o = 32; o > 0; o >>= 1) {
+        if (slot < o) part[slot][column] += part[slot + o][column];
+        __syncthreads();
+    }
+    if (slot == 0 && f < c.F) c.sums[k][f] = part[0][column];
 }
 
 template <bool BF>
@@ -216,6 +615,47 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
 }
 
 constexpr int kSlabs = 256;
+constexpr int64_t kWaves = 4096;                     // of a launch that goes over its rows in turns: 16 on a compute unit
+
+// How rows of F elements lie in lanes (RowLanes); W = 0: too narrow or too wide for registers, element by element.
+struct Layout { int g, w, p; };
+inline Layout layout_of(int F, bool bf) {
+    const int e = bf ? 8 : 4, pieces = (F + e - 1) / e;
+    if (F < e || pieces > 2048) return {0, 0, 0};
+    if (pieces <= 64) return {pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64, 1, 1};
+    if (pieces > 1024) return {64, 16, 2};
+    int w = 2;
+    while (w * 64 < pieces) w *= 2;
+    return {64, w, 1};
+}
+inline int64_t row_blocks(const Layout& l, int64_t n) {
+    const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, most = kWaves / (l.w == 1 ? 4 : l.w), all = (n + rows - 1) / rows;
+    return all < most ? all : most;
+}
+
+template <bool BF, bool MASK, class C>
+void launch_rows(const Layout& l, dim3 grid, hipStream_t s, const C& c) {
+    constexpr bool kBwd = std::is_same_v<C, ResidualNormBwd>;
+#define GAS_ROWS(G, W, P)                                                                                                             \
+    if (l.g == G && l.w == W && l.p == P) {                                                                                           \
+        const dim3 block(W == 1 ? 256 : W * 64);                                                                                      \
+        if constexpr (kBwd) hipLaunchKernelGGL((residual_norm_bwd_rows_kernel<BF, G, W, P, MASK>), grid, block, 0, s, c);             \
+        else hipLaunchKernelGGL((residual_norm_rows_kernel<BF, G, W, P, MASK>), grid, block, 0, s, c);                                \
+        return;                                                                                                                       \
+    }
+    GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 1) GAS_ROWS(64, 2, 1) GAS_ROWS(64, 4, 1) GAS_ROWS(64, 8, 1)
+    GAS_ROWS(64, 16, 1) GAS_ROWS(64, 16, 2)
+#undef GAS_ROWS
+}
+template <class C>
+void launch_rows(const Layout& l, bool bf, int64_t n, hipStream_t s, const C& c) {
+    const dim3 grid((unsigned)row_blocks(l, n));
+    const bool mask = c.F % (bf ? 8 : 4) != 0;
+    if (bf && mask) launch_rows<true, true>(l, grid, s, c);
+    else if (bf) launch_rows<true, false>(l, grid, s, c);
+    else if (mask) launch_rows<false, true>(l, grid, s, c);
+    else launch_rows<false, false>(l, grid, s, c);
+}
 
 inline bool valid_norm(int k) { return k == GAS_NORM_NONE || k == GAS_NORM_RMS || k == GAS_NORM_LAYER; }
 
@@ -249,6 +689,7 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
     GAS_REQUIRE(X && (H || U || push_hist), "%s: null pointer", who);
     GAS_REQUIRE(valid_norm(norm_post) && valid_norm(norm_pre), "%s: unknown norm %d, %d", who, norm_post, norm_pre);
     GAS_REQUIRE(eps > 0.f && eps < INFINITY, "%s: eps=%g", who, (double)eps);
+    GAS_REQUIRE(!stats || aligned16(stats), "%s: the statistics are not aligned to 16 bytes", who);
     GAS_REQUIRE(A || !T, "%s: a gate without a block", who);
     GAS_REQUIRE(!T || gate_cols == 1 || gate_cols == F, "%s: %d gates for rows of %d", who, gate_cols, F);
     GAS_REQUIRE(ldx >= F && (!A || lda >= F) && (!T || ldt >= gate_cols) && (!H || ldh >= F) && (!U || ldu >= F),
@@ -276,6 +717,12 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
     c.p = p; c.p_bias = p_bias; c.s = s; c.q = q; c.q_bias = q_bias; c.alpha = alpha; c.eps = eps;
     c.H = static_cast<char*>(H); c.U = static_cast<char*>(U); c.ldh = ldh; c.ldu = ldu; c.stats = stats;
     c.idx = push_idx; c.hist = static_cast<char*>(push_hist); c.ld_hist = ld_push;
+    const Layout l = layout_of(F, dt == GAS_BF16);
+    if (l.w) {
+        launch_rows(l, dt == GAS_BF16, n_rows, (hipStream_t)stream, c);
+        GAS_CHECK_HIP(hipGetLastError());
+        return GAS_OK;
+    }
     const int64_t blocks = (n_rows + 3) / 4;
     GAS_REQUIRE(blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
     if (dt == GAS_BF16) hipLaunchKernelGGL(residual_norm_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, c);
@@ -286,7 +733,13 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
 
 int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F) {
     if (n_rows <= 0 || F <= 0) return 0;
-    return ((int64_t)kSlabs * 5 * F + 2 * n_rows) * 4;
+    int64_t most = 0;                         // of both types
+    for (int bf = 0; bf < 2; ++bf) {
+        const Layout l = layout_of(F, bf);
+        const int64_t floats = l.w ? row_blocks(l, n_rows) * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
+        most = floats > most ? floats : most;
+    }
+    return most * 4;
 }
 
 gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, int64_t ldgu, const void* H, int64_t ldh, const void* A,
@@ -303,10 +756,10 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     ResidualNormBwd c;
     c.sums[0] = gp; c.sums[1] = gp_bias; c.sums[2] = gs; c.sums[3] = gq; c.sums[4] = gq_bias;
     c.F = F; c.n = n_rows; c.slabs = 0; c.partials = nullptr;
-    const dim3 finish((unsigned)((F + 63) / 64), 5);
+    const dim3 finish((unsigned)((F + 15) / 16), 5);
     if (n_rows == 0) {                        // an empty sum still has to be written
         if (!sums) return GAS_OK;
-        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(64), 0, st, c);
+        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
         GAS_CHECK_HIP(hipGetLastError());
         return GAS_OK;
     }
@@ -318,6 +771,7 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     GAS_REQUIRE(!GU || H, "%s: the gradient of the normed rows without the rows", who);
     GAS_REQUIRE(GX || GA || GT || sums, "%s: null pointer", who);
     GAS_REQUIRE(stats || ((!GU || norm_pre == GAS_NORM_NONE) && (!A || norm_post == GAS_NORM_NONE)), "%s: norms without statistics", who);
+    GAS_REQUIRE(!stats || aligned16(stats), "%s: the statistics are not aligned to 16 bytes", who);
     GAS_REQUIRE(!T || gate_cols == 1 || gate_cols == F, "%s: %d gates for rows of %d", who, gate_cols, F);
     GAS_REQUIRE((!GH || ldgh >= F) && (!GU || (ldgu >= F && ldh >= F)) && (!A || lda >= F) && (!T || ldt >= gate_cols) && (!GX || ldgx >= F) &&
                 (!GA || ldga >= F) && (!GT || ldgt >= gate_cols), "%s: row stride smaller than the row", who);
@@ -341,6 +795,15 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     c.GX = static_cast<char*>(GX); c.GA = static_cast<char*>(GA); c.GT = static_cast<char*>(GT);
     c.ldgx = ldgx; c.ldga = ldga; c.ldgt = ldgt;
     c.partials = static_cast<float*>(workspace);
+    const Layout l = layout_of(F, dt == GAS_BF16);
+    if (l.w) {
+        c.slabs = (int)row_blocks(l, n_rows);
+        launch_rows(l, dt == GAS_BF16, n_rows, st, c);
+        GAS_CHECK_HIP(hipGetLastError());
+        if (sums) hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
+        GAS_CHECK_HIP(hipGetLastError());
+        return GAS_OK;
+    }
     c.row_sums = c.partials + (int64_t)kSlabs * 5 * F;
     c.rows_per_slab = (n_rows + kSlabs - 1) / kSlabs;
     c.slabs = (int)((n_rows + c.rows_per_slab - 1) / c.rows_per_slab);
@@ -353,7 +816,7 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
         hipLaunchKernelGGL(bf ? residual_norm_columns_kernel<true> : residual_norm_columns_kernel<false>,
                            dim3((unsigned)((F + 63) / 64), (unsigned)c.slabs), dim3(256), 0, st, c);
         GAS_CHECK_HIP(hipGetLastError());
-        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(64), 0, st, c);
+        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
         GAS_CHECK_HIP(hipGetLastError());
     }
     if (GX || GA || GT) {
