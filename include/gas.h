@@ -548,7 +548,7 @@ GAS_API gas_status gas_sq_norms(int32_t count, const float* const* x, const int6
  * device: the squared norm of all gradients, gas_sq_norms) min(1, max_norm / (sqrt(sq_norm) + 1e-6)), max_norm > 0, possibly
  * infinite; if sq_norm is an infinity or a NaN, the call changes nothing.
  * State: the tensors' elements one tensor after another, each from a multiple of 256 on: gas_adamw_elements(count, n) elements in
- * all, state_elements of them are there.  Zeros to begin with.
+ * all, state_elements of them are there.  Zeros to begin with; 16-byte aligned.
  *   state_bits 32: m, v fp32.
  *   state_bits 8:  m int8, v uint8, scales fp32[elements / 256, 2], s_m and s_v of every 256 elements, which are the largest
  *                  magnitudes there: m stands for s_m k |k| / 127^2, v for s_v (k / 255)^4.  Values between two codes go to one of

@@ -1,6 +1,8 @@
 // Norms before and after a block, with the block's gate, its residual scale and the residual stream, forward and backward:
 //     y = N_post(a) p + p_bias,   h = x + alpha s sigmoid(t) y,   u = N_pre(h) q + q_bias.
-// One wavefront per row, element by element; statistics, sums and the row itself in 32 bits, each output rounded once.
+// Statistics, sums and the row itself in 32 bits, each output rounded once.  Bound by memory: forward 3.1 M x 256 bf16 1.27 ms, 6.3 TB/s of
+// the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.94 ms, 5.2 TB/s of 4.9 GB.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -23,6 +25,7 @@ struct ResidualNorm {
     const int32_t* idx;
     char* hist;
     int64_t ld_hist;
+    int turns;                           // of a workgroup, RowLanes::kRows rows each
 };
 
 template <bool BF>
@@ -58,6 +61,8 @@ __device__ __forceinline__ void row_stats(int kind, int F, float eps, V value, f
     *r = 1.f / sqrtf(wave_sum(sq) / (float)F + eps);
 }
 
+// Rows that are narrower than a piece of 16 bytes or do not fit the registers: a wavefront to a row, element by element, read anew for every
+// sum.
 template <bool BF>
 __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm c) {
     const int lane = threadIdx.x & 63;
@@ -128,38 +133,44 @@ struct RowLanes {
     static constexpr int kThreads = W == 1 ? 256 : W * 64;
     static constexpr int kRows = W == 1 ? 4 * (64 / G) : 1;           // of a workgroup at a time
     static_assert(W == 1 || G == 64, "several wavefronts have all of their lanes");
-    int place, c[P], skip[P];            // place in the row's lanes; a piece's first element, and its elements that another piece has
-    bool on[P];
+    int place, team, c[P], skip[P];      // place in the row's lanes, row among the wavefront's; a piece's first element, and its elements that another piece has
+    bool on[P];                          // a lane behind the row's end loads its first piece and neither counts nor stores it
     __device__ __forceinline__ RowLanes(int F) {
         place = W == 1 ? threadIdx.x % G : threadIdx.x;
+        team = W == 1 ? (threadIdx.x & 63) / G : 0;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             c[i] = (place + i * G * W) * E;
             on[i] = c[i] < F;
             skip[i] = 0;
             if constexpr (MASK)
-                if (on[i] && c[i] + E > F) {
+                if (c[i] + E > F) {
                     skip[i] = c[i] + E - F;
                     c[i] = F - E;
                 }
+            if (!on[i]) c[i] = 0;
         }
     }
-    // the row that this thread's lanes take in the workgroup's turn that begins with `base`
-    static __device__ __forceinline__ int64_t row(int64_t base) { return W == 1 ? base + threadIdx.x / G : base; }
+    // the wavefront's first row: the same in all of its lanes, so addresses are a scalar's and a lane's 32 bits
+    static __device__ __forceinline__ int64_t first(int turns) {
+        return (int64_t)blockIdx.x * turns * kRows + (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / G) : 0);
+    }
+    __device__ __forceinline__ uint32_t offset(int64_t ld, int i) const { return (uint32_t)(team * (int)ld + c[i]) * EB; }
     // 16 bytes of any alignment: the same load
-    __device__ __forceinline__ void load(const char* m, int64_t ld, int64_t r, bool live, u32x4 (&v)[P]) const {
-        typedef u32x4 piece __attribute__((aligned(2)));
+    typedef u32x4 piece __attribute__((aligned(2)));
+    __device__ __forceinline__ void load(const char* m, int64_t ld, int64_t base, u32x4 (&v)[P]) const {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-            v[i] = u32x4{0u, 0u, 0u, 0u};
-            if (live && on[i]) v[i] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(m + (r * ld + c[i]) * EB));
-        }
+        for (int i = 0; i < P; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(m + base * ld * EB + offset(ld, i)));
     }
-    __device__ __forceinline__ void store(char* m, int64_t ld, int64_t r, const u32x4 (&v)[P]) const {
-        typedef u32x4 piece __attribute__((aligned(2)));
+    __device__ __forceinline__ void store(char* m, int64_t ld, int64_t base, const u32x4 (&v)[P]) const {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + (r * ld + c[i]) * EB));
+            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + base * ld * EB + offset(ld, i)));
+    }
+    __device__ __forceinline__ void store_at(char* m, int64_t ld, int64_t row, const u32x4 (&v)[P]) const {
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + (row * ld + c[i]) * EB));
     }
     __device__ __forceinline__ void vector(const float* v, float otherwise, float (&x)[P][E]) const {
         typedef f32x4 piece __attribute__((aligned(4)));
@@ -168,7 +179,7 @@ struct RowLanes {
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 f32x4 w = {otherwise, otherwise, otherwise, otherwise};
-                if (v && on[i]) w = *reinterpret_cast<const piece*>(v + c[i] + e);
+                if (v) w = *reinterpret_cast<const piece*>(v + c[i] + e);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[i][e + j] = w[j];
             }
@@ -195,6 +206,30 @@ struct RowLanes {
             sum += on[i] ? part : 0.f;
         }
         return sum;
+    }
+};
+
+// The vectors of a row's columns, N of them, for the pieces of a lane: in its registers, or, where a lane has several pieces, in LDS (PARKED), from
+// where they are read again for every row.
+template <class L, int N, int P, int E, bool PARKED>
+struct Vectors {
+    float held[PARKED ? 1 : N][PARKED ? 1 : P][E];
+    f32x4 (*parked)[64];                 // [N * P * E / 4][64]
+    __device__ __forceinline__ void set(const L& lanes, int k, const float* v, float otherwise) {
+        float x[P][E];
+        lanes.vector(v, otherwise, x);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if constexpr (!PARKED) held[k][i][e] = x[i][e];
+                else if (e % 4 == 0 && threadIdx.x < 64) parked[(k * P + i) * (E / 4) + e / 4][threadIdx.x] = f32x4{x[i][e], x[i][e + 1], x[i][e + 2], x[i][e + 3]};
+    }
+    __device__ __forceinline__ void get(int k, int i, float (&x)[E]) const {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if constexpr (!PARKED) x[e] = held[k][i][e];
+            else x[e] = parked[(k * P + i) * (E / 4) + e / 4][threadIdx.x & 63][e % 4];
     }
 };
 
@@ -241,42 +276,51 @@ __device__ __forceinline__ float centre(const L& lanes, int kind, int F, float e
     return rsqrtf(sum[0] / (float)F + eps);
 }
 
-// One pass over the rows: the next row of a team is on its way while this one is worked on.
-template <bool BF, int G, int W, int P, bool MASK>
+// One pass over the rows: the next row of a team is on its way while this one is worked on.  ALL: x, a, h and u are there and no push,
+// known beforehand.
+template <bool BF, int G, int W, int P, bool MASK, bool ALL>
 __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void residual_norm_rows_kernel(ResidualNorm c) {
     using L = RowLanes<BF, G, W, P, MASK>;
     constexpr int E = L::E;
     __shared__ float red[2][3][16];
     int turn = 0;
     const L lanes(c.F);
-    const int64_t step = (int64_t)gridDim.x * L::kRows;
-    int64_t base = (int64_t)blockIdx.x * L::kRows + (W == 1 ? (threadIdx.x >> 6) * (64 / G) : 0);      // the wavefront's first row
-    const int64_t team = W == 1 ? (threadIdx.x & 63) / G : 0;
+    const bool has_a = ALL || c.A, has_h = ALL || c.H, has_u = ALL || c.U, push = !ALL && c.hist;
+    const int64_t end = min(c.n, (int64_t)(blockIdx.x + 1) * c.turns * L::kRows);
+    int64_t base = L::first(c.turns);
     u32x4 x[P], a[P], t[P];
-    float t1 = 0.f;
+    float t1;
     int32_t to = 0;
+    auto fetch = [&](int64_t base) {
+        const int64_t row = base + lanes.team;
+        if (row < c.n) {
+            lanes.load(c.X, c.ldx, base, x);
+            if (has_a) lanes.load(c.A, c.lda, base, a);
+            if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
+            if (c.gate_cols == 1) t1 = load_one<BF>(c.T, row * c.ldt);
+            if (push) to = c.idx[row];
+        }
+    };
+    t1 = 0.f;
 #pragma unroll
     for (int i = 0; i < P; ++i) x[i] = a[i] = t[i] = u32x4{0u, 0u, 0u, 0u};
-    auto fetch = [&](int64_t row) {
-        const bool live = row < c.n;
-        lanes.load(c.X, c.ldx, row, live, x);
-        if (c.A) lanes.load(c.A, c.lda, row, live, a);
-        if (c.gate_cols > 1) lanes.load(c.T, c.ldt, row, live, t);
-        if (c.gate_cols == 1 && live) t1 = load_one<BF>(c.T, row * c.ldt);
-        if (c.hist && live) to = c.idx[row];
-    };
-    fetch(base + team);
-    float p[P][E], p_bias[P][E], s[P][E], q[P][E], q_bias[P][E];
-    lanes.vector(c.p, 1.f, p);
-    lanes.vector(c.p_bias, 0.f, p_bias);
-    lanes.vector(c.s, 1.f, s);
-    lanes.vector(c.q, 1.f, q);
-    lanes.vector(c.q_bias, 0.f, q_bias);
-    const bool normed = c.U || c.hist || c.stats;
-    for (; base < c.n; base += step) {
-        const int64_t row = base + team;
+    if (base < end) fetch(base);
+    constexpr bool kParked = W == 1 && P > 1;
+    __shared__ f32x4 parked[kParked ? 5 * P * E / 4 : 1][64];
+    Vectors<L, 5, P, E, kParked> vec;
+    vec.parked = parked;
+    vec.set(lanes, 0, c.p, 1.f);
+    vec.set(lanes, 1, c.p_bias, 0.f);
+    vec.set(lanes, 2, c.s, 1.f);
+    vec.set(lanes, 3, c.q, 1.f);
+    vec.set(lanes, 4, c.q_bias, 0.f);
+    if constexpr (kParked) __syncthreads();
+    const bool normed = has_u || push || c.stats;
+    for (; base < end; base += L::kRows) {
+        if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
+        const bool live = base + lanes.team < c.n;
         float h[P][E], y[P][E], g[P][E];
-        const float gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
+        const float gate = c.alpha * (c.gate_cols == 1 ? fast_gate(t1) : 1.f);
         const int64_t place = to;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -284,36 +328,52 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             unpack<BF>(a[i], y[i]);
             unpack<BF>(t[i], g[i]);
         }
-        if (base + step < c.n) fetch(row + step);
+        if (base + L::kRows < end) fetch(base + L::kRows);
         float mean_a = 0.f, r_a = 1.f, mean_h, r_h;
-        if (c.A) {
+        if (has_a) {
             r_a = centre<L, G, W>(lanes, c.post, c.F, c.eps, y, &mean_a, red, turn);
+            if (c.gate_cols > 1) {
 #pragma unroll
-            for (int i = 0; i < P; ++i)
+                for (int i = 0; i < P; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float k = c.alpha * s[i][e] * (c.gate_cols > 1 ? fast_gate(g[i][e]) : gate);
-                    h[i][e] = fmaf(k, fmaf(y[i][e] * r_a, p[i][e], p_bias[i][e]), h[i][e]);
-                }
+                    for (int e = 0; e < E; ++e) g[i][e] = c.alpha * fast_gate(g[i][e]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[i][e] = gate;
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float p[E], p_bias[E], s[E];
+                vec.get(0, i, p);
+                vec.get(1, i, p_bias);
+                vec.get(2, i, s);
+#pragma unroll
+                for (int e = 0; e < E; ++e) h[i][e] = fmaf(g[i][e] * s[e], fmaf(y[i][e] * r_a, p[e], p_bias[e]), h[i][e]);
+            }
         }
         u32x4 out[P];
-        if (c.H && row < c.n) {
+        if (has_h && live) {
 #pragma unroll
             for (int i = 0; i < P; ++i) out[i] = pack<BF>(h[i]);
-            lanes.store(c.H, c.ldh, row, out);
+            lanes.store(c.H, c.ldh, base, out);
         }
         if (!normed) continue;
         r_h = centre<L, G, W>(lanes, c.pre, c.F, c.eps, h, &mean_h, red, turn);
-        if (row >= c.n) continue;
-        if (c.stats && lanes.place == 0) reinterpret_cast<f32x4*>(c.stats)[row] = f32x4{mean_a, r_a, mean_h, r_h};
+        if (!live) continue;
+        if (c.stats && lanes.place == 0) reinterpret_cast<f32x4*>(c.stats)[base + lanes.team] = f32x4{mean_a, r_a, mean_h, r_h};
 #pragma unroll
         for (int i = 0; i < P; ++i) {
+            float q[E], q_bias[E];
+            vec.get(3, i, q);
+            vec.get(4, i, q_bias);
 #pragma unroll
-            for (int e = 0; e < E; ++e) h[i][e] = fmaf(h[i][e] * r_h, q[i][e], q_bias[i][e]);
+            for (int e = 0; e < E; ++e) h[i][e] = fmaf(h[i][e] * r_h, q[e], q_bias[e]);
             out[i] = pack<BF>(h[i]);
         }
-        if (c.U) lanes.store(c.U, c.ldu, row, out);
-        if (c.hist) lanes.store(c.hist, c.ld_hist, place, out);
+        if (has_u) lanes.store(c.U, c.ldu, base, out);
+        if (push) lanes.store_at(c.hist, c.ld_hist, place, out);
     }
 }
 
@@ -334,7 +394,7 @@ struct ResidualNormBwd {
     float* sums[5];                      // gradients of p, p_bias, s, q, q_bias, or null
     float* row_sums;                     // [n][2]: means of d and of d hn
     float* partials;                     // [slabs][5][F]
-    int slabs;
+    int slabs, turns;
     int64_t rows_per_slab;
 };
 
@@ -413,8 +473,8 @@ __global__ __launch_bounds__(256) void residual_norm_columns_kernel(ResidualNorm
 }
 
 // The backward pass with the row in registers: every matrix is read once and written once, and a lane keeps the sums of its columns
-// over all rows that it takes.
-template <bool BF, int G, int W, int P, bool MASK>
+// over all rows that it takes.  ALL: every input and output is there but the gate's, known beforehand.
+template <bool BF, int G, int W, int P, bool MASK, bool ALL>
 __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void residual_norm_bwd_rows_kernel(ResidualNormBwd c) {
     using L = RowLanes<BF, G, W, P, MASK>;
     constexpr int E = L::E;
@@ -422,32 +482,40 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     __shared__ float columns[W == 1 ? 4 : 1][W == 1 ? G * P * E : 1];
     int turn = 0;
     const L lanes(c.F);
-    const int64_t step = (int64_t)gridDim.x * L::kRows;
-    int64_t base = (int64_t)blockIdx.x * L::kRows + (W == 1 ? (threadIdx.x >> 6) * (64 / G) : 0);
-    const int64_t team = W == 1 ? (threadIdx.x & 63) / G : 0;
+    const bool has_gh = ALL || c.GH, has_gu = ALL || c.GU, has_a = ALL || c.A, has_gx = ALL || c.GX, has_ga = ALL || c.GA, has_stats = ALL || c.stats;
+    const int64_t end = min(c.n, (int64_t)(blockIdx.x + 1) * c.turns * L::kRows);
+    int64_t base = L::first(c.turns);
     u32x4 gh[P], gu[P], h[P], a[P], t[P];
-    f32x4 st;
-    float t1;
+    f32x4 st = {0.f, 1.f, 0.f, 1.f};
+    float t1 = 0.f;
 #pragma unroll
     for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = a[i] = t[i] = u32x4{0u, 0u, 0u, 0u};
-    auto fetch = [&](int64_t row) {
-        const bool live = row < c.n;
-        if (c.GH) lanes.load(c.GH, c.ldgh, row, live, gh);
-        if (c.GU) {
-            lanes.load(c.GU, c.ldgu, row, live, gu);
-            lanes.load(c.H, c.ldh, row, live, h);
+    auto fetch = [&](int64_t base) {
+        const int64_t row = base + lanes.team;
+        if (row < c.n) {
+            if (has_gh) lanes.load(c.GH, c.ldgh, base, gh);
+            if (has_gu) lanes.load(c.GU, c.ldgu, base, gu);
+            if (has_gu) lanes.load(c.H, c.ldh, base, h);
+            if (has_a) lanes.load(c.A, c.lda, base, a);
+            if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
+            if (c.gate_cols == 1) t1 = load_one<BF>(c.T, row * c.ldt);
+            if (has_stats) st = reinterpret_cast<const f32x4*>(c.stats)[row];
+        } else {                             // a row that is not there adds nothing to the sums
+#pragma unroll
+            for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = a[i] = u32x4{0u, 0u, 0u, 0u};
+            st = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        if (c.A) lanes.load(c.A, c.lda, row, live, a);
-        if (c.gate_cols > 1) lanes.load(c.T, c.ldt, row, live, t);
-        t1 = c.gate_cols == 1 && live ? load_one<BF>(c.T, row * c.ldt) : 0.f;
-        st = !live ? f32x4{0.f, 0.f, 0.f, 0.f} : c.stats ? reinterpret_cast<const f32x4*>(c.stats)[row] : f32x4{0.f, 1.f, 0.f, 1.f};
     };
-    fetch(base + team);
-    float p[P][E], p_bias[P][E], s[P][E], q[P][E];
-    lanes.vector(c.p, 1.f, p);
-    lanes.vector(c.p_bias, 0.f, p_bias);
-    lanes.vector(c.s, 1.f, s);
-    lanes.vector(c.q, 1.f, q);
+    if (base < end) fetch(base);
+    constexpr bool kParked = W == 1 && P > 1;
+    __shared__ f32x4 parked[kParked ? P * E : 1][64];
+    Vectors<L, 4, P, E, kParked> vec;
+    vec.parked = parked;
+    vec.set(lanes, 0, c.p, 1.f);
+    vec.set(lanes, 1, c.p_bias, 0.f);
+    vec.set(lanes, 2, c.s, 1.f);
+    vec.set(lanes, 3, c.q, 1.f);
+    if constexpr (kParked) __syncthreads();
     float sum[5][P][E];
 #pragma unroll
     for (int k = 0; k < 5; ++k)
@@ -456,30 +524,35 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[k][i][e] = 0.f;
     const float inv_f = 1.f / (float)c.F;
-    for (; base < c.n; base += step) {
-        const int64_t row = base + team;
+    for (; base < end; base += L::kRows) {
+        if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
+        const bool live = base + lanes.team < c.n;
         const float mean_a = st[0], r_a = st[1], mean_h = st[2], r_h = st[3];
-        const float gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
+        const float row_gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
         float e_[P][E], hn[P][E], d[P][E], an[P][E], g[P][E];
+        u32x4 a_now[P], t_now[P];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             unpack<BF>(gh[i], e_[i]);
             unpack<BF>(gu[i], d[i]);
             unpack<BF>(h[i], hn[i]);
-            unpack<BF>(a[i], an[i]);
-            unpack<BF>(t[i], g[i]);
+            a_now[i] = a[i];
+            t_now[i] = t[i];
         }
-        if (base + step < c.n) fetch(row + step);
-        if (c.GU) {
+        if (base + L::kRows < end) fetch(base + L::kRows);
+        if (has_gu) {
 #pragma unroll
-            for (int i = 0; i < P; ++i)
+            for (int i = 0; i < P; ++i) {
+                float q[E];
+                vec.get(3, i, q);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     hn[i][e] = (hn[i][e] - mean_h) * r_h;
                     sum[3][i][e] = fmaf(d[i][e], hn[i][e], sum[3][i][e]);
                     sum[4][i][e] += d[i][e];
-                    d[i][e] *= q[i][e];
+                    d[i][e] *= q[e];
                 }
+            }
             float m[2] = {0.f, 0.f};
             if (c.pre != GAS_NORM_NONE) {
                 m[0] = lanes.own(d);
@@ -488,32 +561,55 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
                 m[0] = c.pre == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
                 m[1] *= inv_f;
             }
+            const float off = -r_h * m[0], along = -r_h * m[1];
 #pragma unroll
             for (int i = 0; i < P; ++i)
 #pragma unroll
-                for (int e = 0; e < E; ++e) e_[i][e] = fmaf(r_h, d[i][e] - m[0] - hn[i][e] * m[1], e_[i][e]);
+                for (int e = 0; e < E; ++e) e_[i][e] += fmaf(r_h, d[i][e], fmaf(along, hn[i][e], off));
         }
         u32x4 out[P];
-        if (c.GX && row < c.n) {
+        if (has_gx && live) {
 #pragma unroll
             for (int i = 0; i < P; ++i) out[i] = pack<BF>(e_[i]);
-            lanes.store(c.GX, c.ldgx, row, out);
+            lanes.store(c.GX, c.ldgx, base, out);
         }
-        if (!c.A) continue;
-        // from here on: e_ the gradient at the gated branch before s, then c = dy p; hn the gate's gradient; d what is left of y
+        if (!has_a) continue;
 #pragma unroll
-        for (int i = 0; i < P; ++i)
+        for (int i = 0; i < P; ++i) {
+            unpack<BF>(a_now[i], an[i]);
+            unpack<BF>(t_now[i], g[i]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) an[i][e] = (an[i][e] - mean_a) * r_a;
+        }
+        if (c.gate_cols > 1) {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[i][e] = fast_gate(g[i][e]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i)
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[i][e] = row_gate;
+        }
+        // from here on: hn the gate's gradient, d = dy p
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float p[E], p_bias[E], s[E];
+            vec.get(0, i, p);
+            vec.get(1, i, p_bias);
+            vec.get(2, i, s);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                an[i][e] = (an[i][e] - mean_a) * r_a;
-                const float y = fmaf(an[i][e], p[i][e], p_bias[i][e]), ge = c.gate_cols > 1 ? fast_gate(g[i][e]) : gate;
-                const float branch = e_[i][e] * (c.alpha * ge), dy = branch * s[i][e];
+                const float y = fmaf(an[i][e], p[e], p_bias[e]);
+                const float branch = e_[i][e] * (c.alpha * g[i][e]), dy = branch * s[e];
                 sum[0][i][e] = fmaf(dy, an[i][e], sum[0][i][e]);
                 sum[1][i][e] += dy;
                 sum[2][i][e] = fmaf(branch, y, sum[2][i][e]);
-                hn[i][e] = dy * y * (1.f - ge);
-                d[i][e] = dy * p[i][e];
+                hn[i][e] = dy * y * (1.f - g[i][e]);
+                d[i][e] = dy * p[e];
             }
+        }
         float m[3] = {0.f, 0.f, 0.f};
         if (c.post != GAS_NORM_NONE || c.gate_cols == 1) {
             m[0] = lanes.own(d);
@@ -523,21 +619,22 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             m[0] = c.post == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
             m[1] = c.post != GAS_NORM_NONE ? m[1] * inv_f : 0.f;
         }
-        if (row >= c.n) continue;
-        if (c.GA) {
+        if (!live) continue;
+        if (has_ga) {
+            const float off = -r_a * m[0], along = -r_a * m[1];
 #pragma unroll
             for (int i = 0; i < P; ++i) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) d[i][e] = r_a * (d[i][e] - m[0] - an[i][e] * m[1]);
+                for (int e = 0; e < E; ++e) d[i][e] = fmaf(r_a, d[i][e], fmaf(along, an[i][e], off));
                 out[i] = pack<BF>(d[i]);
             }
-            lanes.store(c.GA, c.ldga, row, out);
+            lanes.store(c.GA, c.ldga, base, out);
         }
-        if (c.GT && c.gate_cols == 1 && lanes.place == 0) store_one<BF>(c.GT, row * c.ldgt, m[2]);
+        if (c.GT && c.gate_cols == 1 && lanes.place == 0) store_one<BF>(c.GT, (base + lanes.team) * c.ldgt, m[2]);
         if (c.GT && c.gate_cols > 1) {
 #pragma unroll
             for (int i = 0; i < P; ++i) out[i] = pack<BF>(hn[i]);
-            lanes.store(c.GT, c.ldgt, row, out);
+            lanes.store(c.GT, c.ldgt, base, out);
         }
     }
     // the workgroup's sums: across the teams of a wavefront by moves, across its wavefronts in LDS
@@ -615,46 +712,69 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
 }
 
 constexpr int kSlabs = 256;
-constexpr int64_t kWaves = 4096;                     // of a launch that goes over its rows in turns: 16 on a compute unit
 
-// How rows of F elements lie in lanes (RowLanes); W = 0: too narrow or too wide for registers, element by element.
-struct Layout { int g, w, p; };
-inline Layout layout_of(int F, bool bf) {
+// How rows of F elements lie in lanes (RowLanes), and the workgroups' turns; w = 0: too narrow or too wide for registers, element by element.
+// Up to 192 pieces of 16 bytes a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
+// 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 and 115; but 20,000 x 2,000 bf16 262 and 147,
+// where four pieces of bf16 no longer fit the registers.  Element by element 2,000 floats x 20,000 take 890 us, eight wavefronts to a
+// row 258; beyond 1,024 pieces a lane's share spills more than it saves (8,000 x 8,200 bf16: 3.4 ms, element by element 1.7).
+// Turns: forward, a workgroup takes few rows, next to each other, so that the rows in flight are one stretch of memory that moves along
+// (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
+// 121, two 129).  Backward, each workgroup leaves partial sums, so there are no more of them than keep memory busy (50,000 x 256
+// bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 625,000 x 256 bf16 504, 506, 504; where a lane has several pieces or a row
+// eight wavefronts 256, 19,997 x 1,433 floats, six wavefronts, 512 workgroups 180 and 256 201).
+struct Layout {
+    int g, w, p, turns;
+    int64_t blocks;
+};
+inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld) {
     const int e = bf ? 8 : 4, pieces = (F + e - 1) / e;
-    if (F < e || pieces > 2048) return {0, 0, 0};
-    if (pieces <= 64) return {pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64, 1, 1};
-    if (pieces > 1024) return {64, 16, 2};
-    int w = 2;
-    while (w * 64 < pieces) w *= 2;
-    return {64, w, 1};
-}
-inline int64_t row_blocks(const Layout& l, int64_t n) {
-    const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, most = kWaves / (l.w == 1 ? 4 : l.w), all = (n + rows - 1) / rows;
-    return all < most ? all : most;
+    Layout l = {64, 1, 1, 1, 0};
+    if (F < e || pieces > 1024) return {0, 0, 0, 0, 0};
+    if (pieces <= 64) l.g = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
+    else if (pieces <= 192) l.p = (pieces + 63) / 64;
+    else
+        for (int w : {16, 12, 8, 6, 4})
+            if (pieces <= w * 64) l.w = w;
+    const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, all = (n + rows - 1) / rows;
+    const int64_t fewest = !bwd || (l.w == 1 ? l.p == 1 : !bf && l.w < 8) ? 512 : 256, turns = (all + fewest - 1) / fewest;
+    const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
+    l.turns = (int)(bwd ? turns : std::min(turns, most));
+    l.blocks = (all + l.turns - 1) / l.turns;
+    if (longest_ld > (1 << 26)) {        // rows of a wavefront lie within 32 bits of each other, or there is one
+        l.turns *= 64 / l.g;
+        l.g = 64;
+    }
+    return l;
 }
 
-template <bool BF, bool MASK, class C>
+template <bool BF, bool MASK, bool ALL, class C>
 void launch_rows(const Layout& l, dim3 grid, hipStream_t s, const C& c) {
     constexpr bool kBwd = std::is_same_v<C, ResidualNormBwd>;
 #define GAS_ROWS(G, W, P)                                                                                                             \
     if (l.g == G && l.w == W && l.p == P) {                                                                                           \
         const dim3 block(W == 1 ? 256 : W * 64);                                                                                      \
-        if constexpr (kBwd) hipLaunchKernelGGL((residual_norm_bwd_rows_kernel<BF, G, W, P, MASK>), grid, block, 0, s, c);             \
-        else hipLaunchKernelGGL((residual_norm_rows_kernel<BF, G, W, P, MASK>), grid, block, 0, s, c);                                \
+        if constexpr (kBwd) hipLaunchKernelGGL((residual_norm_bwd_rows_kernel<BF, G, W, P, MASK, ALL>), grid, block, 0, s, c);        \
+        else hipLaunchKernelGGL((residual_norm_rows_kernel<BF, G, W, P, MASK, ALL>), grid, block, 0, s, c);                           \
         return;                                                                                                                       \
     }
-    GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 1) GAS_ROWS(64, 2, 1) GAS_ROWS(64, 4, 1) GAS_ROWS(64, 8, 1)
-    GAS_ROWS(64, 16, 1) GAS_ROWS(64, 16, 2)
+    GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 1) GAS_ROWS(64, 1, 2) GAS_ROWS(64, 1, 3)
+    GAS_ROWS(64, 4, 1) GAS_ROWS(64, 6, 1) GAS_ROWS(64, 8, 1) GAS_ROWS(64, 12, 1) GAS_ROWS(64, 16, 1)
 #undef GAS_ROWS
 }
 template <class C>
-void launch_rows(const Layout& l, bool bf, int64_t n, hipStream_t s, const C& c) {
-    const dim3 grid((unsigned)row_blocks(l, n));
+void launch_rows(const Layout& l, bool bf, hipStream_t s, C& c) {
+    const dim3 grid((unsigned)l.blocks);
+    c.turns = l.turns;
     const bool mask = c.F % (bf ? 8 : 4) != 0;
-    if (bf && mask) launch_rows<true, true>(l, grid, s, c);
-    else if (bf) launch_rows<true, false>(l, grid, s, c);
-    else if (mask) launch_rows<false, true>(l, grid, s, c);
-    else launch_rows<false, false>(l, grid, s, c);
+    bool all;
+    if constexpr (std::is_same_v<C, ResidualNormBwd>) all = c.GH && c.GU && c.A && c.GX && c.GA && c.stats;
+    else all = c.A && c.H && c.U && !c.hist;
+#define GAS_ROWS(BF, MASK, ALL) \
+    if (bf == BF && mask == MASK && all == ALL) return launch_rows<BF, MASK, ALL>(l, grid, s, c);
+    GAS_ROWS(false, false, false) GAS_ROWS(false, false, true) GAS_ROWS(false, true, false) GAS_ROWS(false, true, true)
+    GAS_ROWS(true, false, false) GAS_ROWS(true, false, true) GAS_ROWS(true, true, false) GAS_ROWS(true, true, true)
+#undef GAS_ROWS
 }
 
 inline bool valid_norm(int k) { return k == GAS_NORM_NONE || k == GAS_NORM_RMS || k == GAS_NORM_LAYER; }
@@ -717,9 +837,10 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
     c.p = p; c.p_bias = p_bias; c.s = s; c.q = q; c.q_bias = q_bias; c.alpha = alpha; c.eps = eps;
     c.H = static_cast<char*>(H); c.U = static_cast<char*>(U); c.ldh = ldh; c.ldu = ldu; c.stats = stats;
     c.idx = push_idx; c.hist = static_cast<char*>(push_hist); c.ld_hist = ld_push;
-    const Layout l = layout_of(F, dt == GAS_BF16);
+    const Layout l = layout_of(n_rows, F, dt == GAS_BF16, false, std::max({ldx, A ? lda : 0, T ? ldt : 0, H ? ldh : 0, U ? ldu : 0}));
+    GAS_REQUIRE(l.blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
     if (l.w) {
-        launch_rows(l, dt == GAS_BF16, n_rows, (hipStream_t)stream, c);
+        launch_rows(l, dt == GAS_BF16, (hipStream_t)stream, c);
         GAS_CHECK_HIP(hipGetLastError());
         return GAS_OK;
     }
@@ -735,8 +856,8 @@ int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F) {
     if (n_rows <= 0 || F <= 0) return 0;
     int64_t most = 0;                         // of both types
     for (int bf = 0; bf < 2; ++bf) {
-        const Layout l = layout_of(F, bf);
-        const int64_t floats = l.w ? row_blocks(l, n_rows) * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
+        const Layout l = layout_of(n_rows, F, bf, true, 0);
+        const int64_t floats = l.w ? l.blocks * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
         most = floats > most ? floats : most;
     }
     return most * 4;
@@ -795,10 +916,12 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     c.GX = static_cast<char*>(GX); c.GA = static_cast<char*>(GA); c.GT = static_cast<char*>(GT);
     c.ldgx = ldgx; c.ldga = ldga; c.ldgt = ldgt;
     c.partials = static_cast<float*>(workspace);
-    const Layout l = layout_of(F, dt == GAS_BF16);
+    const Layout l = layout_of(n_rows, F, dt == GAS_BF16, true, std::max({GH ? ldgh : 0, GU ? std::max(ldgu, ldh) : 0, A ? lda : 0, T ? ldt : 0,
+                                                                          GX ? ldgx : 0, GA ? ldga : 0, GT ? ldgt : 0}));
+    GAS_REQUIRE(l.blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
     if (l.w) {
-        c.slabs = (int)row_blocks(l, n_rows);
-        launch_rows(l, dt == GAS_BF16, n_rows, st, c);
+        c.slabs = (int)l.blocks;
+        launch_rows(l, dt == GAS_BF16, st, c);
         GAS_CHECK_HIP(hipGetLastError());
         if (sums) hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
         GAS_CHECK_HIP(hipGetLastError());
