@@ -1,35 +1,46 @@
 // The step of a model with many tensors: the squared norm of all gradients, and AdamW with states in 32 bits or in 8.
 //     g = c dW,  m <- b1 m + (1 - b1) g,  v <- b2 v + (1 - b2) g^2,
 //     W <- W - lr wd W - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
-// One wavefront takes the 256 elements that share a scale; both kernels are bound by memory, small models by the launch.
+// Bound by memory, small models by the launches.
+#include <algorithm>
+
 #include "common.h"
-#include "wave.h"
 
 namespace gas {
 namespace {
 
-constexpr int kTensors = 112;                       // of a launch: their descriptions fit the 4 KB of a launch's arguments
 constexpr int kBlock = 256;                         // elements that share a scale: four for every lane
 constexpr int kNormChunk = 16384;                   // elements of a partial sum
+// Tensors of a launch: their descriptions fit the 4 KB of a launch's arguments.  Models of few tensors have a launch with room for no more: it is
+// copied for every call.
+constexpr int kNormTensors = 256, kTensors = 144, kFew = 16;
 
-// Index of the tensor that unit `u` (a block, a chunk) belongs to: the last one whose first unit is not behind it.
-template <class T>
-__device__ __forceinline__ int tensor_of(const T& b, uint32_t u) {
-    int lo = 0, hi = b.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (b.first[mid] <= u) lo = mid;
-        else hi = mid;
+// Index of the tensor that unit `u` (a block, a chunk) belongs to: the last one whose first unit is not behind it.  The lanes look at 64 at a
+// time, so it takes one reading, not one after another.
+template <int N>
+__device__ __forceinline__ int tensor_of(const uint32_t (&first)[N], int count, uint32_t u) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < (N + 63) / 64; ++i) {
+        const int k = i * 64 + lane;
+        before += __popcll(__ballot(k < count && first[k < count ? k : 0] <= u));
     }
-    return lo;
+    return __builtin_amdgcn_readfirstlane(before - 1);
 }
 
+// Four elements of any alignment.
+typedef f32x4 four_f32 __attribute__((aligned(4)));
+typedef u32x2 four_bf16 __attribute__((aligned(2)));
+
 // ---- the squared norm of many tensors
+template <int N>
 struct NormBatch {
-    const float* x[kTensors];
-    int64_t n[kTensors];
-    uint32_t first[kTensors];                       // chunk that the tensor begins with
+    const float* x[N];
+    uint32_t first[N];                              // chunk that the tensor begins with
+    uint16_t last[N];                               // elements of its last chunk
     int count;
+    uint32_t chunks;
     double* partials;
 };
 
@@ -39,55 +50,82 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
-__global__ __launch_bounds__(256) void sq_norms_kernel(NormBatch b) {
+// A workgroup to a chunk; sums in 64 bits, for which a product of two floats is exact.
+template <int N>
+__global__ __launch_bounds__(256) void sq_norms_kernel(NormBatch<N> b) {
     __shared__ double part[4];
-    const int k = tensor_of(b, blockIdx.x);
-    const float* x = b.x[k];
-    const int64_t e0 = (int64_t)(blockIdx.x - b.first[k]) * kNormChunk;
-    const int64_t e1 = e0 + kNormChunk < b.n[k] ? e0 + kNormChunk : b.n[k];
-    double s = 0.0;
-    for (int64_t i = e0 + threadIdx.x; i < e1; i += 256) s = fma((double)x[i], (double)x[i], s);
-    s = wave_sum64(s);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+    const int k = tensor_of(b.first, b.count, blockIdx.x);
+    const float* x = b.x[k] + (int64_t)(blockIdx.x - b.first[k]) * kNormChunk;
+    const bool whole = blockIdx.x + 1 < (k + 1 < b.count ? b.first[k + 1] : b.chunks);
+    const int n = whole ? kNormChunk : b.last[k];
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    int i = 4 * threadIdx.x;
+    for (; i + 3 * 1024 + 4 <= n; i += 4 * 1024) {
+        f32x4 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const four_f32*>(x + i + 1024 * j));
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] = fma((double)v[j][e], (double)v[j][e], s[e]);
+    }
+    for (; i < n; i += 1024)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const double v = i + e < n ? (double)x[i + e] : 0.0;
+            s[e] = fma(v, v, s[e]);
+        }
+    const double sum = wave_sum64((s[0] + s[1]) + (s[2] + s[3]));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) b.partials[blockIdx.x] = (part[0] + part[1]) + (part[2] + part[3]);
 }
 
-__global__ __launch_bounds__(256) void sq_norms_finish_kernel(const double* partials, int64_t n, float* out, int32_t* steps) {
-    __shared__ double part[4];
-    double s = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += 256) s += partials[i];
-    s = wave_sum64(s);
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+__global__ __launch_bounds__(1024) void sq_norms_finish_kernel(const double* partials, int64_t n, float* out, int32_t* steps) {
+    __shared__ double part[16];
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
+    int64_t i = threadIdx.x;
+    for (; i + 3 * 1024 < n; i += 4 * 1024)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] += partials[i + 1024 * j];
+    for (; i < n; i += 1024) s[0] += partials[i];
+    const double sum = wave_sum64((s[0] + s[1]) + (s[2] + s[3]));
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        const float total = (float)((part[0] + part[1]) + (part[2] + part[3]));
+        double all = 0.0;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) all += part[w];
+        const float total = (float)all;
         out[0] = total;
         if (steps && total < INFINITY) ++*steps;    // neither an infinity nor a NaN
     }
 }
 
 // ---- AdamW
-struct AdamBatch {
-    char* W[kTensors];
-    const float* g[kTensors];
-    int64_t n[kTensors];
-    uint32_t first[kTensors];                       // block that the tensor begins with, counted from `base`
-    float decay[kTensors];                          // lr times the weight decay
-    uint8_t bf[kTensors];
+template <int N>
+struct AdamTensors {
+    char* W[N];
+    const float* g[N];
+    uint32_t first[N];                              // block that the tensor begins with, counted from `base`
+    float decay[N];                                 // lr times the weight decay
+    uint16_t last[N];                               // elements of its last block; kHalf: bf16
     int count;
-    int64_t base;                                   // the launch's first block
+};
+struct AdamStep {
     uint32_t blocks;
+    int64_t base;                                   // the launch's first block
     void *m, *v;
     float *scales, *master;
-    float lr, b1, b2, rate1, rate2, eps;
-    float c1, c2;                                   // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
+    float b1, b2, rate1, rate2, eps;
+    float lr, c1, c2;                               // 1 / (1 - b1^t), 1 / sqrt(1 - b2^t)
     float ln1, ln2;                                 // logarithms of b1, b2, for a step that is read on the device
     uint32_t step;
     const int32_t* steps;
     const float* sq_norm;
     float max_norm;
 };
+constexpr uint16_t kHalf = 0x8000;
 
 // Two numbers of 16 bits from an element's place in the state and the step: multiplied and folded until every bit of both
 // has reached all others.
@@ -120,104 +158,180 @@ __device__ __forceinline__ int encode(float x, uint32_t die) {
     return (int)k + (((float)die + 0.5f) * (1.f / 65536.f) * (upper - lower) < x - lower ? 1 : 0);
 }
 
-// The largest magnitude of the wavefront's values, by their bits: a NaN is larger than all.
-__device__ __forceinline__ float largest(const float (&x)[4]) {
+// The largest magnitude of the wavefront's values, by their bits: a NaN is larger than all.  By data-parallel moves within 16 lanes and swaps
+// beyond: through LDS the two of a block took 12 steps of some 60 cycles.
+__device__ __forceinline__ float largest(const f32x4& x) {
     uint32_t u = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) u = max(u, __float_as_uint(fabsf(x[i])));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) u = max(u, (uint32_t)__shfl_xor(u, o));
-    return __uint_as_float(u);
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp(u, 0xB1, 0xf, 0xf, true));           // quad_perm 1 0 3 2
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp(u, 0x4E, 0xf, 0xf, true));           // quad_perm 2 3 0 1
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp(u, 0x141, 0xf, 0xf, true));          // row_half_mirror
+    u = max(u, (uint32_t)__builtin_amdgcn_mov_dpp(u, 0x140, 0xf, 0xf, true));          // row_mirror
+    const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    u = max(s[0], s[1]);
+    const auto t = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __uint_as_float(max(t[0], t[1]));
 }
 
-template <bool EIGHT>
-__global__ __launch_bounds__(256) void adamw_kernel(AdamBatch b) {
-    const uint32_t unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+// A wavefront takes one block.  What it loads waits for nothing that it can do without: the clipping factor comes last.  32 bits: 28 bytes an
+// element and some 30 operations: 335 us for 70 M, 5.9 TB/s, as a copy.  8 bits: 16 (float weights) and some 100, half of them the rounding: 154 M
+// bf16 weights with masters, 18 bytes each, 500 us, 5.5 TB/s.  Two or four blocks to a wavefront: 8 bits, 270,000 elements 17 us, 19 and 25, 16 M 78, 80
+// and 86, 154 M with their unpacking 665, 651 and 654; 32 bits, 154 M 715, 759 and 756.  Roots and quotients are the instructions' own, to one unit in the last
+// place.
+template <bool EIGHT, int N>
+__global__ __launch_bounds__(256) void adamw_kernel(AdamTensors<N> l, AdamStep b) {
+    const int lane = threadIdx.x & 63;
+    const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= b.blocks) return;
-    float c = 1.f;
-    if (b.sq_norm) {
-        const float total = *b.sq_norm;
-        if (!(total < INFINITY)) return;            // the whole launch alike
-        c = fminf(1.f, (float)((double)b.max_norm / (sqrt((double)total) + 1e-6)));
+    const float total = b.sq_norm ? *b.sq_norm : 0.f;
+    uint32_t step = b.steps ? (uint32_t)*b.steps : b.step;
+    const int k = tensor_of(l.first, l.count, unit);
+    const uint32_t next = k + 1 < l.count ? l.first[k + 1] : b.blocks;
+    const int64_t e = (int64_t)(unit - l.first[k]) * kBlock + 4 * lane, at = (b.base + unit) * kBlock + 4 * lane;
+    const bool half = l.last[k] & kHalf, own = half && b.master;
+    const int there = unit + 1 < next ? 4 : (int)(l.last[k] & ~kHalf) - 4 * lane;       // of the lane's four elements
+    const uint16_t* w16 = reinterpret_cast<const uint16_t*>(l.W[k]) + e;
+    const float* w32 = own ? b.master + at : reinterpret_cast<const float*>(l.W[k]) + e;
+    f32x4 g = {0.f, 0.f, 0.f, 0.f}, w = g, m, v;
+    uint32_t km, kv;
+    f32x2_t scale;
+    if (there >= 4) {
+        g = __builtin_nontemporal_load(reinterpret_cast<const four_f32*>(l.g[k] + e));
+        if (half && !own) {
+            const u32x2 x = __builtin_nontemporal_load(reinterpret_cast<const four_bf16*>(w16));
+            w = f32x4{bf16_lo(x[0]), bf16_hi(x[0]), bf16_lo(x[1]), bf16_hi(x[1])};
+        } else {
+            w = __builtin_nontemporal_load(reinterpret_cast<const four_f32*>(w32));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < there) {
+                g[i] = l.g[k][e + i];
+                w[i] = half && !own ? __uint_as_float((uint32_t)w16[i] << 16) : w32[i];
+            }
     }
-    float c1 = b.c1, c2 = b.c2;
-    uint32_t step = b.step;
+    if constexpr (EIGHT) {
+        km = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(reinterpret_cast<const int8_t*>(b.m) + at));
+        kv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(b.v) + at));
+        scale = *reinterpret_cast<const f32x2_t*>(b.scales + 2 * (b.base + unit));
+    } else {
+        m = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(b.m) + at));
+        v = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(b.v) + at));
+    }
+    if (!(total < INFINITY)) return;                // the whole call alike
+    float c = 1.f, c1 = b.c1, c2 = b.c2;
+    if (b.sq_norm) c = fminf(1.f, (float)((double)b.max_norm / (sqrt((double)total) + 1e-6)));
     if (b.steps) {
-        step = (uint32_t)*b.steps;
         c1 = 1.f / -expm1f((float)step * b.ln1);
         c2 = 1.f / sqrtf(-expm1f((float)step * b.ln2));
     }
-    const int lane = threadIdx.x & 63, k = tensor_of(b, unit);
-    const int64_t e0 = (int64_t)(unit - b.first[k]) * kBlock, s0 = (b.base + unit) * kBlock;
-    const int64_t n = b.n[k];
-    float m[4], v[4];
+    if constexpr (EIGHT) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = decode_m((int8_t)(km >> (8 * i)), scale[0]);
+            v[i] = decode_v((kv >> (8 * i)) & 255u, scale[1]);
+        }
+    }
+    const float decay = l.decay[k], rate = b.lr * c1;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int64_t e = e0 + lane + 64 * i, at = s0 + lane + 64 * i;
-        m[i] = v[i] = 0.f;
-        if (e >= n) continue;
-        if constexpr (EIGHT) {
-            m[i] = decode_m(reinterpret_cast<const int8_t*>(b.m)[at], b.scales[2 * (b.base + unit)]);
-            v[i] = decode_v(reinterpret_cast<const uint8_t*>(b.v)[at], b.scales[2 * (b.base + unit) + 1]);
-        } else {
-            m[i] = reinterpret_cast<const float*>(b.m)[at];
-            v[i] = reinterpret_cast<const float*>(b.v)[at];
-        }
-        const float g = c * b.g[k][e];
+        const float gi = c * g[i];
         // every product and sum rounds by itself: the codes do not depend on what a compiler contracts
-        m[i] = __fadd_rn(__fmul_rn(m[i], b.b1), __fmul_rn(g, b.rate1));
-        v[i] = __fadd_rn(__fmul_rn(v[i], b.b2), __fmul_rn(__fmul_rn(g, g), b.rate2));
-        const bool half = b.bf[k];
-        float w;
-        if (half && b.master) w = b.master[at];
-        else w = half ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(b.W[k])[e] << 16) : reinterpret_cast<const float*>(b.W[k])[e];
-        w = w - w * b.decay[k] - m[i] * (b.lr * c1) / (sqrtf(v[i]) * c2 + b.eps);
-        if (half && b.master) b.master[at] = w;
-        if (half) reinterpret_cast<uint16_t*>(b.W[k])[e] = (uint16_t)f32_to_bf16(w);
-        else reinterpret_cast<float*>(b.W[k])[e] = w;
-        if constexpr (!EIGHT) {
-            reinterpret_cast<float*>(b.m)[at] = m[i];
-            reinterpret_cast<float*>(b.v)[at] = v[i];
-        }
+        m[i] = __fadd_rn(__fmul_rn(m[i], b.b1), __fmul_rn(gi, b.rate1));
+        v[i] = __fadd_rn(__fmul_rn(v[i], b.b2), __fmul_rn(__fmul_rn(gi, gi), b.rate2));
+        const float change = m[i] * rate * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), c2, b.eps));
+        w[i] -= fmaf(w[i], decay, change);
+    }
+    const u32x2 low = {pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3])};
+    char* W = l.W[k] + e * (half ? 2 : 4);
+    if (own) __builtin_nontemporal_store(w, reinterpret_cast<f32x4*>(b.master + at));
+    if (there >= 4) {
+        if (half) __builtin_nontemporal_store(low, reinterpret_cast<four_bf16*>(W));
+        else __builtin_nontemporal_store(w, reinterpret_cast<four_f32*>(W));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < there) {
+                if (half) reinterpret_cast<uint16_t*>(W)[i] = (uint16_t)(low[i >> 1] >> (16 * (i & 1)));
+                else reinterpret_cast<float*>(W)[i] = w[i];
+            }
     }
     if constexpr (EIGHT) {
         float sm = largest(m), sv = largest(v);
         sm = sm < 1.17549435e-38f ? 0.f : sm;       // below the normal numbers: nothing
         sv = sv < 1.17549435e-38f ? 0.f : sv;
         const float im = sm > 0.f ? 1.f / sm : 0.f, iv = sv > 0.f ? 1.f / sv : 0.f;
-        if (lane == 0) {
-            b.scales[2 * (b.base + unit)] = sm;
-            b.scales[2 * (b.base + unit) + 1] = sv;
-        }
+        if (lane == 0) *reinterpret_cast<f32x2_t*>(b.scales + 2 * (b.base + unit)) = f32x2_t{sm, sv};
+        km = kv = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t e = e0 + lane + 64 * i, at = s0 + lane + 64 * i;
-            if (e >= n) continue;
-            const uint32_t die = dice(at, step);
-            const int km = encode<2, 127>(fabsf(m[i]) * im * 16129.f, die & 0xFFFFu);
-            int kv = encode<4, 255>(v[i] * iv * 4228250625.f, die >> 16);
-            if (kv == 0 && v[i] > 0.f && sv > 0.f) kv = 1;      // a denominator never becomes nothing
-            reinterpret_cast<int8_t*>(b.m)[at] = (int8_t)(m[i] < 0.f ? -km : km);
-            reinterpret_cast<uint8_t*>(b.v)[at] = (uint8_t)kv;
+            const uint32_t die = dice(at + i, step);
+            const int x = encode<2, 127>(fabsf(m[i]) * im * 16129.f, die & 0xFFFFu);
+            int z = encode<4, 255>(v[i] * iv * 4228250625.f, die >> 16);
+            if (z == 0 && v[i] > 0.f && sv > 0.f) z = 1;        // a denominator never becomes nothing
+            km |= (uint32_t)((m[i] < 0.f ? -x : x) & 255) << (8 * i);
+            kv |= (uint32_t)z << (8 * i);
         }
+        __builtin_nontemporal_store(km, reinterpret_cast<uint32_t*>(reinterpret_cast<int8_t*>(b.m) + at));
+        __builtin_nontemporal_store(kv, reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(b.v) + at));
+    } else {
+        __builtin_nontemporal_store(m, reinterpret_cast<f32x4*>(reinterpret_cast<float*>(b.m) + at));
+        __builtin_nontemporal_store(v, reinterpret_cast<f32x4*>(reinterpret_cast<float*>(b.v) + at));
     }
 }
 
+// A wavefront takes four blocks; every instruction stores one stretch of memory.
 template <bool BF>
-__global__ __launch_bounds__(256) void adamw_unpack_kernel(const int8_t* m, const uint8_t* v, const float* scales, int64_t n, char* m_out, char* v_out) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    const float a = decode_m(m[i], scales[2 * (i / kBlock)]), b = decode_v(v[i], scales[2 * (i / kBlock) + 1]);
-    if constexpr (BF) {
-        reinterpret_cast<uint16_t*>(m_out)[i] = (uint16_t)f32_to_bf16(a);
-        reinterpret_cast<uint16_t*>(v_out)[i] = (uint16_t)f32_to_bf16(b);
-    } else {
-        reinterpret_cast<float*>(m_out)[i] = a;
-        reinterpret_cast<float*>(v_out)[i] = b;
-    }
+__global__ __launch_bounds__(256) void adamw_unpack_kernel(const int8_t* m, const uint8_t* v, const float* scales, int64_t blocks, char* m_out, char* v_out) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 4;
+    uint32_t km[4], kv[4];
+    f32x2_t s[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (unit + r < blocks) {
+            km[r] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(m) + (unit + r) * 64 + lane);
+            kv[r] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(v) + (unit + r) * 64 + lane);
+            s[r] = reinterpret_cast<const f32x2_t*>(scales)[unit + r];
+        }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        if (unit + r < blocks) {
+            f32x4 a, b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a[e] = decode_m((int8_t)(km[r] >> (8 * e)), s[r][0]);
+                b[e] = decode_v((kv[r] >> (8 * e)) & 255u, s[r][1]);
+            }
+            const int64_t to = (unit + r) * 64 + lane;
+            if constexpr (BF) {
+                __builtin_nontemporal_store(u32x2{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3])}, reinterpret_cast<u32x2*>(m_out) + to);
+                __builtin_nontemporal_store(u32x2{pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])}, reinterpret_cast<u32x2*>(v_out) + to);
+            } else {
+                __builtin_nontemporal_store(a, reinterpret_cast<f32x4*>(m_out) + to);
+                __builtin_nontemporal_store(b, reinterpret_cast<f32x4*>(v_out) + to);
+            }
+        }
 }
 
 constexpr int64_t kMostBlocks = 0x7FFFFFFFLL;
+
+// Stretches of memory that are apart from each other, in order.
+struct Stretches {
+    uintptr_t from[kTensors], to[kTensors];
+    int count = 0;
+    bool add(uintptr_t a, uintptr_t b) {                     // false, and nothing is added, if it meets one that is there
+        int i = count;
+        while (i > 0 && from[i - 1] >= b) --i;               // most lists are in the order of their addresses already
+        if (i > 0 && to[i - 1] > a) return false;
+        for (int j = count; j > i; --j) from[j] = from[j - 1], to[j] = to[j - 1];
+        from[i] = a; to[i] = b;
+        ++count;
+        return true;
+    }
+};
 
 }  // namespace
 }  // namespace gas
@@ -246,22 +360,33 @@ gas_status gas_sq_norms(int32_t count, const float* const* x, const int64_t* n, 
     double* partials = static_cast<double*>(workspace);
     int64_t done = 0;
     for (int32_t i = 0; i < count;) {
-        NormBatch b;
+        NormBatch<kNormTensors> b;
         b.count = 0;
         b.partials = partials + done;
         int64_t chunks = 0;
-        for (; i < count && b.count < kTensors; ++i) {
+        for (; i < count && b.count < kNormTensors; ++i) {
             if (n[i] == 0) continue;
-            b.x[b.count] = x[i]; b.n[b.count] = n[i]; b.first[b.count] = (uint32_t)chunks;
+            const int64_t more = (n[i] + kNormChunk - 1) / kNormChunk;
+            b.x[b.count] = x[i]; b.first[b.count] = (uint32_t)chunks; b.last[b.count] = (uint16_t)(n[i] - (more - 1) * kNormChunk);
             ++b.count;
-            chunks += (n[i] + kNormChunk - 1) / kNormChunk;
+            chunks += more;
         }
         if (chunks == 0) continue;
-        hipLaunchKernelGGL(sq_norms_kernel, dim3((unsigned)chunks), dim3(256), 0, (hipStream_t)stream, b);
+        b.chunks = (uint32_t)chunks;
+        if (b.count <= kFew) {
+            NormBatch<kFew> few;
+            std::copy_n(b.x, b.count, few.x);
+            std::copy_n(b.first, b.count, few.first);
+            std::copy_n(b.last, b.count, few.last);
+            few.count = b.count; few.chunks = b.chunks; few.partials = b.partials;
+            hipLaunchKernelGGL(sq_norms_kernel<kFew>, dim3(b.chunks), dim3(256), 0, (hipStream_t)stream, few);
+        } else {
+            hipLaunchKernelGGL(sq_norms_kernel<kNormTensors>, dim3(b.chunks), dim3(256), 0, (hipStream_t)stream, b);
+        }
         GAS_CHECK_HIP(hipGetLastError());
         done += chunks;
     }
-    hipLaunchKernelGGL(sq_norms_finish_kernel, dim3(1), dim3(256), 0, (hipStream_t)stream, partials, done, out, steps);
+    hipLaunchKernelGGL(sq_norms_finish_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, partials, done, out, steps);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
 }
@@ -287,11 +412,13 @@ gas_status gas_adamw_steps(int32_t count, void* const* W, const int32_t* dtypes,
     GAS_REQUIRE(state_bits == 32 || scales || count == 0, "%s: states of 8 bits without scales", who);
     GAS_REQUIRE(state_elements >= gas_adamw_elements(count, n), "%s: the state has %lld elements, %lld are needed", who,
                 (long long)state_elements, (long long)gas_adamw_elements(count, n));
+    GAS_REQUIRE(aligned16(m) && aligned16(v) && aligned16(master) && ((uintptr_t)scales & 7u) == 0, "%s: the state is not aligned to 16 bytes", who);
     GAS_REQUIRE(rate1 > 0.f && rate1 <= 1.f && rate2 > 0.f && rate2 <= 1.f && eps > 0.f, "%s: beta1=%g beta2=%g eps=%g", who, 1.0 - rate1,
                 1.0 - rate2, (double)eps);
     GAS_REQUIRE(steps || (step >= 1 && step <= 0x7FFFFFFF), "%s: step=%lld", who, (long long)step);
     GAS_REQUIRE(!sq_norm || max_norm > 0.f, "%s: max_norm=%g", who, (double)max_norm);
-    AdamBatch b;
+    AdamStep b;
+    AdamTensors<kTensors> l;
     b.m = m; b.v = v; b.scales = scales; b.master = master;
     const double beta1 = 1.0 - rate1, beta2 = 1.0 - rate2;
     b.lr = lr; b.b1 = (float)beta1; b.b2 = (float)beta2; b.rate1 = rate1; b.rate2 = rate2; b.eps = eps;
@@ -301,29 +428,40 @@ gas_status gas_adamw_steps(int32_t count, void* const* W, const int32_t* dtypes,
     b.c2 = steps ? 1.f : (float)(1.0 / sqrt(1.0 - pow(beta2, (double)step)));
     int64_t base = 0;
     for (int32_t i = 0; i < count;) {
-        b.count = 0;
+        Stretches taken;
+        l.count = 0;
         b.base = base;
         int64_t blocks = 0;
-        for (; i < count && b.count < kTensors; ++i) {
+        for (; i < count && l.count < kTensors; ++i) {
             if (n[i] == 0) continue;
             const int64_t more = (n[i] + kBlock - 1) / kBlock;
             GAS_REQUIRE(more <= kMostBlocks, "%s: tensor %d is too large", who, i);
-            char* w = static_cast<char*>(W[i]);
-            const int64_t bytes = n[i] * elem_bytes((gas_dtype)dtypes[i]);
-            bool apart = blocks + more <= kMostBlocks;       // memory that an earlier tensor of the launch updates too waits for the next one
-            for (int j = 0; j < b.count && apart; ++j) apart = w + bytes <= b.W[j] || b.W[j] + b.n[j] * (b.bf[j] ? 2 : 4) <= w;
-            if (!apart) break;
-            b.W[b.count] = w; b.g[b.count] = dW[i]; b.n[b.count] = n[i]; b.first[b.count] = (uint32_t)blocks;
-            b.decay[b.count] = weight_decay ? lr * weight_decay[i] : 0.f;
-            b.bf[b.count] = dtypes[i] == GAS_BF16;
-            ++b.count;
+            const uintptr_t w = (uintptr_t)W[i];
+            // memory that an earlier tensor of the launch updates too waits for the next one
+            if (blocks + more > kMostBlocks || !taken.add(w, w + n[i] * elem_bytes((gas_dtype)dtypes[i]))) break;
+            l.W[l.count] = static_cast<char*>(W[i]); l.g[l.count] = dW[i]; l.first[l.count] = (uint32_t)blocks;
+            l.decay[l.count] = weight_decay ? lr * weight_decay[i] : 0.f;
+            l.last[l.count] = (uint16_t)(n[i] - (more - 1) * kBlock) | (dtypes[i] == GAS_BF16 ? kHalf : 0);
+            ++l.count;
             blocks += more;
         }
         if (blocks == 0) continue;
         b.blocks = (uint32_t)blocks;
         base += blocks;
-        hipLaunchKernelGGL(state_bits == 8 ? adamw_kernel<true> : adamw_kernel<false>, dim3((unsigned)((blocks + 3) / 4)), dim3(256), 0,
-                           (hipStream_t)stream, b);
+        const dim3 grid((unsigned)((blocks + 3) / 4));
+        if (l.count <= kFew) {
+            AdamTensors<kFew> few;
+            std::copy_n(l.W, l.count, few.W);
+            std::copy_n(l.g, l.count, few.g);
+            std::copy_n(l.first, l.count, few.first);
+            std::copy_n(l.decay, l.count, few.decay);
+            std::copy_n(l.last, l.count, few.last);
+            few.count = l.count;
+            hipLaunchKernelGGL((state_bits == 8 ? adamw_kernel<true, kFew> : adamw_kernel<false, kFew>), grid, dim3(256), 0, (hipStream_t)stream, few, b);
+        } else {
+            hipLaunchKernelGGL((state_bits == 8 ? adamw_kernel<true, kTensors> : adamw_kernel<false, kTensors>), grid, dim3(256), 0,
+                               (hipStream_t)stream, l, b);
+        }
         GAS_CHECK_HIP(hipGetLastError());
     }
     return GAS_OK;
@@ -335,9 +473,11 @@ gas_status gas_adamw_unpack(const void* m, const void* v, const float* scales, i
     GAS_REQUIRE(n >= 0 && n % kBlock == 0, "%s: n=%lld", who, (long long)n);
     if (n == 0) return GAS_OK;
     GAS_REQUIRE(m && v && scales && m_out && v_out, "%s: null pointer", who);
-    GAS_REQUIRE(n / 256 <= kMostBlocks, "%s: too many elements for one launch", who);
-    hipLaunchKernelGGL(dt == GAS_BF16 ? adamw_unpack_kernel<true> : adamw_unpack_kernel<false>, dim3((unsigned)(n / 256)), dim3(256), 0,
-                       (hipStream_t)stream, static_cast<const int8_t*>(m), static_cast<const uint8_t*>(v), scales, n, static_cast<char*>(m_out),
+    GAS_REQUIRE(aligned16(m) && aligned16(v) && aligned16(m_out) && aligned16(v_out) && ((uintptr_t)scales & 7u) == 0,
+                "%s: the state or its values are not aligned to 16 bytes", who);
+    GAS_REQUIRE(n / 4096 < kMostBlocks, "%s: too many elements for one launch", who);
+    hipLaunchKernelGGL(dt == GAS_BF16 ? adamw_unpack_kernel<true> : adamw_unpack_kernel<false>, dim3((unsigned)((n + 4095) / 4096)), dim3(256), 0,
+                       (hipStream_t)stream, static_cast<const int8_t*>(m), static_cast<const uint8_t*>(v), scales, n / kBlock, static_cast<char*>(m_out),
                        static_cast<char*>(v_out));
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
