@@ -136,15 +136,18 @@ class _Calls:
     any ctypes objects, as before."""
 
     def __init__(self):
-        global _mat, _size, _ptr, _tensors
+        global _mat, _size, _ptr, _tensors, _floats, _alike, _vectors
         lib()
         native = _marshalling()
         if native is None:
-            _mat, _size, _ptr, _tensors = _mat_any, _size_any, _ptr_any, _tensors_any
+            _mat, _size, _ptr = _mat_any, _size_any, _ptr_any
+            _tensors, _floats, _alike, _vectors = _tensors_any, _floats_any, _alike_any, _vectors_any
         else:
             native.set_slow(_mat_any, _size_any, _ptr_any)
-            _mat, _size, _ptr = native.mat, native.size, native.ptr
+            _mat, _size, _ptr, _floats = native.mat, native.size, native.ptr, native.floats
             _tensors = lambda ts: native.tensors(ts) or _tensors_any(ts)
+            _alike = lambda what, *ts: native.alike(*ts) or _alike_any(what, *ts)
+            _vectors = lambda what, width, *vs: native.vectors(width, *vs) or _vectors_any(what, width, *vs)
         raw = C.CDLL(LIB_PATH)
         types = dict(p=C.c_void_p, q=C.c_int64, i=C.c_int32, f=C.c_float)
         for name, sig in _SIGNATURES.items():
@@ -211,7 +214,33 @@ def _tensors_any(ts):
                                                           ("i", [_dt(t) for t in ts])))
 
 
-_mat, _size, _ptr, _tensors = _mat_any, _size_any, _ptr_any, _tensors_any        # until the library is loaded (_Calls)
+def _floats_any(vs):
+    """Numbers as a host array of float32 in bytes."""
+    return array.array("f", vs).tobytes()
+
+
+def _alike_any(what, like, *ts):
+    """Rows, columns and dtype code of a matrix, and address and row stride of each of `ts`, which have the same (0 and 0 for None)."""
+    _, _, *size = _size_any(like)
+    out = list(size)
+    for t in ts:
+        p, ld, *of = (0, 0, *size) if t is None else _size_any(t)
+        if of != size:
+            raise ValueError(f"{what}: shapes or dtypes do not match")
+        out += (p, ld)
+    return tuple(out)
+
+
+def _vectors_any(what, width, *vs):
+    """Addresses of float32 vectors of `width`, 0 for None."""
+    for v in vs:
+        if v is not None and v.numel() != width:
+            raise ValueError(f"{what}: a vector of {v.numel()} for rows of {width}")
+    return tuple(_ptr_any(v, torch.float32) for v in vs)
+
+
+_mat, _size, _ptr = _mat_any, _size_any, _ptr_any        # until the library is loaded (_Calls)
+_tensors, _floats, _alike, _vectors = _tensors_any, _floats_any, _alike_any, _vectors_any
 _NONE = (0, 0, 0, 0, None)                               # _size of an argument that is not given
 
 
@@ -738,33 +767,21 @@ def gas_sgd_step_clipped(w, dw, lr, sq_norms, max_norm, weight_decay=0.0):
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 
 
-def _vector(v, width, what):
-    """Address of a float32 vector of `width`, 0 for None."""
-    if v is None:
-        return 0
-    if v.numel() != width:
-        raise ValueError(f"{what}: a vector of {v.numel()} for rows of {width}")
-    return _ptr(v, torch.float32)
-
-
 def gas_residual_norm(x, h=None, u=None, a=None, t=None, post=NORM_NONE, p=None, p_bias=None, s=None, alpha=1.0, pre=NORM_NONE, q=None,
                       q_bias=None, eps=1e-5, stats=None, idx=None, hist=None):
     """h = x + alpha * s * sigmoid(t) * (N_post(a) * p + p_bias) and u = N_pre(h) * q + q_bias, either of them or both; x, a, h, u: [n, F],
     t: [n, F] or [n, 1], vectors float32 [F].  stats: float32 [n, 4], kept for the backward call.  idx, hist: u[i] also to hist[idx[i]]."""
-    xp, ldx, n, width, dt = _size(x)
-    rows = (n, width, dt)
-    ap, lda, *like_a = (0, 0, *rows) if a is None else _size(a)
-    hp, ldh, *like_h = (0, 0, *rows) if h is None else _size(h)
-    up, ldu, *like_u = (0, 0, *rows) if u is None else _size(u)
+    calls, who = _calls(), "gas_residual_norm"
+    n, width, dt, xp, ldx, ap, lda, hp, ldh, up, ldu = _alike(who, x, x, a, h, u)
     tp, ldt, nt, gates, dtt = (0, 0, n, 0, dt) if t is None else _size(t)
     gp, ldg, n_hist, fg, dtg = (0, 0, 0, width, dt) if hist is None else _size(hist)
-    if not (tuple(like_a) == tuple(like_h) == tuple(like_u) == rows) or nt != n or dtt != dt or dtg != dt or fg != width or \
-            (hist is None) != (idx is None) or (idx is not None and idx.numel() != n) or (stats is not None and stats.shape != (n, 4)):
+    if nt != n or dtt != dt or dtg != dt or fg != width or (hist is None) != (idx is None) or (idx is not None and idx.numel() != n) or \
+            (stats is not None and stats.shape != (n, 4)):
         raise ValueError("gas_residual_norm: shapes or dtypes do not match")
-    vec = lambda v: _vector(v, width, "gas_residual_norm")
-    _check(_calls().gas_residual_norm(
-        xp, ldx, ap, lda, tp, ldt, gates, n, width, dt, post, vec(p), vec(p_bias), vec(s), alpha, pre, vec(q), vec(q_bias), eps,
-        hp, ldh, up, ldu, _ptr(stats, torch.float32), _ptr(idx, torch.int32), gp, n_hist, ldg, _stream()))
+    pp, pbp, sp, qp, qbp = _vectors(who, width, p, p_bias, s, q, q_bias)
+    _check(calls.gas_residual_norm(
+        xp, ldx, ap, lda, tp, ldt, gates, n, width, dt, post, pp, pbp, sp, alpha, pre, qp, qbp, eps, hp, ldh, up, ldu,
+        0 if stats is None else _ptr(stats, torch.float32), 0 if idx is None else _ptr(idx, torch.int32), gp, n_hist, ldg, _stream()))
 
 
 def gas_residual_norm_bwd(gh, gu, h, stats, gx=None, ga=None, gt=None, a=None, t=None, post=NORM_NONE, p=None, p_bias=None, s=None, alpha=1.0,
@@ -772,30 +789,21 @@ def gas_residual_norm_bwd(gh, gu, h, stats, gx=None, ga=None, gt=None, a=None, t
     """Backward of gas_residual_norm: gh, gu: gradients at h and u (None: none there); h and stats as the forward call left them.  gx, ga, gt:
     [n, F] (gt as t), gp, gp_bias, gs, gq, gq_bias: float32 [F], each optional.  workspace: a uint8 tensor of at least
     gas_residual_norm_bwd_workspace(n, F) bytes, allocated here if not given."""
-    like = next((m for m in (gh, gu, gx, ga) if m is not None), None)
+    calls, who = _calls(), "gas_residual_norm_bwd"
+    like = gh if gh is not None else gu
     if like is None:
         raise ValueError("gas_residual_norm_bwd: no gradient is given")
-    _, _, n, width, dt = _size(like)
-    mats = []
-    for m in (gh, gu, h, a, gx, ga):
-        if m is None:
-            mats.append((0, 0))
-            continue
-        mp, ld, rows, cols, dtm = _size(m)
-        if rows != n or cols != width or dtm != dt:
-            raise ValueError("gas_residual_norm_bwd: shapes or dtypes do not match")
-        mats.append((mp, ld))
-    (ghp, ldgh), (gup, ldgu), (hp, ldh), (ap, lda), (gxp, ldgx), (gap, ldga) = mats
+    n, width, dt, ghp, ldgh, gup, ldgu, hp, ldh, ap, lda, gxp, ldgx, gap, ldga = _alike(who, like, gh, gu, h, a, gx, ga)
     tp, ldt, nt, gates, dtt = (0, 0, n, 0, dt) if t is None else _size(t)
     gtp, ldgt, ngt, fgt, dtgt = (0, 0, n, gates, dt) if gt is None else _size(gt)
     if nt != n or dtt != dt or ngt != n or fgt != gates or dtgt != dt or (stats is not None and stats.shape != (n, 4)):
         raise ValueError("gas_residual_norm_bwd: shapes or dtypes do not match")
+    pp, pbp, sp, qp, gpp, gpbp, gsp, gqp, gqbp = _vectors(who, width, p, p_bias, s, q, gp, gp_bias, gs, gq, gq_bias)
     if workspace is None:
-        workspace = torch.empty(_calls().gas_residual_norm_bwd_workspace(n, width), dtype=torch.uint8, device=like.device)
-    vec = lambda v: _vector(v, width, "gas_residual_norm_bwd")
-    _check(_calls().gas_residual_norm_bwd(
-        ghp, ldgh, gup, ldgu, hp, ldh, ap, lda, tp, ldt, gates, _ptr(stats, torch.float32), n, width, dt, post, vec(p), vec(p_bias), vec(s),
-        alpha, pre, vec(q), gxp, ldgx, gap, ldga, gtp, ldgt, vec(gp), vec(gp_bias), vec(gs), vec(gq), vec(gq_bias), _ptr(workspace),
+        workspace = torch.empty(calls.gas_residual_norm_bwd_workspace(n, width), dtype=torch.uint8, device=like.device)
+    _check(calls.gas_residual_norm_bwd(
+        ghp, ldgh, gup, ldgu, hp, ldh, ap, lda, tp, ldt, gates, 0 if stats is None else _ptr(stats, torch.float32), n, width, dt, post, pp, pbp,
+        sp, alpha, pre, qp, gxp, ldgx, gap, ldga, gtp, ldgt, gpp, gpbp, gsp, gqp, gqbp, _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream()))
 
 
@@ -809,7 +817,7 @@ def gas_sq_norms(xs, out, steps=None, workspace=None):
     calls = _calls()
     n = len(xs)
     ptrs, sizes, codes = _tensors(xs)
-    if any(codes):
+    if codes != bytes(4 * n):                            # F32 all of them
         raise TypeError("gas_sq_norms: tensors of float32")
     if out.numel() < 1 or (steps is not None and steps.numel() < 1):
         raise ValueError("gas_sq_norms: no place for the result")
@@ -835,7 +843,7 @@ def gas_adamw_steps(ws, dws, m, v, lr, step=0, beta1=0.9, beta2=0.999, eps=1e-8,
     n, calls = len(ws), _calls()
     ptrs, sizes, codes = _tensors(ws)
     grads, grad_sizes, grad_codes = _tensors(dws)
-    if grad_sizes != sizes or any(grad_codes):
+    if grad_sizes != sizes or grad_codes != bytes(4 * n):
         raise ValueError("gas_adamw_steps: gradients of the tensors' sizes, float32")
     bits = 32 if m.dtype == torch.float32 else 8
     room = m.numel()
@@ -843,9 +851,9 @@ def gas_adamw_steps(ws, dws, m, v, lr, step=0, beta1=0.9, beta2=0.999, eps=1e-8,
             (scales is not None and scales.numel() < 2 * (room // 256)) or (sq_norm is not None and sq_norm.numel() < 1):
         raise ValueError("gas_adamw_steps: the parts of the state do not match")
     if isinstance(weight_decay, (int, float)):
-        decay = (array.array("f", [weight_decay]) * n).tobytes()
+        decay = _floats([weight_decay]) * n
     else:
-        decay = array.array("f", weight_decay).tobytes()
+        decay = _floats(weight_decay)
         if len(decay) != 4 * n:
             raise ValueError("gas_adamw_steps: one weight decay for each tensor")
     _check(calls.gas_adamw_steps(

@@ -129,6 +129,74 @@ PyObject* tensors(PyObject*, PyObject* o) {
     return out;
 }
 
+// floats(list): numbers as float32 in bytes
+PyObject* floats(PyObject*, PyObject* o) {
+    PyObject* list = PySequence_Fast(o, "a list of numbers");
+    if (!list) return nullptr;
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    PyObject* out = PyBytes_FromStringAndSize(nullptr, n * 4);
+    for (Py_ssize_t i = 0; out && i < n; ++i) {
+        const double v = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(list, i));
+        if (v == -1.0 && PyErr_Occurred()) Py_CLEAR(out);
+        else {
+            const float f = (float)v;
+            memcpy(PyBytes_AS_STRING(out) + 4 * i, &f, 4);
+        }
+    }
+    Py_DECREF(list);
+    return out;
+}
+
+// alike(like, t, ...): (rows, columns, dtype code, address and row stride of t, ...) of matrices of the feature types and of like's sizes and
+// type, 0 and 0 for None.  None if any of them is something else, which the Python function decides about
+PyObject* alike(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    try {
+        int64_t ld;
+        const at::Tensor* like = n > 0 ? plain(args[0]) : nullptr;
+        const at::ScalarType s = like ? like->scalar_type() : at::kDouble;
+        if (like && (s == at::kFloat || s == at::kBFloat16) && matrix(*like, &ld)) {
+            PyObject* out = PyTuple_New(3 + 2 * (n - 1));
+            if (!out) return nullptr;
+            PyTuple_SET_ITEM(out, 0, PyLong_FromLongLong(like->size(0)));
+            PyTuple_SET_ITEM(out, 1, PyLong_FromLongLong(like->size(1)));
+            PyTuple_SET_ITEM(out, 2, PyLong_FromLong(s == at::kFloat ? GAS_F32 : GAS_BF16));
+            for (Py_ssize_t i = 1; i < n; ++i) {
+                const at::Tensor* t = args[i] == Py_None ? nullptr : plain(args[i]);
+                if (args[i] != Py_None && (!t || t->scalar_type() != s || !matrix(*t, &ld) || t->size(0) != like->size(0) || t->size(1) != like->size(1))) {
+                    Py_DECREF(out);
+                    Py_RETURN_NONE;
+                }
+                PyTuple_SET_ITEM(out, 2 * i + 1, PyLong_FromVoidPtr(t ? t->data_ptr() : nullptr));
+                PyTuple_SET_ITEM(out, 2 * i + 2, PyLong_FromLongLong(t ? ld : 0));
+            }
+            return out;
+        }
+    } catch (...) {
+    }
+    Py_RETURN_NONE;
+}
+
+// vectors(width, v, ...): addresses of contiguous float32 tensors of `width` elements, 0 for None; None if any of them is something else
+PyObject* vectors(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    try {
+        const long long width = n > 0 ? PyLong_AsLongLong(args[0]) : -1;
+        if (width == -1 && PyErr_Occurred()) return nullptr;
+        PyObject* out = PyTuple_New(n > 0 ? n - 1 : 0);
+        if (!out) return nullptr;
+        for (Py_ssize_t i = 1; i < n; ++i) {
+            const at::Tensor* t = args[i] == Py_None ? nullptr : plain(args[i]);
+            if (args[i] != Py_None && (!t || t->scalar_type() != at::kFloat || t->numel() != width || !t->is_contiguous())) {
+                Py_DECREF(out);
+                Py_RETURN_NONE;
+            }
+            PyTuple_SET_ITEM(out, i - 1, PyLong_FromVoidPtr(t ? t->data_ptr() : nullptr));
+        }
+        return out;
+    } catch (...) {
+    }
+    Py_RETURN_NONE;
+}
+
 // ---- calls
 // A pointer argument: an address, None, a ctypes array (its memory) or a ctypes pointer (its value).
 bool get(PyObject* o, uintptr_t* out) {
@@ -209,6 +277,9 @@ PyMethodDef methods[] = {
     {"size", size, METH_O, nullptr},
     {"ptr", (PyCFunction)(void (*)())ptr, METH_FASTCALL, nullptr},
     {"tensors", tensors, METH_O, nullptr},
+    {"floats", floats, METH_O, nullptr},
+    {"alike", (PyCFunction)(void (*)())alike, METH_FASTCALL, nullptr},
+    {"vectors", (PyCFunction)(void (*)())vectors, METH_FASTCALL, nullptr},
     {"set_slow", set_slow, METH_VARARGS, nullptr},
     GAS_CALL(gas_pull), GAS_CALL(gas_push), GAS_CALL(gas_pull_host), GAS_CALL(gas_push_host), GAS_CALL(gas_gcn_norm),
     GAS_CALL(gas_spmm), GAS_CALL(gas_spmm_hist), GAS_CALL(gas_spmm_table), GAS_CALL(gas_fuse_sources), GAS_CALL(gas_spmm_t),
