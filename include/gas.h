@@ -510,7 +510,7 @@ GAS_API gas_status gas_sgd_step_clipped(void* W, int64_t n, gas_dtype dt, const 
  *     dy = e alpha s g,  c = dy p,   GA = r_a (c - [mean c] - an mean(c an)),   GT = dy y (1 - g) (one gate of a row: the row's sum),
  *     gp = sum dy an, gp_bias = sum dy, gs = sum e alpha g y, gq = sum GU hn, gq_bias = sum GU     over the rows, fp32[F].
  * H as stored and stats as written by the forward call.  Any output may be NULL; GX may be GH, GA may be A, and so on, as above;
- * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace: gas_residual_norm_bwd_workspace(n_rows, F) bytes
+ * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace: gas_residual_norm_bwd_workspace(n_rows, F) bytes (enough for fewer rows too)
  * from a multiple of 16 on.
  */
 typedef enum { GAS_NORM_NONE = 0, GAS_NORM_RMS = 1, GAS_NORM_LAYER = 2 } gas_norm_kind;

@@ -725,12 +725,12 @@ constexpr int kSlabs = 256;
 // eight wavefronts 256, 19,997 x 1,433 floats, six wavefronts, 512 workgroups 180 and 256 201).
 struct Layout {
     int g, w, p, turns;
-    int64_t blocks;
+    int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
 };
 inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld) {
     const int e = bf ? 8 : 4, pieces = (F + e - 1) / e;
-    Layout l = {64, 1, 1, 1, 0};
-    if (F < e || pieces > 1024) return {0, 0, 0, 0, 0};
+    Layout l = {64, 1, 1, 1, 0, 0};
+    if (F < e || pieces > 1024) return {0, 0, 0, 0, 0, 0};
     if (pieces <= 64) l.g = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
     else if (pieces <= 192) l.p = (pieces + 63) / 64;
     else
@@ -741,6 +741,7 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
     l.turns = (int)(bwd ? turns : std::min(turns, most));
     l.blocks = (all + l.turns - 1) / l.turns;
+    l.most_blocks = std::min(all, fewest);
     if (longest_ld > (1 << 26)) {        // rows of a wavefront lie within 32 bits of each other, or there is one
         l.turns *= 64 / l.g;
         l.g = 64;
@@ -857,7 +858,7 @@ int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F) {
     int64_t most = 0;                         // of both types
     for (int bf = 0; bf < 2; ++bf) {
         const Layout l = layout_of(n_rows, F, bf, true, 0);
-        const int64_t floats = l.w ? l.blocks * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
+        const int64_t floats = l.w ? l.most_blocks * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
         most = floats > most ? floats : most;
     }
     return most * 4;

@@ -37,3 +37,13 @@ def test_gradients(kind, gate, bias):
             step = 1e-5
             slope = (loss(**{k: leaf + step * direction}) - loss(**{k: leaf - step * direction})) / (2 * step)
         assert abs(slope - (leaf.grad * direction).sum()) <= 1e-7 * (1 + leaf.grad.norm() * direction.norm()), k
+
+
+def test_workspace_of_the_backward_pass_serves_fewer_rows():
+    from paper_2106_05609_amd import binding as B
+    for f in (1, 7, 47, 64, 100, 256, 520, 1433, 2000, 5000, 9000):
+        last = 0
+        for n in [*range(0, 3000, 7), 21_248, 50_000, 50_001, 262_143, 600_000, 3_125_002]:
+            need = B.gas_residual_norm_bwd_workspace(n, f)
+            assert need >= last, (n, f)
+            last = need
