@@ -479,7 +479,8 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     using L = RowLanes<BF, G, W, P, MASK>;
     constexpr int E = L::E;
     __shared__ float red[2][3][16];
-    __shared__ float columns[W == 1 ? 4 : 1][W == 1 ? G * P * E : 1];
+    constexpr int kAtOnce = P == 1 ? 5 : 1;              // vectors of sums that share a barrier: 40 KB at most
+    __shared__ float columns[W == 1 ? 4 : 1][W == 1 ? kAtOnce : 1][W == 1 ? G * P * E : 1];
     int turn = 0;
     const L lanes(c.F);
     const bool has_gh = ALL || c.GH, has_gu = ALL || c.GU, has_a = ALL || c.A, has_gx = ALL || c.GX, has_ga = ALL || c.GA, has_stats = ALL || c.stats;
@@ -490,23 +491,36 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     float t1 = 0.f;
 #pragma unroll
     for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = a[i] = t[i] = u32x4{0u, 0u, 0u, 0u};
-    auto fetch = [&](int64_t base) {
+    // What the norm before the next block needs of a row, and what the block needs: each is fetched for the next row when this row's
+    // has been used, into the same registers.
+    auto fetch_pre = [&](int64_t base) {
         const int64_t row = base + lanes.team;
         if (row < c.n) {
             if (has_gh) lanes.load(c.GH, c.ldgh, base, gh);
             if (has_gu) lanes.load(c.GU, c.ldgu, base, gu);
             if (has_gu) lanes.load(c.H, c.ldh, base, h);
-            if (has_a) lanes.load(c.A, c.lda, base, a);
-            if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
-            if (c.gate_cols == 1) t1 = load_one<BF>(c.T, row * c.ldt);
             if (has_stats) st = reinterpret_cast<const f32x4*>(c.stats)[row];
         } else {                             // a row that is not there adds nothing to the sums
 #pragma unroll
-            for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = a[i] = u32x4{0u, 0u, 0u, 0u};
+            for (int i = 0; i < P; ++i) gh[i] = gu[i] = h[i] = u32x4{0u, 0u, 0u, 0u};
             st = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     };
-    if (base < end) fetch(base);
+    auto fetch_post = [&](int64_t base) {
+        const int64_t row = base + lanes.team;
+        if (row < c.n) {
+            if (has_a) lanes.load(c.A, c.lda, base, a);
+            if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
+            if (c.gate_cols == 1) t1 = load_one<BF>(c.T, row * c.ldt);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) a[i] = u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    if (base < end) {
+        fetch_pre(base);
+        fetch_post(base);
+    }
     constexpr bool kParked = W == 1 && P > 1;
     __shared__ f32x4 parked[kParked ? P * E : 1][64];
     Vectors<L, 4, P, E, kParked> vec;
@@ -529,17 +543,14 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
         const bool live = base + lanes.team < c.n;
         const float mean_a = st[0], r_a = st[1], mean_h = st[2], r_h = st[3];
         const float row_gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
-        float e_[P][E], hn[P][E], d[P][E], an[P][E], g[P][E];
-        u32x4 a_now[P], t_now[P];
+        float e_[P][E], hn[P][E], d[P][E];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             unpack<BF>(gh[i], e_[i]);
             unpack<BF>(gu[i], d[i]);
             unpack<BF>(h[i], hn[i]);
-            a_now[i] = a[i];
-            t_now[i] = t[i];
         }
-        if (base + L::kRows < end) fetch(base + L::kRows);
+        if (base + L::kRows < end) fetch_pre(base + L::kRows);
         if (has_gu) {
 #pragma unroll
             for (int i = 0; i < P; ++i) {
@@ -574,51 +585,42 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             lanes.store(c.GX, c.ldgx, base, out);
         }
         if (!has_a) continue;
+        // from here on: d = dy p
+        float an[P][E], m[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            unpack<BF>(a_now[i], an[i]);
-            unpack<BF>(t_now[i], g[i]);
-#pragma unroll
-            for (int e = 0; e < E; ++e) an[i][e] = (an[i][e] - mean_a) * r_a;
-        }
-        if (c.gate_cols > 1) {
-#pragma unroll
-            for (int i = 0; i < P; ++i)
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[i][e] = fast_gate(g[i][e]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i)
-#pragma unroll
-                for (int e = 0; e < E; ++e) g[i][e] = row_gate;
-        }
-        // from here on: hn the gate's gradient, d = dy p
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            float p[E], p_bias[E], s[E];
+            float g[E], p[E], p_bias[E], s[E], part[3] = {0.f, 0.f, 0.f};
+            unpack<BF>(a[i], an[i]);
+            unpack<BF>(t[i], g);
             vec.get(0, i, p);
             vec.get(1, i, p_bias);
             vec.get(2, i, s);
 #pragma unroll
+            for (int e = 0; e < E; ++e) g[e] = c.gate_cols > 1 ? fast_gate(g[e]) : row_gate;
+#pragma unroll
             for (int e = 0; e < E; ++e) {
+                an[i][e] = (an[i][e] - mean_a) * r_a;
                 const float y = fmaf(an[i][e], p[e], p_bias[e]);
-                const float branch = e_[i][e] * (c.alpha * g[i][e]), dy = branch * s[e];
+                const float branch = e_[i][e] * (c.alpha * g[e]), dy = branch * s[e];
                 sum[0][i][e] = fmaf(dy, an[i][e], sum[0][i][e]);
                 sum[1][i][e] += dy;
                 sum[2][i][e] = fmaf(branch, y, sum[2][i][e]);
-                hn[i][e] = dy * y * (1.f - g[i][e]);
                 d[i][e] = dy * p[e];
+                g[e] = dy * y * (1.f - g[e]);                          // the gate's gradient
+                const float counted = MASK && e < lanes.skip[i] ? 0.f : d[i][e];
+                part[0] += counted;
+                part[1] = fmaf(counted, an[i][e], part[1]);
+                part[2] += MASK && e < lanes.skip[i] ? 0.f : g[e];
             }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) m[k] += lanes.on[i] ? part[k] : 0.f;
+            out[i] = pack<BF>(g);
         }
-        float m[3] = {0.f, 0.f, 0.f};
-        if (c.post != GAS_NORM_NONE || c.gate_cols == 1) {
-            m[0] = lanes.own(d);
-            m[1] = lanes.own_dot(d, an);
-            if (c.gate_cols == 1) m[2] = lanes.own(hn);
-            row_sums<G, W>(m, red, turn);
-            m[0] = c.post == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
-            m[1] = c.post != GAS_NORM_NONE ? m[1] * inv_f : 0.f;
-        }
+        if (base + L::kRows < end) fetch_post(base + L::kRows);
+        if (c.GT && c.gate_cols > 1 && live) lanes.store(c.GT, c.ldgt, base, out);
+        if (c.post != GAS_NORM_NONE || c.gate_cols == 1) row_sums<G, W>(m, red, turn);
+        m[0] = c.post == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
+        m[1] = c.post != GAS_NORM_NONE ? m[1] * inv_f : 0.f;
         if (!live) continue;
         if (has_ga) {
             const float off = -r_a * m[0], along = -r_a * m[1];
@@ -631,36 +633,39 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             lanes.store(c.GA, c.ldga, base, out);
         }
         if (c.GT && c.gate_cols == 1 && lanes.place == 0) store_one<BF>(c.GT, (base + lanes.team) * c.ldgt, m[2]);
-        if (c.GT && c.gate_cols > 1) {
-#pragma unroll
-            for (int i = 0; i < P; ++i) out[i] = pack<BF>(hn[i]);
-            lanes.store(c.GT, c.ldgt, base, out);
-        }
     }
     // the workgroup's sums: across the teams of a wavefront by moves, across its wavefronts in LDS
     float* to = c.partials + (int64_t)blockIdx.x * 5 * c.F;
+    if constexpr (W > 1) {
 #pragma unroll
-    for (int k = 0; k < 5; ++k) {
-        if (!c.sums[k]) continue;
-        if constexpr (W > 1) {
+        for (int k = 0; k < 5; ++k)
+            if (c.sums[k])
 #pragma unroll
-            for (int i = 0; i < P; ++i)
-                if (lanes.on[i])
+                for (int i = 0; i < P; ++i)
+                    if (lanes.on[i])
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (!MASK || e >= lanes.skip[i]) to[(int64_t)k * c.F + lanes.c[i] + e] = sum[k][i][e];
-        } else {
+                        for (int e = 0; e < E; ++e)
+                            if (!MASK || e >= lanes.skip[i]) to[(int64_t)k * c.F + lanes.c[i] + e] = sum[k][i][e];
+    } else {
 #pragma unroll
-            for (int i = 0; i < P; ++i)
+        for (int k0 = 0; k0 < 5; k0 += kAtOnce) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float v = across_groups<G>(sum[k][i][e]);
-                    if ((threadIdx.x & 63) < G && lanes.on[i] && (!MASK || e >= lanes.skip[i])) columns[threadIdx.x >> 6][lanes.c[i] + e] = v;
-                }
+            for (int k = k0; k < k0 + kAtOnce && k < 5; ++k)
+#pragma unroll
+                for (int i = 0; i < P; ++i)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const float v = across_groups<G>(sum[k][i][e]);
+                        if ((threadIdx.x & 63) < G && lanes.on[i] && (!MASK || e >= lanes.skip[i]))
+                            columns[threadIdx.x >> 6][k - k0][lanes.c[i] + e] = v;
+                    }
             __syncthreads();
-            for (int f = threadIdx.x; f < c.F; f += 256)
-                to[(int64_t)k * c.F + f] = (columns[0][f] + columns[1][f]) + (columns[2][f] + columns[3][f]);
-            __syncthreads();
+#pragma unroll
+            for (int k = k0; k < k0 + kAtOnce && k < 5; ++k)
+                if (c.sums[k])
+                    for (int f = threadIdx.x; f < c.F; f += 256)
+                        to[(int64_t)k * c.F + f] = (columns[0][k - k0][f] + columns[1][k - k0][f]) + (columns[2][k - k0][f] + columns[3][k - k0][f]);
+            if (k0 + kAtOnce < 5) __syncthreads();
         }
     }
 }
@@ -671,8 +676,17 @@ __global__ __launch_bounds__(1024) void residual_norm_finish_kernel(ResidualNorm
     const int k = blockIdx.y, column = threadIdx.x & 15, slot = threadIdx.x >> 4, f = blockIdx.x * 16 + column;
     if (!c.sums[k]) return;
     float sum = 0.f;
-    if (f < c.F)
-        for (int j = slot; j < c.slabs; j += 64) sum += c.partials[((int64_t)j * 5 + k) * c.F + f];
+    if (f < c.F) {
+        const float* at = c.partials + (int64_t)k * c.F + f;
+        const int64_t row = (int64_t)5 * c.F;
+        for (int j0 = 0; j0 < c.slabs; j0 += 512) {          // eight on their way at a time
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = j0 + 64 * i + slot < c.slabs ? at[(j0 + 64 * i + slot) * row] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += x[i];
+        }
+    }
     part[slot][column] = sum;
     __syncthreads();
     for (int o = 32; o > 0; o >>= 1) {
@@ -717,12 +731,14 @@ constexpr int kSlabs = 256;
 // Up to 192 pieces of 16 bytes a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
 // 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 and 115; but 20,000 x 2,000 bf16 262 and 147,
 // where four pieces of bf16 no longer fit the registers.  Element by element 2,000 floats x 20,000 take 890 us, eight wavefronts to a
-// row 258; beyond 1,024 pieces a lane's share spills more than it saves (8,000 x 8,200 bf16: 3.4 ms, element by element 1.7).
+// row 258; beyond 1,024 pieces a lane's share no longer fits (8,000 x 8,200 bf16: backward 3.4 ms with spilt registers, element by
+// element 1.8; forward 0.6 and 0.9).
 // Turns: forward, a workgroup takes few rows, next to each other, so that the rows in flight are one stretch of memory that moves along
 // (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
 // 121, two 129).  Backward, each workgroup leaves partial sums, so there are no more of them than keep memory busy (50,000 x 256
-// bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 625,000 x 256 bf16 504, 506, 504; where a lane has several pieces or a row
-// eight wavefronts 256, 19,997 x 1,433 floats, six wavefronts, 512 workgroups 180 and 256 201).
+// bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 625,000 x 256 bf16 504, 506, 504).  256 are best where a lane has several pieces
+// (80,000 rows of 1,433 bf16 354) or a row many wavefronts (13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x
+// 2,000 bf16, 183 and 148; 19,997 x 1,433 floats, six, 210 and 200).
 struct Layout {
     int g, w, p, turns;
     int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
@@ -737,7 +753,7 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
         for (int w : {16, 12, 8, 6, 4})
             if (pieces <= w * 64) l.w = w;
     const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, all = (n + rows - 1) / rows;
-    const int64_t fewest = !bwd || (l.w == 1 ? l.p == 1 : !bf && l.w < 8) ? 512 : 256, turns = (all + fewest - 1) / fewest;
+    const int64_t fewest = !bwd || (l.p == 1 && l.w <= (bf ? 4 : 6)) ? 512 : 256, turns = (all + fewest - 1) / fewest;
     const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
     l.turns = (int)(bwd ? turns : std::min(turns, most));
     l.blocks = (all + l.turns - 1) / l.turns;
