@@ -10,7 +10,7 @@ namespace gas {
 namespace {
 
 constexpr int kBlock = 256;                         // elements that share a scale: four for every lane
-constexpr int kNormChunk = 16384;                   // elements of a partial sum
+constexpr int kNormChunk = 32768;                   // elements of a partial sum
 // Tensors of a launch: their descriptions fit the 4 KB of a launch's arguments.  Models of few tensors have a launch with room for no more: it is
 // copied for every call.
 constexpr int kNormTensors = 256, kTensors = 144, kFew = 16;
@@ -60,12 +60,12 @@ __global__ __launch_bounds__(256) void sq_norms_kernel(NormBatch<N> b) {
     const int n = whole ? kNormChunk : b.last[k];
     double s[4] = {0.0, 0.0, 0.0, 0.0};
     int i = 4 * threadIdx.x;
-    for (; i + 3 * 1024 + 4 <= n; i += 4 * 1024) {
-        f32x4 v[4];
+    for (; i + 7 * 1024 + 4 <= n; i += 8 * 1024) {
+        f32x4 v[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const four_f32*>(x + i + 1024 * j));
+        for (int j = 0; j < 8; ++j) v[j] = __builtin_nontemporal_load(reinterpret_cast<const four_f32*>(x + i + 1024 * j));
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[e] = fma((double)v[j][e], (double)v[j][e], s[e]);
     }

@@ -126,7 +126,7 @@ __device__ __forceinline__ float across_groups(float v) {
 
 // How a row lies in the lanes: W = 1: in a team of G lanes, 64 / G rows to a wavefront, four wavefronts to a workgroup; W > 1: in the W
 // wavefronts of a workgroup (G = 64).  A lane has P pieces of 16 bytes.  MASK: F is no multiple of a piece; the last piece is the
-// row's last 16 bytes then, and what of them the piece before has already is left out of the sums (both store the same values there).
+// row's last 16 bytes then, and what of them the piece before has already is left out of the sums.
 template <bool BF, int G, int W, int P, bool MASK>
 struct RowLanes {
     static constexpr int E = Elems<BF>::E, EB = BF ? 2 : 4;
@@ -165,12 +165,27 @@ struct RowLanes {
     __device__ __forceinline__ void store(char* m, int64_t ld, int64_t base, const u32x4 (&v)[P]) const {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + base * ld * EB + offset(ld, i)));
+            if (on[i]) store_piece(m + base * ld * EB + offset(ld, i), i, v[i]);
     }
     __device__ __forceinline__ void store_at(char* m, int64_t ld, int64_t row, const u32x4 (&v)[P]) const {
 #pragma unroll
         for (int i = 0; i < P; ++i)
-            if (on[i]) __builtin_nontemporal_store(v[i], reinterpret_cast<piece*>(m + (row * ld + c[i]) * EB));
+            if (on[i]) store_piece(m + (row * ld + c[i]) * EB, i, v[i]);
+    }
+    // Where an output lies in its input, another wavefront may have stored what this lane then reads as the elements that it does not own:
+    // across wavefronts it stores its own only.  Within one, all of a row is read before any of it is stored.
+    __device__ __forceinline__ void store_piece(char* at, int i, const u32x4& v) const {
+        if constexpr (MASK && W > 1)
+            if (skip[i]) {
+#pragma unroll
+                for (int e = 1; e < E; ++e)
+                    if (e >= skip[i]) {
+                        if constexpr (BF) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
+                        else reinterpret_cast<uint32_t*>(at)[e] = v[e];
+                    }
+                return;
+            }
+        __builtin_nontemporal_store(v, reinterpret_cast<piece*>(at));
     }
     __device__ __forceinline__ void vector(const float* v, float otherwise, float (&x)[P][E]) const {
         typedef f32x4 piece __attribute__((aligned(4)));
@@ -552,9 +567,10 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
         }
         if (base + L::kRows < end) fetch_pre(base + L::kRows);
         if (has_gu) {
+            float m[2] = {0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < P; ++i) {
-                float q[E];
+                float q[E], part[2] = {0.f, 0.f};
                 vec.get(3, i, q);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
@@ -562,16 +578,16 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
                     sum[3][i][e] = fmaf(d[i][e], hn[i][e], sum[3][i][e]);
                     sum[4][i][e] += d[i][e];
                     d[i][e] *= q[e];
+                    const float counted = MASK && e < lanes.skip[i] ? 0.f : d[i][e];
+                    part[0] += counted;
+                    part[1] = fmaf(counted, hn[i][e], part[1]);
                 }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) m[k] += lanes.on[i] ? part[k] : 0.f;
             }
-            float m[2] = {0.f, 0.f};
-            if (c.pre != GAS_NORM_NONE) {
-                m[0] = lanes.own(d);
-                m[1] = lanes.own_dot(d, hn);
-                row_sums<G, W>(m, red, turn);
-                m[0] = c.pre == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
-                m[1] *= inv_f;
-            }
+            if (c.pre != GAS_NORM_NONE) row_sums<G, W>(m, red, turn);
+            m[0] = c.pre == GAS_NORM_LAYER ? m[0] * inv_f : 0.f;
+            m[1] = c.pre != GAS_NORM_NONE ? m[1] * inv_f : 0.f;
             const float off = -r_h * m[0], along = -r_h * m[1];
 #pragma unroll
             for (int i = 0; i < P; ++i)

@@ -234,7 +234,7 @@ def test_unpack(n, dtype):
     gas.gas_adamw_unpack(m[:0], v[:0], scales[:0], out[0][:0], out[1][:0])
 
 
-@pytest.mark.parametrize("sizes", [[], [0], [1], [3, 0, 5], [16384], [16385, 1, 40_000], [(911 * i) % 20_000 for i in range(260)], [5_000_001], [12] * 700])
+@pytest.mark.parametrize("sizes", [[], [0], [1], [3, 0, 5], [16384], [16385, 1, 40_000], [32_768], [32_769, 65_536], [(911 * i) % 20_000 for i in range(260)], [5_000_001], [12] * 700])
 @pytest.mark.parametrize("offset", [0, 1])
 def test_squared_norm(sizes, offset):
     gen = torch.Generator().manual_seed(3)
