@@ -541,7 +541,7 @@ GAS_API gas_status gas_sq_norms(int32_t count, const float* const* x, const int6
  * AdamW with decoupled weight decay on `count` tensors, which share launches:
  *     g = c dW,  m <- beta1 m + rate1 g,  v <- beta2 v + rate2 g^2,  beta = 1 - rate,
  *     W <- W - lr wd W - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
- * The rates are what is passed: 1 - 0.999 from a float has lost five of its digits.
+ * The rates are what is passed: 1 - 0.999 from a float has lost five of its digits.  eps: a normal number.
  * W, dtypes (a gas_dtype each), n, dW, weight_decay (NULL: none): host arrays of `count`; W[i], dW[i] (fp32): n[i] contiguous
  * elements.  Tensors that share memory are updated in order; a gradient must not overlap a tensor of the call.
  * t: `step` >= 1, or, if `steps` is given, what it holds on the device, >= 1 (so a captured step counts on).  c = 1, or with sq_norm (fp32[1],

@@ -61,8 +61,7 @@ __device__ __forceinline__ void row_stats(int kind, int F, float eps, V value, f
     *r = 1.f / sqrtf(wave_sum(sq) / (float)F + eps);
 }
 
-// Rows that are narrower than a piece of 16 bytes or do not fit the registers: a wavefront to a row, element by element, read anew for every
-// sum.
+// Rows that do not fit the registers: a wavefront to a row, element by element, read anew for every sum.
 template <bool BF>
 __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm c) {
     const int lane = threadIdx.x & 63;
@@ -95,9 +94,9 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm c) {
 // swaps of rows of 16 and of halves beyond.  Through LDS (shuffles) a step takes some 60 cycles, this way some 8.
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));            // quad_perm 1 0 3 2
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));            // quad_perm 2 3 0 1
-    v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));           // row_half_mirror
+    if constexpr (G >= 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xB1, 0xf, 0xf, true));     // quad_perm 1 0 3 2
+    if constexpr (G >= 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4E, 0xf, 0xf, true));     // quad_perm 2 3 0 1
+    if constexpr (G >= 8) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true));    // row_half_mirror
     if constexpr (G >= 16) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x140, 0xf, 0xf, true));   // row_mirror
     if constexpr (G >= 32) {
         const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -112,7 +111,10 @@ __device__ __forceinline__ float group_sum(float v) {
 // The same over the lanes with the same place in their groups of G: what the groups of a wavefront have between them.
 template <int G>
 __device__ __forceinline__ float across_groups(float v) {
-    if constexpr (G <= 8) v += other_half(v);
+    if constexpr (G <= 1) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x121, 0xf, 0xf, true));    // row_ror:1
+    if constexpr (G <= 2) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x122, 0xf, 0xf, true));    // row_ror:2
+    if constexpr (G <= 4) v += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x124, 0xf, 0xf, true));    // row_ror:4
+    if constexpr (G <= 8) v += other_half(v);                                                                         // row_ror:8
     if constexpr (G <= 16) {
         const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(s[0]) + __uint_as_float(s[1]);
@@ -132,6 +134,7 @@ struct RowLanes {
     static constexpr int E = Elems<BF>::E, EB = BF ? 2 : 4;
     static constexpr int kThreads = W == 1 ? 256 : W * 64;
     static constexpr int kRows = W == 1 ? 4 * (64 / G) : 1;           // of a workgroup at a time
+    static constexpr bool kTiny = MASK && G == 1;                     // a row is narrower than a piece: its elements are the piece's last ones, one by one
     static_assert(W == 1 || G == 64, "several wavefronts have all of their lanes");
     int place, team, c[P], skip[P];      // place in the row's lanes, row among the wavefront's; a piece's first element, and its elements that another piece has
     bool on[P];                          // a lane behind the row's end loads its first piece and neither counts nor stores it
@@ -155,12 +158,28 @@ struct RowLanes {
     static __device__ __forceinline__ int64_t first(int turns) {
         return (int64_t)blockIdx.x * turns * kRows + (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / G) : 0);
     }
-    __device__ __forceinline__ uint32_t offset(int64_t ld, int i) const { return (uint32_t)(team * (int)ld + c[i]) * EB; }
+    __device__ __forceinline__ auto offset(int64_t ld, int i) const {
+        if constexpr (kTiny) return (team * ld + c[i]) * EB;          // may lie before the first row
+        else return (uint32_t)(team * (int)ld + c[i]) * EB;
+    }
     // 16 bytes of any alignment: the same load
     typedef u32x4 piece __attribute__((aligned(2)));
     __device__ __forceinline__ void load(const char* m, int64_t ld, int64_t base, u32x4 (&v)[P]) const {
 #pragma unroll
-        for (int i = 0; i < P; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(m + base * ld * EB + offset(ld, i)));
+        for (int i = 0; i < P; ++i) {
+            const char* at = m + base * ld * EB + offset(ld, i);
+            if constexpr (kTiny) {
+                v[i] = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int e = 1; e < E; ++e)
+                    if (e >= skip[i]) {
+                        if constexpr (BF) v[i][e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(at)[e] << (16 * (e & 1));
+                        else v[i][e] = reinterpret_cast<const uint32_t*>(at)[e];
+                    }
+            } else {
+                v[i] = __builtin_nontemporal_load(reinterpret_cast<const piece*>(at));
+            }
+        }
     }
     __device__ __forceinline__ void store(char* m, int64_t ld, int64_t base, const u32x4 (&v)[P]) const {
 #pragma unroll
@@ -175,7 +194,7 @@ struct RowLanes {
     // Where an output lies in its input, another wavefront may have stored what this lane then reads as the elements that it does not own:
     // across wavefronts it stores its own only.  Within one, all of a row is read before any of it is stored.
     __device__ __forceinline__ void store_piece(char* at, int i, const u32x4& v) const {
-        if constexpr (MASK && W > 1)
+        if constexpr (MASK && (W > 1 || kTiny))
             if (skip[i]) {
 #pragma unroll
                 for (int e = 1; e < E; ++e)
@@ -194,7 +213,13 @@ struct RowLanes {
 #pragma unroll
             for (int e = 0; e < E; e += 4) {
                 f32x4 w = {otherwise, otherwise, otherwise, otherwise};
-                if (v) w = *reinterpret_cast<const piece*>(v + c[i] + e);
+                if constexpr (kTiny) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (v && e + j >= skip[i]) w[j] = v[c[i] + e + j];
+                } else if (v) {
+                    w = *reinterpret_cast<const piece*>(v + c[i] + e);
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) x[i][e + j] = w[j];
             }
@@ -743,8 +768,10 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
 
 constexpr int kSlabs = 256;
 
-// How rows of F elements lie in lanes (RowLanes), and the workgroups' turns; w = 0: too narrow or too wide for registers, element by element.
-// Up to 192 pieces of 16 bytes a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
+// How rows of F elements lie in lanes (RowLanes), and the workgroups' turns; w = 0: too wide for registers, element by element.
+// A team has as many lanes as the row has pieces of 16 bytes, rounded up to a power of two (3 M rows of 8 bf16, us: forward 42, in teams of eight
+// 214; backward 84 and 294; of 16 floats 149 and 188, 305 and 318).
+// Up to 192 pieces a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
 // 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 and 115; but 20,000 x 2,000 bf16 262 and 147,
 // where four pieces of bf16 no longer fit the registers.  Element by element 2,000 floats x 20,000 take 890 us, eight wavefronts to a
 // row 258; beyond 1,024 pieces a lane's share no longer fits (8,000 x 8,200 bf16: backward 3.4 ms with spilt registers, element by
@@ -762,9 +789,11 @@ struct Layout {
 inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld) {
     const int e = bf ? 8 : 4, pieces = (F + e - 1) / e;
     Layout l = {64, 1, 1, 1, 0, 0};
-    if (F < e || pieces > 1024) return {0, 0, 0, 0, 0, 0};
-    if (pieces <= 64) l.g = pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
-    else if (pieces <= 192) l.p = (pieces + 63) / 64;
+    if (pieces > 1024) return {0, 0, 0, 0, 0, 0};
+    if (pieces <= 64)
+        while (l.g / 2 >= pieces) l.g /= 2;
+    else if (pieces <= 192)
+        l.p = (pieces + 63) / 64;
     else
         for (int w : {16, 12, 8, 6, 4})
             if (pieces <= w * 64) l.w = w;
@@ -791,6 +820,7 @@ void launch_rows(const Layout& l, dim3 grid, hipStream_t s, const C& c) {
         else hipLaunchKernelGGL((residual_norm_rows_kernel<BF, G, W, P, MASK, ALL>), grid, block, 0, s, c);                           \
         return;                                                                                                                       \
     }
+    if constexpr (!ALL) { GAS_ROWS(1, 1, 1) GAS_ROWS(2, 1, 1) GAS_ROWS(4, 1, 1) }
     GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 1) GAS_ROWS(64, 1, 2) GAS_ROWS(64, 1, 3)
     GAS_ROWS(64, 4, 1) GAS_ROWS(64, 6, 1) GAS_ROWS(64, 8, 1) GAS_ROWS(64, 12, 1) GAS_ROWS(64, 16, 1)
 #undef GAS_ROWS
@@ -803,6 +833,7 @@ void launch_rows(const Layout& l, bool bf, hipStream_t s, C& c) {
     bool all;
     if constexpr (std::is_same_v<C, ResidualNormBwd>) all = c.GH && c.GU && c.A && c.GX && c.GA && c.stats;
     else all = c.A && c.H && c.U && !c.hist;
+    all = all && l.g >= 8;
 #define GAS_ROWS(BF, MASK, ALL) \
     if (bf == BF && mask == MASK && all == ALL) return launch_rows<BF, MASK, ALL>(l, grid, s, c);
     GAS_ROWS(false, false, false) GAS_ROWS(false, false, true) GAS_ROWS(false, true, false) GAS_ROWS(false, true, true)

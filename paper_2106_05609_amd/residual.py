@@ -147,6 +147,8 @@ class AdamW:
         if bits not in (8, 32):
             raise ValueError(f"AdamW: states of {bits} bits")
         self.tensors, self.lr, self.max_norm = list(tensors), lr, max_norm
+        if not self.tensors:
+            raise ValueError("AdamW: no tensors")
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps)
         dev = self.tensors[0].device
         self.steps, self.sq_norm = torch.zeros(1, dtype=torch.int32, device=dev), torch.zeros(1, device=dev)

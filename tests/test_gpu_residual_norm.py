@@ -13,7 +13,7 @@ from tests import residual_reference as R
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
-SIZES = [(1, 1), (3, 2), (2, 3), (5, 7), (4, 8), (67, 8), (33, 31), (130, 47), (1, 64), (257, 64), (66, 65), (63, 100), (129, 128), (1000, 200), (1, 256),
+SIZES = [(1, 1), (3, 2), (2, 3), (5, 7), (4, 8), (67, 8), (700, 5), (260, 9), (513, 12), (301, 16), (1030, 4), (130, 24), (33, 31), (130, 47), (1, 64), (257, 64), (66, 65), (63, 100), (129, 128), (1000, 200), (1, 256),
          (300, 256), (31, 257), (40, 512), (9, 520), (21, 1000), (19, 1433), (7, 2048), (6, 2049), (5, 4100), (3, 8200), (2, 16384), (2, 16390)]
 
 
