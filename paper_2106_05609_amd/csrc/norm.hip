@@ -135,6 +135,7 @@ struct RowLanes {
     static constexpr int kThreads = W == 1 ? 256 : W * 64;
     static constexpr int kRows = W == 1 ? 4 * (64 / G) : 1;           // of a workgroup at a time
     static constexpr bool kTiny = MASK && G == 1;                     // a row is narrower than a piece: its elements are the piece's last ones, one by one
+    static constexpr bool kAlone = G == 64;                           // a wavefront has one row at a time: the loop's bound is enough
     static_assert(W == 1 || G == 64, "several wavefronts have all of their lanes");
     int place, team, c[P], skip[P];      // place in the row's lanes, row among the wavefront's; a piece's first element, and its elements that another piece has
     bool on[P];                          // a lane behind the row's end loads its first piece and neither counts nor stores it
@@ -333,7 +334,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     int32_t to = 0;
     auto fetch = [&](int64_t base) {
         const int64_t row = base + lanes.team;
-        if (row < c.n) {
+        if (L::kAlone || row < c.n) {
             lanes.load(c.X, c.ldx, base, x);
             if (has_a) lanes.load(c.A, c.lda, base, a);
             if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
@@ -358,7 +359,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     const bool normed = has_u || push || c.stats;
     for (; base < end; base += L::kRows) {
         if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
-        const bool live = base + lanes.team < c.n;
+        const bool live = L::kAlone || base + lanes.team < c.n;
         float h[P][E], y[P][E], g[P][E];
         const float gate = c.alpha * (c.gate_cols == 1 ? fast_gate(t1) : 1.f);
         const int64_t place = to;
@@ -535,7 +536,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     // has been used, into the same registers.
     auto fetch_pre = [&](int64_t base) {
         const int64_t row = base + lanes.team;
-        if (row < c.n) {
+        if (L::kAlone || row < c.n) {
             if (has_gh) lanes.load(c.GH, c.ldgh, base, gh);
             if (has_gu) lanes.load(c.GU, c.ldgu, base, gu);
             if (has_gu) lanes.load(c.H, c.ldh, base, h);
@@ -548,7 +549,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     };
     auto fetch_post = [&](int64_t base) {
         const int64_t row = base + lanes.team;
-        if (row < c.n) {
+        if (L::kAlone || row < c.n) {
             if (has_a) lanes.load(c.A, c.lda, base, a);
             if (c.gate_cols > 1) lanes.load(c.T, c.ldt, base, t);
             if (c.gate_cols == 1) t1 = load_one<BF>(c.T, row * c.ldt);
@@ -580,7 +581,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     const float inv_f = 1.f / (float)c.F;
     for (; base < end; base += L::kRows) {
         if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
-        const bool live = base + lanes.team < c.n;
+        const bool live = L::kAlone || base + lanes.team < c.n;
         const float mean_a = st[0], r_a = st[1], mean_h = st[2], r_h = st[3];
         const float row_gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
         float e_[P][E], hn[P][E], d[P][E];
@@ -636,8 +637,14 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             vec.get(0, i, p);
             vec.get(1, i, p_bias);
             vec.get(2, i, s);
+            if (c.gate_cols > 1) {               // a branch, not a choice of both: 11 issue slots an element
 #pragma unroll
-            for (int e = 0; e < E; ++e) g[e] = c.gate_cols > 1 ? fast_gate(g[e]) : row_gate;
+                for (int e = 0; e < E; ++e) g[e] = fast_gate(g[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] = row_gate;
+            }
+            float w[E];                          // dy y: of it the gate's gradient is a part
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 an[i][e] = (an[i][e] - mean_a) * r_a;
@@ -647,15 +654,22 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
                 sum[1][i][e] += dy;
                 sum[2][i][e] = fmaf(branch, y, sum[2][i][e]);
                 d[i][e] = dy * p[e];
-                g[e] = dy * y * (1.f - g[e]);                          // the gate's gradient
+                w[e] = dy * y;
                 const float counted = MASK && e < lanes.skip[i] ? 0.f : d[i][e];
                 part[0] += counted;
                 part[1] = fmaf(counted, an[i][e], part[1]);
-                part[2] += MASK && e < lanes.skip[i] ? 0.f : g[e];
+            }
+            if (c.gate_cols > 1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) w[e] *= 1.f - g[e];
+                out[i] = pack<BF>(w);
+            } else if (c.gate_cols == 1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) part[2] += MASK && e < lanes.skip[i] ? 0.f : w[e];
+                part[2] *= 1.f - row_gate;
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k) m[k] += lanes.on[i] ? part[k] : 0.f;
-            out[i] = pack<BF>(g);
         }
         if (base + L::kRows < end) fetch_post(base + L::kRows);
         if (c.GT && c.gate_cols > 1 && live) lanes.store(c.GT, c.ldgt, base, out);
