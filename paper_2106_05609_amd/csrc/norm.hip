@@ -1,7 +1,7 @@
 // Norms before and after a block, with the block's gate, its residual scale and the residual stream, forward and backward:
 //     y = N_post(a) p + p_bias,   h = x + alpha s sigmoid(t) y,   u = N_pre(h) q + q_bias.
-// Statistics, sums and the row itself in 32 bits, each output rounded once.  Bound by memory: forward 3.1 M x 256 bf16 1.27 ms, 6.3 TB/s of
-// the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.94 ms, 5.2 TB/s of 4.9 GB.
+// Statistics, sums and the row itself in 32 bits, each output rounded once.  Bound by memory: forward 3.1 M x 256 bf16 1.29 ms, 6.2 TB/s of
+// the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.95 ms, 5.2 TB/s of 4.9 GB.
 #include <algorithm>
 #include <type_traits>
 
@@ -790,7 +790,7 @@ constexpr int kSlabs = 256;
 // A team has as many lanes as the row has pieces of 16 bytes, rounded up to a power of two (3 M rows of 8 bf16, us: forward 42, in teams of eight
 // 214; backward 84 and 294; of 16 floats 149 and 188, 305 and 318).
 // Up to 192 pieces a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
-// 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 and 115; but 20,000 x 2,000 bf16 262 and 147,
+// 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 (92 since) and 115; but 20,000 x 2,000 bf16 262 and 147,
 // where four pieces of bf16 no longer fit the registers.  Element by element 2,000 floats x 20,000 take 890 us, eight wavefronts to a
 // row 258; beyond 1,024 pieces a lane's share no longer fits (8,000 x 8,200 bf16: backward 3.4 ms with spilt registers, element by
 // element 1.8; forward 0.6 and 0.9).
@@ -798,7 +798,7 @@ constexpr int kSlabs = 256;
 // (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
 // 121, two 129).  Backward, each workgroup leaves partial sums, so there are no more of them than keep memory busy (50,000 x 256
 // bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 625,000 x 256 bf16 504, 506, 504).  256 are best where a lane has several pieces
-// (80,000 rows of 1,433 bf16 354) or a row many wavefronts (13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x
+// (19,997 x 1,433 bf16 108, with 512 123) or a row many wavefronts (13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x
 // 2,000 bf16, 183 and 148; 19,997 x 1,433 floats, six, 210 and 200).
 struct Layout {
     int g, w, p, turns;
