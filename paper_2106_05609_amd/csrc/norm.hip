@@ -1,7 +1,7 @@
 // Norms before and after a block, with the block's gate, its residual scale and the residual stream, forward and backward:
 //     y = N_post(a) p + p_bias,   h = x + alpha s sigmoid(t) y,   u = N_pre(h) q + q_bias.
 // Statistics, sums and the row itself in 32 bits, each output rounded once.  Bound by memory: forward 3.1 M x 256 bf16 1.29 ms, 6.2 TB/s of
-// the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.95 ms, 5.2 TB/s of 4.9 GB.
+// the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.87 ms, 5.6 TB/s of 4.9 GB.
 #include <algorithm>
 #include <type_traits>
 
@@ -729,30 +729,34 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
     }
 }
 
-// Sums over the workgroups' sums: 16 columns to a workgroup, 64 of the partial rows side by side, added up in order.
-__global__ __launch_bounds__(1024) void residual_norm_finish_kernel(ResidualNormBwd c) {
-    __shared__ float part[64][17];
-    const int k = blockIdx.y, column = threadIdx.x & 15, slot = threadIdx.x >> 4, f = blockIdx.x * 16 + column;
+// Sums over the workgroups' sums: COLUMNS columns to a workgroup, 1,024 / COLUMNS of the partial rows side by side, added up in order.  Thousands of them
+// are added up in two launches, first `per` at a time onto `onto`, by 64 columns so that a load is a stretch of 256 bytes.
+template <int COLUMNS>
+__global__ __launch_bounds__(1024) void residual_norm_finish_kernel(ResidualNormBwd c, const float* from, int slabs, int per, float* onto) {
+    constexpr int kSlots = 1024 / COLUMNS;
+    __shared__ float part[kSlots][COLUMNS + 1];
+    const int k = blockIdx.y, column = threadIdx.x % COLUMNS, slot = threadIdx.x / COLUMNS, f = blockIdx.x * COLUMNS + column;
     if (!c.sums[k]) return;
+    const int first = blockIdx.z * per, end = min(slabs, first + per);
     float sum = 0.f;
     if (f < c.F) {
-        const float* at = c.partials + (int64_t)k * c.F + f;
+        const float* at = from + (int64_t)k * c.F + f;
         const int64_t row = (int64_t)5 * c.F;
-        for (int j0 = 0; j0 < c.slabs; j0 += 512) {          // eight on their way at a time
+        for (int j0 = first + slot; j0 < end; j0 += 8 * kSlots) {          // eight on their way at a time
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = j0 + 64 * i + slot < c.slabs ? at[(j0 + 64 * i + slot) * row] : 0.f;
+            for (int i = 0; i < 8; ++i) x[i] = j0 + kSlots * i < end ? at[(j0 + kSlots * i) * row] : 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += x[i];
         }
     }
     part[slot][column] = sum;
     __syncthreads();
-    for (int o = 32; o > 0; o >>= 1) {
+    for (int o = kSlots / 2; o > 0; o >>= 1) {
         if (slot < o) part[slot][column] += part[slot + o][column];
         __syncthreads();
     }
-    if (slot == 0 && f < c.F) c.sums[k][f] = part[0][column];
+    if (slot == 0 && f < c.F) (onto ? onto + ((int64_t)blockIdx.z * 5 + k) * c.F : c.sums[k])[f] = part[0][column];
 }
 
 template <bool BF>
@@ -784,7 +788,7 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
     if (c.GT && c.gate_cols == 1 && lane == 0) store_one<BF>(c.GT, row * c.ldgt, sg);
 }
 
-constexpr int kSlabs = 256;
+constexpr int kSlabs = 256, kSplits = 32;          // kSplits: parts that thousands of partial sums are added up in
 
 // How rows of F elements lie in lanes (RowLanes), and the workgroups' turns; w = 0: too wide for registers, element by element.
 // A team has as many lanes as the row has pieces of 16 bytes, rounded up to a power of two (3 M rows of 8 bf16, us: forward 42, in teams of eight
@@ -796,10 +800,11 @@ constexpr int kSlabs = 256;
 // element 1.8; forward 0.6 and 0.9).
 // Turns: forward, a workgroup takes few rows, next to each other, so that the rows in flight are one stretch of memory that moves along
 // (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
-// 121, two 129).  Backward, each workgroup leaves partial sums, so there are no more of them than keep memory busy (50,000 x 256
-// bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 625,000 x 256 bf16 504, 506, 504).  256 are best where a lane has several pieces
-// (19,997 x 1,433 bf16 108, with 512 123) or a row many wavefronts (13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x
-// 2,000 bf16, 183 and 148; 19,997 x 1,433 floats, six, 210 and 200).
+// 121, two 129).  Backward, each workgroup leaves partial sums, so of up to 32,768 turns in all there are no more of them than keep memory
+// busy (50,000 x 256 bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 256 are best where a lane has several pieces, 19,997 x 1,433 bf16 108, with 512
+// 123, or a row many wavefronts, 13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x 2,000 bf16, 183 and 148).  Of more turns
+// what few turns save outweighs the sums: 512 workgroups and 16, 8, 4, 2 turns: 600,000 x 256 floats 940, 922, 913, 888, 934, 1 M x 256 bf16 803, 751,
+// 730, 771, 947, 1 M x 47 floats 345, 331, 296, 279; 200,000 x 256 floats 324, 317, 303, 309, 302; but two pieces of bf16, 200,000 x 600, 450, 517, 552.
 struct Layout {
     int g, w, p, turns;
     int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
@@ -818,9 +823,12 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, all = (n + rows - 1) / rows;
     const int64_t fewest = !bwd || (l.p == 1 && l.w <= (bf ? 4 : 6)) ? 512 : 256, turns = (all + fewest - 1) / fewest;
     const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
-    l.turns = (int)(bwd ? (all <= 4 ? all : turns) : std::min(turns, most));      // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
+    const bool many = bwd && l.w == 1 && (l.p == 1 || !bf) && all >= 32768;
+    if (!bwd) l.turns = (int)std::min(turns, most);
+    else if (many) l.turns = bf || all < 65536 ? 8 : 4;
+    else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
     l.blocks = (all + l.turns - 1) / l.turns;
-    l.most_blocks = std::min(all, fewest);
+    l.most_blocks = many ? l.blocks : std::min(all, fewest);
     if (longest_ld > (1 << 26)) {        // rows of a wavefront lie within 32 bits of each other, or there is one
         l.turns *= 64 / l.g;
         l.g = 64;
@@ -857,6 +865,20 @@ void launch_rows(const Layout& l, bool bf, hipStream_t s, C& c) {
     GAS_ROWS(false, false, false) GAS_ROWS(false, false, true) GAS_ROWS(false, true, false) GAS_ROWS(false, true, true)
     GAS_ROWS(true, false, false) GAS_ROWS(true, false, true) GAS_ROWS(true, true, false) GAS_ROWS(true, true, true)
 #undef GAS_ROWS
+}
+
+gas_status finish_sums(const ResidualNormBwd& c, int slabs, float* spare, hipStream_t s) {
+    const float* from = c.partials;
+    if (slabs > 1024) {
+        const int per = ((slabs + kSplits - 1) / kSplits + 127) / 128 * 128, parts = (slabs + per - 1) / per;
+        hipLaunchKernelGGL(residual_norm_finish_kernel<64>, dim3((unsigned)((c.F + 63) / 64), 5, parts), dim3(1024), 0, s, c, from, slabs, per, spare);
+        GAS_CHECK_HIP(hipGetLastError());
+        from = spare;
+        slabs = parts;
+    }
+    hipLaunchKernelGGL(residual_norm_finish_kernel<16>, dim3((unsigned)((c.F + 15) / 16), 5), dim3(1024), 0, s, c, from, slabs, slabs, nullptr);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
 }
 
 inline bool valid_norm(int k) { return k == GAS_NORM_NONE || k == GAS_NORM_RMS || k == GAS_NORM_LAYER; }
@@ -939,7 +961,7 @@ int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F) {
     int64_t most = 0;                         // of both types
     for (int bf = 0; bf < 2; ++bf) {
         const Layout l = layout_of(n_rows, F, bf, true, 0);
-        const int64_t floats = l.w ? l.most_blocks * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
+        const int64_t floats = l.w ? (l.most_blocks + (l.most_blocks > 1024 ? kSplits : 0)) * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
         most = floats > most ? floats : most;
     }
     return most * 4;
@@ -959,12 +981,9 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     ResidualNormBwd c;
     c.sums[0] = gp; c.sums[1] = gp_bias; c.sums[2] = gs; c.sums[3] = gq; c.sums[4] = gq_bias;
     c.F = F; c.n = n_rows; c.slabs = 0; c.partials = nullptr;
-    const dim3 finish((unsigned)((F + 15) / 16), 5);
     if (n_rows == 0) {                        // an empty sum still has to be written
         if (!sums) return GAS_OK;
-        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
-        GAS_CHECK_HIP(hipGetLastError());
-        return GAS_OK;
+        return finish_sums(c, 0, nullptr, st);
     }
     GAS_REQUIRE(GH || GU, "%s: null pointer", who);
     GAS_REQUIRE(valid_norm(norm_post) && valid_norm(norm_pre), "%s: unknown norm %d, %d", who, norm_post, norm_pre);
@@ -1005,9 +1024,7 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
         c.slabs = (int)l.blocks;
         launch_rows(l, dt == GAS_BF16, st, c);
         GAS_CHECK_HIP(hipGetLastError());
-        if (sums && c.slabs > 1) hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
-        GAS_CHECK_HIP(hipGetLastError());
-        return GAS_OK;
+        return sums && c.slabs > 1 ? finish_sums(c, c.slabs, c.partials + l.most_blocks * 5 * F, st) : GAS_OK;
     }
     c.row_sums = c.partials + (int64_t)kSlabs * 5 * F;
     c.rows_per_slab = (n_rows + kSlabs - 1) / kSlabs;
@@ -1021,8 +1038,8 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
         hipLaunchKernelGGL(bf ? residual_norm_columns_kernel<true> : residual_norm_columns_kernel<false>,
                            dim3((unsigned)((F + 63) / 64), (unsigned)c.slabs), dim3(256), 0, st, c);
         GAS_CHECK_HIP(hipGetLastError());
-        hipLaunchKernelGGL(residual_norm_finish_kernel, finish, dim3(1024), 0, st, c);
-        GAS_CHECK_HIP(hipGetLastError());
+        const gas_status got = finish_sums(c, c.slabs, nullptr, st);
+        if (got != GAS_OK) return got;
     }
     if (GX || GA || GT) {
         hipLaunchKernelGGL(bf ? residual_norm_bwd_kernel<true> : residual_norm_bwd_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, c);

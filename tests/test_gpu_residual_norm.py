@@ -309,6 +309,15 @@ def test_many_rows():
     assert torch.equal(u, want["u"]) and torch.equal(far, near["x"])
 
 
+@pytest.mark.parametrize("n,f,dtype", [(600_001, 8, "f32"), (530_003, 64, "f32"), (1_100_003, 8, "bf16"), (300_007, 40, "bf16")])
+def test_sums_over_thousands_of_workgroups(n, f, dtype):
+    """So many rows that the workgroups' sums are added up in two launches."""
+    c, mat = make(n, f, dtype, 2)
+    fwd = run_forward(c, 2, 2)
+    gh, gu = mat(f), mat(f)
+    compare_backward(c, fwd, gh, gu, 2, 2, run_backward(c, fwd, gh, gu, 2, 2), dtype)
+
+
 def test_no_rows():
     c, mat = make(0, 64, "f32", 2)
     fwd = run_forward(c, 2, 2)
