@@ -800,11 +800,13 @@ constexpr int kSlabs = 256, kSplits = 32;          // kSplits: parts that thousa
 // element 1.8; forward 0.6 and 0.9).
 // Turns: forward, a workgroup takes few rows, next to each other, so that the rows in flight are one stretch of memory that moves along
 // (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
-// 121, two 129).  Backward, each workgroup leaves partial sums, so of up to 32,768 turns in all there are no more of them than keep memory
+// 121, two 129).  Backward, each workgroup leaves partial sums, so of few turns in all there are no more of them than keep memory
 // busy (50,000 x 256 bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 256 are best where a lane has several pieces, 19,997 x 1,433 bf16 108, with 512
 // 123, or a row many wavefronts, 13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x 2,000 bf16, 183 and 148).  Of more turns
-// what few turns save outweighs the sums: 512 workgroups and 16, 8, 4, 2 turns: 600,000 x 256 floats 940, 922, 913, 888, 934, 1 M x 256 bf16 803, 751,
-// 730, 771, 947, 1 M x 47 floats 345, 331, 296, 279; 200,000 x 256 floats 324, 317, 303, 309, 302; but two pieces of bf16, 200,000 x 600, 450, 517, 552.
+// what few turns save outweighs the sums: by 512 workgroups and by 16, 8, 4, 2 turns: 1 M x 256 bf16 813, 763, 727, 779, 999; 600,000 x 256 floats 956, 921,
+// 906, 875, 909; 1 M x 47 floats 352, 333, 300, 282, 315; 100,000 x 256 floats 166, 166, 156, 159, 154, but 25,000 45, -, 48, 48.  Not with bf16 in rows that
+// leave a quarter of the lanes without a piece, 1 M x 136 487, 521, 567, 682, or that give them two, 200,000 x 600 456, 524, 565, 676, 917: there the
+// sums weigh more (three quarters, 1 M x 192, 624, 593, 609, 707; 28 of 32 lanes, 1 M x 224, 724, 678, 670, 738).
 struct Layout {
     int g, w, p, turns;
     int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
@@ -823,9 +825,9 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, all = (n + rows - 1) / rows;
     const int64_t fewest = !bwd || (l.p == 1 && l.w <= (bf ? 4 : 6)) ? 512 : 256, turns = (all + fewest - 1) / fewest;
     const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
-    const bool many = bwd && l.w == 1 && (l.p == 1 || !bf) && all >= 32768;
+    const bool many = bwd && l.w == 1 && (bf ? l.p == 1 && 4 * pieces > 3 * l.g && all >= 32768 : all >= 16384);
     if (!bwd) l.turns = (int)std::min(turns, most);
-    else if (many) l.turns = bf || all < 65536 ? 8 : 4;
+    else if (many) l.turns = bf || all < 32768 ? 8 : 4;
     else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
     l.blocks = (all + l.turns - 1) / l.turns;
     l.most_blocks = many ? l.blocks : std::min(all, fewest);

@@ -309,7 +309,7 @@ def test_many_rows():
     assert torch.equal(u, want["u"]) and torch.equal(far, near["x"])
 
 
-@pytest.mark.parametrize("n,f,dtype", [(600_001, 8, "f32"), (530_003, 64, "f32"), (1_100_003, 8, "bf16"), (300_007, 40, "bf16")])
+@pytest.mark.parametrize("n,f,dtype", [(600_001, 8, "f32"), (530_003, 64, "f32"), (1_100_003, 8, "bf16"), (300_007, 40, "bf16"), (131_101, 505, "bf16"), (65_601, 700, "f32")])
 def test_sums_over_thousands_of_workgroups(n, f, dtype):
     """So many rows that the workgroups' sums are added up in two launches."""
     c, mat = make(n, f, dtype, 2)
