@@ -103,6 +103,10 @@ __global__ __launch_bounds__(1024) void sq_norms_finish_kernel(const double* par
 }
 
 // ---- AdamW
+// From here on every product and sum rounds by itself, but where fmaf is written: states and codes do not depend on what a compiler fuses
+// (the _rn intrinsics do not say that: here they are the operators).
+#pragma clang fp contract(off)
+
 template <int N>
 struct AdamTensors {
     char* W[N];
@@ -238,9 +242,8 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamTensors<N> l, AdamStep b
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float gi = c * g[i];
-        // every product and sum rounds by itself: the codes do not depend on what a compiler contracts
-        m[i] = __fadd_rn(__fmul_rn(m[i], b.b1), __fmul_rn(gi, b.rate1));
-        v[i] = __fadd_rn(__fmul_rn(v[i], b.b2), __fmul_rn(__fmul_rn(gi, gi), b.rate2));
+        m[i] = m[i] * b.b1 + gi * b.rate1;
+        v[i] = v[i] * b.b2 + gi * gi * b.rate2;
         const float change = m[i] * rate * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[i]), c2, b.eps));
         w[i] -= fmaf(w[i], decay, change);
     }
