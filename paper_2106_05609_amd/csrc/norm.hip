@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "common.h"
+#include "norm_layout.h"
 #include "wave.h"
 
 namespace gas {
@@ -144,18 +145,8 @@ struct RowLanes {
         team = W == 1 ? (threadIdx.x & 63) / G : 0;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            c[i] = (place + i * G * W) * E;
-            // A lane has as many pieces as its row needs, so only the last may be cut or missing.  Said of three pieces it saves every seventh
-            // instruction (backward, 1,433 bf16: 101 us, so 92); of two the registers come out worse (100,000 x 400 floats 254 and 269).
-            const bool whole = P > 2 && i < P - 1;
-            on[i] = whole || c[i] < F;
-            skip[i] = 0;
-            if constexpr (MASK)
-                if (!whole && c[i] + E > F) {
-                    skip[i] = c[i] + E - F;
-                    c[i] = F - E;
-                }
-            if (!on[i]) c[i] = 0;
+            const Piece piece = piece_of<E, MASK, P>(place + i * G * W, i, F);
+            c[i] = piece.c; skip[i] = piece.skip; on[i] = piece.on;
         }
     }
     // the wavefront's first row: the same in all of its lanes, so addresses are a scalar's and a lane's 32 bits
@@ -163,8 +154,8 @@ struct RowLanes {
         return (int64_t)blockIdx.x * turns * kRows + (W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / G) : 0);
     }
     __device__ __forceinline__ auto offset(int64_t ld, int i) const {
-        if constexpr (kTiny) return (team * ld + c[i]) * EB;          // may lie before the first row
-        else return (uint32_t)(team * (int)ld + c[i]) * EB;
+        if constexpr (kTiny) return tiny_offset<EB>(team, ld, c[i]);
+        else return piece_offset<EB>(team, ld, c[i]);
     }
     // 16 bytes of any alignment: the same load
     typedef u32x4 piece __attribute__((aligned(2)));
@@ -789,54 +780,6 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
 }
 
 constexpr int kSlabs = 256, kSplits = 32;          // kSplits: parts that thousands of partial sums are added up in
-
-// How rows of F elements lie in lanes (RowLanes), and the workgroups' turns; w = 0: too wide for registers, element by element.
-// A team has as many lanes as the row has pieces of 16 bytes, rounded up to a power of two (3 M rows of 8 bf16, us: forward 42, in teams of eight
-// 214; backward 84 and 294; of 16 floats 149 and 188, 305 and 318).
-// Up to 192 pieces a row is one wavefront's, so nothing waits at a barrier: backward, us, against a wavefront for every 64 pieces:
-// 66,667 x 600 bf16 161 and 168, 40,000 x 1,000 bf16 143 and 152, 19,997 x 1,433 bf16 108 (92 since) and 115; but 20,000 x 2,000 bf16 262 and 147,
-// where four pieces of bf16 no longer fit the registers.  Element by element 2,000 floats x 20,000 take 890 us, eight wavefronts to a
-// row 258; beyond 1,024 pieces a lane's share no longer fits (8,000 x 8,200 bf16: backward 3.4 ms with spilt registers, element by
-// element 1.8; forward 0.6 and 0.9).
-// Turns: forward, a workgroup takes few rows, next to each other, so that the rows in flight are one stretch of memory that moves along
-// (3.1 M x 256 bf16, us: two turns 1,267, four 1,318, eight 1,374, a grid that goes round once and again 1,785; 600,000 x 64 floats: one
-// 121, two 129).  Backward, each workgroup leaves partial sums, so of few turns in all there are no more of them than keep memory
-// busy (50,000 x 256 bf16: 512 workgroups 46 us, 1,024 50, 2,048 57; 256 are best where a lane has several pieces, 19,997 x 1,433 bf16 108, with 512
-// 123, or a row many wavefronts, 13,333 x 3,000 bf16, six wavefronts, 167 and with 512 175; four, 20,000 x 2,000 bf16, 183 and 148).  Of more turns
-// what few turns save outweighs the sums: by 512 workgroups and by 16, 8, 4, 2 turns: 1 M x 256 bf16 813, 763, 727, 779, 999; 600,000 x 256 floats 956, 921,
-// 906, 875, 909; 1 M x 47 floats 352, 333, 300, 282, 315; 100,000 x 256 floats 166, 166, 156, 159, 154, but 25,000 45, -, 48, 48.  Not with bf16 in rows that
-// leave a quarter of the lanes without a piece, 1 M x 136 487, 521, 567, 682, or that give them two, 200,000 x 600 456, 524, 565, 676, 917: there the
-// sums weigh more (three quarters, 1 M x 192, 624, 593, 609, 707; 28 of 32 lanes, 1 M x 224, 724, 678, 670, 738).
-struct Layout {
-    int g, w, p, turns;
-    int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
-};
-inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld) {
-    const int e = bf ? 8 : 4, pieces = (F + e - 1) / e;
-    Layout l = {64, 1, 1, 1, 0, 0};
-    if (pieces > 1024) return {0, 0, 0, 0, 0, 0};
-    if (pieces <= 64)
-        while (l.g / 2 >= pieces) l.g /= 2;
-    else if (pieces <= 192)
-        l.p = (pieces + 63) / 64;
-    else
-        for (int w : {16, 12, 8, 6, 4})
-            if (pieces <= w * 64) l.w = w;
-    const int64_t rows = l.w == 1 ? 4 * (64 / l.g) : 1, all = (n + rows - 1) / rows;
-    const int64_t fewest = !bwd || (l.p == 1 && l.w <= (bf ? 4 : 6)) ? 512 : 256, turns = (all + fewest - 1) / fewest;
-    const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
-    const bool many = bwd && l.w == 1 && (bf ? l.p == 1 && 4 * pieces > 3 * l.g && all >= 32768 : all >= 16384);
-    if (!bwd) l.turns = (int)std::min(turns, most);
-    else if (many) l.turns = bf || all < 32768 ? 8 : 4;
-    else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
-    l.blocks = (all + l.turns - 1) / l.turns;
-    l.most_blocks = many ? l.blocks : std::min(all, fewest);
-    if (longest_ld > (1 << 26)) {        // rows of a wavefront lie within 32 bits of each other, or there is one
-        l.turns *= 64 / l.g;
-        l.g = 64;
-    }
-    return l;
-}
 
 template <bool BF, bool MASK, bool ALL, class C>
 void launch_rows(const Layout& l, dim3 grid, hipStream_t s, const C& c) {

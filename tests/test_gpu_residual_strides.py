@@ -1,0 +1,64 @@
+"""Rows that lie far apart: blocks of columns of one matrix whose rows are tens of millions of elements long, against the same call on rows next to
+each other.  Every row's results have to be the same bits; the sums over the rows are added up in another order."""
+import pytest
+import torch
+
+import paper_2106_05609_amd as gas
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+ROWS = ("x", "a", "t", "h", "u", "gh", "gu", "gx", "ga", "gt")
+SUMS = ("gp", "gp_bias", "gs", "gq", "gq_bias")
+
+
+def passes(c, f, post, pre):
+    """Forward and backward into c's own outputs."""
+    common = dict(a=c["a"], t=c["t"], post=post, p=c["p"], p_bias=c["p_bias"], s=c["s"], alpha=0.7, pre=pre, q=c["q"])
+    gas.gas_residual_norm(c["x"], h=c["h"], u=c["u"], q_bias=c["q_bias"], stats=c["stats"], **common)
+    gas.gas_residual_norm_bwd(c["gh"], c["gu"], c["h"], c["stats"], gx=c["gx"], ga=c["ga"], gt=c["gt"], **{k: c[k] for k in SUMS}, **common)
+
+
+def compare(n, f, ld, dtype, gate):
+    room = f + 2                                          # a column either side that has to stay as it is
+    assert ld >= len(ROWS) * room
+    big = torch.empty(n * ld, dtype=DT[dtype], device="cuda").view(n, ld) if n > 1 else torch.empty(1, ld, dtype=DT[dtype], device="cuda")
+    used = big[:, :len(ROWS) * room]
+    used.fill_(7.0)
+    gen = torch.Generator().manual_seed(n + f)
+    vec = lambda around: (around + 0.3 * torch.randn(f, generator=gen)).cuda()
+    far, near = {}, {}
+    for i, k in enumerate(ROWS):
+        cols = gate if k in ("t", "gt") else f
+        far[k] = used[:, i * room + 1:i * room + 1 + cols]
+        assert far[k].stride(0) == ld
+        if k in ("x", "a", "t", "gh", "gu"):
+            far[k].copy_(torch.randn(n, cols, generator=gen).to(DT[dtype]))
+        near[k] = far[k].contiguous() if n > 1 else far[k].clone(memory_format=torch.contiguous_format).view(1, cols)
+    for c in (far, near):
+        c["stats"] = torch.empty(n, 4, device="cuda")
+        c.update({k: torch.full((f,), float("nan"), device="cuda") for k in SUMS})
+    for k, around in (("p", 1.0), ("p_bias", 0.0), ("s", 0.5), ("q", 1.0), ("q_bias", 0.0)):
+        far[k] = near[k] = vec(around)
+    for post, pre in ((2, 2), (1, 0), (0, 1)):
+        for c in (far, near):
+            passes(c, f, post, pre)
+        for k in ("h", "u", "stats", "gx", "ga", "gt"):
+            assert torch.equal(far[k], near[k]), (k, post, pre)
+        for k in SUMS:                                    # n addends in another order: 2^-24 a step of what they add up to
+            scale = n ** 0.5 * 2.0 ** -24 * 64 * (1.0 + near[k].abs().max())
+            assert (far[k] - near[k]).abs().max() <= scale, (k, post, pre)
+    edges = [i * room + j for i, k in enumerate(ROWS) for j in ((0, f + 1) if k not in ("t", "gt") else (0, gate + 1)) if j < room]
+    assert (used[:, edges] == 7.0).all()
+
+
+@pytest.mark.parametrize("gate", ["row", "element"])
+@pytest.mark.parametrize("dtype,f", [("f32", 1), ("f32", 2), ("f32", 3), ("bf16", 1), ("bf16", 3), ("bf16", 5), ("bf16", 7)])
+@pytest.mark.parametrize("n,ld", [(1, (1 << 26) + 8), (5, (1 << 26) + 9), (70, 17_300_001)])
+def test_rows_narrower_than_a_piece(n, ld, dtype, f, gate):
+    compare(n, f, ld, dtype, f if gate == "element" else 1)
+
+
+@pytest.fixture(autouse=True)
+def memory_back():
+    yield
+    torch.cuda.empty_cache()

@@ -1,0 +1,28 @@
+"""How rows lie in the lanes of the norms' kernels (paper_2106_05609_amd/csrc/norm_layout.h): csrc/norm_check.cpp under the address and
+undefined-behaviour sanitizers.  Host code only; no GPU is involved."""
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(os.path.dirname(HERE), "paper_2106_05609_amd", "csrc")
+
+
+@pytest.fixture(scope="module")
+def checker(tmp_path_factory):
+    exe = str(tmp_path_factory.mktemp("norm") / "norm_check")
+    subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-o", exe,
+                           os.path.join(CSRC, "norm_check.cpp")])
+    return exe
+
+
+def run(*cmd):
+    env = dict(os.environ, ASAN_OPTIONS="verify_asan_link_order=0:detect_leaks=1", UBSAN_OPTIONS="halt_on_error=1")
+    res = subprocess.run(cmd, env=env, capture_output=True, text=True, timeout=600)
+    assert res.returncode == 0, res.stdout[-2000:] + res.stderr[-4000:]
+    assert " 0 failures" in res.stdout
+
+
+def test_pieces_lie_in_their_rows(checker):
+    run(checker, "pieces")
