@@ -28,7 +28,7 @@ constexpr Piece piece_of(int index, int i, int F) {
 }
 // Bytes from the wavefront's first row to element c of its row `team`.  Rows narrower than a piece: c may lie before the row.
 template <int EB>
-constexpr uint32_t piece_offset(int team, int64_t ld, int c) { return (uint32_t)(team * (int)ld + c) * EB; }
+constexpr uint32_t piece_offset(int team, int64_t ld, int c) { return ((uint32_t)team * (uint32_t)ld + (uint32_t)c) * EB; }
 template <int EB>
 constexpr int64_t tiny_offset(int team, int64_t ld, int c) { return (team * ld + c) * EB; }
 
@@ -73,9 +73,9 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
     l.blocks = (all + l.turns - 1) / l.turns;
     l.most_blocks = many ? l.blocks : std::min(all, fewest);
-    // Rows of a wavefront lie within 32 bits of each other, or there is one.  Rows narrower than a piece have offsets of 64 bits, and one lane: they
-    // cannot be loaded whole.
-    if (longest_ld > (1 << 26) && F >= e) {
+    // A wavefront's last byte lies within 32 bits of its first row, or the wavefront has one row.  Rows narrower than a piece have offsets of 64 bits, and one
+    // lane: they cannot be loaded whole.
+    if (F >= e && ((64 / l.g - 1) * longest_ld + F) * (bf ? 2 : 4) > 0xFFFFFFFFLL) {
         l.turns *= 64 / l.g;
         l.g = 64;
     }

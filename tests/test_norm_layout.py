@@ -26,3 +26,7 @@ def run(*cmd):
 
 def test_pieces_lie_in_their_rows(checker):
     run(checker, "pieces")
+
+
+def test_offsets_in_32_bits(checker):
+    run(checker, "offsets")
