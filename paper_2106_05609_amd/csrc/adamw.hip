@@ -320,7 +320,8 @@ __global__ __launch_bounds__(256) void adamw_unpack_kernel(const int8_t* m, cons
         }
 }
 
-constexpr int64_t kMostBlocks = 0x7FFFFFFFLL;
+// Workgroups of 256 threads: a launch has less than 2^32 threads (beyond them the grid wraps, without an error).
+constexpr int64_t kMostGroups = 0xFFFFFFFFLL / 256, kMostBlocks = 4 * kMostGroups;
 
 // Stretches of memory that are apart from each other, in order.
 struct Stretches {
@@ -360,7 +361,7 @@ gas_status gas_sq_norms(int32_t count, const float* const* x, const int64_t* n, 
     const int64_t need = gas_sq_norms_workspace(count, n);
     GAS_REQUIRE(need == 0 || (workspace && workspace_bytes >= need && ((uintptr_t)workspace & 7u) == 0),
                 "%s: the workspace has %lld bytes, %lld are needed, from a multiple of 8 on", who, (long long)workspace_bytes, (long long)need);
-    GAS_REQUIRE(need / 8 <= kMostBlocks, "%s: too many elements", who);
+    GAS_REQUIRE(need / 8 <= kMostGroups, "%s: too many elements", who);
     double* partials = static_cast<double*>(workspace);
     int64_t done = 0;
     for (int32_t i = 0; i < count;) {
@@ -411,6 +412,7 @@ gas_status gas_adamw_steps(int32_t count, void* const* W, const int32_t* dtypes,
     for (int32_t i = 0; i < count; ++i) {
         GAS_REQUIRE(n[i] >= 0 && (n[i] == 0 || (W[i] && dW[i])), "%s: tensor %d", who, i);
         if (!valid_dtype(dtypes[i])) return fail(GAS_ERR_DTYPE, "%s: unknown dtype %d of tensor %d", who, dtypes[i], i);
+        GAS_REQUIRE(n[i] <= kMostBlocks * kBlock, "%s: tensor %d is too large", who, i);
     }
     GAS_REQUIRE(state_bits == 8 || state_bits == 32, "%s: states of %d bits", who, state_bits);
     GAS_REQUIRE(state_bits == 32 || scales || count == 0, "%s: states of 8 bits without scales", who);
@@ -439,7 +441,6 @@ gas_status gas_adamw_steps(int32_t count, void* const* W, const int32_t* dtypes,
         for (; i < count && l.count < kTensors; ++i) {
             if (n[i] == 0) continue;
             const int64_t more = (n[i] + kBlock - 1) / kBlock;
-            GAS_REQUIRE(more <= kMostBlocks, "%s: tensor %d is too large", who, i);
             const uintptr_t w = (uintptr_t)W[i];
             // memory that an earlier tensor of the launch updates too waits for the next one
             if (blocks + more > kMostBlocks || !taken.add(w, w + n[i] * elem_bytes((gas_dtype)dtypes[i]))) break;
@@ -479,7 +480,7 @@ gas_status gas_adamw_unpack(const void* m, const void* v, const float* scales, i
     GAS_REQUIRE(m && v && scales && m_out && v_out, "%s: null pointer", who);
     GAS_REQUIRE(aligned16(m) && aligned16(v) && aligned16(m_out) && aligned16(v_out) && ((uintptr_t)scales & 7u) == 0,
                 "%s: the state or its values are not aligned to 16 bytes", who);
-    GAS_REQUIRE(n / 4096 < kMostBlocks, "%s: too many elements for one launch", who);
+    GAS_REQUIRE((n + 4095) / 4096 <= kMostGroups, "%s: too many elements for one launch", who);
     hipLaunchKernelGGL(dt == GAS_BF16 ? adamw_unpack_kernel<true> : adamw_unpack_kernel<false>, dim3((unsigned)((n + 4095) / 4096)), dim3(256), 0,
                        (hipStream_t)stream, static_cast<const int8_t*>(m), static_cast<const uint8_t*>(v), scales, n / kBlock, static_cast<char*>(m_out),
                        static_cast<char*>(v_out));

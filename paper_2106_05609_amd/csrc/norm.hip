@@ -887,14 +887,13 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
     c.H = static_cast<char*>(H); c.U = static_cast<char*>(U); c.ldh = ldh; c.ldu = ldu; c.stats = stats;
     c.idx = push_idx; c.hist = static_cast<char*>(push_hist); c.ld_hist = ld_push;
     const Layout l = layout_of(n_rows, F, dt == GAS_BF16, false, std::max({ldx, A ? lda : 0, T ? ldt : 0, H ? ldh : 0, U ? ldu : 0}));
-    GAS_REQUIRE(l.blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
     if (l.w) {
         launch_rows(l, dt == GAS_BF16, (hipStream_t)stream, c);
         GAS_CHECK_HIP(hipGetLastError());
         return GAS_OK;
     }
     const int64_t blocks = (n_rows + 3) / 4;
-    GAS_REQUIRE(blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
+    GAS_REQUIRE(blocks <= 0xFFFFFFFFLL / 256, "%s: too many rows for one launch", who);
     if (dt == GAS_BF16) hipLaunchKernelGGL(residual_norm_kernel<true>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, c);
     else hipLaunchKernelGGL(residual_norm_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, (hipStream_t)stream, c);
     GAS_CHECK_HIP(hipGetLastError());
@@ -964,7 +963,6 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     c.partials = static_cast<float*>(workspace);
     const Layout l = layout_of(n_rows, F, dt == GAS_BF16, true, std::max({GH ? ldgh : 0, GU ? std::max(ldgu, ldh) : 0, A ? lda : 0, T ? ldt : 0,
                                                                           GX ? ldgx : 0, GA ? ldga : 0, GT ? ldgt : 0}));
-    GAS_REQUIRE(l.blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
     if (l.w) {
         c.slabs = (int)l.blocks;
         launch_rows(l, dt == GAS_BF16, st, c);
@@ -975,7 +973,7 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
     c.rows_per_slab = (n_rows + kSlabs - 1) / kSlabs;
     c.slabs = (int)((n_rows + c.rows_per_slab - 1) / c.rows_per_slab);
     const int64_t blocks = (n_rows + 3) / 4;
-    GAS_REQUIRE(blocks <= 0x7FFFFFFFLL, "%s: too many rows for one launch", who);
+    GAS_REQUIRE(blocks <= 0xFFFFFFFFLL / 256, "%s: too many rows for one launch", who);
     const bool bf = dt == GAS_BF16;
     hipLaunchKernelGGL(bf ? residual_norm_row_sums_kernel<true> : residual_norm_row_sums_kernel<false>, dim3((unsigned)blocks), dim3(256), 0, st, c);
     GAS_CHECK_HIP(hipGetLastError());

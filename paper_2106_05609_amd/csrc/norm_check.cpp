@@ -60,6 +60,8 @@ static void rows(const Layout& l, int F, int64_t n, const char* what) {
     const int64_t a_turn = l.w == 1 ? 4 * (64 / l.g) : 1;
     CHECK(l.turns >= 1 && l.blocks * l.turns * a_turn >= n && (l.blocks - 1) * l.turns * a_turn < n, "%s: F=%d, %lld rows: %lld workgroups of %d turns", what, F,
           (long long)n, (long long)l.blocks, l.turns);
+    CHECK(l.blocks * (l.w == 1 ? 256 : l.w * 64) <= 0xFFFFFFFFLL, "%s: F=%d, %lld rows: %lld workgroups, more threads than a launch has", what, F, (long long)n,
+          (long long)l.blocks);
     CHECK(l.blocks <= l.most_blocks || strcmp(what, "backward") != 0, "%s: F=%d, %lld rows: %lld workgroups, room for %lld", what, F, (long long)n,
           (long long)l.blocks, (long long)l.most_blocks);
 }
@@ -89,6 +91,19 @@ int main(int argc, char** argv) {
                     }
                 }
         }
+    if (argc > 1 && strcmp(argv[1], "rows") == 0)
+        for (int bf = 0; bf < 2; ++bf)
+            for (int bwd = 0; bwd < 2; ++bwd)
+                for (int F : widths)
+                    for (int b = 0; b < 38; ++b)                  // up to 2^38 rows
+                        for (int k = 0; k < 8; ++k) {
+                            const int64_t n = ((int64_t)1 << b) + (k < 4 ? k : ((int64_t)1 << b) * (k - 3) / 5);
+                            for (int64_t ld : {(int64_t)F, (int64_t)1 << 30}) {
+                                if (n > ((int64_t)1 << 58) / ld) continue;                 // no such matrix
+                                const Layout l = layout_of(n, F, bf, bwd, ld);
+                                if (l.w) rows(l, F, n, bwd ? "backward" : "forward");
+                            }
+                        }
     printf("%d layouts, %d failures\n", checked, failures);
     return failures != 0;
 }

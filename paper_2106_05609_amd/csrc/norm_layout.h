@@ -71,6 +71,9 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     if (!bwd) l.turns = (int)std::min(turns, most);
     else if (many) l.turns = bf || all < 32768 ? 8 : 4;
     else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
+    // a launch has less than 2^32 threads: what is more goes by more turns (67,108,869 x 129 floats and up)
+    const int64_t room = 0xFFFFFFFFLL / (l.w == 1 ? 256 : l.w * 64);
+    l.turns = (int)std::max((int64_t)l.turns, (all + room - 1) / room);
     l.blocks = (all + l.turns - 1) / l.turns;
     l.most_blocks = many ? l.blocks : std::min(all, fewest);
     // A wavefront's last byte lies within 32 bits of its first row, or the wavefront has one row.  Rows narrower than a piece have offsets of 64 bits, and one

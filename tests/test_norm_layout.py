@@ -30,3 +30,7 @@ def test_pieces_lie_in_their_rows(checker):
 
 def test_offsets_in_32_bits(checker):
     run(checker, "offsets")
+
+
+def test_workgroups_for_any_number_of_rows(checker):
+    run(checker, "rows")
