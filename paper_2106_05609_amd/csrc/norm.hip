@@ -2,6 +2,8 @@
 //     y = N_post(a) p + p_bias,   h = x + alpha s sigmoid(t) y,   u = N_pre(h) q + q_bias.
 // Statistics, sums and the row itself in 32 bits, each output rounded once.  Bound by memory: forward 3.1 M x 256 bf16 1.29 ms, 6.2 TB/s of
 // the 8.0 GB that it has to move (a copy of 4 GB goes at 5.6); backward 600,000 x 256 floats 0.87 ms, 5.6 TB/s of 4.9 GB.
+#include <float.h>
+
 #include <algorithm>
 #include <type_traits>
 
@@ -40,7 +42,15 @@ __device__ __forceinline__ void store_one(char* p, int64_t i, float v) {
     else reinterpret_cast<float*>(p)[i] = v;
 }
 __device__ __forceinline__ float at(const float* v, int f, float otherwise) { return v ? v[f] : otherwise; }
-__device__ __forceinline__ float gate_of(float t) { return 1.f / (1.f + expf(-t)); }
+
+// A gate, g = 1 / (1 + z) with z = exp(-t), and 1 - g = z g, which has its own digits: the difference from 1 has none left where the gate is open
+// (1e-3 of it off at t = 10, 0 from t = 17 on).  Where z is an infinity g is 0, and so is every gradient that goes with g (1 - g).
+struct Gate { float g, rest; };
+__device__ __forceinline__ Gate gate_from(float z, float g) { return {g, fminf(z, FLT_MAX) * g}; }
+__device__ __forceinline__ Gate gate_of(float t) {
+    const float z = expf(-t);
+    return gate_from(z, 1.f / (1.f + z));
+}
 
 // Mean and 1 / deviation over the F values that value(f) gives, the same in every lane.
 template <class V>
@@ -70,12 +80,12 @@ __global__ __launch_bounds__(256) void residual_norm_kernel(ResidualNorm c) {
     if (row >= c.n) return;
     float mean_a = 0.f, r_a = 1.f, mean_h, r_h;
     if (c.A) row_stats(c.post, c.F, c.eps, [&](int f) { return load_one<BF>(c.A, row * c.lda + f); }, &mean_a, &r_a);
-    const float row_gate = c.gate_cols == 1 ? gate_of(load_one<BF>(c.T, row * c.ldt)) : 1.f;
+    const float row_gate = c.gate_cols == 1 ? gate_of(load_one<BF>(c.T, row * c.ldt)).g : 1.f;
     auto h_of = [&](int f) {
         const float x = load_one<BF>(c.X, row * c.ldx + f);
         if (!c.A) return x;
         const float y = fmaf((load_one<BF>(c.A, row * c.lda + f) - mean_a) * r_a, at(c.p, f, 1.f), at(c.p_bias, f, 0.f));
-        const float g = c.gate_cols > 1 ? gate_of(load_one<BF>(c.T, row * c.ldt + f)) : row_gate;
+        const float g = c.gate_cols > 1 ? gate_of(load_one<BF>(c.T, row * c.ldt + f)).g : row_gate;
         return fmaf(c.alpha * at(c.s, f, 1.f) * g, y, x);
     };
     row_stats(c.U || c.hist || c.stats ? c.pre : GAS_NORM_NONE, c.F, c.eps, h_of, &mean_h, &r_h);
@@ -289,7 +299,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[3][16], int
         turn ^= 1;
     }
 }
-__device__ __forceinline__ float fast_gate(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269504f)); }
+__device__ __forceinline__ Gate fast_gate(float t) {
+    const float z = __builtin_amdgcn_exp2f(t * -1.44269504f);
+    return gate_from(z, __builtin_amdgcn_rcpf(1.f + z));
+}
 
 // z becomes what it is beyond its mean; returns 1 / deviation.
 template <class L, int G, int W, int P, int E>
@@ -355,7 +368,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
         if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
         const bool live = L::kAlone || base + lanes.team < c.n;
         float h[P][E], y[P][E], g[P][E];
-        const float gate = c.alpha * (c.gate_cols == 1 ? fast_gate(t1) : 1.f);
+        const float gate = c.alpha * (c.gate_cols == 1 ? fast_gate(t1).g : 1.f);
         const int64_t place = to;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -371,7 +384,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
 #pragma unroll
                 for (int i = 0; i < P; ++i)
 #pragma unroll
-                    for (int e = 0; e < E; ++e) g[i][e] = c.alpha * fast_gate(g[i][e]);
+                    for (int e = 0; e < E; ++e) g[i][e] = c.alpha * fast_gate(g[i][e]).g;
             } else {
 #pragma unroll
                 for (int i = 0; i < P; ++i)
@@ -433,7 +446,7 @@ struct ResidualNormBwd {
     int64_t rows_per_slab;
 };
 
-struct Element { float hn, gu, e, an, y, g, dy; };
+struct Element { float hn, gu, e, an, y, dy; Gate gate; };
 
 // What one element's gradients are made of; d_mean, dh_mean: the row's means of d and d hn.
 template <bool BF>
@@ -444,12 +457,12 @@ __device__ __forceinline__ Element element(const ResidualNormBwd& c, int64_t row
     const float d = v.gu * at(c.q, f, 1.f);
     v.e = (c.GH ? load_one<BF>(c.GH, row * c.ldgh + f) : 0.f) + st[3] * (d - d_mean - v.hn * dh_mean);
     v.an = v.y = v.dy = 0.f;
-    v.g = 1.f;
+    v.gate = {1.f, 0.f};
     if (c.A) {
         v.an = (load_one<BF>(c.A, row * c.lda + f) - st[0]) * st[1];
         v.y = fmaf(v.an, at(c.p, f, 1.f), at(c.p_bias, f, 0.f));
-        if (c.gate_cols) v.g = gate_of(load_one<BF>(c.T, row * c.ldt + (c.gate_cols == 1 ? 0 : f)));
-        v.dy = v.e * c.alpha * at(c.s, f, 1.f) * v.g;
+        if (c.gate_cols) v.gate = gate_of(load_one<BF>(c.T, row * c.ldt + (c.gate_cols == 1 ? 0 : f)));
+        v.dy = v.e * c.alpha * at(c.s, f, 1.f) * v.gate.g;
     }
     return v;
 }
@@ -494,7 +507,7 @@ __global__ __launch_bounds__(256) void residual_norm_columns_kernel(ResidualNorm
             const Element v = element<BF>(c, row, f, st, c.row_sums[row * 2], c.row_sums[row * 2 + 1]);
             sum[0] = fmaf(v.dy, v.an, sum[0]);
             sum[1] += v.dy;
-            sum[2] = fmaf(v.e * c.alpha * v.g, v.y, sum[2]);
+            sum[2] = fmaf(v.e * c.alpha * v.gate.g, v.y, sum[2]);
             sum[3] = fmaf(v.gu, v.hn, sum[3]);
             sum[4] += v.gu;
         }
@@ -577,7 +590,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
         if constexpr (kParked) asm volatile("" ::: "memory");        // what is parked stays there
         const bool live = L::kAlone || base + lanes.team < c.n;
         const float mean_a = st[0], r_a = st[1], mean_h = st[2], r_h = st[3];
-        const float row_gate = c.gate_cols == 1 ? fast_gate(t1) : 1.f;
+        const Gate row_gate = c.gate_cols == 1 ? fast_gate(t1) : Gate{1.f, 0.f};
         float e_[P][E], hn[P][E], d[P][E];
 #pragma unroll
         for (int i = 0; i < P; ++i) {
@@ -625,7 +638,7 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
         float an[P][E], m[3] = {0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            float g[E], p[E], p_bias[E], s[E], part[3] = {0.f, 0.f, 0.f};
+            float g[E], rest[E], p[E], p_bias[E], s[E], part[3] = {0.f, 0.f, 0.f};
             unpack<BF>(a[i], an[i]);
             unpack<BF>(t[i], g);
             vec.get(0, i, p);
@@ -633,10 +646,14 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             vec.get(2, i, s);
             if (c.gate_cols > 1) {               // a branch, not a choice of both: 11 issue slots an element
 #pragma unroll
-                for (int e = 0; e < E; ++e) g[e] = fast_gate(g[e]);
+                for (int e = 0; e < E; ++e) {
+                    const Gate gate = fast_gate(g[e]);
+                    g[e] = gate.g;
+                    rest[e] = gate.rest;
+                }
             } else {
 #pragma unroll
-                for (int e = 0; e < E; ++e) g[e] = row_gate;
+                for (int e = 0; e < E; ++e) g[e] = row_gate.g;
             }
             float w[E];                          // dy y: of it the gate's gradient is a part
 #pragma unroll
@@ -655,12 +672,12 @@ __global__ __launch_bounds__((RowLanes<BF, G, W, P, MASK>::kThreads)) void resid
             }
             if (c.gate_cols > 1) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) w[e] *= 1.f - g[e];
+                for (int e = 0; e < E; ++e) w[e] *= rest[e];
                 out[i] = pack<BF>(w);
             } else if (c.gate_cols == 1) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) part[2] += MASK && e < lanes.skip[i] ? 0.f : w[e];
-                part[2] *= 1.f - row_gate;
+                part[2] *= row_gate.rest;
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k) m[k] += lanes.on[i] ? part[k] : 0.f;
@@ -764,7 +781,7 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
             const float cc = v.dy * at(c.p, f, 1.f);
             sc += cc;
             sca = fmaf(cc, v.an, sca);
-            sg = fmaf(v.dy * v.y, 1.f - v.g, sg);
+            sg = fmaf(v.dy * v.y, v.gate.rest, sg);
         }
     sc = c.post == GAS_NORM_LAYER ? wave_sum(sc) / (float)c.F : 0.f;
     sca = c.post == GAS_NORM_NONE ? 0.f : wave_sum(sca) / (float)c.F;
@@ -773,7 +790,7 @@ __global__ __launch_bounds__(256) void residual_norm_bwd_kernel(ResidualNormBwd 
         const Element v = element<BF>(c, row, f, st, d_mean, dh_mean);
         if (c.GX) store_one<BF>(c.GX, row * c.ldgx + f, v.e);
         if (c.GA) store_one<BF>(c.GA, row * c.ldga + f, st[1] * (v.dy * at(c.p, f, 1.f) - sc - v.an * sca));
-        if (c.GT && c.gate_cols != 1) store_one<BF>(c.GT, row * c.ldgt + f, v.dy * v.y * (1.f - v.g));
+        if (c.GT && c.gate_cols != 1) store_one<BF>(c.GT, row * c.ldgt + f, v.dy * v.y * v.gate.rest);
     }
     // after every lane has read the row's gate, which may lie there
     if (c.GT && c.gate_cols == 1 && lane == 0) store_one<BF>(c.GT, row * c.ldgt, sg);
