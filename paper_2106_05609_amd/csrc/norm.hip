@@ -299,8 +299,12 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float (*red)[3][16], int
         turn ^= 1;
     }
 }
+// exp(-t) as a power of 2: the exponent's rounding and that of its factor move it by up to |t| units (62 at |t| = 80), so it is multiplied by what they left out.
+// Costs nothing beside memory: huge rows 1,283 us, without it 1,297, 19,997 x 1,433 bf16 backward 93.1 and 92.4.
 __device__ __forceinline__ Gate fast_gate(float t) {
-    const float z = __builtin_amdgcn_exp2f(t * -1.44269504f);
+    const float u = t * -1.44269504f, left = fmaf(t, -1.92596299e-8f, fmaf(t, -1.44269504f, -u));
+    const float rough = __builtin_amdgcn_exp2f(u);
+    const float z = fabsf(t) <= 88.f ? fmaf(rough, left * 0.693147181f, rough) : rough;       // beyond it is an infinity or below the normal numbers
     return gate_from(z, __builtin_amdgcn_rcpf(1.f + z));
 }
 

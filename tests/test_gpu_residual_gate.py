@@ -55,3 +55,22 @@ def by_formula(gh, gu, h, stats, a, t, p, p_bias, s, q):
     e = gh + r_h * (gu * q - hn * (gu * q * hn).mean(1, keepdim=True))
     each = e * 0.7 * s * ((a - mean_a) * r_a * p + p_bias)
     return (each if t.shape == a.shape else each.sum(1, keepdim=True)) * torch.sigmoid(t) * torch.sigmoid(-t)
+
+
+@pytest.mark.parametrize("cols", ["element", "row"])
+@pytest.mark.parametrize("n,f", [(8000, 1), (4000, 5), (600, 64), (20, 1433), (4, 5000)])
+def test_gates_themselves(n, f, cols):
+    """h = g and gt = g (1 - g), no norm: |t| up to 80, every step of it some units: the exponential one, its factor's digits and the product's remainder
+    one each, 1 + z a half, the reciprocal one, the products a half each: below 16 half units, and 24 for the two factors."""
+    gen = torch.Generator().manual_seed(f)
+    t = ((torch.rand(n, f if cols == "element" else 1, generator=gen) - 0.5) * 160).cuda()
+    a, x = torch.ones(n, f, device="cuda"), torch.zeros(n, f, device="cuda")
+    h, gx, gt = torch.empty_like(a), torch.empty_like(a), torch.empty_like(t)
+    gas.gas_residual_norm(x, h=h, a=a, t=t)
+    gas.gas_residual_norm_bwd(a, None, None, None, gx=gx, gt=gt, a=a, t=t)
+    g, rest = torch.sigmoid(t.double()), torch.sigmoid(-t.double())
+    off = (h.double() / g - 1).abs().max().item()
+    assert off <= 16 * R.EPS32, off / R.EPS32
+    off = (gt.double() / (g * rest * (f if cols == "row" else 1)) - 1).abs().max().item()
+    # a row's sum: F / 64 additions and six more, whose roundings are half units each
+    assert off <= (24 + (f / 64 + 14 if cols == "row" else 0)) * R.EPS32, off / R.EPS32
