@@ -553,7 +553,9 @@ GAS_API gas_status gas_sq_norms(int32_t count, const float* const* x, const int6
  *   state_bits 8:  m int8, v uint8, scales fp32[elements / 256, 2], s_m and s_v of every 256 elements, which are the largest
  *                  magnitudes there: m stands for s_m k |k| / 127^2, v for s_v (k / 255)^4.  Values between two codes go to one of
  *                  them at random with the value as expectation, by the step's number and the element's place, so results are
- *                  the same from run to run; a v > 0 is never 0.  256 elements with an infinity or a NaN read as NaN from then on.
+ *                  the same from run to run; a v > 0 is never 0, unless the largest of its 256 is below float32's normal numbers: then all
+ *                  of them are.  256 elements of m or of v with an infinity or a NaN among them read as NaN from then on, whichever of them it was (the
+ *                  square of a gradient above 1.8e19 is one): the next step makes their W NaN too.
  * master (optional, fp32 in the state's layout): the values of the GAS_BF16 tensors, which are updated in its place; W is set to them,
  * rounded.  Without it bf16 tensors are read, updated in fp32 and rounded to nearest.  The places of GAS_F32 tensors are not used.
  *

@@ -263,8 +263,10 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamTensors<N> l, AdamStep b
     }
     if constexpr (EIGHT) {
         float sm = largest(m), sv = largest(v);
-        sm = sm < 1.17549435e-38f ? 0.f : sm;       // below the normal numbers: nothing
-        sv = sv < 1.17549435e-38f ? 0.f : sv;
+        // A block with an infinity or a NaN is lost and reads as NaN, all of it: beside an infinite scale no element would move any more, without a word.
+        // Below the normal numbers: nothing.
+        sm = sm < INFINITY ? (sm < 1.17549435e-38f ? 0.f : sm) : NAN;
+        sv = sv < INFINITY ? (sv < 1.17549435e-38f ? 0.f : sv) : NAN;
         const float im = sm > 0.f ? 1.f / sm : 0.f, iv = sv > 0.f ? 1.f / sv : 0.f;
         if (lane == 0) *reinterpret_cast<f32x2_t*>(b.scales + 2 * (b.base + unit)) = f32x2_t{sm, sv};
         km = kv = 0;
