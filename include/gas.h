@@ -511,7 +511,8 @@ GAS_API gas_status gas_sgd_step_clipped(void* W, int64_t n, gas_dtype dt, const 
  *     gp = sum dy an, gp_bias = sum dy, gs = sum e alpha g y, gq = sum GU hn, gq_bias = sum GU     over the rows, fp32[F].
  * H as stored and stats as written by the forward call.  Any output may be NULL; GX may be GH, GA may be A, and so on, as above;
  * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace: gas_residual_norm_bwd_workspace(n_rows, F) bytes (enough for fewer rows too)
- * from a multiple of 16 on.
+ * from a multiple of 16 on: partial sums, at most 1 MB for every column however many rows there are (of rows of more than 4,096 floats or 8,192
+ * bf16 5 KB for every column and 8 bytes for every row).
  */
 typedef enum { GAS_NORM_NONE = 0, GAS_NORM_RMS = 1, GAS_NORM_LAYER = 2 } gas_norm_kind;
 GAS_API gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t lda, const void* T, int64_t ldt,

@@ -62,6 +62,7 @@ static void rows(const Layout& l, int F, int64_t n, const char* what) {
           (long long)n, (long long)l.blocks, l.turns);
     CHECK(l.blocks * (l.w == 1 ? 256 : l.w * 64) <= 0xFFFFFFFFLL, "%s: F=%d, %lld rows: %lld workgroups, more threads than a launch has", what, F, (long long)n,
           (long long)l.blocks);
+    CHECK(l.most_blocks <= kMostSums, "%s: F=%d, %lld rows: sums of %lld workgroups", what, F, (long long)n, (long long)l.most_blocks);
     CHECK(l.blocks <= l.most_blocks || strcmp(what, "backward") != 0, "%s: F=%d, %lld rows: %lld workgroups, room for %lld", what, F, (long long)n,
           (long long)l.blocks, (long long)l.most_blocks);
 }

@@ -49,6 +49,10 @@ constexpr int64_t tiny_offset(int team, int64_t ld, int c) { return (team * ld +
 // 906, 875, 909; 1 M x 47 floats 352, 333, 300, 282, 315; 100,000 x 256 floats 166, 166, 156, 159, 154, but 25,000 45, -, 48, 48.  Not with bf16 in rows that
 // leave a quarter of the lanes without a piece, 1 M x 136 487, 521, 567, 682, or that give them two, 200,000 x 600 456, 524, 565, 676, 917: there the
 // sums weigh more (three quarters, 1 M x 192, 624, 593, 609, 707; 28 of 32 lanes, 1 M x 224, 724, 678, 670, 738).
+// At most kMostSums workgroups leave sums, so these take at most 1 MB for every column however many rows there are (a third of a float matrix without
+// that): us without a bound, with 65,536, 32,768 and 16,384: 600,000 x 256 floats 882, 884, 908, 927; 3,125,002 x 256 floats 4,976, 4,894, 4,858, 4,905; 3,125,002 x 64 floats 1,117,
+// 1,120, 1,155, 1,195; 3,125,002 x 256 bf16 2,352, 2,344, 2,368, 2,447; 1 M x 400 floats 2,500, 2,501, 2,366, 2,512.
+constexpr int64_t kMostSums = 49152;
 struct Layout {
     int g, w, p, turns;
     int64_t blocks, most_blocks;         // and of any fewer rows: never less where there are more rows
@@ -68,14 +72,15 @@ inline Layout layout_of(int64_t n, int F, bool bf, bool bwd, int64_t longest_ld)
     const int64_t fewest = !bwd || (l.p == 1 && l.w <= (bf ? 4 : 6)) ? 512 : 256, turns = (all + fewest - 1) / fewest;
     const int64_t most = l.w > 1 ? (bf ? 4 : 2) : bf || l.p > 1 ? 2 : 1;
     const bool many = bwd && l.w == 1 && (bf ? l.p == 1 && 4 * pieces > 3 * l.g && all >= 32768 : all >= 16384);
+    const int64_t few = bf || all < 32768 ? 8 : 4;
     if (!bwd) l.turns = (int)std::min(turns, most);
-    else if (many) l.turns = bf || all < 32768 ? 8 : 4;
+    else if (many) l.turns = (int)std::max(few, (all + kMostSums - 1) / kMostSums);
     else l.turns = (int)(all <= 4 ? all : turns);        // up to four turns by one workgroup, whose sums need no second launch (16 x 256 floats 9.7 and 7.6 us)
     // a launch has less than 2^32 threads: what is more goes by more turns (67,108,869 x 129 floats and up)
     const int64_t room = 0xFFFFFFFFLL / (l.w == 1 ? 256 : l.w * 64);
     l.turns = (int)std::max((int64_t)l.turns, (all + room - 1) / room);
     l.blocks = (all + l.turns - 1) / l.turns;
-    l.most_blocks = many ? l.blocks : std::min(all, fewest);
+    l.most_blocks = many ? std::min((all + few - 1) / few, kMostSums) : std::min(all, fewest);
     // A wavefront's last byte lies within 32 bits of its first row, or the wavefront has one row.  Rows narrower than a piece have offsets of 64 bits, and one
     // lane: they cannot be loaded whole.
     if (F >= e && ((64 / l.g - 1) * longest_ld + F) * (bf ? 2 : 4) > 0xFFFFFFFFLL) {

@@ -34,3 +34,11 @@ def test_offsets_in_32_bits(checker):
 
 def test_workgroups_for_any_number_of_rows(checker):
     run(checker, "rows")
+
+
+def test_workspace_of_the_backward_pass_is_bounded():
+    """At most 1 MB for every column while rows are whole in registers, however many there are."""
+    from paper_2106_05609_amd import binding as B
+    for f in (1, 8, 47, 64, 256, 400, 768, 1433, 4096):
+        for n in (1, 600_000, 3_125_002, 24_700_000, 111_059_956, 1 << 33):
+            assert B.gas_residual_norm_bwd_workspace(n, f) <= (1 << 20) * f, (n, f)
