@@ -510,9 +510,10 @@ GAS_API gas_status gas_sgd_step_clipped(void* W, int64_t n, gas_dtype dt, const 
  *     dy = e alpha s g,  c = dy p,   GA = r_a (c - [mean c] - an mean(c an)),   GT = dy y (1 - g) (one gate of a row: the row's sum),
  *     gp = sum dy an, gp_bias = sum dy, gs = sum e alpha g y, gq = sum GU hn, gq_bias = sum GU     over the rows, fp32[F].
  * H as stored and stats as written by the forward call.  Any output may be NULL; GX may be GH, GA may be A, and so on, as above;
- * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace: gas_residual_norm_bwd_workspace(n_rows, F) bytes (enough for fewer rows too)
- * from a multiple of 16 on: partial sums, at most 1 MB for every column however many rows there are (of rows of more than 4,096 floats or 8,192
- * bf16 5 KB for every column and 8 bytes for every row).
+ * n_rows = 0 writes zeros to the sums.  The sums have a fixed order.  workspace, from a multiple of 16 on: the partial sums of
+ * gas_residual_norm_bwd_typed_workspace(n_rows, F, dt) bytes, enough for fewer rows too, at most 1 MB for every column however many rows there are (of rows
+ * of more than 4,096 floats or 8,192 bf16 5 KB for every column and 8 bytes for every row).  gas_residual_norm_bwd_workspace: enough for
+ * either type; bf16 alone often needs a small part of it.
  */
 typedef enum { GAS_NORM_NONE = 0, GAS_NORM_RMS = 1, GAS_NORM_LAYER = 2 } gas_norm_kind;
 GAS_API gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t lda, const void* T, int64_t ldt,
@@ -521,6 +522,7 @@ GAS_API gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, 
                          float eps, void* H, int64_t ldh, void* U, int64_t ldu, float* stats, const int32_t* push_idx,
                          void* push_hist, int64_t n_hist_rows, int64_t ld_push, void* stream);
 GAS_API int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F);
+GAS_API int64_t gas_residual_norm_bwd_typed_workspace(int64_t n_rows, int32_t F, gas_dtype dt);
 GAS_API gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, int64_t ldgu, const void* H, int64_t ldh,
                          const void* A, int64_t lda, const void* T, int64_t ldt, int32_t gate_cols, const float* stats,
                          int64_t n_rows, int32_t F, gas_dtype dt, int32_t norm_post, const float* p, const float* p_bias,

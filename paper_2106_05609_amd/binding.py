@@ -30,7 +30,7 @@ EXPORTS = [
     "gas_gat_aggregate_bwd_heads", "gas_pna_aggregate_bwd_workspace", "gas_gat_aggregate_bwd_workspace",
     "gas_gat_aggregate_bwd_heads_workspace", "gas_linear_in_order", "gas_gat_aggregate_push", "gas_pna_aggregate_own", "gas_pna_aggregate_bwd_bounded",
     "gas_gat_aggregate_bwd_bounded",
-    "gas_residual_norm", "gas_residual_norm_bwd", "gas_residual_norm_bwd_workspace", "gas_sq_norms", "gas_sq_norms_workspace",
+    "gas_residual_norm", "gas_residual_norm_bwd", "gas_residual_norm_bwd_workspace", "gas_residual_norm_bwd_typed_workspace", "gas_sq_norms", "gas_sq_norms_workspace",
     "gas_adamw_elements", "gas_adamw_steps", "gas_adamw_unpack",
     "gas_disk_open", "gas_disk_close", "gas_disk_pull", "gas_disk_push", "gas_disk_wait", "gas_disk_read_rows",
     "gas_disk_write_rows", "gas_disk_sync",
@@ -65,7 +65,7 @@ def lib():
         L.gas_pna_aggregate_bwd_workspace.restype = C.c_int64
         L.gas_gat_aggregate_bwd_workspace.restype = C.c_int64
         L.gas_gat_aggregate_bwd_heads_workspace.restype = C.c_int64
-        for name in ("gas_residual_norm_bwd_workspace", "gas_sq_norms_workspace", "gas_adamw_elements"):
+        for name in ("gas_residual_norm_bwd_workspace", "gas_residual_norm_bwd_typed_workspace", "gas_sq_norms_workspace", "gas_adamw_elements"):
             getattr(L, name).restype = C.c_int64
         for name in EXPORTS:
             if name not in ("gas_last_error", "gas_version", "gas_plan_destroy") and not name.endswith(_COUNTS):
@@ -102,6 +102,7 @@ _SIGNATURES = dict(
     gas_disk_pull="ppqqpqpp", gas_disk_push="ppqqpqpp", gas_disk_wait="pq", gas_disk_read_rows="ppqqpq",
     gas_disk_write_rows="ppqqpq", gas_disk_sync="p",
     gas_residual_norm="pqpqpqiqiiipppfippfpqpqpppqqp", gas_residual_norm_bwd_workspace="qi",
+    gas_residual_norm_bwd_typed_workspace="qii",
     gas_residual_norm_bwd="pqpqpqpqpqipqiiipppfippqpqpqppppppqp", gas_sq_norms="ipppppqp", gas_sq_norms_workspace="ip",
     gas_adamw_elements="ip", gas_adamw_steps="ippppppppqiffffpqppfp", gas_adamw_unpack="pppqippp",
 )
@@ -788,7 +789,7 @@ def gas_residual_norm_bwd(gh, gu, h, stats, gx=None, ga=None, gt=None, a=None, t
                           pre=NORM_NONE, q=None, gp=None, gp_bias=None, gs=None, gq=None, gq_bias=None, workspace=None):
     """Backward of gas_residual_norm: gh, gu: gradients at h and u (None: none there); h and stats as the forward call left them.  gx, ga, gt:
     [n, F] (gt as t), gp, gp_bias, gs, gq, gq_bias: float32 [F], each optional.  workspace: a uint8 tensor of at least
-    gas_residual_norm_bwd_workspace(n, F) bytes, allocated here if not given."""
+    gas_residual_norm_bwd_workspace(n, F, dtype) bytes, allocated here if not given."""
     calls, who = _calls(), "gas_residual_norm_bwd"
     like = gh if gh is not None else gu
     if like is None:
@@ -800,15 +801,18 @@ def gas_residual_norm_bwd(gh, gu, h, stats, gx=None, ga=None, gt=None, a=None, t
         raise ValueError("gas_residual_norm_bwd: shapes or dtypes do not match")
     pp, pbp, sp, qp, gpp, gpbp, gsp, gqp, gqbp = _vectors(who, width, p, p_bias, s, q, gp, gp_bias, gs, gq, gq_bias)
     if workspace is None:
-        workspace = torch.empty(calls.gas_residual_norm_bwd_workspace(n, width), dtype=torch.uint8, device=like.device)
+        workspace = torch.empty(calls.gas_residual_norm_bwd_typed_workspace(n, width, dt), dtype=torch.uint8, device=like.device)
     _check(calls.gas_residual_norm_bwd(
         ghp, ldgh, gup, ldgu, hp, ldh, ap, lda, tp, ldt, gates, 0 if stats is None else _ptr(stats, torch.float32), n, width, dt, post, pp, pbp,
         sp, alpha, pre, qp, gxp, ldgx, gap, ldga, gtp, ldgt, gpp, gpbp, gsp, gqp, gqbp, _ptr(workspace),
         workspace.numel() * workspace.element_size(), _stream()))
 
 
-def gas_residual_norm_bwd_workspace(n_rows, width) -> int:
-    return int(_calls().gas_residual_norm_bwd_workspace(n_rows, width))
+def gas_residual_norm_bwd_workspace(n_rows, width, dtype=None) -> int:
+    """Bytes for rows of `dtype`, of either type if not given."""
+    if dtype is None:
+        return int(_calls().gas_residual_norm_bwd_workspace(n_rows, width))
+    return int(_calls().gas_residual_norm_bwd_typed_workspace(n_rows, width, _dt(torch.empty(0, dtype=dtype))))
 
 
 def gas_sq_norms(xs, out, steps=None, workspace=None):

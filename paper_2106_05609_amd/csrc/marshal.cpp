@@ -292,7 +292,7 @@ PyMethodDef methods[] = {
     GAS_CALL(gas_pna_aggregate_own), GAS_CALL(gas_pna_aggregate_bwd_bounded), GAS_CALL(gas_pna_aggregate_bwd_workspace),
     GAS_CALL(gas_pna_groups), GAS_CALL(gas_pna_groups_workspace), GAS_CALL(gas_pna_linear), GAS_CALL(gas_pna_linear_workspace),
     GAS_CALL(gas_pna_linear_bwd_input), GAS_CALL(gas_pna_linear_bwd_weight), GAS_CALL(gas_pna_linear_bwd_weight_workspace),
-    GAS_CALL(gas_residual_norm), GAS_CALL(gas_residual_norm_bwd), GAS_CALL(gas_residual_norm_bwd_workspace), GAS_CALL(gas_sq_norms),
+    GAS_CALL(gas_residual_norm), GAS_CALL(gas_residual_norm_bwd), GAS_CALL(gas_residual_norm_bwd_workspace), GAS_CALL(gas_residual_norm_bwd_typed_workspace), GAS_CALL(gas_sq_norms),
     GAS_CALL(gas_sq_norms_workspace), GAS_CALL(gas_adamw_elements), GAS_CALL(gas_adamw_steps), GAS_CALL(gas_adamw_unpack),
     GAS_CALL(gas_gat_aggregate_push), GAS_CALL(gas_gat_aggregate_bwd_bounded), GAS_CALL(gas_gat_aggregate_bwd_heads_workspace),
     {nullptr, nullptr, 0, nullptr}};

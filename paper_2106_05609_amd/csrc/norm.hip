@@ -921,15 +921,14 @@ gas_status gas_residual_norm(const void* X, int64_t ldx, const void* A, int64_t 
     return GAS_OK;
 }
 
+int64_t gas_residual_norm_bwd_typed_workspace(int64_t n_rows, int32_t F, gas_dtype dt) {
+    if (n_rows <= 0 || F <= 0 || !valid_dtype(dt)) return 0;
+    const Layout l = layout_of(n_rows, F, dt == GAS_BF16, true, 0);
+    return 4 * (l.w ? (l.most_blocks + (l.most_blocks > 1024 ? kSplits : 0)) * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows);
+}
+
 int64_t gas_residual_norm_bwd_workspace(int64_t n_rows, int32_t F) {
-    if (n_rows <= 0 || F <= 0) return 0;
-    int64_t most = 0;                         // of both types
-    for (int bf = 0; bf < 2; ++bf) {
-        const Layout l = layout_of(n_rows, F, bf, true, 0);
-        const int64_t floats = l.w ? (l.most_blocks + (l.most_blocks > 1024 ? kSplits : 0)) * 5 * F : (int64_t)kSlabs * 5 * F + 2 * n_rows;
-        most = floats > most ? floats : most;
-    }
-    return most * 4;
+    return std::max(gas_residual_norm_bwd_typed_workspace(n_rows, F, GAS_F32), gas_residual_norm_bwd_typed_workspace(n_rows, F, GAS_BF16));
 }
 
 gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, int64_t ldgu, const void* H, int64_t ldh, const void* A,
@@ -972,8 +971,8 @@ gas_status gas_residual_norm_bwd(const void* GH, int64_t ldgh, const void* GU, i
         for (int k = 0; k < o; ++k)
             GAS_REQUIRE(!share(out[o].p, out[o].ld, out[o].cols, out[k].p, out[k].ld, out[k].cols, n_rows, eb), "%s: the outputs share memory", who);
     }
-    GAS_REQUIRE(workspace && workspace_bytes >= gas_residual_norm_bwd_workspace(n_rows, F), "%s: the workspace has %lld bytes, %lld are needed", who,
-                (long long)workspace_bytes, (long long)gas_residual_norm_bwd_workspace(n_rows, F));
+    const int64_t need = gas_residual_norm_bwd_typed_workspace(n_rows, F, dt);
+    GAS_REQUIRE(workspace && workspace_bytes >= need, "%s: the workspace has %lld bytes, %lld are needed", who, (long long)workspace_bytes, (long long)need);
     GAS_REQUIRE(aligned16(workspace), "%s: the workspace is not aligned to 16 bytes", who);
     c.GH = static_cast<const char*>(GH); c.GU = static_cast<const char*>(GU); c.H = static_cast<const char*>(H);
     c.A = static_cast<const char*>(A); c.T = static_cast<const char*>(T);

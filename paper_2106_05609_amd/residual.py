@@ -93,7 +93,7 @@ def residual_train_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories
     g_out = wg.add(kept["u"], gy)
     gu, gh = new(nb), None
     B.gas_linear_bwd_input(gy, model.w_out, gu)
-    room = torch.empty(max(1, B.gas_residual_norm_bwd_workspace(nv, f)), dtype=torch.uint8, device=dev)
+    room = torch.empty(max(1, B.gas_residual_norm_bwd_workspace(nv, f, dt)), dtype=torch.uint8, device=dev)
     g_layers, g_pre = [None] * L, [None] * (L + 1)
     for l in range(L, 0, -1):
         layer, (q, q_bias) = model.layers[l - 1], model.pre[l]

@@ -42,3 +42,19 @@ def test_workspace_of_the_backward_pass_is_bounded():
     for f in (1, 8, 47, 64, 256, 400, 768, 1433, 4096):
         for n in (1, 600_000, 3_125_002, 24_700_000, 111_059_956, 1 << 33):
             assert B.gas_residual_norm_bwd_workspace(n, f) <= (1 << 20) * f, (n, f)
+
+
+def test_workspace_of_either_type():
+    import torch
+    from paper_2106_05609_amd import binding as B
+    for f in (1, 7, 64, 256, 600, 1433, 5000, 9000):
+        last = {}
+        for n in [*range(0, 3000, 13), 50_000, 262_143, 600_000, 3_125_002, 111_059_956]:
+            both = [B.gas_residual_norm_bwd_workspace(n, f, dt) for dt in (torch.float32, torch.bfloat16)]
+            assert max(both) == B.gas_residual_norm_bwd_workspace(n, f)
+            for dt, need in enumerate(both):
+                assert need >= last.get(dt, 0)
+                last[dt] = need
+    assert B.gas_residual_norm_bwd_workspace(200_000, 600, torch.bfloat16) == 256 * 5 * 600 * 4
+    with pytest.raises(TypeError):
+        B.gas_residual_norm_bwd_workspace(1, 1, torch.float16)
