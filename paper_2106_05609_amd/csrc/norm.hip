@@ -813,8 +813,8 @@ void launch_rows(const Layout& l, dim3 grid, hipStream_t s, const C& c) {
         return;                                                                                                                       \
     }
     if constexpr (!ALL) { GAS_ROWS(1, 1, 1) GAS_ROWS(2, 1, 1) GAS_ROWS(4, 1, 1) }
-    GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 1) GAS_ROWS(64, 1, 2) GAS_ROWS(64, 1, 3)
-    GAS_ROWS(64, 4, 1) GAS_ROWS(64, 6, 1) GAS_ROWS(64, 8, 1) GAS_ROWS(64, 12, 1) GAS_ROWS(64, 16, 1)
+    GAS_ROWS(8, 1, 1) GAS_ROWS(16, 1, 1) GAS_ROWS(32, 1, 1) GAS_ROWS(64, 1, 2) GAS_ROWS(64, 1, 3)
+    if constexpr (!(kBwd && ALL)) { GAS_ROWS(64, 1, 1) GAS_ROWS(64, 4, 1) GAS_ROWS(64, 6, 1) GAS_ROWS(64, 8, 1) GAS_ROWS(64, 12, 1) GAS_ROWS(64, 16, 1) }
 #undef GAS_ROWS
 }
 template <class C>
@@ -823,7 +823,12 @@ void launch_rows(const Layout& l, bool bf, hipStream_t s, C& c) {
     c.turns = l.turns;
     const bool mask = c.F % (bf ? 8 : 4) != 0;
     bool all;
-    if constexpr (std::is_same_v<C, ResidualNormBwd>) all = c.GH && c.GU && c.A && c.GX && c.GA && c.stats;
+    // Kernels that know beforehand what there is, us against those that look.  Forward from eight lanes on: 3.1 M x 256 bf16 1,317 and 1,329, 1 M x 100 bf16 189 and 192,
+    // 20,000 x 1,433 floats 105 and 109, 8,000 x 8,192 bf16 154 and 157, elsewhere alike.  Backward they have more registers, which pays in teams of 8 to 32 lanes (600,000 x
+    // 64 floats 222 and 230, x 128 435 and 442; but x 40 158 and 142) and with several pieces (66,667 x 600 bf16 172 and 181, 19,997 x 1,433 bf16 93 and 100, 200,000 x 400 floats
+    // 476 and 478), not with one piece in 64 lanes (300,000 x 512 bf16 476 and 453, 600,000 x 256 floats 884 and 878) nor with several wavefronts (13,333 x 3,000 bf16 168 and
+    // 148, 10,000 x 6,000 313 and 232, 8,000 x 8,192 738 and 566).
+    if constexpr (std::is_same_v<C, ResidualNormBwd>) all = c.GH && c.GU && c.A && c.GX && c.GA && c.stats && l.w == 1 && (l.g < 64 || l.p > 1);
     else all = c.A && c.H && c.U && !c.hist;
     all = all && l.g >= 8;
 #define GAS_ROWS(BF, MASK, ALL) \
