@@ -132,7 +132,8 @@ struct AdamStep {
 constexpr uint16_t kHalf = 0x8000;
 
 // Two numbers of 16 bits from an element's place in the state and the step: multiplied and folded until every bit of both
-// has reached all others.
+// has reached all others.  Shifts and multipliers of the folding are those of C. Wellons' published search for 32-bit mixing functions of low bias (2018); the place's
+// high half comes in by a multiplier of A. Appleby's published 32-bit hash finalizer, the step by 2^32 over the golden ratio.
 __device__ __forceinline__ uint32_t dice(int64_t place, uint32_t step) {
     uint32_t x = (uint32_t)place + (uint32_t)(place >> 32) * 0x85EBCA6Bu;
     x ^= step * 0x9E3779B9u;
@@ -179,10 +180,10 @@ __device__ __forceinline__ float largest(const f32x4& x) {
 }
 
 // A wavefront takes one block.  What it loads waits for nothing that it can do without: the clipping factor comes last.  32 bits: 28 bytes an
-// element and some 30 operations: 311 us for 70 M, 6.3 TB/s, as a copy.  8 bits: 16 (float weights) and some 110, half of them the rounding: 154 M
-// bf16 weights with masters, 18 bytes each, 507 us, 5.4 TB/s, 71% of it instructions.  Two or four blocks to a wavefront: 8 bits, 270,000 elements 17 us, 19 and 25, 16 M 78, 80
-// and 86, 154 M with their unpacking 665, 651 and 654; 32 bits, 154 M 715, 759 and 756.  Roots and quotients are the instructions' own, to one unit in the last
-// place.
+// element and some 35 operations: 311 to 340 us for 70 M, 5.8 to 6.3 TB/s, near a copy.  8 bits: 16 (float weights) and some 115, half of them the rounding: 154 M
+// bf16 weights with masters, 18 bytes each, 483 to 548 us, 5.1 to 5.7 TB/s, bound by issuing them (2% faster when the compiler may fuse).  Two or four
+// blocks to a wavefront (measured while it might): 8 bits, 270,000 elements 17 us, 19 and 25, 16 M 78, 80 and 86, 154 M with their unpacking 665, 651 and 654; 32 bits,
+// 154 M 715, 759 and 756.  Roots and quotients are the instructions' own, to one unit in the last place.
 template <bool EIGHT, int N>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamTensors<N> l, AdamStep b) {
     const int lane = threadIdx.x & 63;
