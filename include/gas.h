@@ -546,7 +546,8 @@ GAS_API gas_status gas_sq_norms(int32_t count, const float* const* x, const int6
  *     W <- W - lr wd W - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps).
  * The rates are what is passed: 1 - 0.999 from a float has lost five of its digits.  eps: a normal number.
  * W, dtypes (a gas_dtype each), n, dW, weight_decay (NULL: none): host arrays of `count`; W[i], dW[i] (fp32): n[i] contiguous
- * elements.  Tensors that share memory are updated in order; a gradient must not overlap a tensor of the call.
+ * elements.  Tensors that share memory are updated in order (GAS_BF16 with masters, each of its own: the last one's value
+ * stays); a gradient must not overlap a tensor of the call.
  * t: `step` >= 1, or, if `steps` is given, what it holds on the device, >= 1 (so a captured step counts on).  c = 1, or with sq_norm (fp32[1],
  * device: the squared norm of all gradients, gas_sq_norms) min(1, max_norm / (sqrt(sq_norm) + 1e-6)), max_norm > 0, possibly
  * infinite; if sq_norm is an infinity or a NaN, the call changes nothing.

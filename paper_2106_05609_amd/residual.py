@@ -139,7 +139,7 @@ def residual_train_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories
 class AdamW:
     """The AdamW step of a list of tensors (float32 or bfloat16) with gradients in float32, clipped by their global norm.  bits: of the states; with 8,
     tensors of fewer than SMALL elements keep 32, which costs little and keeps gains and biases exact.  bfloat16 tensors are
-    updated through float32 masters.  Tensors with one dimension (gains, biases) are not decayed.  A step whose gradients hold an infinity or a NaN
+    updated through float32 masters, so they must not share memory.  Tensors with one dimension (gains, biases) are not decayed.  A step whose gradients hold an infinity or a NaN
     changes nothing, the number of steps included.  The number is kept on the device, so a captured step() counts on."""
     SMALL = 4096
 
@@ -149,6 +149,9 @@ class AdamW:
         self.tensors, self.lr, self.max_norm = list(tensors), lr, max_norm
         if not self.tensors:
             raise ValueError("AdamW: no tensors")
+        spans = sorted((t.data_ptr(), t.data_ptr() + 2 * t.numel()) for t in self.tensors if t.dtype == torch.bfloat16 and t.numel())
+        if any(one[1] > next_[0] for one, next_ in zip(spans, spans[1:])):
+            raise ValueError("AdamW: bfloat16 tensors that share memory, each with a master of its own: only the last one's gradient would count")
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps)
         dev = self.tensors[0].device
         self.steps, self.sq_norm = torch.zeros(1, dtype=torch.int32, device=dev), torch.zeros(1, device=dev)
