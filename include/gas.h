@@ -473,6 +473,68 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
                          float lr, float weight_decay, void* stream);
 
 /*
+ * The output layer over many classes, without its logits: with X [n_rows, F], W [F, n_classes] and bias [n_classes] (or NULL) of type dt,
+ *     z_i = X[i] W + bias
+ * is formed a tile at a time on the matrix cores, used, and dropped.  Products are summed in fp32 (fp32 operands by three bf16 parts each,
+ * as in gas_linear), statistics of a row and sums over rows are fp32.  F up to 65536, n_classes up to 4194304; the calls are meant for
+ * classes by the thousand (for a few dozen gas_linear and gas_softmax_xent take less).  A bias of -infinity takes a class out: its
+ * probability is 0.  An infinity or NaN of X stays in its row, one of W makes its class's logits NaN.
+ *
+ * gas_linear_xent: cross-entropy of the rows with a label, 0 <= labels[i] < n_classes:
+ *     lse[i] = log sum_c exp z_ic,   loss_rows[i] = lse[i] - z_{i, labels[i]};   rows without one: 0 and 0, at no cost.
+ * loss_rows, lse: fp32[n_rows]; loss_sum: optional fp32[1], the sum of loss_rows in a fixed order (double accumulation).
+ *
+ * gas_linear_xent_bwd: with lse as the forward call left it and r = row_scale (fp32[n_rows], NULL: 1), the gradient of
+ * scale * sum_i r_i loss_rows[i]:
+ *     G[i, c] = r_i (exp(z_ic - lse_i) - [c == labels[i]]),   GX = scale G W^T,   GW = scale X^T G,   gbias = scale sum_i G[i]
+ * GX [n_rows, F] of type dt; GW [F, n_classes] of dt_gw, fp32 or W's type; gbias fp32[n_classes]; each may be NULL, not all of them.  Rows
+ * without a label get zeros in GX.  The logits are formed again, a piece of the classes at a time, and G of the piece is rounded to
+ * bf16 for its products where dt is GAS_BF16 (before scale; gbias sums it unrounded).  n_rows = 0 writes zeros to GW and gbias.
+ *
+ * gas_linear_distill: a student's loss against a teacher's k top logits, with labels beside it (labels not NULL) or without.  ids int32
+ * [n_rows, k], values fp32 [n_rows, k]: classes and logits in any order, as gas_linear_top writes them; an entry whose id is
+ * outside 0 .. n_classes - 1, or whose value is -infinity, is not there.  With T = temperature, q = softmax(values / T) over the entries of
+ * the row, p = softmax(z), p^T = softmax(z / T):
+ *     loss_rows[i] = b T^2 sum_k q_k (log q_k - log p^T_{ids_k}) - a log p_{labels[i]}
+ * a = label_weight and b = 1 - label_weight with labels, else b = 1; a row without entries has b = 0, without a label a = 0, without
+ * either it costs nothing and all its results are 0.  A class named twice has both entries' weight.  k up to 256.
+ * lse: fp32[n_rows, 2], log sum exp z and log sum exp (z / T).  gas_linear_distill_bwd: the gradient as above, with
+ *     G[i, c] = r_i (a (p_c - [c == labels[i]]) + b T (p^T_c - q_c)).
+ *
+ * gas_linear_top: the k largest logits of every row, the largest first, of equal ones those of lower classes first: ids int32
+ * [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
+ *
+ * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
+ * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X and, unless W
+ * is bf16 with 16-byte aligned rows of whole 16-byte pieces, W as the products take them; statistics of every 256 classes;
+ * backward a piece of G, 0.5 GB (fp32: 1.5 GB) or 256 classes of it if they are more.
+ */
+GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
+GAS_API gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, const int32_t* labels, float* loss_rows, float* loss_sum, float* lse,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+GAS_API int64_t gas_linear_xent_bwd_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
+GAS_API gas_status gas_linear_xent_bwd(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, const int32_t* labels, const float* lse, float scale,
+                           const float* row_scale, void* GX, int64_t ldgx, void* GW, int64_t ldgw, gas_dtype dt_gw, float* gbias,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+GAS_API int64_t gas_linear_distill_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt, int32_t k);
+GAS_API gas_status gas_linear_distill(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, const int32_t* ids, int64_t ld_ids, const float* values, int64_t ld_values,
+                           int32_t k, float temperature, const int32_t* labels, float label_weight, float* loss_rows, float* loss_sum,
+                           float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+GAS_API int64_t gas_linear_distill_bwd_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt, int32_t k);
+GAS_API gas_status gas_linear_distill_bwd(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, const int32_t* ids, int64_t ld_ids, const float* values, int64_t ld_values,
+                           int32_t k, float temperature, const int32_t* labels, float label_weight, const float* lse, float scale,
+                           const float* row_scale, void* GX, int64_t ldgx, void* GW, int64_t ldgw, gas_dtype dt_gw, float* gbias,
+                           void* workspace, int64_t workspace_bytes, void* stream);
+GAS_API int64_t gas_linear_top_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt, int32_t k);
+GAS_API gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, int32_t k, int32_t* ids, int64_t ld_ids, float* values, int64_t ld_values,
+                           float* lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
  * Gradient clipping by the global norm (Section 3 of the paper: clipping keeps
  * the parameters, and so the histories, from changing too fast).
  * gas_sq_norm: out[0] = sum of x[i]^2, i in [0, n) (fp64 accumulation in a

@@ -10,4 +10,6 @@ from .binding import (  # noqa: F401
     gas_softmax_xent, gas_sgd_step, gas_sgd_steps, gas_sq_norm, gas_sgd_step_clipped, gas_axpy, gas_row_distance, gas_row_distance_bwd, gas_row_dot,
     gas_pna_aggregate, gas_gat_aggregate, gas_pna_aggregate_bwd, gas_gat_aggregate_bwd,
     NORM_NONE, NORM_RMS, NORM_LAYER, gas_residual_norm, gas_residual_norm_bwd, gas_residual_norm_bwd_workspace,
+    gas_linear_xent, gas_linear_xent_bwd, gas_linear_distill, gas_linear_distill_bwd, gas_linear_top,
+    gas_linear_xent_workspace, gas_linear_xent_bwd_workspace, gas_linear_distill_workspace, gas_linear_distill_bwd_workspace, gas_linear_top_workspace,
     gas_sq_norms, gas_adamw_elements, gas_adamw_steps, gas_adamw_unpack)

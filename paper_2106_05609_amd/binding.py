@@ -32,6 +32,8 @@ EXPORTS = [
     "gas_gat_aggregate_bwd_bounded",
     "gas_residual_norm", "gas_residual_norm_bwd", "gas_residual_norm_bwd_workspace", "gas_residual_norm_bwd_typed_workspace", "gas_sq_norms", "gas_sq_norms_workspace",
     "gas_adamw_elements", "gas_adamw_steps", "gas_adamw_unpack",
+    "gas_linear_xent", "gas_linear_xent_bwd", "gas_linear_distill", "gas_linear_distill_bwd", "gas_linear_top", "gas_linear_xent_workspace",
+    "gas_linear_xent_bwd_workspace", "gas_linear_distill_workspace", "gas_linear_distill_bwd_workspace", "gas_linear_top_workspace",
     "gas_disk_open", "gas_disk_close", "gas_disk_pull", "gas_disk_push", "gas_disk_wait", "gas_disk_read_rows",
     "gas_disk_write_rows", "gas_disk_sync",
 ]
@@ -66,6 +68,9 @@ def lib():
         L.gas_gat_aggregate_bwd_workspace.restype = C.c_int64
         L.gas_gat_aggregate_bwd_heads_workspace.restype = C.c_int64
         for name in ("gas_residual_norm_bwd_workspace", "gas_residual_norm_bwd_typed_workspace", "gas_sq_norms_workspace", "gas_adamw_elements"):
+            getattr(L, name).restype = C.c_int64
+        for name in ("gas_linear_xent_workspace", "gas_linear_xent_bwd_workspace", "gas_linear_distill_workspace",
+                     "gas_linear_distill_bwd_workspace", "gas_linear_top_workspace"):
             getattr(L, name).restype = C.c_int64
         for name in EXPORTS:
             if name not in ("gas_last_error", "gas_version", "gas_plan_destroy") and not name.endswith(_COUNTS):
@@ -104,6 +109,10 @@ _SIGNATURES = dict(
     gas_residual_norm="pqpqpqiqiiipppfippfpqpqpppqqp", gas_residual_norm_bwd_workspace="qi",
     gas_residual_norm_bwd_typed_workspace="qii",
     gas_residual_norm_bwd="pqpqpqpqpqipqiiipppfippqpqpqppppppqp", gas_sq_norms="ipppppqp", gas_sq_norms_workspace="ip",
+    gas_linear_xent="pqqipqipipppppqp", gas_linear_xent_workspace="qiii", gas_linear_xent_bwd="pqqipqipippfppqpqippqp",
+    gas_linear_xent_bwd_workspace="qiii", gas_linear_distill="pqqipqipipqpqifpfppppqp", gas_linear_distill_workspace="qiiii",
+    gas_linear_distill_bwd="pqqipqipipqpqifpfpfppqpqippqp", gas_linear_distill_bwd_workspace="qiiii",
+    gas_linear_top="pqqipqipiipqpqppqp", gas_linear_top_workspace="qiiii",
     gas_adamw_elements="ip", gas_adamw_steps="ippppppppqiffffpqppfp", gas_adamw_unpack="pppqippp",
 )
 
@@ -873,6 +882,150 @@ def gas_adamw_unpack(m, v, scales, m_out, v_out):
         raise ValueError("gas_adamw_unpack: shapes or dtypes do not match")
     _check(_calls().gas_adamw_unpack(_ptr(m, torch.int8), _ptr(v, torch.uint8), _ptr(scales, torch.float32), n, _dt(m_out), _ptr(m_out),
                                      _ptr(v_out), _stream()))
+
+
+def _layer_of(who, x, w, bias):
+    """Arguments of X, W and the bias of an output layer."""
+    xp, ldx, n, width, dt = _size(x)
+    wp, ldw, rows, classes, dtw = _size(w)
+    if rows != width or dtw != dt or (bias is not None and (bias.numel() != classes or bias.dtype != w.dtype)):
+        raise ValueError(f"{who}: shapes or dtypes do not match")
+    return (xp, ldx, n, width, wp, ldw, classes, _ptr(bias), dt)
+
+
+def _here(who, like, *ts):
+    """All on the current device, whose stream the call takes."""
+    dev = like.device
+    if any(t is not None and t.device != dev for t in ts) or (dev.type == "cuda" and dev.index != torch.cuda.current_device()):
+        raise ValueError(f"{who}: tensors on different devices, or not on the current one")
+
+
+def _rows_of(who, n, *vs):
+    """Addresses of vectors (tensor, dtype) of one value a row, 0 for None."""
+    for v, _ in vs:
+        if v is not None and v.numel() != n:
+            raise ValueError(f"{who}: a vector of {v.numel()} for {n} rows")
+    return tuple(_ptr(v, dtype) for v, dtype in vs)
+
+
+def _entries_of(who, n, ids, values):
+    """Arguments of a teacher's entries: two matrices [n, k]."""
+    ip, ldi, ni, k, _ = _size(ids)
+    vp, ldv, nv, kv, dtv = _size(values)
+    if ids.dtype != torch.int32 or dtv != F32 or ni != n or nv != n or kv != k:
+        raise ValueError(f"{who}: ids int32 and values float32, [{n}, k]")
+    return ip, ldi, vp, ldv, k
+
+
+def _room(workspace, need, like):
+    """Address and bytes of a workspace, allocated here if not given; need: -1 for sizes that the call refuses itself."""
+    if workspace is None:
+        workspace = torch.empty(max(0, need), dtype=torch.uint8, device=like.device)
+    return workspace, _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _gradients_of(who, x, w, gx, gw, gbias):
+    """Arguments of the gradients at X, W and the bias."""
+    gxp, ldgx, n, f, dtx = (0, 0, *_size(x)[2:]) if gx is None else _size(gx)
+    gwp, ldgw, fw, c, dtg = (0, 0, *_size(w)[2:]) if gw is None else _size(gw)
+    if (n, f, dtx) != _size(x)[2:] or (fw, c) != _size(w)[2:4] or (gbias is not None and gbias.numel() != c):
+        raise ValueError(f"{who}: shapes or dtypes do not match")
+    return gxp, ldgx, gwp, ldgw, dtg, _ptr(gbias, torch.float32)
+
+
+def gas_linear_xent(x, w, labels, loss_rows, lse, bias=None, loss_sum=None, workspace=None):
+    """Cross-entropy of the logits x @ w + bias over many classes, which are not kept: loss_rows, lse float32 [n] (0 where labels, int32 [n], name
+    no class), loss_sum float32 [1].  workspace: a uint8 tensor of gas_linear_xent_workspace(n, F, classes, dtype) bytes, allocated here if
+    not given."""
+    calls, who = _calls(), "gas_linear_xent"
+    layer = _layer_of(who, x, w, bias)
+    n, dt = layer[2], layer[-1]
+    _here(who, x, w, labels, loss_rows, lse, bias, loss_sum, workspace)
+    lp, rp, sp = _rows_of(who, n, (labels, torch.int32), (loss_rows, torch.float32), (lse, torch.float32))
+    room, at, size = _room(workspace, calls.gas_linear_xent_workspace(n, layer[3], layer[6], dt), x)
+    _check(calls.gas_linear_xent(*layer, lp, rp, _ptr(loss_sum, torch.float32), sp, at, size, _stream()))
+
+
+def gas_linear_xent_bwd(x, w, labels, lse, gx=None, gw=None, gbias=None, bias=None, scale=1.0, row_scale=None, workspace=None):
+    """Backward of gas_linear_xent, of scale * sum(row_scale * loss_rows): gx as x, gw [F, classes] float32 or as w, gbias float32 [classes], each
+    optional; lse as the forward call left it; row_scale float32 [n].  workspace: gas_linear_xent_bwd_workspace(...) bytes."""
+    calls, who = _calls(), "gas_linear_xent_bwd"
+    layer = _layer_of(who, x, w, bias)
+    n, dt = layer[2], layer[-1]
+    _here(who, x, w, labels, lse, gx, gw, gbias, bias, row_scale, workspace)
+    lp, sp, rp = _rows_of(who, n, (labels, torch.int32), (lse, torch.float32), (row_scale, torch.float32))
+    gxp, ldgx, gwp, ldgw, dtg, gbp = _gradients_of(who, x, w, gx, gw, gbias)
+    room, at, size = _room(workspace, calls.gas_linear_xent_bwd_workspace(n, layer[3], layer[6], dt), x)
+    _check(calls.gas_linear_xent_bwd(*layer, lp, sp, scale, rp, gxp, ldgx, gwp, ldgw, dtg, gbp, at, size, _stream()))
+
+
+def gas_linear_distill(x, w, ids, values, loss_rows, lse, bias=None, labels=None, temperature=1.0, label_weight=0.5, loss_sum=None, workspace=None):
+    """Distillation of the logits x @ w + bias from a teacher's top logits (ids int32 and values float32 [n, k], an id < 0: no entry) and, with
+    weight label_weight, from labels (int32 [n], None: none): loss_rows float32 [n], lse float32 [n, 2]."""
+    calls, who = _calls(), "gas_linear_distill"
+    layer = _layer_of(who, x, w, bias)
+    n, dt = layer[2], layer[-1]
+    _here(who, x, w, ids, values, labels, loss_rows, lse, bias, loss_sum, workspace)
+    ip, ldi, vp, ldv, k = _entries_of(who, n, ids, values)
+    if tuple(lse.shape) != (n, 2):
+        raise ValueError(f"{who}: lse [{n}, 2]")
+    lp, rp = _rows_of(who, n, (labels, torch.int32), (loss_rows, torch.float32))
+    room, at, size = _room(workspace, calls.gas_linear_distill_workspace(n, layer[3], layer[6], dt, k), x)
+    _check(calls.gas_linear_distill(*layer, ip, ldi, vp, ldv, k, temperature, lp, label_weight, rp, _ptr(loss_sum, torch.float32),
+                                    _ptr(lse, torch.float32), at, size, _stream()))
+
+
+def gas_linear_distill_bwd(x, w, ids, values, lse, gx=None, gw=None, gbias=None, bias=None, labels=None, temperature=1.0, label_weight=0.5, scale=1.0,
+                           row_scale=None, workspace=None):
+    """Backward of gas_linear_distill; gradients as in gas_linear_xent_bwd."""
+    calls, who = _calls(), "gas_linear_distill_bwd"
+    layer = _layer_of(who, x, w, bias)
+    n, dt = layer[2], layer[-1]
+    _here(who, x, w, ids, values, labels, lse, gx, gw, gbias, bias, row_scale, workspace)
+    ip, ldi, vp, ldv, k = _entries_of(who, n, ids, values)
+    if tuple(lse.shape) != (n, 2):
+        raise ValueError(f"{who}: lse [{n}, 2]")
+    lp, rp = _rows_of(who, n, (labels, torch.int32), (row_scale, torch.float32))
+    gxp, ldgx, gwp, ldgw, dtg, gbp = _gradients_of(who, x, w, gx, gw, gbias)
+    room, at, size = _room(workspace, calls.gas_linear_distill_bwd_workspace(n, layer[3], layer[6], dt, k), x)
+    _check(calls.gas_linear_distill_bwd(*layer, ip, ldi, vp, ldv, k, temperature, lp, label_weight, _ptr(lse, torch.float32), scale, rp, gxp, ldgx, gwp,
+                                        ldgw, dtg, gbp, at, size, _stream()))
+
+
+def gas_linear_top(x, w, ids, values, lse=None, bias=None, workspace=None):
+    """The k largest of the logits x @ w + bias of every row, the largest first, and their classes: ids int32, values float32 [n, k]; lse float32 [n]."""
+    calls, who = _calls(), "gas_linear_top"
+    layer = _layer_of(who, x, w, bias)
+    n, dt = layer[2], layer[-1]
+    _here(who, x, w, ids, values, lse, bias, workspace)
+    ip, ldi, vp, ldv, k = _entries_of(who, n, ids, values)
+    lp, = _rows_of(who, n, (lse, torch.float32))
+    room, at, size = _room(workspace, calls.gas_linear_top_workspace(n, layer[3], layer[6], dt, k), x)
+    _check(calls.gas_linear_top(*layer, k, ip, ldi, vp, ldv, lp, at, size, _stream()))
+
+
+def _layer_bytes(name, n_rows, width, classes, dtype, *k) -> int:
+    return int(getattr(_calls(), name)(n_rows, width, classes, _dt(torch.empty(0, dtype=dtype)), *k))
+
+
+def gas_linear_xent_workspace(n_rows, width, classes, dtype) -> int:
+    return _layer_bytes("gas_linear_xent_workspace", n_rows, width, classes, dtype)
+
+
+def gas_linear_xent_bwd_workspace(n_rows, width, classes, dtype) -> int:
+    return _layer_bytes("gas_linear_xent_bwd_workspace", n_rows, width, classes, dtype)
+
+
+def gas_linear_distill_workspace(n_rows, width, classes, dtype, k) -> int:
+    return _layer_bytes("gas_linear_distill_workspace", n_rows, width, classes, dtype, k)
+
+
+def gas_linear_distill_bwd_workspace(n_rows, width, classes, dtype, k) -> int:
+    return _layer_bytes("gas_linear_distill_bwd_workspace", n_rows, width, classes, dtype, k)
+
+
+def gas_linear_top_workspace(n_rows, width, classes, dtype, k) -> int:
+    return _layer_bytes("gas_linear_top_workspace", n_rows, width, classes, dtype, k)
 
 
 ANY_LENGTH = 0x7FFFFFFF          # of rows and columns: nothing is known

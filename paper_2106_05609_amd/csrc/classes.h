@@ -1,0 +1,276 @@
+// The output layer over many classes, none of whose logits are kept: what its losses (classes.hip) and its top logits
+// (classes_top.hip) share.
+//     z_i = x_i W + bias,     X [n, F], W [F, C] of fp32 or bf16
+// Rows that do not count (no label, no entry of a teacher's) have no product: those that do are numbered one after another on the device
+// (`count` of them), and a kernel sized for all of them ends at once where there are none left.  What a later launch's shape
+// depends on (the width of a piece of the classes, parts of a split sum) is worked out from `count` in every kernel alike.
+#pragma once
+#include "tile_product.h"
+
+namespace gas {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kTileC = 256;                       // classes of a tile
+constexpr int kMaxClasses = 1 << 22;              // a tile's 256 rows of W then lie within 4 GB
+constexpr int kMaxWidth = 1 << 16;
+constexpr int kMaxEntries = 256;                  // of a teacher's row
+constexpr int kHeldEntries = 4;                   // of a row in one tile that are fetched before the products
+
+inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// What kernels know of the layer.
+struct Layer {
+    const uint16_t* x;            // [planes][rows up to 256][fp], packed, zero beyond the row and beyond the last row
+    const uint16_t* w;            // [planes][F][ldw], columns up to cw readable
+    int64_t ldw, w_plane, x_plane;
+    const float* bias;            // [C up to 256], -inf beyond C
+    const int32_t* count;         // rows that count
+    int32_t F, fp, C, cw, terms, most;     // fp: F up to 64; most: rows up to 256
+};
+
+// ---- rows that count
+
+struct Targets {
+    const int32_t* labels;        // [n] or NULL
+    const int32_t* ids;           // [n, k] or NULL
+    const float* values;
+    int64_t ld_ids, ld_values, n;
+    int32_t k, C;
+};
+
+__device__ __forceinline__ bool entry_counts(int32_t id, float v, int C) { return id >= 0 && id < C && !(v == -INFINITY); }
+
+__device__ __forceinline__ bool row_counts(const Targets& t, int64_t i) {
+    if (t.labels && t.labels[i] >= 0 && t.labels[i] < t.C) return true;
+    if (!t.ids) return false;
+    for (int k = 0; k < t.k; ++k)
+        if (entry_counts(t.ids[i * t.ld_ids + k], t.values[i * t.ld_values + k], t.C)) return true;
+    return false;
+}
+
+// ---- packing
+
+// elements 8 at a time into the planes: `to` in elements of a plane
+__device__ __forceinline__ void put8(const float (&v)[8], int terms, uint16_t* p, int64_t plane, int64_t at) {
+    u32x4 h, m, l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        uint32_t a, b, c;
+        split_pair(v[2 * e], v[2 * e + 1], a, b, c);
+        h[e] = a; m[e] = b; l[e] = c;
+    }
+    *reinterpret_cast<u32x4*>(p + at) = h;
+    if (terms > 1) {
+        *reinterpret_cast<u32x4*>(p + at + plane) = m;
+        *reinterpret_cast<u32x4*>(p + at + 2 * plane) = l;
+    }
+}
+
+// eight elements of a row of any alignment, zero from `width` on
+template <bool BF>
+__device__ __forceinline__ void get8(const void* row, int c, int width, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float x = 0.f;
+        if (c + e < width) {
+            if constexpr (BF) x = __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[c + e] << 16);
+            else x = static_cast<const float*>(row)[c + e];
+        }
+        v[e] = x;
+    }
+}
+
+struct PackArgs {
+    const void *X, *W, *bias;
+    int64_t ldx, ldw, n;
+    const int32_t* idx;           // NULL: every row counts
+    int32_t* count;               // written where every row counts
+    uint16_t *x, *w;              // w NULL: read where it lies
+    float* biasp;
+    int64_t x_plane, w_plane;
+    int32_t F, fp, C, cw, cp, terms;
+    unsigned x_blocks, w_blocks;  // then one workgroup for every 256 of the bias
+};
+
+// X's rows, W and the bias as the tile products take them, a workgroup a row or 2048 columns of one
+template <bool BF>
+__global__ __launch_bounds__(256) void classes_pack_kernel(PackArgs a) {
+    constexpr int EB = BF ? 2 : 4;
+    unsigned b = blockIdx.x;
+    if (b < a.x_blocks) {
+        const int64_t count = a.idx ? *a.count : a.n;
+        if (!a.idx && b == 0 && threadIdx.x == 0) *a.count = (int32_t)a.n;
+        const int64_t rows = (count + 255) / 256 * 256;
+        const int pieces = a.fp / 8;
+        for (int64_t q = (int64_t)b * 256 + threadIdx.x; q < rows * pieces; q += (int64_t)a.x_blocks * 256) {
+            const int64_t r = q / pieces;
+            const int c = (int)(q % pieces) * 8;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (r < count) get8<BF>(static_cast<const char*>(a.X) + (a.idx ? a.idx[r] : r) * a.ldx * EB, c, a.F, v);
+            put8(v, a.terms, a.x, a.x_plane, r * a.fp + c);
+        }
+        return;
+    }
+    b -= a.x_blocks;
+    if (b < a.w_blocks) {
+        const int pieces = a.cw / 8;
+        for (int64_t q = (int64_t)b * 256 + threadIdx.x; q < (int64_t)a.F * pieces; q += (int64_t)a.w_blocks * 256) {
+            const int64_t r = q / pieces;
+            const int c = (int)(q % pieces) * 8;
+            float v[8];
+            get8<BF>(static_cast<const char*>(a.W) + r * a.ldw * EB, c, a.C, v);
+            put8(v, a.terms, a.w, a.w_plane, r * a.cw + c);
+        }
+        return;
+    }
+    b -= a.w_blocks;
+    const int c = (int)(b * 256 + threadIdx.x);
+    if (c >= a.cp) return;
+    float v = -INFINITY;
+    if (c < a.C) {
+        if (!a.bias) v = 0.f;
+        else if constexpr (BF) v = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.bias)[c] << 16);
+        else v = static_cast<const float*>(a.bias)[c];
+    }
+    a.biasp[c] = v;
+}
+
+// ---- which tile a workgroup has
+// Workgroups are dealt to the eight XCDs in turn; each XCD takes a contiguous range of the tiles, and in it eight row tiles by all
+// column tiles after one another, so that what runs there at a time reads few rows and few columns.
+__device__ __forceinline__ bool tile_of(unsigned block, int nm, int nc, int& m, int& c) {
+    const int64_t total = (int64_t)nm * nc, per = (total + 7) / 8;
+    const int64_t id = (int64_t)(block & 7) * per + (block >> 3);
+    if ((int64_t)(block >> 3) >= per || id >= total) return false;
+    const int64_t group = id / (8LL * nc), in = id % (8LL * nc);
+    const int first = (int)group * 8, rows = nm - first < 8 ? nm - first : 8;
+    m = first + (int)(in % rows);
+    c = (int)(in / rows);
+    return true;
+}
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The number of an accumulator's element along the first operand in its 32 x 32 block.
+__device__ __forceinline__ int acc_row(int r, int lh) { return 8 * (r / 4) + 4 * lh + (r % 4); }
+
+// ---- statistics of a row's logits, tile by tile: the largest, and the sums of the exponentials from there
+struct Parts {
+    float *most, *sum, *sum_t, *picked;      // [class tiles][most rows]; sum_t: at the temperature; picked: sum of weighted target logits
+};
+
+// A row's statistics over `n` tiles from `first` on in steps of `step`, joined.  (most, sum, sum_t) hold what was joined so far.
+__device__ __forceinline__ void join(float& most, float& sum, float& sum_t, float m, float s, float st, float inv_t) {
+    const float top = fmaxf(most, m), base = top == -INFINITY ? 0.f : top;
+    const float a = exp2_of((most - base) * kLog2e), b = exp2_of((m - base) * kLog2e);
+    const float at = exp2_of((most - base) * kLog2e * inv_t), bt = exp2_of((m - base) * kLog2e * inv_t);
+    sum = sum * a + s * b;
+    sum_t = sum_t * at + st * bt;
+    most = top;
+}
+
+inline unsigned blocks_for(int64_t items, int64_t per, int64_t most) {
+    const int64_t b = (items + per - 1) / per;
+    return (unsigned)(b < 1 ? 1 : (b < most ? b : most));
+}
+
+// ---- the workspace, piece after piece
+struct Room {
+    char* base;
+    int64_t used = 0;
+    template <class T>
+    T* take(int64_t n) {
+        T* p = reinterpret_cast<T*>(base + used);
+        used += round_up(n * (int64_t)sizeof(T), 256);
+        return p;
+    }
+};
+
+// The parts of the workspace that every call has, and the layer as its kernels take it.
+struct Common {
+    Layer layer;
+    PackArgs pack;
+    int32_t *idx, *pos, *block_counts;
+};
+inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, const void* W, int64_t ldw, int C, const void* bias,
+                      gas_dtype dt, bool compact) {
+    Common c = {};
+    const int planes = dt == GAS_F32 ? 3 : 1;
+    const int64_t most = round_up(n, 256), fp = round_up(F, 64), cp = round_up(C, kTileC);
+    // W where it lies if its rows can be read in whole pieces
+    const bool in_place = dt == GAS_BF16 && C % 8 == 0 && ldw % 8 == 0 && ldw <= kMaxClasses && aligned16(W);
+    const int64_t cw = in_place ? C : round_up(C, 64);
+    c.layer.terms = dt == GAS_F32 ? 6 : 1;
+    int32_t* count = room.take<int32_t>(1);
+    c.idx = compact ? room.take<int32_t>(most) : nullptr;
+    c.pos = compact ? room.take<int32_t>(most) : nullptr;
+    c.block_counts = compact ? room.take<int32_t>(most / 256) : nullptr;
+    uint16_t* x = room.take<uint16_t>(planes * most * fp);
+    uint16_t* w = in_place ? nullptr : room.take<uint16_t>(planes * (int64_t)F * cw);
+    float* biasp = room.take<float>(cp);
+    c.layer.x = x;
+    c.layer.w = in_place ? static_cast<const uint16_t*>(W) : w;
+    c.layer.ldw = in_place ? ldw : cw;
+    c.layer.w_plane = (int64_t)F * cw;
+    c.layer.x_plane = most * fp;
+    c.layer.bias = biasp;
+    c.layer.count = count;
+    c.layer.F = F;
+    c.layer.fp = (int32_t)fp;
+    c.layer.C = C;
+    c.layer.cw = (int32_t)cw;
+    c.layer.most = (int32_t)most;
+    c.pack = PackArgs{X, W, bias, ldx, ldw, n, c.idx, count, x, w, biasp, c.layer.x_plane, c.layer.w_plane, F, (int32_t)fp, C, (int32_t)cw,
+                      (int32_t)cp, c.layer.terms, blocks_for(most * fp / 8, 256, 4096), in_place ? 0u : blocks_for((int64_t)F * cw / 8, 256, 8192)};
+    return c;
+}
+
+inline gas_status run_pack(const Common& c, gas_dtype dt, hipStream_t s) {
+    const unsigned blocks = c.pack.x_blocks + c.pack.w_blocks + (unsigned)(c.pack.cp / 256);
+    if (dt == GAS_BF16) hipLaunchKernelGGL(classes_pack_kernel<true>, dim3(blocks), dim3(256), 0, s, c.pack);
+    else hipLaunchKernelGGL(classes_pack_kernel<false>, dim3(blocks), dim3(256), 0, s, c.pack);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
+// Checks that every call makes of the layer.
+inline gas_status check_layer(const char* who, const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t C,
+                              gas_dtype dt) {
+    if (!valid_dtype(dt)) return fail(GAS_ERR_DTYPE, "%s: unknown dtype %d", who, (int)dt);
+    GAS_REQUIRE(n_rows >= 0 && n_rows <= (1 << 28), "%s: n_rows=%lld, at most 2^28 are taken", who, (long long)n_rows);
+    GAS_REQUIRE(F > 0 && F <= kMaxWidth, "%s: F=%d, 1 to 65536 are taken", who, F);
+    GAS_REQUIRE(C > 0 && C <= kMaxClasses, "%s: n_classes=%d, 1 to 4194304 are taken", who, C);
+    if (n_rows == 0) return GAS_OK;
+    GAS_REQUIRE(X && W, "%s: null pointer", who);
+    GAS_REQUIRE(ldx >= F && ldw >= C, "%s: row stride smaller than the row", who);
+    return GAS_OK;
+}
+
+// Memory that a call reads or writes, for its check that no output overlaps anything else.
+struct Span {
+    const void* p;
+    int64_t bytes;
+};
+inline int64_t span(int64_t rows, int64_t ld, int64_t cols, int bytes) { return rows > 0 ? ((rows - 1) * ld + cols) * bytes : 0; }
+template <int NI, int NO>
+gas_status check_overlaps(const char* who, const Span (&in)[NI], const Span (&out)[NO]) {
+    auto meet = [](const Span& a, const Span& b) {
+        const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+        return a.p && b.p && p < q + (uintptr_t)b.bytes && q < p + (uintptr_t)a.bytes;
+    };
+    for (int i = 0; i < NO; ++i) {
+        for (const Span& o : in) GAS_REQUIRE(!meet(out[i], o), "%s: an output overlaps another matrix of the call", who);
+        for (int j = 0; j < i; ++j) GAS_REQUIRE(!meet(out[i], out[j]), "%s: two outputs overlap", who);
+    }
+    return GAS_OK;
+}
+
+template <class Kernel>
+gas_status lds_of(Kernel kernel, int bytes) {
+    GAS_CHECK_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return GAS_OK;
+}
+
+}  // namespace
+}  // namespace gas

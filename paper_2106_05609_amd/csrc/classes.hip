@@ -1,0 +1,800 @@
+// Losses of an output layer over many classes, forward and backward, without its logits: cross-entropy with labels, and
+// distillation from a teacher's top logits (with labels beside them or without).
+//
+// A row's loss is a (lse - z_y) + b T^2 (sum_k q_k log q_k + lse_T - sum_k q_k z_k / T), its gradient at the logits
+//     a exp(z - lse) + b T exp(z / T - lse_T) - w,     w_y += a, w_k += b T q_k:
+// both losses are two sums of exponentials and a short list of weighted targets, so one kernel forms either from a tile of logits.
+// Forward: tiles of logits leave a row's largest logit, its sums from there and its weighted target logits, which a second kernel
+// joins.  Backward: a piece of the classes at a time, the gradient at its logits (formed again from the products) is stored in the
+// products' type and multiplied by W and X.
+#include "classes_logits.h"
+
+namespace gas {
+namespace {
+
+// ---- rows that count, numbered in order
+
+// Rows that count in every 256; one workgroup does it all where there are few rows.
+__global__ __launch_bounds__(256) void classes_count_kernel(Targets t, int32_t* block_counts) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool on = i < t.n && row_counts(t, i);
+    const int n = __syncthreads_count(on);
+    if (threadIdx.x == 0) block_counts[blockIdx.x] = n;
+}
+
+// idx[r] = the r-th row that counts, pos[i] = its number or -1, count
+__global__ __launch_bounds__(256) void classes_number_kernel(Targets t, const int32_t* block_counts, int32_t* idx, int32_t* pos, int32_t* count) {
+    __shared__ int part[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    for (int b = tid; b < (int)blockIdx.x; b += 256) before += block_counts[b];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
+    if (lane == 0) part[wave] = before;
+    __syncthreads();
+    before = part[0] + part[1] + part[2] + part[3];
+    __syncthreads();
+    const int64_t i = (int64_t)blockIdx.x * 256 + tid;
+    const bool on = i < t.n && row_counts(t, i);
+    const uint64_t mask = __ballot(on);
+    if (lane == 0) part[wave] = __popcll(mask);
+    __syncthreads();
+    int r = before + __popcll(mask & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) r += part[w];
+    if (on) idx[r] = (int32_t)i;
+    if (i < t.n) pos[i] = on ? r : -1;
+    if (blockIdx.x + 1 == gridDim.x && tid == 0) *count = before + part[0] + part[1] + part[2] + part[3];
+}
+
+// ---- targets of the rows that count
+
+struct RowsArgs {
+    Targets t;
+    const int32_t *idx, *count;
+    const float* lse;             // backward: [n] (labels alone) or [n, 2]
+    const float* row_scale;       // backward: [n] or NULL
+    float label_weight, temperature;
+    int32_t* labels;              // [rows]: labels alone
+    f32x4* info;                  // [rows]: see LogitsArgs
+    float* entropy;               // [rows]: b T^2 sum q log q
+    int2* entries;
+    uint16_t* starts;
+    int32_t k, tiles;             // k: of a row in `entries`
+};
+
+// labels alone: a thread a row
+__global__ __launch_bounds__(256) void classes_labels_kernel(RowsArgs a) {
+    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (r >= *a.count) return;
+    const int64_t i = a.idx[r];
+    a.labels[r] = a.t.labels[i];
+    if (a.lse) a.info[r] = f32x4{a.lse[i], 0.f, a.row_scale ? a.row_scale[i] : 1.f, 0.f};
+}
+
+// A wavefront a row: the teacher's distribution over the entries that are there, the label among them, put in the order of their
+// classes by counting how many come before each, and where each tile of classes begins in them.
+__global__ __launch_bounds__(64) void classes_entries_kernel(RowsArgs a) {
+    constexpr int N = (kMaxEntries + 1 + 63) / 64;
+    __shared__ int32_t ids[kMaxEntries + 1], sorted[kMaxEntries + 1];
+    const int64_t r = blockIdx.x;
+    if (r >= *a.count) return;
+    const int64_t i = a.idx[r];
+    const int lane = threadIdx.x;
+    const float inv_t = 1.f / a.temperature;
+    int32_t id[N];
+    float v[N];
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int k = lane + 64 * j;
+        id[j] = 0x7FFFFFFF;
+        v[j] = -INFINITY;
+        if (k < a.t.k) {
+            const int32_t c = a.t.ids[i * a.t.ld_ids + k];
+            const float x = a.t.values[i * a.t.ld_values + k];
+            if (entry_counts(c, x, a.t.C)) {
+                id[j] = c;
+                v[j] = x * inv_t;
+                most = fmaxf(most, v[j]);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+    float total = 0.f, e[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        e[j] = id[j] == 0x7FFFFFFF ? 0.f : expf(v[j] - most);
+        total += e[j];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+    const bool some = __any(id[0] != 0x7FFFFFFF || id[1] != 0x7FFFFFFF || id[2] != 0x7FFFFFFF || id[3] != 0x7FFFFFFF || id[4] != 0x7FFFFFFF);
+    const int32_t label = a.t.labels ? a.t.labels[i] : -1;
+    const bool labelled = label >= 0 && label < a.t.C;
+    const float scale = a.row_scale ? a.row_scale[i] : 1.f;
+    const float wa = labelled ? a.label_weight * scale : 0.f;
+    const float wt = some ? (a.t.labels ? 1.f - a.label_weight : 1.f) * a.temperature * scale : 0.f;
+    const float log_total = logf(total);
+    float entropy = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const float q = e[j] / total;
+        if (id[j] != 0x7FFFFFFF && e[j] != 0.f) entropy = fmaf(q, v[j] - most - log_total, entropy);
+        e[j] = wt * q;
+        if (id[j] == 0x7FFFFFFF || e[j] == 0.f) {           // nothing is left of it: its logit may be anything
+            id[j] = 0x7FFFFFFF;
+            e[j] = 0.f;
+        }
+        const int k = lane + 64 * j;
+        if (k == a.t.k && labelled && wa != 0.f) {
+            id[j] = label;
+            e[j] = wa;
+        }
+        if (k <= a.t.k) ids[k] = id[j];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) entropy += __shfl_xor(entropy, o);
+    __syncthreads();
+    int there = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int k = lane + 64 * j;
+        if (k > a.t.k) continue;
+        int before = 0;
+        for (int o = 0; o <= a.t.k; ++o) before += ids[o] < id[j] || (ids[o] == id[j] && o < k);
+        sorted[before] = id[j];
+        if (before < a.k) a.entries[r * a.k + before] = int2{id[j], __float_as_int(e[j])};
+        there += id[j] != 0x7FFFFFFF;
+    }
+    __syncthreads();
+    for (int t = lane; t <= a.tiles; t += 64) {
+        int from = 0, to = a.t.k + 1;
+        const int64_t c = (int64_t)t * kTileC;
+        while (from < to) {
+            const int mid = (from + to) / 2;
+            if (sorted[mid] < c) from = mid + 1;
+            else to = mid;
+        }
+        a.starts[r * (a.tiles + 1) + t] = (uint16_t)from;
+    }
+    if (lane == 0) {
+        f32x4 info = {0.f, 0.f, wa, wt};
+        if (a.lse) {
+            info[0] = a.lse[2 * i];
+            info[1] = a.lse[2 * i + 1];
+        }
+        a.info[r] = info;
+        a.entropy[r] = wt * a.temperature * entropy;
+    }
+}
+
+// ---- forward: the rows' statistics joined
+
+struct LossArgs {
+    Layer layer;
+    Parts parts;
+    const int32_t* pos;
+    const f32x4* info;            // NULL: labels alone
+    const float* entropy;
+    int64_t n;
+    int32_t tiles, two;
+    float inv_t, temperature;
+    float *loss, *lse;
+};
+
+// sixteen rows a workgroup, sixteen threads a row: each joins every sixteenth tile, then they are joined one by one
+__global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
+    __shared__ float red[4][16][17];
+    const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int64_t i = (int64_t)blockIdx.x * 16 + row;
+    const int64_t r = i < a.n ? a.pos[i] : -1;
+    float most = -INFINITY, sum = 0.f, sum_t = 0.f, picked = 0.f;
+    if (r >= 0) {
+        for (int t = part; t < a.tiles; t += 16) {
+            const int64_t at = (int64_t)t * a.layer.most + r;
+            join(most, sum, sum_t, a.parts.most[at], a.parts.sum[at], a.two ? a.parts.sum_t[at] : 0.f, a.inv_t);
+            if (a.info) picked += a.parts.picked[at];
+        }
+    }
+    red[0][part][row] = most;
+    red[1][part][row] = sum;
+    red[2][part][row] = sum_t;
+    red[3][part][row] = picked;
+    __syncthreads();
+    if (part > 0 || i >= a.n) return;
+    for (int p = 1; p < 16; ++p) {
+        join(most, sum, sum_t, red[0][p][row], red[1][p][row], red[2][p][row], a.inv_t);
+        picked += red[3][p][row];
+    }
+    const float lse = most + logf(sum);
+    if (!a.info) {
+        a.loss[i] = r < 0 ? 0.f : lse - a.parts.picked[r];
+        a.lse[i] = r < 0 ? 0.f : lse;
+        return;
+    }
+    float loss = 0.f, lse_t = 0.f;
+    if (r >= 0) {
+        const f32x4 info = a.info[r];
+        lse_t = a.two ? most * a.inv_t + logf(sum_t) : lse;
+        if (info[2] != 0.f) loss = info[2] * lse;
+        if (info[3] != 0.f) loss = fmaf(info[3] * a.temperature, lse_t, loss) + a.entropy[r];
+        loss -= picked;
+    }
+    a.loss[i] = loss;
+    a.lse[2 * i] = r < 0 ? 0.f : lse;
+    a.lse[2 * i + 1] = lse_t;
+}
+
+// the sum of the rows' losses in a fixed order, in double
+__global__ __launch_bounds__(1024) void classes_sum_kernel(const float* x, int64_t n, float* out) {
+    __shared__ double part[1024];
+    double s = 0.0;
+    int64_t i = threadIdx.x;
+    for (; i + 7 * 1024 < n; i += 8 * 1024) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = x[i + 1024 * j];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += (double)v[j];
+    }
+    for (; i < n; i += 1024) s += (double)x[i];
+    part[threadIdx.x] = s;
+    __syncthreads();
+    for (int w = 512; w > 0; w >>= 1) {
+        if ((int)threadIdx.x < w) part[threadIdx.x] += part[threadIdx.x + w];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) out[0] = (float)part[0];
+}
+
+// ---- backward: the products with the gradient at the logits
+
+struct GradArgs {
+    Layer layer;
+    const uint16_t* g;
+    int64_t g_plane, cap;
+    int32_t piece;
+    float scale;
+    float* part;                  // gx: [split][rows][fp]; gw: [split][F][width]
+    void* gw;
+    int64_t ldgw;
+    int32_t gw_bf16;
+};
+
+// Parts of a sum, so that its tiles fill the card: as few as leave the compute units with something to do, at least eight steps each.
+constexpr int kFill = 512, kMostSplits = 16;
+__device__ __host__ __forceinline__ int splits_of(int64_t tiles, int steps) {
+    int64_t s = kFill / (tiles > 0 ? tiles : 1);
+    if (s > kMostSplits) s = kMostSplits;
+    if (s > steps / 8) s = steps / 8;
+    return s < 1 ? 1 : (int)s;
+}
+
+// what a launch finds from the number of rows
+struct Shape {
+    int rows, width, c_first, cols;          // rows up to 256; classes of this piece
+    bool on;
+};
+__device__ __forceinline__ Shape shape_of(const GradArgs& a) {
+    Shape s;
+    s.rows = (*a.layer.count + 255) / 256 * 256;
+    s.on = s.rows > 0;
+    s.width = piece_width(a.cap, s.on ? s.rows : 256, a.layer.C);
+    const int64_t from = (int64_t)a.piece * s.width;
+    s.on = from < a.layer.C;
+    s.c_first = (int)from;
+    s.cols = (int)(a.layer.C - from < s.width ? a.layer.C - from : s.width);
+    return s;
+}
+
+// gx += G W^T over a piece of the classes: lanes end up with four neighbouring inputs of one row
+template <int BA, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB) void classes_gx_kernel(GradArgs a) {
+    using P = TileProduct<BA, 256, WA, WB, false, false>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const Layer& l = a.layer;
+    const Shape s = shape_of(a);
+    if (!s.on || s.rows == 0) return;
+    const int nm = s.rows / 256, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
+    const int full = (s.width + kStepK - 1) / kStepK, splits = splits_of((int64_t)nm * nf, full);
+    int ft, at;
+    if (!tile_of(blockIdx.x, nf, nm * splits, ft, at)) return;
+    const int mt = at % nm, part = at / nm;
+    const int per = (full + splits - 1) / splits;
+    const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
+    const int m0 = mt * 256, f0 = ft * BA;
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
+    f32x16 acc[P::TA][P::TB];
+    P product;
+    const TileOperand oa = {l.w + (int64_t)f0 * l.ldw + s.c_first, l.ldw, l.w_plane, l.F - 1 - f0, l.cw - s.c_first};
+    const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, 255, s.width};
+    product.run(oa, ob, first, last, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    float* out = a.part + (int64_t)part * s.rows * l.fp;
+#pragma unroll
+    for (int j = 0; j < P::TB; ++j) {
+        float* row = out + (int64_t)(m0 + wb0 + 32 * j + li) * l.fp;
+#pragma unroll
+        for (int i = 0; i < P::TA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int f = f0 + wa0 + 32 * i + 8 * q + 4 * lh;
+                if (f >= l.fp) continue;
+                f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (a.piece > 0) v += *reinterpret_cast<const f32x4*>(row + f);
+                *reinterpret_cast<f32x4*>(row + f) = v;
+            }
+    }
+}
+
+__device__ __forceinline__ void put4(void* base, int64_t at, const f32x4& v, int n, bool bf, bool whole) {
+    if (bf) {
+        uint16_t* p = static_cast<uint16_t*>(base) + at;
+        if (whole) *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        else
+            for (int e = 0; e < n; ++e) p[e] = (uint16_t)f32_to_bf16(v[e]);
+    } else {
+        float* p = static_cast<float*>(base) + at;
+        if (whole) *reinterpret_cast<f32x4*>(p) = v;
+        else
+            for (int e = 0; e < n; ++e) p[e] = v[e];
+    }
+}
+// whether four elements from column 4 c of every row are aligned as one
+__device__ __host__ __forceinline__ bool fours(const void* p, int64_t ld, bool bf) { return ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & (bf ? 7 : 15)) == 0; }
+
+// gw = X^T G of a piece of the classes, or a part of the sum over the rows: lanes end up with four neighbouring classes of one input
+template <int BB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB) void classes_gw_kernel(GradArgs a) {
+    using P = TileProduct<256, BB, WA, WB, true, true>;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const Layer& l = a.layer;
+    const Shape s = shape_of(a);
+    if (!s.on) return;
+    const int nc = (s.cols + 255) / 256, nf = (l.fp + BB - 1) / BB, steps = (*l.count + kStepK - 1) / kStepK;
+    const int splits = splits_of((int64_t)((s.width + 255) / 256) * nf, steps);
+    int ft, at;
+    if (!tile_of(blockIdx.x, nf, nc * splits, ft, at)) return;
+    const int ct = at % nc, part = at / nc;
+    const int per = (steps + splits - 1) / splits;
+    const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
+    const int c0 = ct * 256, f0 = ft * BB;
+    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
+    f32x16 acc[P::TA][P::TB];
+    P product;
+    const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, l.most};
+    const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
+    product.run(oa, ob, first, last, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
+#pragma unroll
+    for (int j = 0; j < P::TB; ++j) {
+        const int f = f0 + wb0 + 32 * j + li;
+        if (f >= l.F) continue;
+#pragma unroll
+        for (int i = 0; i < P::TA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int c = c0 + wa0 + 32 * i + 8 * q + 4 * lh;
+                f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (splits > 1) {
+                    if (c < s.width) *reinterpret_cast<f32x4*>(a.part + ((int64_t)part * l.F + f) * s.width + c) = v;
+                } else if (c < s.cols) {
+                    v *= a.scale;
+                    put4(a.gw, (int64_t)f * a.ldgw + s.c_first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+                }
+            }
+    }
+}
+
+// gw of a piece whose sum over the rows came in parts
+__global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a, int nf) {
+    const Layer& l = a.layer;
+    const Shape s = shape_of(a);
+    if (!s.on) return;
+    const int splits = splits_of((int64_t)((s.width + 255) / 256) * nf, (*l.count + kStepK - 1) / kStepK);
+    if (splits == 1) return;
+    const int fours_ = (s.cols + 3) / 4;
+    const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)l.F * fours_; q += (int64_t)gridDim.x * 256) {
+        const int64_t f = q / fours_;
+        const int c = (int)(q % fours_) * 4;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part + (p * l.F + f) * s.width + c);
+        v *= a.scale;
+        put4(a.gw, f * a.ldgw + s.c_first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+    }
+}
+
+// gx of every row: the parts added up, zero for rows that don't count
+__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, int nf, void* gx, int64_t ldgx, int bf) {
+    const Layer& l = a.layer;
+    const Shape s = shape_of(a);
+    const int splits = splits_of((int64_t)(s.rows / 256) * nf, (s.width + kStepK - 1) / kStepK);
+    const int fours_ = (l.F + 3) / 4;
+    const bool whole = fours(gx, ldgx, bf);
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n * fours_; q += (int64_t)gridDim.x * 256) {
+        const int64_t i = q / fours_;
+        const int f = (int)(q % fours_) * 4;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        const int64_t r = pos[i];
+        if (r >= 0)
+            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part + (p * (int64_t)s.rows + r) * l.fp + f);
+        v *= a.scale;
+        put4(gx, i * ldgx + f, v, l.F - f < 4 ? l.F - f : 4, bf, whole && f + 4 <= l.F);
+    }
+}
+
+// gbias: the row tiles' sums added up
+__global__ __launch_bounds__(256) void classes_gbias_kernel(const float* part, const int32_t* count, int tile_rows, int C, float scale, float* gbias) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= C) return;
+    const int tiles = (*count + tile_rows - 1) / tile_rows;
+    const int64_t cp = ((int64_t)C + 255) / 256 * 256;
+    float v = 0.f;
+    for (int t = 0; t < tiles; ++t) v += part[t * cp + c];
+    gbias[c] = v * scale;
+}
+
+// ---- host
+
+struct Call {
+    const char* who;
+    const void* X;
+    int64_t ldx, n;
+    int32_t F;
+    const void* W;
+    int64_t ldw;
+    int32_t C;
+    const void* bias;
+    gas_dtype dt;
+    Targets t;
+    float temperature, label_weight;
+    void* workspace;
+    int64_t workspace_bytes;
+    hipStream_t s;
+};
+
+// The workspace of the targets: RowsArgs' arrays
+inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bool distill) {
+    RowsArgs r = {};
+    const int64_t most = common.layer.most;
+    r.t = c.t;
+    r.idx = common.idx;
+    r.count = common.layer.count;
+    r.label_weight = c.label_weight;
+    r.temperature = c.temperature;
+    r.tiles = (int32_t)((c.C + kTileC - 1) / kTileC);
+    r.info = room.take<f32x4>(most);
+    if (!distill) {
+        r.labels = room.take<int32_t>(most);
+    } else {
+        r.k = c.t.k + 1;
+        r.entropy = room.take<float>(most);
+        r.entries = room.take<int2>(most * r.k);
+        r.starts = room.take<uint16_t>(most * (r.tiles + 1));
+    }
+    return r;
+}
+
+inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& r, bool distill) {
+    const unsigned blocks = (unsigned)((c.n + 255) / 256);
+    hipLaunchKernelGGL(classes_count_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts);
+    hipLaunchKernelGGL(classes_number_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts, common.idx, common.pos,
+                       const_cast<int32_t*>(common.layer.count));
+    GAS_CHECK_HIP(hipGetLastError());
+    if (distill) hipLaunchKernelGGL(classes_entries_kernel, dim3((unsigned)c.n), dim3(64), 0, c.s, r);
+    else hipLaunchKernelGGL(classes_labels_kernel, dim3(blocks), dim3(256), 0, c.s, r);
+    GAS_CHECK_HIP(hipGetLastError());
+    return run_pack(common, c.dt, c.s);
+}
+
+// What the forward call needs beside: the tiles' statistics
+inline Parts lay_out_parts(Room& room, const Common& common, bool distill) {
+    const int64_t tiles = (common.layer.C + kTileC - 1) / kTileC, n = tiles * common.layer.most;
+    Parts p = {};
+    p.most = room.take<float>(n);
+    p.sum = room.take<float>(n);
+    p.sum_t = distill ? room.take<float>(n) : nullptr;
+    p.picked = room.take<float>(distill ? n : common.layer.most);
+    return p;
+}
+
+inline LogitsArgs logits_args(const Call& c, const Common& common, const RowsArgs& r, bool distill) {
+    LogitsArgs a = {};
+    a.layer = common.layer;
+    a.labels = distill ? nullptr : r.labels;
+    a.entries = r.entries;
+    a.starts = r.starts;
+    a.k = r.k;
+    a.tiles = r.tiles;
+    a.inv_t = 1.f / c.temperature;
+    a.info = r.info;
+    a.first = 0;
+    a.width = r.tiles * kTileC;
+    return a;
+}
+
+inline gas_status run_sum(const float* loss, int64_t n, float* out, hipStream_t s) {
+    if (!out) return GAS_OK;
+    hipLaunchKernelGGL(classes_sum_kernel, dim3(1), dim3(1024), 0, s, loss, n, out);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
+#define GAS_TRY(expr)                       \
+    do {                                    \
+        const gas_status st_ = (expr);      \
+        if (st_ != GAS_OK) return st_;      \
+    } while (0)
+
+gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* lse) {
+    Room room{static_cast<char*>(c.workspace)};
+    const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
+    const RowsArgs rows = lay_out_rows(room, c, common, distill);
+    const Parts parts = lay_out_parts(room, common, distill);
+    GAS_TRY(run_rows(c, common, rows, distill));
+    LogitsArgs a = logits_args(c, common, rows, distill);
+    a.parts = parts;
+    a.two = distill && c.temperature != 1.f;
+    GAS_TRY(launch_logits<LOGITS_STATS>(a, c.n, rows.tiles, c.s));
+    const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, a.two, a.inv_t,
+                        c.temperature, loss, lse};
+    hipLaunchKernelGGL(classes_loss_kernel, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
+    GAS_CHECK_HIP(hipGetLastError());
+    return run_sum(loss, c.n, sum, c.s);
+}
+
+// Room for the gradient at the logits of a piece, in elements.
+constexpr int64_t kPieceElements = 1LL << 28;
+inline int64_t piece_cap(int64_t most, int C) {
+    const int64_t all = most * round_up(C, 256), least = most * 256;
+    const int64_t cap = all < kPieceElements ? all : kPieceElements;
+    return cap > least ? cap : least;
+}
+inline int tile_of_width(int64_t fp) { return fp <= 64 ? 64 : (fp <= 128 ? 128 : 256); }
+
+struct Grads {
+    void* gx;
+    int64_t ldgx;
+    void* gw;
+    int64_t ldgw;
+    gas_dtype dt_gw;
+    float* gbias;
+    float scale;
+    const float *lse, *row_scale;
+};
+
+struct BackwardRoom {
+    uint16_t* g;
+    float *gx, *gw, *gbias;
+    int64_t cap;
+};
+inline BackwardRoom lay_out_backward(Room& room, const Common& common, bool gx, bool gw, bool gbias) {
+    BackwardRoom b = {};
+    const Layer& l = common.layer;
+    const int64_t most = l.most, bf = tile_of_width(l.fp);
+    b.cap = piece_cap(most, l.C);
+    b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
+    // parts of a sum are made only where there are at most kFill tiles of them
+    const int64_t parts = kFill * 256 * bf, whole_x = most * l.fp;
+    b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
+    b.gw = gw ? room.take<float>(parts) : nullptr;
+    b.gbias = gbias ? room.take<float>(most / 256 * round_up(l.C, 256)) : nullptr;
+    return b;
+}
+
+template <int BA, int WA, int WB>
+gas_status launch_gx(const GradArgs& a, int64_t blocks, hipStream_t s) {
+    constexpr int smem = TileProduct<BA, 256, WA, WB, false, false>::kLdsBytes;
+    static const gas_status attr = lds_of(classes_gx_kernel<BA, WA, WB>, smem);
+    if (attr != GAS_OK) return attr;
+    hipLaunchKernelGGL((classes_gx_kernel<BA, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+template <int BB, int WA, int WB>
+gas_status launch_gw(const GradArgs& a, int64_t blocks, hipStream_t s) {
+    constexpr int smem = TileProduct<256, BB, WA, WB, true, true>::kLdsBytes;
+    static const gas_status attr = lds_of(classes_gw_kernel<BB, WA, WB>, smem);
+    if (attr != GAS_OK) return attr;
+    hipLaunchKernelGGL((classes_gw_kernel<BB, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
+gas_status backward(const Call& c, bool distill, const Grads& g) {
+    Room room{static_cast<char*>(c.workspace)};
+    const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
+    RowsArgs rows = lay_out_rows(room, c, common, distill);
+    const BackwardRoom b = lay_out_backward(room, common, g.gx, g.gw, g.gbias);
+    rows.lse = g.lse;
+    rows.row_scale = g.row_scale;
+    GAS_TRY(run_rows(c, common, rows, distill));
+    const Layer& l = common.layer;
+    LogitsArgs a = logits_args(c, common, rows, distill);
+    a.two = !distill ? 1 : (c.t.labels ? 3 : 2);
+    a.g = b.g;
+    a.g_plane = b.cap;
+    a.gbias = b.gbias;
+    a.cap = b.cap;
+    GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, nullptr, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
+    const int64_t bf = tile_of_width(l.fp), nf = (l.fp + bf - 1) / bf;
+    // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
+    const int least = piece_width(b.cap, l.most, l.C);
+    const int pieces = (c.C + least - 1) / least;
+    for (int p = 0; p < pieces; ++p) {
+        // the widest that piece p can be, and the most tiles that it can have: width * rows <= cap, or 256 classes
+        a.piece = d.piece = p;
+        const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
+        const int64_t all = rows_most / 256 * (cols_most / 256), fit = b.cap / (256 * 256);
+        GAS_TRY((c.n <= 64 ? launch_logits_tile<LOGITS_GRAD, 64, 4, 1>(a, 64, cols_most / 256, c.s)
+                           : launch_logits_tile<LOGITS_GRAD, 256, 2, 4>(a, 256, all < fit ? all : fit, c.s)));
+        if (g.gx) {
+            d.part = b.gx;
+            int64_t blocks = rows_most / 256 * nf;
+            if (blocks < kFill) blocks = kFill;
+            GAS_TRY((bf == 64 ? launch_gx<64, 1, 4>(d, blocks, c.s) : bf == 128 ? launch_gx<128, 2, 4>(d, blocks, c.s) : launch_gx<256, 2, 4>(d, blocks, c.s)));
+        }
+        if (g.gw) {
+            d.part = b.gw;
+            int64_t blocks = cols_most / 256 * nf;
+            if (blocks < kFill) blocks = kFill;
+            GAS_TRY((bf == 64 ? launch_gw<64, 4, 1>(d, blocks, c.s) : bf == 128 ? launch_gw<128, 4, 2>(d, blocks, c.s) : launch_gw<256, 2, 4>(d, blocks, c.s)));
+            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d, (int)nf);
+            GAS_CHECK_HIP(hipGetLastError());
+        }
+    }
+    if (g.gx) {
+        d.part = b.gx;
+        d.piece = 0;
+        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n, (int)nf,
+                           g.gx, g.ldgx, c.dt == GAS_BF16);
+        GAS_CHECK_HIP(hipGetLastError());
+    }
+    if (g.gbias) {
+        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, c.n <= 64 ? 64 : 256, c.C,
+                           g.scale, g.gbias);
+        GAS_CHECK_HIP(hipGetLastError());
+    }
+    return GAS_OK;
+}
+
+__global__ __launch_bounds__(256) void classes_zero_kernel(void* p, int64_t ld, int64_t rows, int64_t cols, int bytes) {
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < rows * cols; q += (int64_t)gridDim.x * 256) {
+        const int64_t at = q / cols * ld + q % cols;
+        if (bytes == 2) static_cast<uint16_t*>(p)[at] = 0;
+        else static_cast<uint32_t*>(p)[at] = 0;
+    }
+}
+gas_status zero(void* p, int64_t ld, int64_t rows, int64_t cols, int bytes, hipStream_t s) {
+    if (!p || rows * cols == 0) return GAS_OK;
+    hipLaunchKernelGGL(classes_zero_kernel, dim3(blocks_for(rows * cols, 256, 4096)), dim3(256), 0, s, p, ld, rows, cols, bytes);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
+// bytes of a call, for the widest that its arguments allow
+int64_t workspace_of(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k, bool bwd) {
+    if (n < 0 || n > (1 << 28) || F <= 0 || F > kMaxWidth || C <= 0 || C > kMaxClasses || k < 0 || k > kMaxEntries || !valid_dtype(dt)) return -1;
+    if (n == 0) return 0;
+    Room room{nullptr};
+    Call c = {};
+    c.n = n; c.C = C; c.t.k = k;
+    const Common common = lay_out(room, nullptr, F, n, F, reinterpret_cast<const void*>(2), C, C, nullptr, dt, true);
+    lay_out_rows(room, c, common, k > 0);
+    if (bwd) lay_out_backward(room, common, true, true, true);
+    else lay_out_parts(room, common, k > 0);
+    return room.used;
+}
+
+gas_status check_call(const Call& c, bool distill, bool bwd) {
+    GAS_TRY(check_layer(c.who, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.dt));
+    if (distill) {
+        GAS_REQUIRE(c.t.k > 0 && c.t.k <= kMaxEntries, "%s: k=%d, 1 to 256 entries of a row are taken", c.who, c.t.k);
+        GAS_REQUIRE(c.temperature > 0.f && c.temperature < INFINITY, "%s: temperature=%g", c.who, c.temperature);
+        GAS_REQUIRE(c.label_weight >= 0.f && c.label_weight <= 1.f, "%s: label_weight=%g, 0 to 1 are taken", c.who, c.label_weight);
+    }
+    if (c.n == 0) return GAS_OK;
+    if (distill) {
+        GAS_REQUIRE(c.t.ids && c.t.values, "%s: null pointer", c.who);
+        GAS_REQUIRE(c.t.ld_ids >= c.t.k && c.t.ld_values >= c.t.k, "%s: row stride smaller than the row", c.who);
+    } else {
+        GAS_REQUIRE(c.t.labels, "%s: null pointer", c.who);
+    }
+    const int64_t need = workspace_of(c.n, c.F, c.C, c.dt, distill ? c.t.k : 0, bwd);
+    GAS_REQUIRE(c.workspace && c.workspace_bytes >= need, "%s: the workspace has %lld bytes, %lld are needed", c.who, (long long)c.workspace_bytes, (long long)need);
+    GAS_REQUIRE(aligned16(c.workspace), "%s: the workspace is not 16-byte aligned", c.who);
+    return GAS_OK;
+}
+
+gas_status run_forward(const Call& c, bool distill, float* loss, float* sum, float* lse) {
+    GAS_TRY(check_call(c, distill, false));
+    if (c.n == 0) return run_sum(loss, 0, sum, c.s);
+    GAS_REQUIRE(loss && lse, "%s: null pointer", c.who);
+    const int eb = elem_bytes(c.dt);
+    const Span in[] = {
+        {c.X, span(c.n, c.ldx, c.F, eb)}, {c.W, span(c.F, c.ldw, c.C, eb)}, {c.bias, (int64_t)c.C * eb}, {c.t.labels, c.n * 4},
+        {c.t.ids, span(c.n, c.t.ld_ids, c.t.k, 4)}, {c.t.values, span(c.n, c.t.ld_values, c.t.k, 4)}, {c.workspace, c.workspace_bytes}};
+    const Span out[] = {{loss, c.n * 4}, {lse, c.n * (distill ? 8 : 4)}, {sum, 4}};
+    GAS_TRY(check_overlaps(c.who, in, out));
+    return forward(c, distill, loss, sum, lse);
+}
+
+gas_status run_backward(const Call& c, bool distill, const Grads& g) {
+    GAS_TRY(check_call(c, distill, true));
+    if (!valid_dtype(g.dt_gw) || (g.dt_gw == GAS_BF16 && c.dt == GAS_F32)) return fail(GAS_ERR_DTYPE, "%s: GW is of fp32 or of W's type", c.who);
+    GAS_REQUIRE(!g.gw || g.ldgw >= c.C, "%s: row stride smaller than the row", c.who);
+    if (c.n == 0) {
+        GAS_TRY(zero(g.gw, g.ldgw, c.F, c.C, elem_bytes(g.dt_gw), c.s));
+        return zero(g.gbias, c.C, 1, c.C, 4, c.s);
+    }
+    GAS_REQUIRE(g.lse, "%s: null pointer", c.who);
+    GAS_REQUIRE(g.gx || g.gw || g.gbias, "%s: no gradient is asked for", c.who);
+    GAS_REQUIRE(!g.gx || g.ldgx >= c.F, "%s: row stride smaller than the row", c.who);
+    const int eb = elem_bytes(c.dt);
+    const Span in[] = {
+        {c.X, span(c.n, c.ldx, c.F, eb)}, {c.W, span(c.F, c.ldw, c.C, eb)}, {c.bias, (int64_t)c.C * eb}, {c.t.labels, c.n * 4},
+        {c.t.ids, span(c.n, c.t.ld_ids, c.t.k, 4)}, {c.t.values, span(c.n, c.t.ld_values, c.t.k, 4)}, {g.lse, c.n * (distill ? 8 : 4)},
+        {g.row_scale, c.n * 4}, {c.workspace, c.workspace_bytes}};
+    const Span out[] = {{g.gx, span(c.n, g.ldgx, c.F, eb)}, {g.gw, span(c.F, g.ldgw, c.C, elem_bytes(g.dt_gw))}, {g.gbias, (int64_t)c.C * 4}};
+    GAS_TRY(check_overlaps(c.who, in, out));
+    return backward(c, distill, g);
+}
+
+}  // namespace
+}  // namespace gas
+
+using namespace gas;
+
+extern "C" {
+
+int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt) { return workspace_of(n_rows, F, n_classes, dt, 0, false); }
+int64_t gas_linear_xent_bwd_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt) { return workspace_of(n_rows, F, n_classes, dt, 0, true); }
+int64_t gas_linear_distill_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt, int32_t k) {
+    return k > 0 ? workspace_of(n_rows, F, n_classes, dt, k, false) : -1;
+}
+int64_t gas_linear_distill_bwd_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt, int32_t k) {
+    return k > 0 ? workspace_of(n_rows, F, n_classes, dt, k, true) : -1;
+}
+
+gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                           const void* bias, gas_dtype dt, const int32_t* labels, float* loss_rows, float* loss_sum, float* lse,
+                           void* workspace, int64_t workspace_bytes, void* stream) {
+    const Call c = {"gas_linear_xent", X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, {labels, nullptr, nullptr, 0, 0, n_rows, 0, n_classes}, 1.f, 1.f,
+                    workspace, workspace_bytes, (hipStream_t)stream};
+    return run_forward(c, false, loss_rows, loss_sum, lse);
+}
+
+gas_status gas_linear_xent_bwd(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                               const void* bias, gas_dtype dt, const int32_t* labels, const float* lse, float scale,
+                               const float* row_scale, void* GX, int64_t ldgx, void* GW, int64_t ldgw, gas_dtype dt_gw, float* gbias,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+    const Call c = {"gas_linear_xent_bwd", X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, {labels, nullptr, nullptr, 0, 0, n_rows, 0, n_classes}, 1.f, 1.f,
+                    workspace, workspace_bytes, (hipStream_t)stream};
+    return run_backward(c, false, Grads{GX, ldgx, GW, ldgw, dt_gw, gbias, scale, lse, row_scale});
+}
+
+gas_status gas_linear_distill(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                              const void* bias, gas_dtype dt, const int32_t* ids, int64_t ld_ids, const float* values, int64_t ld_values, int32_t k,
+                              float temperature, const int32_t* labels, float label_weight, float* loss_rows, float* loss_sum,
+                              float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+    const Call c = {"gas_linear_distill", X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, {labels, ids, values, ld_ids, ld_values, n_rows, k, n_classes},
+                    temperature, label_weight, workspace, workspace_bytes, (hipStream_t)stream};
+    return run_forward(c, true, loss_rows, loss_sum, lse);
+}
+
+gas_status gas_linear_distill_bwd(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
+                                  const void* bias, gas_dtype dt, const int32_t* ids, int64_t ld_ids, const float* values, int64_t ld_values, int32_t k,
+                                  float temperature, const int32_t* labels, float label_weight, const float* lse, float scale,
+                                  const float* row_scale, void* GX, int64_t ldgx, void* GW, int64_t ldgw, gas_dtype dt_gw, float* gbias,
+                                  void* workspace, int64_t workspace_bytes, void* stream) {
+    const Call c = {"gas_linear_distill_bwd", X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, {labels, ids, values, ld_ids, ld_values, n_rows, k, n_classes},
+                    temperature, label_weight, workspace, workspace_bytes, (hipStream_t)stream};
+    return run_backward(c, true, Grads{GX, ldgx, GW, ldgw, dt_gw, gbias, scale, lse, row_scale});
+}
+
+}  // extern "C"

@@ -294,6 +294,9 @@ PyMethodDef methods[] = {
     GAS_CALL(gas_pna_linear_bwd_input), GAS_CALL(gas_pna_linear_bwd_weight), GAS_CALL(gas_pna_linear_bwd_weight_workspace),
     GAS_CALL(gas_residual_norm), GAS_CALL(gas_residual_norm_bwd), GAS_CALL(gas_residual_norm_bwd_workspace), GAS_CALL(gas_residual_norm_bwd_typed_workspace), GAS_CALL(gas_sq_norms),
     GAS_CALL(gas_sq_norms_workspace), GAS_CALL(gas_adamw_elements), GAS_CALL(gas_adamw_steps), GAS_CALL(gas_adamw_unpack),
+    GAS_CALL(gas_linear_xent), GAS_CALL(gas_linear_xent_bwd), GAS_CALL(gas_linear_distill), GAS_CALL(gas_linear_distill_bwd), GAS_CALL(gas_linear_top),
+    GAS_CALL(gas_linear_xent_workspace), GAS_CALL(gas_linear_xent_bwd_workspace), GAS_CALL(gas_linear_distill_workspace),
+    GAS_CALL(gas_linear_distill_bwd_workspace), GAS_CALL(gas_linear_top_workspace),
     GAS_CALL(gas_gat_aggregate_push), GAS_CALL(gas_gat_aggregate_bwd_bounded), GAS_CALL(gas_gat_aggregate_bwd_heads_workspace),
     {nullptr, nullptr, 0, nullptr}};
 

@@ -1,0 +1,170 @@
+// Products of bf16 matrices by tiles, for the output layer over many classes (classes.hip): the main loop shared by its logits,
+// its input gradient and its weight gradient.
+//
+// A workgroup of WA x WB wavefronts owns BA rows of the first operand by BB rows of the second, sum over k, k in steps of 64.  An
+// operand lies in memory with k contiguous (element (r, k) at p[r ld + k]) or with r contiguous (TURNED: at p[k ld + r]); a turned one is
+// put right on its way out of LDS (ds_read_b64_tr_b16: sixteen lanes read four k of sixteen rows, and a lane receives four k of
+// one row), so nothing is transposed in memory: the logits read W [F, C] turned and X as it lies, the input gradient W and G as they lie, the
+// weight gradient both turned.
+// Loads go from memory to LDS without registers (16 bytes a lane), the next step's under way while one is multiplied.  LDS holds
+// the lanes' pieces in the order of their numbers, so which piece a lane fetches is exchanged instead: of row r, piece p
+// lies at p ^ (r & 7); of a turned operand's k, unit u of 16 bytes at u ^ 4 (k & 3).  Sixteen-byte reads of eight
+// neighbouring rows, and the 32 bytes of each of four k, then fall on banks of their own.
+//
+// fp32 operands come as three bf16 planes (split.h says how and what is dropped): `terms` = 6 products of planes follow one
+// another over the same accumulators, the smallest first, so that only the last one's sums round at the result's size.
+#pragma once
+#include "split.h"
+
+namespace gas {
+namespace {
+
+constexpr int kStepK = 64;
+
+struct TileOperand {
+    const uint16_t* p;        // the tile's first row and first k
+    int64_t ld, plane;        // in elements
+    int last;                 // the last row of the tile that can be read (rows beyond repeat it); turned: the last 8 rows' first
+    int k;                    // k that can be read (beyond, the last ones repeat: the other operand has zeros there)
+};
+
+template <int BA, int BB, int WA, int WB, bool ATURNED, bool BTURNED>
+struct TileProduct {
+    static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB;
+    static constexpr int kStage = (BA + BB) * kStepK;                      // elements
+    static constexpr int kLdsBytes = 2 * kStage * 2;
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+    template <int R, bool TURNED>
+    struct Loads {
+        static constexpr int N = R * kStepK / 8 / T;
+        static_assert(R * kStepK / 8 % T == 0, "every thread brings as many pieces");
+        uint32_t at[N];                                                    // bytes from the step's first element
+        __device__ __forceinline__ void init(const TileOperand& o) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int q = i * T + (int)threadIdx.x;
+                if constexpr (TURNED) {
+                    const int kr = q / (R / 8), unit = (q % (R / 8)) ^ (4 * (kr & 3) & (R / 8 - 1));
+                    at[i] = (uint32_t)((int64_t)kr * o.ld + (8 * unit < o.last ? 8 * unit : o.last)) * 2;
+                } else {
+                    const int row = q >> 3, piece = (q & 7) ^ (row & 7);
+                    at[i] = (uint32_t)((int64_t)(row < o.last ? row : o.last) * o.ld + 8 * piece) * 2;
+                }
+            }
+        }
+        // the 64 k from `from` on, of which `left` can be read
+        __device__ __forceinline__ void bring(const uint16_t* from, int64_t ld, int left, uint16_t* to) const {
+            const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                uint32_t a = at[i];
+                if (left < kStepK) {
+                    const int q = i * T + (int)threadIdx.x;
+                    if constexpr (TURNED) {
+                        const int kr = q / (R / 8), over = kr - (left - 1);
+                        a -= over > 0 ? (uint32_t)(over * ld * 2) : 0u;
+                    } else {
+                        const int over = 8 * ((q & 7) ^ ((q >> 3) & 7)) - (left - 8);
+                        a -= over > 0 ? (uint32_t)over * 2 : 0u;
+                    }
+                }
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void*)(reinterpret_cast<const char*>(from) + a),
+                    (__attribute__((address_space(3))) void*)(to + (i * T + wave * 64) * 8), 16, 0, 0);
+            }
+        }
+    };
+
+    template <int R, bool TURNED>
+    static __device__ __forceinline__ bf16x8 fragment(const uint16_t* tile, int r0, int kk) {
+        const int lane = threadIdx.x & 63, li = lane & 31, lh = lane >> 5;
+        if constexpr (TURNED) {
+            const int i16 = lane & 15, r = r0 + 16 * ((lane >> 4) & 1) + 4 * (i16 & 3);
+            s16x4 h[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int k = 16 * kk + 8 * lh + 4 * t + (i16 >> 2);
+                const uint16_t* p = tile + k * R + 8 * ((r >> 3) ^ (4 * (k & 3) & (R / 8 - 1))) + (r & 7);
+                h[t] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
+            }
+            return __builtin_bit_cast(bf16x8, s16x8{h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
+        } else {
+            const int row = r0 + li;
+            return *reinterpret_cast<const bf16x8*>(tile + (row * 8 + ((2 * kk + lh) ^ (row & 7))) * 8);
+        }
+    }
+
+    Loads<BA, ATURNED> la;
+    Loads<BB, BTURNED> lb;
+
+    // One step: the next one's loads, then this one's products.  `now` and `next` are different halves of LDS, which the compiler has to
+    // know (__restrict__): it would otherwise wait for the loads before every read of LDS.
+    __device__ __forceinline__ void step(const uint16_t* __restrict__ now, uint16_t* __restrict__ next, bool more, const uint16_t* a,
+                                         int64_t lda, int left_a, const uint16_t* b, int64_t ldb, int left_b, int wa0, int wb0,
+                                         f32x16 (&acc)[TA][TB]) const {
+        if (more) {
+            la.bring(a, lda, left_a, next);
+            lb.bring(b, ldb, left_b, next + BA * kStepK);
+        }
+#pragma unroll
+        for (int kk = 0; kk < kStepK / 16; ++kk) {
+            bf16x8 fa[TA], fb[TB];
+#pragma unroll
+            for (int j = 0; j < TB; ++j) fb[j] = fragment<BB, BTURNED>(now + BA * kStepK, wb0 + 32 * j, kk);
+#pragma unroll
+            for (int i = 0; i < TA; ++i) fa[i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
+#pragma unroll
+            for (int i = 0; i < TA; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+        }
+    }
+
+    // acc = the products over steps [first, last) of 64 k of every term.  Called by every thread; LDS is free for other use afterwards.
+    __device__ __forceinline__ void run(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds, int wa0,
+                                        int wb0, f32x16 (&acc)[TA][TB]) {
+        la.init(a);
+        lb.init(b);
+#pragma unroll
+        for (int i = 0; i < TA; ++i)
+#pragma unroll
+            for (int j = 0; j < TB; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+        const int per = last - first, n = per * terms;
+        if (n <= 0) return;
+        const int64_t step_a = ATURNED ? kStepK * a.ld : kStepK, step_b = BTURNED ? kStepK * b.ld : kStepK;
+        // planes of the terms, the smallest product first: m m, l h, h l, m h, h m, h h; one term: h h
+        const uint32_t kOfA = 0x010201u, kOfB = 0x001021u;                 // a nibble a term, from the lowest
+        int term = 0, k = first;
+        auto plane_of = [&](uint32_t which, int t) { return terms == 1 ? 0 : (int)((which >> (4 * t)) & 15); };
+        const uint16_t* pa = a.p + plane_of(kOfA, 0) * a.plane + first * step_a;
+        const uint16_t* pb = b.p + plane_of(kOfB, 0) * b.plane + first * step_b;
+        la.bring(pa, a.ld, a.k - kStepK * k, lds);
+        lb.bring(pb, b.ld, b.k - kStepK * k, lds + BA * kStepK);
+        int half = 0;
+#pragma unroll 1
+        for (int s = 0; s < n; ++s) {
+            __builtin_amdgcn_s_waitcnt(0x0F70);            // the loads of this step have arrived (vmcnt 0)
+            __syncthreads();                               // everyone's; and everyone is done reading the other half
+            if (++k == last) {
+                k = first;
+                ++term;
+                const int t = term < terms ? term : 0;
+                pa = a.p + plane_of(kOfA, t) * a.plane + first * step_a;
+                pb = b.p + plane_of(kOfB, t) * b.plane + first * step_b;
+            } else {
+                pa += step_a;
+                pb += step_b;
+            }
+            step(lds + half * kStage, lds + (half ^ 1) * kStage, s + 1 < n, pa, a.ld, a.k - kStepK * k, pb, b.ld, b.k - kStepK * k, wa0, wb0, acc);
+            half ^= 1;
+        }
+        __syncthreads();
+    }
+};
+
+}  // namespace
+}  // namespace gas
