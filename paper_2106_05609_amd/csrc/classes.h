@@ -139,14 +139,18 @@ __global__ __launch_bounds__(256) void classes_pack_kernel(PackArgs a) {
 // ---- which tile a workgroup has
 // Workgroups are dealt to the eight XCDs in turn; each XCD takes a contiguous range of the tiles, and in it eight row tiles by all
 // column tiles after one another, so that what runs there at a time reads few rows and few columns.
-__device__ __forceinline__ bool tile_of(unsigned block, int nm, int nc, int& m, int& c) {
-    const int64_t total = (int64_t)nm * nc, per = (total + 7) / 8;
-    const int64_t id = (int64_t)(block & 7) * per + (block >> 3);
-    if ((int64_t)(block >> 3) >= per || id >= total) return false;
-    const int64_t group = id / (8LL * nc), in = id % (8LL * nc);
-    const int first = (int)group * 8, rows = nm - first < 8 ? nm - first : 8;
-    m = first + (int)(in % rows);
-    c = (int)(in / rows);
+__device__ __forceinline__ bool tile_of(uint32_t block, uint32_t nm, uint32_t nc, int& m, int& c) {
+    const uint32_t total = nm * nc, per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
+    if ((block >> 3) >= per || id >= total) return false;
+    const uint32_t group = id / (8 * nc), in = id - group * (8 * nc), first = group * 8;
+    if (nm - first >= 8) {
+        m = (int)(first + (in & 7));
+        c = (int)(in >> 3);
+    } else {
+        const uint32_t rows = nm - first;
+        c = (int)(in / rows);
+        m = (int)(first + in - (uint32_t)c * rows);
+    }
     return true;
 }
 
@@ -155,19 +159,24 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 // The number of an accumulator's element along the first operand in its 32 x 32 block.
 __device__ __forceinline__ int acc_row(int r, int lh) { return 8 * (r / 4) + 4 * lh + (r % 4); }
 
-// ---- statistics of a row's logits, tile by tile: the largest, and the sums of the exponentials from there
+// ---- statistics of a row's logits, tile by tile
+// The largest one times log2 e, rounded, and the sum of 2 to the logits times log2 e less that: one fused multiply-add each, whose rounding is of
+// the difference.  A logit that leaves fp32's range by that factor, below -2.3e38, is as one of -infinity.
 struct Parts {
     float *most, *sum, *sum_t, *picked;      // [class tiles][most rows]; sum_t: at the temperature; picked: sum of weighted target logits
 };
+constexpr float kLeastExponent = -3.4028234e38f;
 
-// A row's statistics over `n` tiles from `first` on in steps of `step`, joined.  (most, sum, sum_t) hold what was joined so far.
+// (most, sum, sum_t) holds what was joined so far.
 __device__ __forceinline__ void join(float& most, float& sum, float& sum_t, float m, float s, float st, float inv_t) {
-    const float top = fmaxf(most, m), base = top == -INFINITY ? 0.f : top;
-    const float a = exp2_of((most - base) * kLog2e), b = exp2_of((m - base) * kLog2e);
-    const float at = exp2_of((most - base) * kLog2e * inv_t), bt = exp2_of((m - base) * kLog2e * inv_t);
-    sum = sum * a + s * b;
-    sum_t = sum_t * at + st * bt;
+    const float top = fmaxf(most, m), a = most - top, b = m - top;
+    sum = sum * exp2_of(a) + s * exp2_of(b);
+    sum_t = sum_t * exp2_of(a * inv_t) + st * exp2_of(b * inv_t);
     most = top;
+}
+// The logarithm of a sum so held, at 1 / inv_t; divided by the same rounded log2 e that the logits were multiplied by.
+__device__ __forceinline__ float log_of(float most, float sum, float inv_t) {
+    return (float)((double)most * (double)inv_t / (double)kLog2e + (double)logf(sum));
 }
 
 inline unsigned blocks_for(int64_t items, int64_t per, int64_t most) {

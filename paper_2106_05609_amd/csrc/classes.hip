@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
     const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
     const int64_t i = (int64_t)blockIdx.x * 16 + row;
     const int64_t r = i < a.n ? a.pos[i] : -1;
-    float most = -INFINITY, sum = 0.f, sum_t = 0.f, picked = 0.f;
+    float most = kLeastExponent, sum = 0.f, sum_t = 0.f, picked = 0.f;
     if (r >= 0) {
         for (int t = part; t < a.tiles; t += 16) {
             const int64_t at = (int64_t)t * a.layer.most + r;
@@ -207,7 +207,7 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
         join(most, sum, sum_t, red[0][p][row], red[1][p][row], red[2][p][row], a.inv_t);
         picked += red[3][p][row];
     }
-    const float lse = most + logf(sum);
+    const float lse = log_of(most, sum, 1.f);
     if (!a.info) {
         a.loss[i] = r < 0 ? 0.f : lse - a.parts.picked[r];
         a.lse[i] = r < 0 ? 0.f : lse;
@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
     float loss = 0.f, lse_t = 0.f;
     if (r >= 0) {
         const f32x4 info = a.info[r];
-        lse_t = a.two ? most * a.inv_t + logf(sum_t) : lse;
+        lse_t = a.two ? log_of(most, sum_t, a.inv_t) : lse;
         if (info[2] != 0.f) loss = info[2] * lse;
         if (info[3] != 0.f) loss = fmaf(info[3] * a.temperature, lse_t, loss) + a.entropy[r];
         loss -= picked;
@@ -263,7 +263,7 @@ struct GradArgs {
 };
 
 // Parts of a sum, so that its tiles fill the card: as few as leave the compute units with something to do, at least eight steps each.
-constexpr int kFill = 512, kMostSplits = 16;
+constexpr int kFill = 1024, kMostSplits = 16;
 __device__ __host__ __forceinline__ int splits_of(int64_t tiles, int steps) {
     int64_t s = kFill / (tiles > 0 ? tiles : 1);
     if (s > kMostSplits) s = kMostSplits;
@@ -289,29 +289,30 @@ __device__ __forceinline__ Shape shape_of(const GradArgs& a) {
 }
 
 // gx += G W^T over a piece of the classes: lanes end up with four neighbouring inputs of one row
-template <int BA, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB) void classes_gx_kernel(GradArgs a) {
-    using P = TileProduct<BA, 256, WA, WB, false, false>;
+template <int BA, int BB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB, 2) void classes_gx_kernel(GradArgs a) {
+    using P = TileProduct<BA, BB, WA, WB, false, false>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
     const Shape s = shape_of(a);
     if (!s.on || s.rows == 0) return;
-    const int nm = s.rows / 256, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
+    const int nm = s.rows / BB, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
     const int full = (s.width + kStepK - 1) / kStepK, splits = splits_of((int64_t)nm * nf, full);
     int ft, at;
     if (!tile_of(blockIdx.x, nf, nm * splits, ft, at)) return;
     const int mt = at % nm, part = at / nm;
     const int per = (full + splits - 1) / splits;
     const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
-    const int m0 = mt * 256, f0 = ft * BA;
+    const int m0 = mt * BB, f0 = ft * BA;
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
     f32x16 acc[P::TA][P::TB];
     P product;
     const TileOperand oa = {l.w + (int64_t)f0 * l.ldw + s.c_first, l.ldw, l.w_plane, l.F - 1 - f0, l.cw - s.c_first};
-    const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, 255, s.width};
-    product.run(oa, ob, first, last, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB - 1, s.width};
+    const int end = (s.cols + P::kStepOf - 1) / P::kStepOf, from = first * (kStepK / P::kStepOf), to = last * (kStepK / P::kStepOf);
+    product.run(oa, ob, from < end ? from : end, to < end ? to : end, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     float* out = a.part + (int64_t)part * s.rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
@@ -347,7 +348,7 @@ __device__ __host__ __forceinline__ bool fours(const void* p, int64_t ld, bool b
 
 // gw = X^T G of a piece of the classes, or a part of the sum over the rows: lanes end up with four neighbouring classes of one input
 template <int BB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB) void classes_gw_kernel(GradArgs a) {
+__global__ __launch_bounds__(64 * WA * WB, 2) void classes_gw_kernel(GradArgs a) {
     using P = TileProduct<256, BB, WA, WB, true, true>;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
@@ -368,7 +369,7 @@ __global__ __launch_bounds__(64 * WA * WB) void classes_gw_kernel(GradArgs a) {
     P product;
     const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, l.most};
     const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
-    product.run(oa, ob, first, last, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    product.run(oa, ob, first * (kStepK / P::kStepOf), last * (kStepK / P::kStepOf), l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
@@ -410,10 +411,10 @@ __global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a, int nf)
 }
 
 // gx of every row: the parts added up, zero for rows that don't count
-__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, int nf, void* gx, int64_t ldgx, int bf) {
+__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, int tile_rows, int nf, void* gx, int64_t ldgx, int bf) {
     const Layer& l = a.layer;
     const Shape s = shape_of(a);
-    const int splits = splits_of((int64_t)(s.rows / 256) * nf, (s.width + kStepK - 1) / kStepK);
+    const int splits = splits_of((int64_t)(s.rows / tile_rows) * nf, (s.width + kStepK - 1) / kStepK);
     const int fours_ = (l.F + 3) / 4;
     const bool whole = fours(gx, ldgx, bf);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n * fours_; q += (int64_t)gridDim.x * 256) {
@@ -513,6 +514,7 @@ inline LogitsArgs logits_args(const Call& c, const Common& common, const RowsArg
     a.tiles = r.tiles;
     a.inv_t = 1.f / c.temperature;
     a.info = r.info;
+    a.biased = c.bias != nullptr;
     a.first = 0;
     a.width = r.tiles * kTileC;
     return a;
@@ -539,9 +541,10 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     GAS_TRY(run_rows(c, common, rows, distill));
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.parts = parts;
-    a.two = distill && c.temperature != 1.f;
-    GAS_TRY(launch_logits<LOGITS_STATS>(a, c.n, rows.tiles, c.s));
-    const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, a.two, a.inv_t,
+    const bool two = distill && c.temperature != 1.f;
+    const int64_t tiles = (c.n + rows_of_tile(c.n) - 1) / rows_of_tile(c.n) * rows.tiles;
+    GAS_TRY((two ? launch_logits<LOGITS_STATS, 3>(a, c.n, tiles, c.s) : launch_logits<LOGITS_STATS, 1>(a, c.n, tiles, c.s)));
+    const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
                         c.temperature, loss, lse};
     hipLaunchKernelGGL(classes_loss_kernel, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
     GAS_CHECK_HIP(hipGetLastError());
@@ -555,7 +558,10 @@ inline int64_t piece_cap(int64_t most, int C) {
     const int64_t cap = all < kPieceElements ? all : kPieceElements;
     return cap > least ? cap : least;
 }
-inline int tile_of_width(int64_t fp) { return fp <= 64 ? 64 : (fp <= 128 ? 128 : 256); }
+// Inputs of a tile: gw's 64 or 128; gx's 256 too, where that leaves out no more of the last tile, since it reads G once for each.
+inline int gw_width(int64_t fp) { return fp <= 64 ? 64 : 128; }
+inline int gx_width(int64_t fp) { return fp <= 128 ? gw_width(fp) : (round_up(fp, 256) == round_up(fp, 128) ? 256 : 128); }
+inline int gx_rows(int64_t fp) { return gx_width(fp) == 256 ? 128 : 256; }
 
 struct Grads {
     void* gx;
@@ -576,23 +582,23 @@ struct BackwardRoom {
 inline BackwardRoom lay_out_backward(Room& room, const Common& common, bool gx, bool gw, bool gbias) {
     BackwardRoom b = {};
     const Layer& l = common.layer;
-    const int64_t most = l.most, bf = tile_of_width(l.fp);
+    const int64_t most = l.most;
     b.cap = piece_cap(most, l.C);
     b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
     // parts of a sum are made only where there are at most kFill tiles of them
-    const int64_t parts = kFill * 256 * bf, whole_x = most * l.fp;
+    const int64_t parts = (int64_t)kFill * 128 * 256, whole_x = most * l.fp;
     b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
     b.gw = gw ? room.take<float>(parts) : nullptr;
-    b.gbias = gbias ? room.take<float>(most / 256 * round_up(l.C, 256)) : nullptr;
+    b.gbias = gbias ? room.take<float>(most / kRowsTile * round_up(l.C, 256)) : nullptr;
     return b;
 }
 
-template <int BA, int WA, int WB>
+template <int BA, int BB, int WA, int WB>
 gas_status launch_gx(const GradArgs& a, int64_t blocks, hipStream_t s) {
-    constexpr int smem = TileProduct<BA, 256, WA, WB, false, false>::kLdsBytes;
-    static const gas_status attr = lds_of(classes_gx_kernel<BA, WA, WB>, smem);
+    constexpr int smem = TileProduct<BA, BB, WA, WB, false, false>::kLdsBytes;
+    static const gas_status attr = lds_of(classes_gx_kernel<BA, BB, WA, WB>, smem);
     if (attr != GAS_OK) return attr;
-    hipLaunchKernelGGL((classes_gx_kernel<BA, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
+    hipLaunchKernelGGL((classes_gx_kernel<BA, BB, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
 }
@@ -606,6 +612,14 @@ gas_status launch_gw(const GradArgs& a, int64_t blocks, hipStream_t s) {
     return GAS_OK;
 }
 
+template <int TEMPS>
+gas_status launch_grad_of(const LogitsArgs& a, int64_t n, int64_t tiles, gas_dtype dt, hipStream_t s) {
+    return dt == GAS_F32 ? launch_logits<LOGITS_GRAD, TEMPS, true>(a, n, tiles, s) : launch_logits<LOGITS_GRAD, TEMPS, false>(a, n, tiles, s);
+}
+gas_status launch_grad(const LogitsArgs& a, int64_t n, int64_t tiles, int temps, gas_dtype dt, hipStream_t s) {
+    return temps == 1 ? launch_grad_of<1>(a, n, tiles, dt, s) : temps == 2 ? launch_grad_of<2>(a, n, tiles, dt, s) : launch_grad_of<3>(a, n, tiles, dt, s);
+}
+
 gas_status backward(const Call& c, bool distill, const Grads& g) {
     Room room{static_cast<char*>(c.workspace)};
     const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
@@ -616,13 +630,13 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     GAS_TRY(run_rows(c, common, rows, distill));
     const Layer& l = common.layer;
     LogitsArgs a = logits_args(c, common, rows, distill);
-    a.two = !distill ? 1 : (c.t.labels ? 3 : 2);
     a.g = b.g;
     a.g_plane = b.cap;
     a.gbias = b.gbias;
     a.cap = b.cap;
     GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, nullptr, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
-    const int64_t bf = tile_of_width(l.fp), nf = (l.fp + bf - 1) / bf;
+    const int fx = gx_width(l.fp), rx = gx_rows(l.fp), fw = gw_width(l.fp);
+    const int64_t nfx = (l.fp + fx - 1) / fx, nfw = (l.fp + fw - 1) / fw;
     // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int least = piece_width(b.cap, l.most, l.C);
     const int pieces = (c.C + least - 1) / least;
@@ -630,33 +644,32 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         // the widest that piece p can be, and the most tiles that it can have: width * rows <= cap, or 256 classes
         a.piece = d.piece = p;
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
-        const int64_t all = rows_most / 256 * (cols_most / 256), fit = b.cap / (256 * 256);
-        GAS_TRY((c.n <= 64 ? launch_logits_tile<LOGITS_GRAD, 64, 4, 1>(a, 64, cols_most / 256, c.s)
-                           : launch_logits_tile<LOGITS_GRAD, 256, 2, 4>(a, 256, all < fit ? all : fit, c.s)));
+        const int64_t tile = rows_of_tile(c.n), all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
+        GAS_TRY(launch_grad(a, c.n, all < fit ? all : fit, !distill ? 1 : (c.t.labels ? 3 : 2), c.dt, c.s));
         if (g.gx) {
             d.part = b.gx;
-            int64_t blocks = rows_most / 256 * nf;
+            int64_t blocks = rows_most / rx * nfx;
             if (blocks < kFill) blocks = kFill;
-            GAS_TRY((bf == 64 ? launch_gx<64, 1, 4>(d, blocks, c.s) : bf == 128 ? launch_gx<128, 2, 4>(d, blocks, c.s) : launch_gx<256, 2, 4>(d, blocks, c.s)));
+            GAS_TRY((fx == 64 ? launch_gx<64, 256, 1, 4>(d, blocks, c.s) : fx == 128 ? launch_gx<128, 256, 1, 4>(d, blocks, c.s) : launch_gx<256, 128, 2, 2>(d, blocks, c.s)));
         }
         if (g.gw) {
             d.part = b.gw;
-            int64_t blocks = cols_most / 256 * nf;
+            int64_t blocks = cols_most / 256 * nfw;
             if (blocks < kFill) blocks = kFill;
-            GAS_TRY((bf == 64 ? launch_gw<64, 4, 1>(d, blocks, c.s) : bf == 128 ? launch_gw<128, 4, 2>(d, blocks, c.s) : launch_gw<256, 2, 4>(d, blocks, c.s)));
-            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d, (int)nf);
+            GAS_TRY((fw == 64 ? launch_gw<64, 4, 1>(d, blocks, c.s) : launch_gw<128, 2, 2>(d, blocks, c.s)));
+            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d, (int)nfw);
             GAS_CHECK_HIP(hipGetLastError());
         }
     }
     if (g.gx) {
         d.part = b.gx;
         d.piece = 0;
-        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n, (int)nf,
+        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n, rx, (int)nfx,
                            g.gx, g.ldgx, c.dt == GAS_BF16);
         GAS_CHECK_HIP(hipGetLastError());
     }
     if (g.gbias) {
-        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, c.n <= 64 ? 64 : 256, c.C,
+        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, rows_of_tile(c.n), c.C,
                            g.scale, g.gbias);
         GAS_CHECK_HIP(hipGetLastError());
     }

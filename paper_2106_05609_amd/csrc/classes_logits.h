@@ -6,6 +6,8 @@
 namespace gas {
 namespace {
 
+constexpr int kRowsTile = 128;                     // rows of a tile; 64 where there are no more
+
 enum { LOGITS_STATS = 0, LOGITS_GRAD = 1, LOGITS_TOP = 2 };
 
 struct LogitsArgs {
@@ -17,7 +19,6 @@ struct LogitsArgs {
     const uint16_t* starts;       // [rows][class tiles + 1]: entries of the tiles before
     int32_t k, tiles;             // tiles: of all classes
     float inv_t;
-    int32_t two;                  // statistics: both temperatures; gradient: bit 0 the first, bit 1 the other
     // gradient
     const f32x4* info;            // [rows]: lse, lse at the temperature, weights of their exponentials
     uint16_t* g;                  // [planes][rows][width of a piece]
@@ -30,6 +31,7 @@ struct LogitsArgs {
     float* z;                     // [rows][width of a piece]
     uint32_t* mask;               // [rows][width / 32]: which logits do
     int32_t first, width;         // the piece's first class and its width (a multiple of 256)
+    int32_t biased;               // the bias is to be added in every tile, else in the last one alone, which ends beyond the classes
 };
 
 // Classes of a piece: as many as the room for the gradient at the logits allows, a multiple of 256.
@@ -38,10 +40,18 @@ __device__ __host__ __forceinline__ int piece_width(int64_t cap, int64_t rows, i
     return (int)(fit < 256 ? 256 : (fit < cp ? fit : cp));
 }
 
-template <int KIND, int BB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB) void classes_logits_kernel(LogitsArgs a) {
+// KIND: what is made of the logits.  TEMPS: bit 0, exponentials as they are, bit 1, at the temperature.  SPLIT: the gradient goes to
+// three planes (fp32).
+//
+// What passes between lanes goes through a piece of LDS that belongs to the wavefront, 32 rows of its classes at a time: a lane has 64 classes of a
+// row in fours, memory wants a row's next to each other (stored as they come, 16 bytes to a row, the gradient took ... of a tile's time), and a
+// target's logit lies wherever its class is (found by comparing all 64 it took twice what its sums take).
+template <int KIND, int TEMPS, bool SPLIT, int BB, int WA, int WB>
+__global__ __launch_bounds__(64 * WA * WB, 2) void classes_logits_kernel(LogitsArgs a) {
     using P = TileProduct<kTileC, BB, WA, WB, true, false>;
     constexpr int TA = P::TA, TB = P::TB, T = P::T;
+    constexpr int kRow = 32 * TA + 4;                                            // floats of a row in the wavefront's piece of LDS
+    static_assert(WA * WB * 32 * kRow * 4 <= P::kLdsBytes, "the pieces fit where the operands were");
     extern __shared__ __attribute__((aligned(16))) char smem[];
     uint16_t* lds = reinterpret_cast<uint16_t*>(smem);
     float* bias = reinterpret_cast<float*>(smem + P::kLdsBytes);                 // [256]
@@ -66,7 +76,13 @@ __global__ __launch_bounds__(64 * WA * WB) void classes_logits_kernel(LogitsArgs
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa0 = (wave % WA) * (32 * TA), wb0 = (wave / WA) * (32 * TB);
-    for (int i = tid; i < kTileC; i += T) bias[i] = l.bias[c0 + i];
+    const bool biased = a.biased || c0 + kTileC > l.C;
+    const TileOperand oa = {l.w + c0, l.ldw, l.w_plane, l.cw - 8 - c0, l.F};
+    const TileOperand ob = {l.x + (int64_t)m0 * l.fp, l.fp, l.x_plane, l.most - 1 - m0, l.fp};
+    P product;
+    typename P::Walk walk = product.begin(oa, ob, 0, (l.F + P::kStepOf - 1) / P::kStepOf, l.terms, lds);
+    if (biased)
+        for (int i = tid; i < kTileC; i += T) bias[i] = l.bias[c0 + i];
     if constexpr (KIND != LOGITS_TOP) {
         for (int r = tid; r < BB; r += T) {
             int n = 0;
@@ -92,101 +108,105 @@ __global__ __launch_bounds__(64 * WA * WB) void classes_logits_kernel(LogitsArgs
         }
     }
     f32x16 acc[TA][TB];
-    P product;
-    {
-        const int last_c = l.cw - 8 - c0, last_m = l.most - 1 - m0;
-        const TileOperand oa = {l.w + c0, l.ldw, l.w_plane, last_c, l.F};
-        const TileOperand ob = {l.x + (int64_t)m0 * l.fp, l.fp, l.x_plane, last_m, l.fp};
-        product.run(oa, ob, 0, l.fp / kStepK, l.terms, lds, wa0, wb0, acc);
-    }
-    // entries of row r in this wavefront's classes, one after another: use(index, weight) with the index of the lane's element that it
-    // names, or -1
-    auto each_entry = [&](int r, auto&& use) {
-        const int n = held[r];
-        for (int j = 0; __any(j < n); ++j) {
-            int2 e = {-1, 0};
-            if (j < n) {
-                if (j < kHeldEntries) e = entry[r * kHeldEntries + j];
-                else {
-                    const int64_t m = m0 + r;
-                    e = a.entries[m * a.k + a.starts[m * (a.tiles + 1) + tile] + j];
-                    e.x -= c0;
-                }
+    product.run(walk, oa, ob, lds, wa0, wb0, acc);
+    if (biased) {
+#pragma unroll
+        for (int i = 0; i < TA; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 b = *reinterpret_cast<const f32x4*>(bias + wa0 + 32 * i + 8 * q + 4 * lh);
+#pragma unroll
+                for (int j = 0; j < TB; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += b[e];
             }
-            const int rel = e.x - wa0;
-            const bool mine = j < n && rel >= 0 && rel < 32 * TA && ((rel >> 2) & 1) == lh;
-            if (__any(mine)) use(mine ? (rel >> 5) * 16 + ((rel & 31) >> 3) * 4 + (rel & 3) : -1, __int_as_float(e.y));
+            __builtin_amdgcn_sched_barrier(0);                 // not all of the bias at once: there are no registers for it
         }
-    };
-#pragma unroll
-    for (int i = 0; i < TA; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const f32x4 b = *reinterpret_cast<const f32x4*>(bias + wa0 + 32 * i + 8 * q + 4 * lh);
-#pragma unroll
-            for (int j = 0; j < TB; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += b[e];
-        }
-    if constexpr (KIND == LOGITS_GRAD) {
-        const int64_t rows = (int64_t)(count + 255) / 256 * 256;
-        float column[TA][16];                                  // sums over this lane's rows
+    }
+    float* mine = reinterpret_cast<float*>(smem) + wave * (32 * kRow);
+    auto show = [&](int j) {                                   // the wavefront's rows 32 j .. to its piece of LDS
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) column[i][r] = 0.f;
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<f32x4*>(mine + li * kRow + 32 * i + 8 * q + 4 * lh) =
+                    f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+    };
+    // entries of row r of the tile among the wavefront's classes, by one lane of the row
+    auto each_entry = [&](int r, auto&& use) {
+        const int n = lh == 0 ? held[r] : 0;
+        for (int j = 0; j < n; ++j) {
+            int2 e;
+            if (j < kHeldEntries) e = entry[r * kHeldEntries + j];
+            else {
+                const int64_t m = m0 + r;
+                e = a.entries[m * a.k + a.starts[m * (a.tiles + 1) + tile] + j];
+                e.x -= c0;
+            }
+            const int rel = e.x - wa0;
+            if (rel >= 0 && rel < 32 * TA) use(mine + li * kRow + rel, __int_as_float(e.y));
+        }
+    };
+    if constexpr (KIND == LOGITS_GRAD) {
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
             const int row = wb0 + 32 * j + li;
             const int64_t m = m0 + row;
+            // a exp(z - lse) = (a 2^(rest)) 2^(z log2 e - least), least = lse log2 e rounded, which leaves out `rest`
             f32x4 info = {INFINITY, INFINITY, 0.f, 0.f};
             if (m < count) info = a.info[m];
+            const float least = info[0] * kLog2e, least_t = info[1] * kLog2e, log2e_t = kLog2e * a.inv_t;
+            if (m < count) {
+                if (TEMPS & 1) info[2] *= exp2_of((float)((double)least - (double)info[0] * (double)kLog2e));
+                if (TEMPS & 2) info[3] *= exp2_of((float)((double)least_t - (double)info[1] * (double)kLog2e));
+            }
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float z = acc[i][j][r];
                     float g = 0.f;
-                    if (a.two & 1) g = info[2] * exp2_of((z - info[0]) * kLog2e);
-                    if (a.two & 2) g += info[3] * exp2_of((z * a.inv_t - info[1]) * kLog2e);
+                    if constexpr (TEMPS & 1) g = info[2] * exp2_of(fmaf(z, kLog2e, -least));
+                    if constexpr (TEMPS & 2) g += info[3] * exp2_of(fmaf(z, log2e_t, -least_t));
                     acc[i][j][r] = g;
                 }
-            each_entry(row, [&](int at, float w) {
+            show(j);
+            each_entry(row, [&](float* at, float w) { *at -= w; });
+            if (a.gbias)
 #pragma unroll
                 for (int i = 0; i < TA; ++i)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[i][j][r] -= at == 16 * i + r ? w : 0.f;
-            });
-            if (m >= rows) continue;
-            uint16_t* to = a.g + m * width + (c0 - c_first) + wa0 + 4 * lh;
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 v = *reinterpret_cast<const f32x4*>(mine + li * kRow + 32 * i + 8 * q + 4 * lh);
 #pragma unroll
-            for (int i = 0; i < TA; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t h[2], md[2], lo[2];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) split_pair(acc[i][j][4 * q + 2 * e], acc[i][j][4 * q + 2 * e + 1], h[e], md[e], lo[e]);
-                    uint16_t* at = to + 32 * i + 8 * q;
-                    *reinterpret_cast<u32x2*>(at) = u32x2{h[0], h[1]};
-                    if (l.terms > 1) {
-                        *reinterpret_cast<u32x2*>(at + a.g_plane) = u32x2{md[0], md[1]};
-                        *reinterpret_cast<u32x2*>(at + 2 * a.g_plane) = u32x2{lo[0], lo[1]};
+                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = v[e];
                     }
+            // eight classes of a row a lane, so that a row's are next to each other
+            constexpr int kLanes = 32 * TA / 8, kRows = 64 / kLanes;
+            uint16_t* to = a.g + (int64_t)(m0 + wb0 + 32 * j + lane / kLanes) * width + (c0 - c_first) + wa0 + 8 * (lane % kLanes);
+            const float* from = mine + (lane / kLanes) * kRow + 8 * (lane % kLanes);
+#pragma unroll
+            for (int r = 0; r < 32; r += kRows) {
+                const f32x4 v0 = *reinterpret_cast<const f32x4*>(from + r * kRow), v1 = *reinterpret_cast<const f32x4*>(from + r * kRow + 4);
+                uint16_t* p = to + (int64_t)r * width;
+                if constexpr (SPLIT) {
+                    const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+                    put8(v, 6, p, a.g_plane, 0);
+                } else {
+                    *reinterpret_cast<u32x4*>(p) = u32x4{pack_bf16(v0[0], v0[1]), pack_bf16(v0[2], v0[3]), pack_bf16(v1[0], v1[1]), pack_bf16(v1[2], v1[3])};
                 }
+            }
         }
         if (a.gbias) {
+            __syncthreads();
             float* sums = reinterpret_cast<float*>(smem);      // [WB][256]
-#pragma unroll
-            for (int j = 0; j < TB; ++j)
-#pragma unroll
-                for (int i = 0; i < TA; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) column[i][r] += acc[i][j][r];
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    float v = column[i][r];
+                    float v = acc[i][0][r];
+#pragma unroll
+                    for (int j = 1; j < TB; ++j) v += acc[i][j][r];
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o);
                     if (li == 0) sums[(wave / WA) * kTileC + wa0 + 32 * i + acc_row(r, lh)] = v;
@@ -213,7 +233,9 @@ __global__ __launch_bounds__(64 * WA * WB) void classes_logits_kernel(LogitsArgs
                 uint32_t mask = 0;
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (!(acc[i][j][r] <= floor) && c + acc_row(r, lh) < l.C) mask |= 1u << acc_row(r, lh);
+                    if (!(acc[i][j][r] <= floor)) mask |= 1u << acc_row(r, 0);
+                mask <<= 4 * lh;
+                if (c + 32 > l.C) mask &= c >= l.C ? 0u : 0xFFFFFFFFu >> (32 - (l.C - c));
                 if (!on) mask = 0;
                 if (mask) {
                     float* to = a.z + m * width + (c - c_first);
@@ -227,89 +249,96 @@ __global__ __launch_bounds__(64 * WA * WB) void classes_logits_kernel(LogitsArgs
         }
         if (!a.parts.most) return;
     }
-    float* red = reinterpret_cast<float*>(smem);               // [WA][4][BB]
+    float* red = bias;                                         // [WA][4][BB], over the bias and what follows it
+    float most[TB], sum[TB], sum_t[TB], picked[TB];
 #pragma unroll
     for (int j = 0; j < TB; ++j) {
         const int row = wb0 + 32 * j + li;
-        float most = -INFINITY, sum = 0.f, sum_t = 0.f, picked = 0.f;
+        most[j] = -INFINITY;
+        sum[j] = sum_t[j] = picked[j] = 0.f;
+        if constexpr (KIND == LOGITS_STATS) {
+            if (__any(held[row] > 0)) {
+                show(j);
+                each_entry(row, [&](const float* at, float w) { picked[j] = fmaf(w, *at, picked[j]); });
+            }
+        }
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) most = fmaxf(most, acc[i][j][r]);
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float base = most == -INFINITY ? 0.f : most;
+            for (int r = 0; r < 16; ++r) most[j] = fmaxf(most[j], acc[i][j][r]);
+        most[j] = fmaxf(most[j], __shfl_xor(most[j], 32));
+        most[j] = fmaxf(most[j] * kLog2e, kLeastExponent);
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float d = (acc[i][j][r] - base) * kLog2e;
-                sum += exp2_of(d);
-                if (KIND == LOGITS_STATS && a.two) sum_t += exp2_of(d * a.inv_t);
+                const float d = fmaf(acc[i][j][r], kLog2e, -most[j]);
+                sum[j] += exp2_of(d);
+                if constexpr (TEMPS & 2) sum_t[j] += exp2_of(d * a.inv_t);
             }
-        sum += __shfl_xor(sum, 32);
-        if constexpr (KIND == LOGITS_STATS) {
-            if (a.two) sum_t += __shfl_xor(sum_t, 32);
-            each_entry(row, [&](int at, float w) {
-                float z = 0.f;
+        sum[j] += __shfl_xor(sum[j], 32);
+        if constexpr (TEMPS & 2) sum_t[j] += __shfl_xor(sum_t[j], 32);
+    }
+    int n_held = 0;
+    if (KIND == LOGITS_STATS && tid < BB) n_held = held[tid];
+    __syncthreads();                                           // everyone is done with the bias and the entries
+    if (lh == 0) {
 #pragma unroll
-                for (int i = 0; i < TA; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) z = at == 16 * i + r ? acc[i][j][r] : z;
-                if (at >= 0) picked = fmaf(w, z, picked);
-            });
-            picked += __shfl_xor(picked, 32);
-        }
-        if (lh == 0) {
-            float* to = red + (wave % WA) * 4 * BB + row;
-            to[0] = most;
-            to[BB] = sum;
-            to[2 * BB] = sum_t;
-            to[3 * BB] = picked;
+        for (int j = 0; j < TB; ++j) {
+            float* to = red + (wave % WA) * 4 * BB + wb0 + 32 * j + li;
+            to[0] = most[j];
+            to[BB] = sum[j];
+            to[2 * BB] = sum_t[j];
+            to[3 * BB] = picked[j];
         }
     }
     __syncthreads();
-    for (int r = tid; r < BB; r += T) {
-        const int64_t m = m0 + r;
-        if (m >= count) continue;
-        float most = red[r], sum = red[BB + r], sum_t = red[2 * BB + r], picked = red[3 * BB + r];
+    static_assert(BB <= T, "a thread a row");
+    if (tid < BB && m0 + tid < count) {
+        const int64_t m = m0 + tid;
+        float top = red[tid], s = red[BB + tid], st = red[2 * BB + tid], z = red[3 * BB + tid];
 #pragma unroll
         for (int w = 1; w < WA; ++w) {
-            const float* o = red + w * 4 * BB + r;
-            join(most, sum, sum_t, o[0], o[BB], o[2 * BB], a.inv_t);
-            picked += o[3 * BB];
+            const float* o = red + w * 4 * BB + tid;
+            join(top, s, st, o[0], o[BB], o[2 * BB], a.inv_t);
+            z += o[3 * BB];
         }
         const int64_t at = (int64_t)tile * l.most + m;
-        a.parts.most[at] = most;
-        a.parts.sum[at] = sum;
+        a.parts.most[at] = top;
+        a.parts.sum[at] = s;
         if constexpr (KIND == LOGITS_STATS) {
-            if (a.two) a.parts.sum_t[at] = sum_t;
-            if (!a.labels) a.parts.picked[at] = picked;
-            else if (held[r]) a.parts.picked[m] = picked;
+            if constexpr (TEMPS & 2) a.parts.sum_t[at] = st;
+            if (!a.labels) a.parts.picked[at] = z;
+            else if (n_held) a.parts.picked[m] = z;
         }
     }
 }
 
 template <int BB, int WA, int WB>
-constexpr int logits_lds() { return TileProduct<kTileC, BB, WA, WB, true, false>::kLdsBytes + kTileC * 4 + BB * 4 + BB * kHeldEntries * 8; }
+constexpr int logits_lds() {
+    constexpr int extra = kTileC * 4 + BB * 4 + BB * kHeldEntries * 8, red = WA * 4 * BB * 4;
+    return TileProduct<kTileC, BB, WA, WB, true, false>::kLdsBytes + (extra > red ? extra : red);
+}
 
-template <int KIND, int BB, int WA, int WB>
-gas_status launch_logits_tile(const LogitsArgs& a, int64_t rows, int64_t tiles_c, hipStream_t s) {
+template <int KIND, int TEMPS, bool SPLIT, int BB, int WA, int WB>
+gas_status launch_logits_tile(const LogitsArgs& a, int64_t tiles, hipStream_t s) {
     constexpr int smem = logits_lds<BB, WA, WB>();
-    static_assert(smem <= 160 * 1024, "LDS of a compute unit");
-    static const gas_status attr = lds_of(classes_logits_kernel<KIND, BB, WA, WB>, smem);
+    static_assert(smem <= 80 * 1024, "two workgroups share the LDS of a compute unit");
+    static const gas_status attr = lds_of(classes_logits_kernel<KIND, TEMPS, SPLIT, BB, WA, WB>, smem);
     if (attr != GAS_OK) return attr;
-    const int64_t tiles = (rows + BB - 1) / BB * tiles_c, blocks = (tiles + 7) / 8 * 8;
+    const int64_t blocks = (tiles + 7) / 8 * 8;
     GAS_REQUIRE(blocks <= 0x7FFFFFLL, "too many tiles for one launch");
-    hipLaunchKernelGGL((classes_logits_kernel<KIND, BB, WA, WB>), dim3((unsigned)blocks), dim3(64 * WA * WB), smem, s, a);
+    hipLaunchKernelGGL((classes_logits_kernel<KIND, TEMPS, SPLIT, BB, WA, WB>), dim3((unsigned)blocks), dim3(64 * WA * WB), smem, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
 }
 
-// rows: at most so many count; tiles_c: tiles of 256 classes of the launch
-template <int KIND>
-gas_status launch_logits(const LogitsArgs& a, int64_t rows, int64_t tiles_c, hipStream_t s) {
-    if (rows <= 64) return launch_logits_tile<KIND, 64, 4, 1>(a, rows, tiles_c, s);
-    return launch_logits_tile<KIND, 256, 2, 4>(a, rows, tiles_c, s);
+// tiles: of rows by classes, at most, for tiles of rows_of_tile(n) rows
+inline int rows_of_tile(int64_t n) { return n <= 64 ? 64 : kRowsTile; }
+template <int KIND, int TEMPS, bool SPLIT = false>
+gas_status launch_logits(const LogitsArgs& a, int64_t n, int64_t tiles, hipStream_t s) {
+    if (n <= 64) return launch_logits_tile<KIND, TEMPS, SPLIT, 64, 4, 1>(a, tiles, s);
+    return launch_logits_tile<KIND, TEMPS, SPLIT, kRowsTile, 2, 2>(a, tiles, s);
 }
 
 }  // namespace

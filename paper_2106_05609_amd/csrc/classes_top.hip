@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t m
     __shared__ float red[2][16][17];
     const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
     const int64_t r = (int64_t)blockIdx.x * 16 + row;
-    float most = -INFINITY, sum = 0.f, none = 0.f;
+    float most = kLeastExponent, sum = 0.f, none = 0.f;
     if (r < n)
         for (int t = part; t < tiles; t += 16) join(most, sum, none, parts.most[t * most_rows + r], parts.sum[t * most_rows + r], 0.f, 1.f);
     red[0][part][row] = most;
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t m
     __syncthreads();
     if (part > 0 || r >= n) return;
     for (int p = 1; p < 16; ++p) join(most, sum, none, red[0][p][row], red[1][p][row], 0.f, 1.f);
-    lse[r] = most + logf(sum);
+    lse[r] = log_of(most, sum, 1.f);
 }
 
 inline int64_t top_width(int64_t most, int C) {
@@ -244,6 +244,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     a.layer = t.common.layer;
     if (lse) a.parts = t.parts;
     a.inv_t = 1.f;
+    a.biased = bias != nullptr;
     a.tiles = (n_classes + kTileC - 1) / kTileC;
     a.floor = t.floor;
     a.z = t.z;
@@ -255,7 +256,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
         if (first + width > cp) width = cp - first;
         a.first = (int32_t)first;
         a.width = (int32_t)width;
-        st = launch_logits<LOGITS_TOP>(a, n_rows, width / 256, s);
+        st = launch_logits<LOGITS_TOP, 1>(a, n_rows, (n_rows + rows_of_tile(n_rows) - 1) / rows_of_tile(n_rows) * (width / 256), s);
         if (st != GAS_OK) return st;
         const SelectArgs sel = {t.z, t.mask, t.best, t.floor, a.first, a.width, k, first + width >= cp, ids, values, ld_ids, ld_values};
         hipLaunchKernelGGL(classes_select_kernel, dim3((unsigned)n_rows), dim3(256), 0, s, sel);

@@ -19,7 +19,8 @@
 namespace gas {
 namespace {
 
-constexpr int kStepK = 64;
+constexpr int kStepK = 64;                        // k are a multiple of it, padded or split
+
 
 struct TileOperand {
     const uint16_t* p;        // the tile's first row and first k
@@ -28,18 +29,22 @@ struct TileOperand {
     int k;                    // k that can be read (beyond, the last ones repeat: the other operand has zeros there)
 };
 
-template <int BA, int BB, int WA, int WB, bool ATURNED, bool BTURNED>
+template <int BA, int BB, int WA, int WB, bool ATURNED, bool BTURNED, int STEP = 32, int STAGES = 3>
 struct TileProduct {
     static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB;
-    static constexpr int kStage = (BA + BB) * kStepK;                      // elements
-    static constexpr int kLdsBytes = 2 * kStage * 2;
+    static constexpr int kStage = (BA + BB) * STEP;                        // elements
+    static constexpr int kStepOf = STEP;
+    static constexpr int kLdsBytes = STAGES * kStage * 2;
+    static_assert((STEP == 32 || STEP == 64) && (STAGES == 2 || STAGES == 3), "");
+    // where piece `piece` of row `row` lies, in pieces of 16 bytes
+    static __device__ __forceinline__ int swap(int row) { return STEP == 64 ? row & 7 : (row >> 1) & 3; }
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
 
     template <int R, bool TURNED>
     struct Loads {
-        static constexpr int N = R * kStepK / 8 / T;
-        static_assert(R * kStepK / 8 % T == 0, "every thread brings as many pieces");
+        static constexpr int N = R * STEP / 8 / T;
+        static_assert(R * STEP / 8 % T == 0, "every thread brings as many pieces");
         uint32_t at[N];                                                    // bytes from the step's first element
         __device__ __forceinline__ void init(const TileOperand& o) {
 #pragma unroll
@@ -49,24 +54,24 @@ struct TileProduct {
                     const int kr = q / (R / 8), unit = (q % (R / 8)) ^ (4 * (kr & 3) & (R / 8 - 1));
                     at[i] = (uint32_t)((int64_t)kr * o.ld + (8 * unit < o.last ? 8 * unit : o.last)) * 2;
                 } else {
-                    const int row = q >> 3, piece = (q & 7) ^ (row & 7);
+                    const int row = q / (STEP / 8), piece = (q % (STEP / 8)) ^ swap(row);
                     at[i] = (uint32_t)((int64_t)(row < o.last ? row : o.last) * o.ld + 8 * piece) * 2;
                 }
             }
         }
-        // the 64 k from `from` on, of which `left` can be read
+        // the STEP k from `from` on, of which `left` can be read
         __device__ __forceinline__ void bring(const uint16_t* from, int64_t ld, int left, uint16_t* to) const {
             const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 uint32_t a = at[i];
-                if (left < kStepK) {
+                if (left < STEP) {
                     const int q = i * T + (int)threadIdx.x;
                     if constexpr (TURNED) {
                         const int kr = q / (R / 8), over = kr - (left - 1);
                         a -= over > 0 ? (uint32_t)(over * ld * 2) : 0u;
                     } else {
-                        const int over = 8 * ((q & 7) ^ ((q >> 3) & 7)) - (left - 8);
+                        const int over = 8 * ((q % (STEP / 8)) ^ swap(q / (STEP / 8))) - (left - 8);
                         a -= over > 0 ? (uint32_t)over * 2 : 0u;
                     }
                 }
@@ -92,7 +97,7 @@ struct TileProduct {
             return __builtin_bit_cast(bf16x8, s16x8{h[0][0], h[0][1], h[0][2], h[0][3], h[1][0], h[1][1], h[1][2], h[1][3]});
         } else {
             const int row = r0 + li;
-            return *reinterpret_cast<const bf16x8*>(tile + (row * 8 + ((2 * kk + lh) ^ (row & 7))) * 8);
+            return *reinterpret_cast<const bf16x8*>(tile + (row * (STEP / 8) + ((2 * kk + lh) ^ swap(row))) * 8);
         }
     }
 
@@ -106,13 +111,13 @@ struct TileProduct {
                                          f32x16 (&acc)[TA][TB]) const {
         if (more) {
             la.bring(a, lda, left_a, next);
-            lb.bring(b, ldb, left_b, next + BA * kStepK);
+            lb.bring(b, ldb, left_b, next + BA * STEP);
         }
 #pragma unroll
-        for (int kk = 0; kk < kStepK / 16; ++kk) {
+        for (int kk = 0; kk < STEP / 16; ++kk) {
             bf16x8 fa[TA], fb[TB];
 #pragma unroll
-            for (int j = 0; j < TB; ++j) fb[j] = fragment<BB, BTURNED>(now + BA * kStepK, wb0 + 32 * j, kk);
+            for (int j = 0; j < TB; ++j) fb[j] = fragment<BB, BTURNED>(now + BA * STEP, wb0 + 32 * j, kk);
 #pragma unroll
             for (int i = 0; i < TA; ++i) fa[i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
 #pragma unroll
@@ -122,47 +127,84 @@ struct TileProduct {
         }
     }
 
-    // acc = the products over steps [first, last) of 64 k of every term.  Called by every thread; LDS is free for other use afterwards.
-    __device__ __forceinline__ void run(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds, int wa0,
-                                        int wb0, f32x16 (&acc)[TA][TB]) {
+    // Where the loads of a sum over `terms` terms of steps [first, last) stand.
+    struct Walk {
+        const uint16_t *a, *b;
+        int64_t step_a, step_b;
+        int first, last, k, term, terms, n;               // n: steps of all terms
+    };
+    static constexpr int kLoads = Loads<BA, ATURNED>::N + Loads<BB, BTURNED>::N;      // of a thread for a step
+    static_assert(kLoads * (STAGES - 2) < 64, "the counter of loads under way");
+
+    __device__ __forceinline__ void place(Walk& w, const TileOperand& a, const TileOperand& b) const {
+        // planes of the terms, the smallest product first: m m, l h, h l, m h, h m, h h, a nibble a term from the lowest; one term: h h
+        const int pa = w.terms == 1 ? 0 : 0x010201 >> (4 * w.term) & 15, pb = w.terms == 1 ? 0 : 0x001021 >> (4 * w.term) & 15;
+        w.a = a.p + pa * a.plane + w.first * w.step_a;
+        w.b = b.p + pb * b.plane + w.first * w.step_b;
+    }
+    __device__ __forceinline__ void advance(Walk& w, const TileOperand& a, const TileOperand& b) const {
+        if (++w.k == w.last) {
+            w.k = w.first;
+            if (++w.term < w.terms) place(w, a, b);
+        } else {
+            w.a += w.step_a;
+            w.b += w.step_b;
+        }
+    }
+    __device__ __forceinline__ void bring(const Walk& w, const TileOperand& a, const TileOperand& b, uint16_t* to) const {
+        la.bring(w.a, a.ld, a.k - STEP * w.k, to);
+        lb.bring(w.b, b.ld, b.k - STEP * w.k, to + BA * STEP);
+    }
+    // The first steps' loads; other work may follow before run().
+    __device__ __forceinline__ Walk begin(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds) {
         la.init(a);
         lb.init(b);
+        Walk w;
+        w.step_a = ATURNED ? STEP * a.ld : STEP;
+        w.step_b = BTURNED ? STEP * b.ld : STEP;
+        w.first = w.k = first;
+        w.last = last;
+        w.term = 0;
+        w.terms = terms;
+        w.n = last > first ? (last - first) * terms : 0;
+        place(w, a, b);
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < w.n) {
+                bring(w, a, b, lds + s * kStage);
+                advance(w, a, b);
+            }
+        return w;
+    }
+    // acc = the products.  Called by every thread; LDS is free for other use afterwards.
+    __device__ __forceinline__ void run(Walk& w, const TileOperand& a, const TileOperand& b, uint16_t* lds, int wa0, int wb0, f32x16 (&acc)[TA][TB]) {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
             for (int j = 0; j < TB; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        const int per = last - first, n = per * terms;
-        if (n <= 0) return;
-        const int64_t step_a = ATURNED ? kStepK * a.ld : kStepK, step_b = BTURNED ? kStepK * b.ld : kStepK;
-        // planes of the terms, the smallest product first: m m, l h, h l, m h, h m, h h; one term: h h
-        const uint32_t kOfA = 0x010201u, kOfB = 0x001021u;                 // a nibble a term, from the lowest
-        int term = 0, k = first;
-        auto plane_of = [&](uint32_t which, int t) { return terms == 1 ? 0 : (int)((which >> (4 * t)) & 15); };
-        const uint16_t* pa = a.p + plane_of(kOfA, 0) * a.plane + first * step_a;
-        const uint16_t* pb = b.p + plane_of(kOfB, 0) * b.plane + first * step_b;
-        la.bring(pa, a.ld, a.k - kStepK * k, lds);
-        lb.bring(pb, b.ld, b.k - kStepK * k, lds + BA * kStepK);
-        int half = 0;
+        int now = 0, next = STAGES - 1;
 #pragma unroll 1
-        for (int s = 0; s < n; ++s) {
-            __builtin_amdgcn_s_waitcnt(0x0F70);            // the loads of this step have arrived (vmcnt 0)
-            __syncthreads();                               // everyone's; and everyone is done reading the other half
-            if (++k == last) {
-                k = first;
-                ++term;
-                const int t = term < terms ? term : 0;
-                pa = a.p + plane_of(kOfA, t) * a.plane + first * step_a;
-                pb = b.p + plane_of(kOfB, t) * b.plane + first * step_b;
-            } else {
-                pa += step_a;
-                pb += step_b;
-            }
-            step(lds + half * kStage, lds + (half ^ 1) * kStage, s + 1 < n, pa, a.ld, a.k - kStepK * k, pb, b.ld, b.k - kStepK * k, wa0, wb0, acc);
-            half ^= 1;
+        for (int s = 0; s < w.n; ++s) {
+            // this step's loads have arrived (those of the step after it may be under way), this thread is done with the step before ...
+            if (STAGES == 3 && s + 1 < w.n) __builtin_amdgcn_s_waitcnt(0x0070 | (kLoads & 15) | (kLoads >> 4 << 14));
+            else __builtin_amdgcn_s_waitcnt(0x0070);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();                  // ... and so for everyone
+            asm volatile("" ::: "memory");
+            const bool more = s + STAGES - 1 < w.n;
+            step(lds + now * kStage, lds + next * kStage, more, w.a, a.ld, a.k - STEP * w.k, w.b, b.ld, b.k - STEP * w.k, wa0, wb0, acc);
+            if (more) advance(w, a, b);
+            now = now + 1 == STAGES ? 0 : now + 1;
+            next = next + 1 == STAGES ? 0 : next + 1;
         }
         __syncthreads();
+    }
+    __device__ __forceinline__ void run(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds, int wa0, int wb0,
+                                        f32x16 (&acc)[TA][TB]) {
+        Walk w = begin(a, b, first, last, terms, lds);
+        run(w, a, b, lds, wa0, wb0, acc);
     }
 };
 
