@@ -507,7 +507,7 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
  * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X and, unless W
  * is bf16 with 16-byte aligned rows of whole 16-byte pieces, W as the products take them; statistics of every 256 classes;
- * backward a piece of G, 0.5 GB (fp32: 1.5 GB) or 256 classes of it if they are more.
+ * backward a piece of G, 1 GB (fp32: 3.2 GB) or 256 classes of it if they are more.
  */
 GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
 GAS_API gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,

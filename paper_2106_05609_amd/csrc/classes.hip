@@ -7,6 +7,7 @@
 // Forward: tiles of logits leave a row's largest logit, its sums from there and its weighted target logits, which a second kernel
 // joins.  Backward: a piece of the classes at a time, the gradient at its logits (formed again from the products) is stored in the
 // products' type and multiplied by W and X.
+
 #include "classes_logits.h"
 
 namespace gas {
@@ -263,7 +264,7 @@ struct GradArgs {
 };
 
 // Parts of a sum, so that its tiles fill the card: as few as leave the compute units with something to do, at least eight steps each.
-constexpr int kFill = 1024, kMostSplits = 16;
+constexpr int kFill = 512, kMostSplits = 16;
 __device__ __host__ __forceinline__ int splits_of(int64_t tiles, int steps) {
     int64_t s = kFill / (tiles > 0 ? tiles : 1);
     if (s > kMostSplits) s = kMostSplits;
@@ -289,9 +290,9 @@ __device__ __forceinline__ Shape shape_of(const GradArgs& a) {
 }
 
 // gx += G W^T over a piece of the classes: lanes end up with four neighbouring inputs of one row
-template <int BA, int BB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, 2) void classes_gx_kernel(GradArgs a) {
-    using P = TileProduct<BA, BB, WA, WB, false, false>;
+template <class P>
+__global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
+    constexpr int BA = P::kRowsA, BB = P::kRowsB, WA = BA / 32 / P::TA;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
     const Shape s = shape_of(a);
@@ -347,9 +348,9 @@ __device__ __forceinline__ void put4(void* base, int64_t at, const f32x4& v, int
 __device__ __host__ __forceinline__ bool fours(const void* p, int64_t ld, bool bf) { return ld % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & (bf ? 7 : 15)) == 0; }
 
 // gw = X^T G of a piece of the classes, or a part of the sum over the rows: lanes end up with four neighbouring classes of one input
-template <int BB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, 2) void classes_gw_kernel(GradArgs a) {
-    using P = TileProduct<256, BB, WA, WB, true, true>;
+template <class P>
+__global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
+    constexpr int BB = P::kRowsB, WA = P::kRowsA / 32 / P::TA;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
     const Shape s = shape_of(a);
@@ -552,16 +553,20 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
 }
 
 // Room for the gradient at the logits of a piece, in elements.
-constexpr int64_t kPieceElements = 1LL << 28;
+constexpr int64_t kPieceElements = 1LL << 29;
 inline int64_t piece_cap(int64_t most, int C) {
     const int64_t all = most * round_up(C, 256), least = most * 256;
     const int64_t cap = all < kPieceElements ? all : kPieceElements;
     return cap > least ? cap : least;
 }
-// Inputs of a tile: gw's 64 or 128; gx's 256 too, where that leaves out no more of the last tile, since it reads G once for each.
-inline int gw_width(int64_t fp) { return fp <= 64 ? 64 : 128; }
-inline int gx_width(int64_t fp) { return fp <= 128 ? gw_width(fp) : (round_up(fp, 256) == round_up(fp, 128) ? 256 : 128); }
-inline int gx_rows(int64_t fp) { return gx_width(fp) == 256 ? 128 : 256; }
+// Tiles of the two products by inputs
+using Gx64 = TileProduct<64, 256, 1, 4, false, false, 64, 2>;
+using Gx128 = TileProduct<128, 256, 2, 4, false, false, 64, 2>;
+using Gx256 = TileProduct<256, 256, 2, 4, false, false, 64, 2>;
+using Gw64 = TileProduct<256, 64, 4, 1, true, true, 64, 2>;
+using Gw128 = TileProduct<256, 128, 4, 2, true, true, 64, 2>;
+using Gw256 = TileProduct<256, 256, 2, 4, true, true, 64, 2>;
+inline int width_of_tile(int64_t fp) { return fp <= 64 ? 64 : (fp <= 128 || (round_up(fp, 256) != round_up(fp, 128)) ? 128 : 256); }
 
 struct Grads {
     void* gx;
@@ -586,30 +591,32 @@ inline BackwardRoom lay_out_backward(Room& room, const Common& common, bool gx, 
     b.cap = piece_cap(most, l.C);
     b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
     // parts of a sum are made only where there are at most kFill tiles of them
-    const int64_t parts = (int64_t)kFill * 128 * 256, whole_x = most * l.fp;
+    const int64_t parts = (int64_t)kFill * 256 * 256, whole_x = most * l.fp;
     b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
     b.gw = gw ? room.take<float>(parts) : nullptr;
     b.gbias = gbias ? room.take<float>(most / kRowsTile * round_up(l.C, 256)) : nullptr;
     return b;
 }
 
-template <int BA, int BB, int WA, int WB>
-gas_status launch_gx(const GradArgs& a, int64_t blocks, hipStream_t s) {
-    constexpr int smem = TileProduct<BA, BB, WA, WB, false, false>::kLdsBytes;
-    static const gas_status attr = lds_of(classes_gx_kernel<BA, BB, WA, WB>, smem);
-    if (attr != GAS_OK) return attr;
-    hipLaunchKernelGGL((classes_gx_kernel<BA, BB, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
+template <class P, class Kernel>
+gas_status launch_product(Kernel kernel, const GradArgs& a, int64_t blocks, hipStream_t s) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(P::T), P::kLdsBytes, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
 }
-template <int BB, int WA, int WB>
-gas_status launch_gw(const GradArgs& a, int64_t blocks, hipStream_t s) {
-    constexpr int smem = TileProduct<256, BB, WA, WB, true, true>::kLdsBytes;
-    static const gas_status attr = lds_of(classes_gw_kernel<BB, WA, WB>, smem);
+template <class P>
+gas_status launch_gx(const GradArgs& a, int64_t rows, int64_t fp, hipStream_t s) {
+    static const gas_status attr = lds_of(classes_gx_kernel<P>, P::kLdsBytes);
     if (attr != GAS_OK) return attr;
-    hipLaunchKernelGGL((classes_gw_kernel<BB, WA, WB>), dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(64 * WA * WB), smem, s, a);
-    GAS_CHECK_HIP(hipGetLastError());
-    return GAS_OK;
+    const int64_t blocks = rows / P::kRowsB * ((fp + P::kRowsA - 1) / P::kRowsA);
+    return launch_product<P>(classes_gx_kernel<P>, a, blocks < kFill ? kFill : blocks, s);
+}
+template <class P>
+gas_status launch_gw(const GradArgs& a, int64_t cols, int64_t fp, hipStream_t s) {
+    static const gas_status attr = lds_of(classes_gw_kernel<P>, P::kLdsBytes);
+    if (attr != GAS_OK) return attr;
+    const int64_t blocks = cols / P::kRowsA * ((fp + P::kRowsB - 1) / P::kRowsB);
+    return launch_product<P>(classes_gw_kernel<P>, a, blocks < kFill ? kFill : blocks, s);
 }
 
 template <int TEMPS>
@@ -635,7 +642,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     a.gbias = b.gbias;
     a.cap = b.cap;
     GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, nullptr, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
-    const int fx = gx_width(l.fp), rx = gx_rows(l.fp), fw = gw_width(l.fp);
+    const int fx = width_of_tile(l.fp), rx = 256, fw = fx;
     const int64_t nfx = (l.fp + fx - 1) / fx, nfw = (l.fp + fw - 1) / fw;
     // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int least = piece_width(b.cap, l.most, l.C);
@@ -648,15 +655,11 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         GAS_TRY(launch_grad(a, c.n, all < fit ? all : fit, !distill ? 1 : (c.t.labels ? 3 : 2), c.dt, c.s));
         if (g.gx) {
             d.part = b.gx;
-            int64_t blocks = rows_most / rx * nfx;
-            if (blocks < kFill) blocks = kFill;
-            GAS_TRY((fx == 64 ? launch_gx<64, 256, 1, 4>(d, blocks, c.s) : fx == 128 ? launch_gx<128, 256, 1, 4>(d, blocks, c.s) : launch_gx<256, 128, 2, 2>(d, blocks, c.s)));
+            GAS_TRY((fx == 64 ? launch_gx<Gx64>(d, rows_most, l.fp, c.s) : fx == 128 ? launch_gx<Gx128>(d, rows_most, l.fp, c.s) : launch_gx<Gx256>(d, rows_most, l.fp, c.s)));
         }
         if (g.gw) {
             d.part = b.gw;
-            int64_t blocks = cols_most / 256 * nfw;
-            if (blocks < kFill) blocks = kFill;
-            GAS_TRY((fw == 64 ? launch_gw<64, 4, 1>(d, blocks, c.s) : launch_gw<128, 2, 2>(d, blocks, c.s)));
+            GAS_TRY((fw == 64 ? launch_gw<Gw64>(d, cols_most, l.fp, c.s) : fw == 128 ? launch_gw<Gw128>(d, cols_most, l.fp, c.s) : launch_gw<Gw256>(d, cols_most, l.fp, c.s)));
             hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d, (int)nfw);
             GAS_CHECK_HIP(hipGetLastError());
         }

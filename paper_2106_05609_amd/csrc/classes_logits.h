@@ -6,8 +6,6 @@
 namespace gas {
 namespace {
 
-constexpr int kRowsTile = 128;                     // rows of a tile; 64 where there are no more
-
 enum { LOGITS_STATS = 0, LOGITS_GRAD = 1, LOGITS_TOP = 2 };
 
 struct LogitsArgs {
@@ -40,21 +38,25 @@ __device__ __host__ __forceinline__ int piece_width(int64_t cap, int64_t rows, i
     return (int)(fit < 256 ? 256 : (fit < cp ? fit : cp));
 }
 
+template <class P>
+__host__ __device__ constexpr int logits_tiles_lds() {                           // operands, then the wavefronts' pieces
+    constexpr int pieces = P::T / 64 * 32 * (32 * P::TA + 4) * 4;
+    return pieces > P::kLdsBytes ? pieces : P::kLdsBytes;
+}
+
 // KIND: what is made of the logits.  TEMPS: bit 0, exponentials as they are, bit 1, at the temperature.  SPLIT: the gradient goes to
 // three planes (fp32).
 //
 // What passes between lanes goes through a piece of LDS that belongs to the wavefront, 32 rows of its classes at a time: a lane has 64 classes of a
 // row in fours, memory wants a row's next to each other (stored as they come, 16 bytes to a row, the gradient took ... of a tile's time), and a
 // target's logit lies wherever its class is (found by comparing all 64 it took twice what its sums take).
-template <int KIND, int TEMPS, bool SPLIT, int BB, int WA, int WB>
-__global__ __launch_bounds__(64 * WA * WB, 2) void classes_logits_kernel(LogitsArgs a) {
-    using P = TileProduct<kTileC, BB, WA, WB, true, false>;
-    constexpr int TA = P::TA, TB = P::TB, T = P::T;
+template <int KIND, int TEMPS, bool SPLIT, class P>
+__global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
+    constexpr int TA = P::TA, TB = P::TB, T = P::T, WA = kTileC / 32 / TA, BB = P::kRowsB, WB = BB / 32 / TB;
     constexpr int kRow = 32 * TA + 4;                                            // floats of a row in the wavefront's piece of LDS
-    static_assert(WA * WB * 32 * kRow * 4 <= P::kLdsBytes, "the pieces fit where the operands were");
     extern __shared__ __attribute__((aligned(16))) char smem[];
     uint16_t* lds = reinterpret_cast<uint16_t*>(smem);
-    float* bias = reinterpret_cast<float*>(smem + P::kLdsBytes);                 // [256]
+    float* bias = reinterpret_cast<float*>(smem + logits_tiles_lds<P>());                 // [256]
     int* held = reinterpret_cast<int*>(bias + kTileC);                           // [BB] entries of the row in this tile
     int2* entry = reinterpret_cast<int2*>(held + BB);                            // [BB][kHeldEntries]
     const Layer& l = a.layer;
@@ -314,31 +316,39 @@ __global__ __launch_bounds__(64 * WA * WB, 2) void classes_logits_kernel(LogitsA
     }
 }
 
-template <int BB, int WA, int WB>
+template <class P>
 constexpr int logits_lds() {
-    constexpr int extra = kTileC * 4 + BB * 4 + BB * kHeldEntries * 8, red = WA * 4 * BB * 4;
-    return TileProduct<kTileC, BB, WA, WB, true, false>::kLdsBytes + (extra > red ? extra : red);
+    constexpr int BB = P::kRowsB, extra = kTileC * 4 + BB * 4 + BB * kHeldEntries * 8, red = kTileC / 32 / P::TA * 4 * BB * 4;
+    return logits_tiles_lds<P>() + (extra > red ? extra : red);
 }
 
-template <int KIND, int TEMPS, bool SPLIT, int BB, int WA, int WB>
+template <int KIND, int TEMPS, bool SPLIT, class P>
 gas_status launch_logits_tile(const LogitsArgs& a, int64_t tiles, hipStream_t s) {
-    constexpr int smem = logits_lds<BB, WA, WB>();
-    static_assert(smem <= 80 * 1024, "two workgroups share the LDS of a compute unit");
-    static const gas_status attr = lds_of(classes_logits_kernel<KIND, TEMPS, SPLIT, BB, WA, WB>, smem);
+    constexpr int smem = logits_lds<P>();
+    static_assert(smem <= 160 * 1024, "LDS of a compute unit");
+    static const gas_status attr = lds_of(classes_logits_kernel<KIND, TEMPS, SPLIT, P>, smem);
     if (attr != GAS_OK) return attr;
     const int64_t blocks = (tiles + 7) / 8 * 8;
     GAS_REQUIRE(blocks <= 0x7FFFFFLL, "too many tiles for one launch");
-    hipLaunchKernelGGL((classes_logits_kernel<KIND, TEMPS, SPLIT, BB, WA, WB>), dim3((unsigned)blocks), dim3(64 * WA * WB), smem, s, a);
+    hipLaunchKernelGGL((classes_logits_kernel<KIND, TEMPS, SPLIT, P>), dim3((unsigned)blocks), dim3(P::T), smem, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
 }
 
 // tiles: of rows by classes, at most, for tiles of rows_of_tile(n) rows
+using FewRows = TileProduct<kTileC, 64, 4, 1, true, false>;
+#ifdef VARIANT_A
+constexpr int kRowsTile = 128;
+using ManyRows = TileProduct<kTileC, 128, 2, 2, true, false>;
+#else
+constexpr int kRowsTile = 256;
+using ManyRows = TileProduct<kTileC, 256, 2, 4, true, false, 64, 2>;
+#endif
 inline int rows_of_tile(int64_t n) { return n <= 64 ? 64 : kRowsTile; }
 template <int KIND, int TEMPS, bool SPLIT = false>
 gas_status launch_logits(const LogitsArgs& a, int64_t n, int64_t tiles, hipStream_t s) {
-    if (n <= 64) return launch_logits_tile<KIND, TEMPS, SPLIT, 64, 4, 1>(a, tiles, s);
-    return launch_logits_tile<KIND, TEMPS, SPLIT, kRowsTile, 2, 2>(a, tiles, s);
+    if (n <= 64) return launch_logits_tile<KIND, TEMPS, SPLIT, FewRows>(a, tiles, s);
+    return launch_logits_tile<KIND, TEMPS, SPLIT, ManyRows>(a, tiles, s);
 }
 
 }  // namespace

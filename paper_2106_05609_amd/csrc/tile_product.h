@@ -33,7 +33,7 @@ template <int BA, int BB, int WA, int WB, bool ATURNED, bool BTURNED, int STEP =
 struct TileProduct {
     static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB;
     static constexpr int kStage = (BA + BB) * STEP;                        // elements
-    static constexpr int kStepOf = STEP;
+    static constexpr int kStepOf = STEP, kRowsA = BA, kRowsB = BB;
     static constexpr int kLdsBytes = STAGES * kStage * 2;
     static_assert((STEP == 32 || STEP == 64) && (STAGES == 2 || STAGES == 3), "");
     // where piece `piece` of row `row` lies, in pieces of 16 bytes

@@ -253,7 +253,7 @@ def test_empty_batch():
 def test_pieces_of_the_classes(dtype):
     """More gradients at the logits than there is room for: several pieces, of which the last is narrower; and with few rows that count the same
     call takes them in one."""
-    n, f, c = 5000, 40, 70_001
+    n, f, c = 6500, 40, 100_001
     gen = torch.Generator(device="cuda").manual_seed(5)
     x, w = torch.randn(n, f, generator=gen, device="cuda").to(DT[dtype]), (torch.randn(f, c, generator=gen, device="cuda") * 0.2).to(DT[dtype])
     labels = torch.randint(0, c, (n,), generator=gen, device="cuda", dtype=torch.int32)
