@@ -25,10 +25,11 @@ struct LogitsArgs {
     int64_t cap;                  // elements of a plane of g
     int32_t piece;
     // top
-    const float* floor;           // [rows]: NaN, or the value that a logit has to exceed
+    const float* floor;           // [rows]: the value that a logit has to exceed
     float* z;                     // [rows][width of a piece]
     uint32_t* mask;               // [rows][width / 32]: which logits do
     int32_t first, width;         // the piece's first class and its width (a multiple of 256)
+    int32_t all;                  // every logit is stored, without bits
     int32_t biased;               // the bias is to be added in every tile, else in the last one alone, which ends beyond the classes
 };
 
@@ -228,6 +229,17 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
         for (int j = 0; j < TB; ++j) {
             const int64_t m = m0 + wb0 + 32 * j + li;
             const bool on = m < count;
+            float* row = a.z + m * width + (c0 - c_first) + wa0 + 4 * lh;
+            if (a.all) {                                       // columns up to the piece's width are there, beyond the classes too
+                if (on)
+#pragma unroll
+                    for (int i = 0; i < TA; ++i)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+                            *reinterpret_cast<f32x4*>(row + 32 * i + 8 * q) =
+                                f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                continue;
+            }
             const float floor = on ? a.floor[m] : 0.f;
 #pragma unroll
             for (int i = 0; i < TA; ++i) {
@@ -236,15 +248,14 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (!(acc[i][j][r] <= floor)) mask |= 1u << acc_row(r, 0);
-                mask <<= 4 * lh;
-                if (c + 32 > l.C) mask &= c >= l.C ? 0u : 0xFFFFFFFFu >> (32 - (l.C - c));
+                if (c + 32 > l.C) mask &= c >= l.C ? 0u : (0xFFFFFFFFu >> (32 - (l.C - c))) >> (4 * lh);
                 if (!on) mask = 0;
                 if (mask) {
-                    float* to = a.z + m * width + (c - c_first);
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (mask >> acc_row(r, lh) & 1) to[acc_row(r, lh)] = acc[i][j][r];
+                        if (mask >> acc_row(r, 0) & 1) row[32 * i + acc_row(r, 0)] = acc[i][j][r];
                 }
+                mask <<= 4 * lh;
                 mask |= (uint32_t)__shfl_xor((int)mask, 32);
                 if (on && lh == 0) a.mask[m * (width / 32) + (c - c_first) / 32] = mask;
             }

@@ -1,10 +1,13 @@
 // The k largest logits of an output layer over many classes, and the logarithm of the sum of all their exponentials, without its logits
 // (gas_linear_top).
 //
-// The classes are taken in pieces, each twice as wide as the one before. A tile stores only the logits that may still be among the k
-// largest: those above the row's k-th largest of the pieces before (a later class never replaces an equal earlier one), and a bit
-// for each. A row's list of k is then joined with what was stored. The first piece is stored whole; of a later one about k logits a row
-// are left in earnest, and all of it if the logits rise with the class, which costs time and no more.
+// Few rows (64): all logits of them are stored, 4 bytes beside the 2 F or 4 F of W's column, and searched. Up to eight rows have a kernel
+// of their own that reads W as it lies and multiplies by the vector units, bound by reading it.
+//
+// Many rows: the classes are taken in pieces. Of the first, 4,096 classes, all logits are stored; of a later one only those above the row's k-th largest
+// of the pieces before (a later class never replaces an equal earlier one), with a bit for each, and a row's list is joined with them. A piece seven
+// times as wide as all before leaves about 7 k logits a row in earnest, and all of it if the logits rise with the class, which costs
+// time and no more.
 //
 // A logit and its class make one whole number, larger for larger logits and, of equal ones, for lower classes, so the numbers of a
 // row differ and any order of work finds the same k. A NaN counts as less than every number.
@@ -16,7 +19,9 @@ namespace {
 constexpr int kMostTop = 128;
 constexpr int kBuffer = 2048;                     // numbers that a workgroup holds: a row's list, and candidates
 constexpr int kFirstPiece = 4096;                 // classes
-constexpr int64_t kTopElements = 1LL << 28;       // of a piece
+constexpr int kGrowth = 7;                        // of a piece, to all before
+constexpr int64_t kTopElements = 1LL << 29;       // of a piece
+constexpr int kFewRows = 64, kRowsByVector = 8;
 
 __device__ __forceinline__ uint64_t key_of(float z, int c) {
     const uint32_t b = __float_as_uint(z == 0.f ? 0.f : z);
@@ -145,52 +150,272 @@ __global__ __launch_bounds__(256) void classes_select_kernel(SelectArgs a) {
     if (tid == 0) a.floor[r] = logit_of(buf[a.k - 1]);
 }
 
-__global__ __launch_bounds__(256) void classes_floor_kernel(float* floor, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) floor[i] = NAN;
+// ---- all logits of a row, or what is left of its parts, searched
+
+struct PickArgs {
+    const float* z;               // logits, class e at e, or
+    const uint64_t* keys;         // numbers of the parts before (0: none)
+    int64_t ld;
+    int32_t n, per, parts, k;     // a part: `per` of the n, at most kPick
+    uint64_t* best;               // [rows][parts][k], the largest first, 0 beyond what there is
+    float* floor;                 // one part: the k-th largest, may be NULL
+    int32_t* ids;                 // the last one: what the call returns, else NULL
+    float* values;
+    int64_t ld_ids, ld_values;
+};
+constexpr int kPick = 8192;
+
+// A workgroup a part of a row, 32 numbers a thread. The k-th largest of the threads' largest is no more than the k-th largest of all, and
+// little less: what is not below it is put in order. Where that is too much (equal logits), numbers go in 256 at a time.
+template <bool KEYS>
+__global__ __launch_bounds__(256) void classes_pick_kernel(PickArgs a) {
+    __shared__ uint64_t buf[kBuffer];
+    __shared__ int held;
+    constexpr int N = kPick / 256;
+    const int64_t row = blockIdx.x / a.parts;
+    const int part = (int)(blockIdx.x % a.parts), first = part * a.per, tid = threadIdx.x;
+    const int end = first + a.per < a.n ? first + a.per : a.n, there = end - first, k = a.k < there ? a.k : there;
+    uint64_t key[N], largest = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int e = first + tid + 256 * i;
+        key[i] = 0;
+        if (e < end) {
+            if constexpr (KEYS) key[i] = a.keys[row * a.ld + e];
+            else key[i] = key_of(a.z[row * a.ld + e], e);
+        }
+        largest = key[i] > largest ? key[i] : largest;
+    }
+    buf[tid] = largest;
+    if (tid == 0) held = 0;
+    sort_down(buf, 256);
+    const uint64_t from = buf[k - 1];
+    __syncthreads();
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine += key[i] >= from && key[i] != 0;
+    int to = mine ? atomicAdd(&held, mine) : 0;           // in any order: the numbers differ and are put in order below
+    __syncthreads();
+    int n = held;
+    if (n <= kBuffer) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (key[i] >= from && key[i] != 0) buf[to++] = key[i];
+        __syncthreads();
+        sort_down(buf, n);
+    } else {
+        uint64_t least = 0;
+        n = 0;
+        __syncthreads();
+        if (tid == 0) held = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (key[i] > least) buf[atomicAdd(&held, 1)] = key[i];
+            __syncthreads();
+            n = held;
+            if (n + 256 > kBuffer || i + 1 == N) {
+                sort_down(buf, n);
+                n = n < k ? n : k;
+                if (n == k) least = buf[k - 1];
+                __syncthreads();
+                if (tid == 0) held = n;
+            }
+            __syncthreads();
+        }
+    }
+    for (int i = tid; i < a.k; i += 256) {
+        const uint64_t b = i < n ? buf[i] : 0;
+        if (a.best) a.best[((int64_t)row * a.parts + part) * a.k + i] = b;
+        if (a.ids) {
+            a.ids[row * a.ld_ids + i] = (int32_t)~(uint32_t)b;
+            a.values[row * a.ld_values + i] = logit_of(b);
+        }
+    }
+    if (a.floor && tid == 0) a.floor[row] = logit_of(buf[a.k - 1]);
 }
 
-// lse of every row: its tiles' statistics joined as for the losses
+// ---- logits of up to R rows by the vector units
+
+struct VectorArgs {
+    const void *X, *W, *bias;
+    int64_t ldx, ldw, ldz, most;
+    int32_t n, F, C;
+    float* z;                     // [n][ldz]
+    Parts parts;                  // `most` NULL: not asked for
+};
+
+// A workgroup 256 classes, four a lane; its eight wavefronts take every eighth row of W, sixteen rows of it under way at a time, and their sums
+// are added up through LDS. Rows of W need no alignment beyond their elements'.
+template <bool BF, int R>
+__global__ __launch_bounds__(512) void classes_vector_kernel(VectorArgs a) {
+    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    typedef float f32x4_here __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr int kChunk = 512, U = 16;
+    __shared__ __attribute__((aligned(16))) float xs[kChunk * R];
+    __shared__ __attribute__((aligned(16))) float sums[2][8][256];
+    __shared__ float stats[2][2][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c0 = blockIdx.x * 256 + 4 * lane, at = c0 + 4 <= a.C ? c0 : (a.C >= 4 ? a.C - 4 : 0);    // the last whole four where these are not
+    float acc[R][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
+    struct Four { float v[4]; };
+    auto load = [&](int f) {
+        Four w;
+        if (a.C < 4) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t i = (int64_t)f * a.ldw + (e < a.C ? e : 0);
+                w.v[e] = BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.W)[i] << 16) : static_cast<const float*>(a.W)[i];
+            }
+        } else if constexpr (BF) {
+            const u32x2_any v = *reinterpret_cast<const u32x2_any*>(static_cast<const uint16_t*>(a.W) + (int64_t)f * a.ldw + at);
+            w = Four{bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1])};
+        } else {
+            const f32x4_here v = *reinterpret_cast<const f32x4_here*>(static_cast<const float*>(a.W) + (int64_t)f * a.ldw + at);
+            w = Four{v[0], v[1], v[2], v[3]};
+        }
+        return w;
+    };
+    auto use = [&](const Four& w, int i) {                // i: of the row of W in the chunk
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float x = xs[i * R + r];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(x, w.v[e], acc[r][e]);
+        }
+    };
+    for (int f0 = 0; f0 < a.F; f0 += kChunk) {
+        const int fs = a.F - f0 < kChunk ? a.F - f0 : kChunk;
+        __syncthreads();
+        for (int i = tid; i < fs * R; i += 512) {
+            const int r = i / fs, f = i % fs;
+            float x = 0.f;
+            if (r < a.n) {
+                const int64_t j = r * a.ldx + f0 + f;
+                x = BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.X)[j] << 16) : static_cast<const float*>(a.X)[j];
+            }
+            xs[f * R + r] = x;
+        }
+        __syncthreads();
+        int f = wave;
+        for (; f + 8 * (U - 1) < fs; f += 8 * U) {
+            Four w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) w[u] = load(f0 + f + 8 * u);
+#pragma unroll
+            for (int u = 0; u < U; ++u) use(w[u], f + 8 * u);
+        }
+        for (; f < fs; f += 8) use(load(f0 + f), f);
+    }
+#pragma unroll
+    for (int r0 = 0; r0 < R; r0 += 2) {                   // two rows at a time: 256 threads each
+        if (r0 >= a.n) break;
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (r0 + h < R) {
+                if (at == c0) *reinterpret_cast<f32x4*>(&sums[h][wave][4 * lane]) = f32x4{acc[(r0 + h) % R][0], acc[(r0 + h) % R][1], acc[(r0 + h) % R][2], acc[(r0 + h) % R][3]};
+                else
+                    for (int e = 0; e < 4; ++e)
+                        if (at + e >= c0 && at + e < a.C) sums[h][wave][at + e - blockIdx.x * 256] = acc[(r0 + h) % R][e];
+            }
+        __syncthreads();
+        const int h = tid >> 8, t = tid & 255, r = r0 + h, c = blockIdx.x * 256 + t;
+        const bool on = r < a.n && r < R && c < a.C;
+        float z = -INFINITY;
+        if (on) {
+            z = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) z += sums[h][w][t];
+            if (a.bias) z += BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.bias)[c] << 16) : static_cast<const float*>(a.bias)[c];
+            a.z[r * a.ldz + c] = z;
+        }
+        if (a.parts.most) {
+            float most = z;
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+            if (lane == 0) stats[0][h][wave & 3] = most;
+            __syncthreads();
+            most = fmaxf(fmaxf(stats[0][h][0], stats[0][h][1]), fmaxf(stats[0][h][2], stats[0][h][3]));
+            most = fmaxf(most * kLog2e, kLeastExponent);
+            float sum = exp2_of(fmaf(z, kLog2e, -most));
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+            if (lane == 0) stats[1][h][wave & 3] = sum;
+            __syncthreads();
+            if (t == 0 && r < a.n && r < R) {
+                a.parts.most[blockIdx.x * a.most + r] = most;
+                a.parts.sum[blockIdx.x * a.most + r] = stats[1][h][0] + stats[1][h][1] + stats[1][h][2] + stats[1][h][3];
+            }
+        }
+    }
+}
+
+template <bool BF>
+gas_status launch_vector(const VectorArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)((a.C + 255) / 256)), block(512);
+    if (a.n == 1) hipLaunchKernelGGL((classes_vector_kernel<BF, 1>), grid, block, 0, s, a);
+    else if (a.n == 2) hipLaunchKernelGGL((classes_vector_kernel<BF, 2>), grid, block, 0, s, a);
+    else if (a.n <= 4) hipLaunchKernelGGL((classes_vector_kernel<BF, 4>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((classes_vector_kernel<BF, 8>), grid, block, 0, s, a);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
+// ---- lse of every row: its tiles' statistics joined, by 256 / ROWS threads a row, in a fixed tree
+template <int ROWS>
 __global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t most_rows, int64_t n, int tiles, float* lse) {
-    __shared__ float red[2][16][17];
-    const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t r = (int64_t)blockIdx.x * 16 + row;
+    constexpr int PARTS = 256 / ROWS;
+    __shared__ float red[2][PARTS][ROWS];
+    const int row = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
+    const int64_t r = (int64_t)blockIdx.x * ROWS + row;
     float most = kLeastExponent, sum = 0.f, none = 0.f;
     if (r < n)
-        for (int t = part; t < tiles; t += 16) join(most, sum, none, parts.most[t * most_rows + r], parts.sum[t * most_rows + r], 0.f, 1.f);
-    red[0][part][row] = most;
-    red[1][part][row] = sum;
-    __syncthreads();
-    if (part > 0 || r >= n) return;
-    for (int p = 1; p < 16; ++p) join(most, sum, none, red[0][p][row], red[1][p][row], 0.f, 1.f);
-    lse[r] = log_of(most, sum, 1.f);
+        for (int t = part; t < tiles; t += PARTS) join(most, sum, none, parts.most[t * most_rows + r], parts.sum[t * most_rows + r], 0.f, 1.f);
+    for (int half = PARTS / 2; half > 0; half /= 2) {
+        red[0][part][row] = most;
+        red[1][part][row] = sum;
+        __syncthreads();
+        if (part < half) join(most, sum, none, red[0][part + half][row], red[1][part + half][row], 0.f, 1.f);
+        __syncthreads();
+    }
+    if (part == 0 && r < n) lse[r] = log_of(most, sum, 1.f);
 }
 
-inline int64_t top_width(int64_t most, int C) {
+inline int64_t top_width(int64_t n, int C) {
     const int64_t cp = round_up(C, 256);
-    int64_t w = kTopElements / most / 256 * 256;
+    if (n <= kFewRows) return cp;
+    int64_t w = kTopElements / n / 256 * 256;
     if (w < kFirstPiece) w = kFirstPiece;
     return w < cp ? w : cp;
 }
+inline int parts_of(int64_t n) { return (int)((n + kPick - 1) / kPick); }
 
 struct TopRoom {
     Common common;
     Parts parts;
     float *floor, *z;
     uint32_t* mask;
-    uint64_t* best;
+    uint64_t *best, *other;
     int64_t width;
 };
 TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, const void* W, int64_t ldw, int C, const void* bias, gas_dtype dt,
                     int k) {
     TopRoom t = {};
-    t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
+    if (n > kRowsByVector) t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
+    else t.common.layer.most = kRowsByVector;
     const int64_t most = t.common.layer.most, tiles = (C + kTileC - 1) / kTileC;
-    t.width = top_width(most, C);
+    t.width = top_width(n, C);
     t.parts.most = room.take<float>(tiles * most);
     t.parts.sum = room.take<float>(tiles * most);
-    t.floor = room.take<float>(most);
-    t.best = room.take<uint64_t>(most * k);
+    t.floor = room.take<float>(n);
+    const int64_t lists = n <= kFewRows ? parts_of(C) : 1;
+    t.best = room.take<uint64_t>(n * lists * k);
+    t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
     t.mask = room.take<uint32_t>(n * (t.width / 32));
     return t;
@@ -236,34 +461,82 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     hipStream_t s = (hipStream_t)stream;
     Room room{static_cast<char*>(workspace)};
     const TopRoom t = lay_out_top(room, X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, k);
-    st = run_pack(t.common, dt, s);
-    if (st != GAS_OK) return st;
-    hipLaunchKernelGGL(classes_floor_kernel, dim3((unsigned)((n_rows + 255) / 256)), dim3(256), 0, s, t.floor, n_rows);
-    GAS_CHECK_HIP(hipGetLastError());
-    LogitsArgs a = {};
-    a.layer = t.common.layer;
-    if (lse) a.parts = t.parts;
-    a.inv_t = 1.f;
-    a.biased = bias != nullptr;
-    a.tiles = (n_classes + kTileC - 1) / kTileC;
-    a.floor = t.floor;
-    a.z = t.z;
-    a.mask = t.mask;
     const int64_t cp = round_up(n_classes, 256);
-    for (int64_t first = 0, width; first < cp; first += width) {
-        width = first == 0 ? kFirstPiece : 2 * a.width;
-        if (width > t.width) width = t.width;
-        if (first + width > cp) width = cp - first;
-        a.first = (int32_t)first;
-        a.width = (int32_t)width;
-        st = launch_logits<LOGITS_TOP, 1>(a, n_rows, (n_rows + rows_of_tile(n_rows) - 1) / rows_of_tile(n_rows) * (width / 256), s);
+    const int tiles = (int)(cp / kTileC);
+    PickArgs pick = {t.z, nullptr, t.width, n_classes, n_classes, 1, k, t.best, nullptr, nullptr, nullptr, ld_ids, ld_values};
+    if (n_rows <= kRowsByVector) {
+        VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.most, (int32_t)n_rows, F, n_classes, t.z, {}};
+        if (lse) v.parts = t.parts;
+        st = dt == GAS_BF16 ? launch_vector<true>(v, s) : launch_vector<false>(v, s);
         if (st != GAS_OK) return st;
-        const SelectArgs sel = {t.z, t.mask, t.best, t.floor, a.first, a.width, k, first + width >= cp, ids, values, ld_ids, ld_values};
-        hipLaunchKernelGGL(classes_select_kernel, dim3((unsigned)n_rows), dim3(256), 0, s, sel);
-        GAS_CHECK_HIP(hipGetLastError());
+    } else {
+        st = run_pack(t.common, dt, s);
+        if (st != GAS_OK) return st;
+        LogitsArgs a = {};
+        a.layer = t.common.layer;
+        if (lse) a.parts = t.parts;
+        a.inv_t = 1.f;
+        a.biased = bias != nullptr;
+        a.tiles = tiles;
+        a.floor = t.floor;
+        a.z = t.z;
+        a.mask = t.mask;
+        const int64_t row_tiles = (n_rows + rows_of_tile(n_rows) - 1) / rows_of_tile(n_rows);
+        for (int64_t first = 0, width; first < cp; first += width) {
+            width = n_rows <= kFewRows ? cp : first == 0 ? kFirstPiece : kGrowth * first;
+            if (width > t.width) width = t.width;
+            if (first + width > cp) width = cp - first;
+            a.first = (int32_t)first;
+            a.width = (int32_t)width;
+            a.all = first == 0;
+            st = launch_logits<LOGITS_TOP, 1>(a, n_rows, row_tiles * (width / 256), s);
+            if (st != GAS_OK) return st;
+            if (n_rows <= kFewRows) break;
+            const bool last = first + width >= cp;
+            if (first == 0) {
+                pick.ld = width;
+                pick.n = pick.per = (int32_t)(width < n_classes ? width : n_classes);
+                pick.floor = t.floor;
+                pick.ids = last ? ids : nullptr;
+                pick.values = values;
+                hipLaunchKernelGGL(classes_pick_kernel<false>, dim3((unsigned)n_rows), dim3(256), 0, s, pick);
+            } else {
+                const SelectArgs sel = {t.z, t.mask, t.best, t.floor, a.first, a.width, k, last, ids, values, ld_ids, ld_values};
+                hipLaunchKernelGGL(classes_select_kernel, dim3((unsigned)n_rows), dim3(256), 0, s, sel);
+            }
+            GAS_CHECK_HIP(hipGetLastError());
+        }
+    }
+    if (n_rows <= kFewRows) {                             // parts of 8,192, and what is left of them, until one is left
+        int64_t n = n_classes;
+        uint64_t *from = t.best, *to = t.best;
+        for (bool keys = false;; keys = true) {
+            pick.parts = parts_of(n);
+            pick.per = (int32_t)round_up((n + pick.parts - 1) / pick.parts, 256);
+            pick.parts = (int)((n + pick.per - 1) / pick.per);
+            pick.n = (int32_t)n;
+            pick.keys = from;
+            if (keys) pick.ld = n;
+            pick.best = to;
+            if (pick.parts == 1) {
+                pick.best = nullptr;
+                pick.ids = ids;
+                pick.values = values;
+            }
+            const dim3 grid((unsigned)(n_rows * pick.parts));
+            if (keys) hipLaunchKernelGGL(classes_pick_kernel<true>, grid, dim3(256), 0, s, pick);
+            else hipLaunchKernelGGL(classes_pick_kernel<false>, grid, dim3(256), 0, s, pick);
+            GAS_CHECK_HIP(hipGetLastError());
+            if (pick.parts == 1) break;
+            n = (int64_t)pick.parts * k;
+            from = to;
+            to = to == t.best ? t.other : t.best;
+        }
     }
     if (lse) {
-        hipLaunchKernelGGL(classes_lse_kernel, dim3((unsigned)((n_rows + 15) / 16)), dim3(256), 0, s, t.parts, t.common.layer.most, n_rows, a.tiles, lse);
+        const int64_t most = t.common.layer.most;
+        if (n_rows <= 1024) hipLaunchKernelGGL(classes_lse_kernel<1>, dim3((unsigned)n_rows), dim3(256), 0, s, t.parts, most, n_rows, tiles, lse);
+        else hipLaunchKernelGGL(classes_lse_kernel<16>, dim3((unsigned)((n_rows + 15) / 16)), dim3(256), 0, s, t.parts, most, n_rows, tiles, lse);
         GAS_CHECK_HIP(hipGetLastError());
     }
     return GAS_OK;
