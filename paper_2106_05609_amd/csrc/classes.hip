@@ -13,45 +13,11 @@
 namespace gas {
 namespace {
 
-// ---- rows that count, numbered in order
-
-// Rows that count in every 256; one workgroup does it all where there are few rows.
-__global__ __launch_bounds__(256) void classes_count_kernel(Targets t, int32_t* block_counts) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const bool on = i < t.n && row_counts(t, i);
-    const int n = __syncthreads_count(on);
-    if (threadIdx.x == 0) block_counts[blockIdx.x] = n;
-}
-
-// idx[r] = the r-th row that counts, pos[i] = its number or -1, count
-__global__ __launch_bounds__(256) void classes_number_kernel(Targets t, const int32_t* block_counts, int32_t* idx, int32_t* pos, int32_t* count) {
-    __shared__ int part[4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int before = 0;
-    for (int b = tid; b < (int)blockIdx.x; b += 256) before += block_counts[b];
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
-    if (lane == 0) part[wave] = before;
-    __syncthreads();
-    before = part[0] + part[1] + part[2] + part[3];
-    __syncthreads();
-    const int64_t i = (int64_t)blockIdx.x * 256 + tid;
-    const bool on = i < t.n && row_counts(t, i);
-    const uint64_t mask = __ballot(on);
-    if (lane == 0) part[wave] = __popcll(mask);
-    __syncthreads();
-    int r = before + __popcll(mask & ((1ull << lane) - 1));
-    for (int w = 0; w < wave; ++w) r += part[w];
-    if (on) idx[r] = (int32_t)i;
-    if (i < t.n) pos[i] = on ? r : -1;
-    if (blockIdx.x + 1 == gridDim.x && tid == 0) *count = before + part[0] + part[1] + part[2] + part[3];
-}
-
 // ---- targets of the rows that count
 
 struct RowsArgs {
     Targets t;
-    const int32_t *idx, *count;
+    int32_t *idx, *pos, *count;
     const float* lse;             // backward: [n] (labels alone) or [n, 2]
     const float* row_scale;       // backward: [n] or NULL
     float label_weight, temperature;
@@ -63,13 +29,68 @@ struct RowsArgs {
     int32_t k, tiles;             // k: of a row in `entries`
 };
 
-// labels alone: a thread a row
-__global__ __launch_bounds__(256) void classes_labels_kernel(RowsArgs a) {
-    const int64_t r = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (r >= *a.count) return;
-    const int64_t i = a.idx[r];
+// ---- rows that count, numbered in order
+
+// Row i has number r: what is known of it at once. Labels alone: its label and weight.
+__device__ __forceinline__ void number(const RowsArgs& a, int64_t i, int r) {
+    a.pos[i] = r;
+    if (r < 0) return;
+    a.idx[r] = (int32_t)i;
+    if (!a.labels) return;
     a.labels[r] = a.t.labels[i];
-    if (a.lse) a.info[r] = f32x4{a.lse[i], 0.f, a.row_scale ? a.row_scale[i] : 1.f, 0.f};
+    a.info[r] = f32x4{a.lse ? a.lse[i] : 0.f, 0.f, a.row_scale ? a.row_scale[i] : 1.f, 0.f};
+}
+
+// Where there are few rows one workgroup does it all.
+constexpr int kFewToNumber = 4096;
+__global__ __launch_bounds__(1024) void classes_number_few_kernel(RowsArgs a) {
+    __shared__ int part[2][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    for (int64_t i0 = 0, half = 0; i0 < a.t.n; i0 += 1024, half ^= 1) {
+        const int64_t i = i0 + tid;
+        const bool on = i < a.t.n && row_counts(a.t, i);
+        const uint64_t mask = __ballot(on);
+        if (lane == 0) part[half][wave] = __popcll(mask);
+        __syncthreads();
+        int r = before + __popcll(mask & ((1ull << lane) - 1));
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) r += part[half][w];
+            before += part[half][w];
+        }
+        if (i < a.t.n) number(a, i, on ? r : -1);
+    }
+    if (tid == 0) *a.count = before;
+}
+
+// Else: rows that count in every 256, then their numbers.
+__global__ __launch_bounds__(256) void classes_count_kernel(Targets t, int32_t* block_counts) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const bool on = i < t.n && row_counts(t, i);
+    const int n = __syncthreads_count(on);
+    if (threadIdx.x == 0) block_counts[blockIdx.x] = n;
+}
+
+__global__ __launch_bounds__(256) void classes_number_kernel(RowsArgs a, const int32_t* block_counts) {
+    __shared__ int part[4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int before = 0;
+    for (int b = tid; b < (int)blockIdx.x; b += 256) before += block_counts[b];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
+    if (lane == 0) part[wave] = before;
+    __syncthreads();
+    before = part[0] + part[1] + part[2] + part[3];
+    __syncthreads();
+    const int64_t i = (int64_t)blockIdx.x * 256 + tid;
+    const bool on = i < a.t.n && row_counts(a.t, i);
+    const uint64_t mask = __ballot(on);
+    if (lane == 0) part[wave] = __popcll(mask);
+    __syncthreads();
+    int r = before + __popcll(mask & ((1ull << lane) - 1));
+    for (int w = 0; w < wave; ++w) r += part[w];
+    if (i < a.t.n) number(a, i, on ? r : -1);
+    if (blockIdx.x + 1 == gridDim.x && tid == 0) *a.count = before + part[0] + part[1] + part[2] + part[3];
 }
 
 // A wavefront a row: the teacher's distribution over the entries that are there, the label among them, put in the order of their
@@ -263,12 +284,12 @@ struct GradArgs {
     int32_t gw_bf16;
 };
 
-// Parts of a sum, so that its tiles fill the card: as few as leave the compute units with something to do, at least eight steps each.
-constexpr int kFill = 512, kMostSplits = 16;
+// Parts of a sum, so that its tiles fill the card: two for every compute unit, of at least two steps.
+constexpr int kFill = 512, kMostSplits = 32;
 __device__ __host__ __forceinline__ int splits_of(int64_t tiles, int steps) {
     int64_t s = kFill / (tiles > 0 ? tiles : 1);
     if (s > kMostSplits) s = kMostSplits;
-    if (s > steps / 8) s = steps / 8;
+    if (s > steps / 2) s = steps / 2;
     return s < 1 ? 1 : (int)s;
 }
 
@@ -466,7 +487,8 @@ inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bo
     const int64_t most = common.layer.most;
     r.t = c.t;
     r.idx = common.idx;
-    r.count = common.layer.count;
+    r.pos = common.pos;
+    r.count = const_cast<int32_t*>(common.layer.count);
     r.label_weight = c.label_weight;
     r.temperature = c.temperature;
     r.tiles = (int32_t)((c.C + kTileC - 1) / kTileC);
@@ -484,13 +506,17 @@ inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bo
 
 inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& r, bool distill) {
     const unsigned blocks = (unsigned)((c.n + 255) / 256);
-    hipLaunchKernelGGL(classes_count_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts);
-    hipLaunchKernelGGL(classes_number_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts, common.idx, common.pos,
-                       const_cast<int32_t*>(common.layer.count));
+    if (c.n <= kFewToNumber) {
+        hipLaunchKernelGGL(classes_number_few_kernel, dim3(1), dim3(1024), 0, c.s, r);
+    } else {
+        hipLaunchKernelGGL(classes_count_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts);
+        hipLaunchKernelGGL(classes_number_kernel, dim3(blocks), dim3(256), 0, c.s, r, common.block_counts);
+    }
     GAS_CHECK_HIP(hipGetLastError());
-    if (distill) hipLaunchKernelGGL(classes_entries_kernel, dim3((unsigned)c.n), dim3(64), 0, c.s, r);
-    else hipLaunchKernelGGL(classes_labels_kernel, dim3(blocks), dim3(256), 0, c.s, r);
-    GAS_CHECK_HIP(hipGetLastError());
+    if (distill) {
+        hipLaunchKernelGGL(classes_entries_kernel, dim3((unsigned)c.n), dim3(64), 0, c.s, r);
+        GAS_CHECK_HIP(hipGetLastError());
+    }
     return run_pack(common, c.dt, c.s);
 }
 
@@ -516,6 +542,7 @@ inline LogitsArgs logits_args(const Call& c, const Common& common, const RowsArg
     a.inv_t = 1.f / c.temperature;
     a.info = r.info;
     a.biased = c.bias != nullptr;
+    a.square = c.temperature == 2.f;
     a.first = 0;
     a.width = r.tiles * kTileC;
     return a;
@@ -543,8 +570,9 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.parts = parts;
     const bool two = distill && c.temperature != 1.f;
-    const int64_t tiles = (c.n + rows_of_tile(c.n) - 1) / rows_of_tile(c.n) * rows.tiles;
-    GAS_TRY((two ? launch_logits<LOGITS_STATS, 3>(a, c.n, tiles, c.s) : launch_logits<LOGITS_STATS, 1>(a, c.n, tiles, c.s)));
+    const int tile = rows_of_tile(c.n, c.C);
+    const int64_t tiles = (c.n + tile - 1) / tile * rows.tiles;
+    GAS_TRY((two ? launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s) : launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s)));
     const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
                         c.temperature, loss, lse};
     hipLaunchKernelGGL(classes_loss_kernel, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
@@ -584,7 +612,7 @@ struct BackwardRoom {
     float *gx, *gw, *gbias;
     int64_t cap;
 };
-inline BackwardRoom lay_out_backward(Room& room, const Common& common, bool gx, bool gw, bool gbias) {
+inline BackwardRoom lay_out_backward(Room& room, const Common& common, int64_t n, bool gx, bool gw, bool gbias) {
     BackwardRoom b = {};
     const Layer& l = common.layer;
     const int64_t most = l.most;
@@ -594,7 +622,7 @@ inline BackwardRoom lay_out_backward(Room& room, const Common& common, bool gx, 
     const int64_t parts = (int64_t)kFill * 256 * 256, whole_x = most * l.fp;
     b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
     b.gw = gw ? room.take<float>(parts) : nullptr;
-    b.gbias = gbias ? room.take<float>(most / kRowsTile * round_up(l.C, 256)) : nullptr;
+    b.gbias = gbias ? room.take<float>((n + rows_of_tile(n, l.C) - 1) / rows_of_tile(n, l.C) * round_up(l.C, 256)) : nullptr;
     return b;
 }
 
@@ -620,10 +648,10 @@ gas_status launch_gw(const GradArgs& a, int64_t cols, int64_t fp, hipStream_t s)
 }
 
 template <int TEMPS>
-gas_status launch_grad_of(const LogitsArgs& a, int64_t n, int64_t tiles, gas_dtype dt, hipStream_t s) {
+gas_status launch_grad_of(const LogitsArgs& a, int n, int64_t tiles, gas_dtype dt, hipStream_t s) {
     return dt == GAS_F32 ? launch_logits<LOGITS_GRAD, TEMPS, true>(a, n, tiles, s) : launch_logits<LOGITS_GRAD, TEMPS, false>(a, n, tiles, s);
 }
-gas_status launch_grad(const LogitsArgs& a, int64_t n, int64_t tiles, int temps, gas_dtype dt, hipStream_t s) {
+gas_status launch_grad(const LogitsArgs& a, int n, int64_t tiles, int temps, gas_dtype dt, hipStream_t s) {
     return temps == 1 ? launch_grad_of<1>(a, n, tiles, dt, s) : temps == 2 ? launch_grad_of<2>(a, n, tiles, dt, s) : launch_grad_of<3>(a, n, tiles, dt, s);
 }
 
@@ -631,7 +659,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     Room room{static_cast<char*>(c.workspace)};
     const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
     RowsArgs rows = lay_out_rows(room, c, common, distill);
-    const BackwardRoom b = lay_out_backward(room, common, g.gx, g.gw, g.gbias);
+    const BackwardRoom b = lay_out_backward(room, common, c.n, g.gx, g.gw, g.gbias);
     rows.lse = g.lse;
     rows.row_scale = g.row_scale;
     GAS_TRY(run_rows(c, common, rows, distill));
@@ -645,14 +673,15 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     const int fx = width_of_tile(l.fp), rx = 256, fw = fx;
     const int64_t nfx = (l.fp + fx - 1) / fx, nfw = (l.fp + fw - 1) / fw;
     // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
+    const int tile = rows_of_tile(c.n, c.C);
     const int least = piece_width(b.cap, l.most, l.C);
     const int pieces = (c.C + least - 1) / least;
     for (int p = 0; p < pieces; ++p) {
         // the widest that piece p can be, and the most tiles that it can have: width * rows <= cap, or 256 classes
         a.piece = d.piece = p;
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
-        const int64_t tile = rows_of_tile(c.n), all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
-        GAS_TRY(launch_grad(a, c.n, all < fit ? all : fit, !distill ? 1 : (c.t.labels ? 3 : 2), c.dt, c.s));
+        const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
+        GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : (c.t.labels ? 3 : 2), c.dt, c.s));
         if (g.gx) {
             d.part = b.gx;
             GAS_TRY((fx == 64 ? launch_gx<Gx64>(d, rows_most, l.fp, c.s) : fx == 128 ? launch_gx<Gx128>(d, rows_most, l.fp, c.s) : launch_gx<Gx256>(d, rows_most, l.fp, c.s)));
@@ -672,7 +701,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         GAS_CHECK_HIP(hipGetLastError());
     }
     if (g.gbias) {
-        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, rows_of_tile(c.n), c.C,
+        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, tile, c.C,
                            g.scale, g.gbias);
         GAS_CHECK_HIP(hipGetLastError());
     }
@@ -702,7 +731,7 @@ int64_t workspace_of(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k, b
     c.n = n; c.C = C; c.t.k = k;
     const Common common = lay_out(room, nullptr, F, n, F, reinterpret_cast<const void*>(2), C, C, nullptr, dt, true);
     lay_out_rows(room, c, common, k > 0);
-    if (bwd) lay_out_backward(room, common, true, true, true);
+    if (bwd) lay_out_backward(room, common, n, true, true, true);
     else lay_out_parts(room, common, k > 0);
     return room.used;
 }

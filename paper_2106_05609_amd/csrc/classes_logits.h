@@ -27,9 +27,10 @@ struct LogitsArgs {
     // top
     const float* floor;           // [rows]: the value that a logit has to exceed
     float* z;                     // [rows][width of a piece]
-    uint32_t* mask;               // [rows][width / 32]: which logits do
+    uint32_t* mask;               // [rows][width / 32]: which logits do, see class_of_bit
     int32_t first, width;         // the piece's first class and its width (a multiple of 256)
     int32_t all;                  // every logit is stored, without bits
+    int32_t square;               // the temperature is 2: e^z is the square of e^(z / 2)
     int32_t biased;               // the bias is to be added in every tile, else in the last one alone, which ends beyond the classes
 };
 
@@ -44,6 +45,9 @@ __host__ __device__ constexpr int logits_tiles_lds() {                          
     constexpr int pieces = P::T / 64 * 32 * (32 * P::TA + 4) * 4;
     return pieces > P::kLdsBytes ? pieces : P::kLdsBytes;
 }
+
+// The class that bit `bit` of a mask's word stands for, from the word's first class.
+__device__ __forceinline__ int class_of_bit(int bit) { return acc_row(bit & 15, bit >> 4); }
 
 // KIND: what is made of the logits.  TEMPS: bit 0, exponentials as they are, bit 1, at the temperature.  SPLIT: the gradient goes to
 // three planes (fp32).
@@ -151,6 +155,8 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
         }
     };
     if constexpr (KIND == LOGITS_GRAD) {
+        constexpr int kOwn = 32 * TA / 64;                     // classes whose sum over the rows a lane has
+        float column[kOwn] = {};
 #pragma unroll
         for (int j = 0; j < TB; ++j) {
             const int row = wb0 + 32 * j + li;
@@ -160,30 +166,38 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
             if (m < count) info = a.info[m];
             const float least = info[0] * kLog2e, least_t = info[1] * kLog2e, log2e_t = kLog2e * a.inv_t;
             if (m < count) {
-                if (TEMPS & 1) info[2] *= exp2_of((float)((double)least - (double)info[0] * (double)kLog2e));
-                if (TEMPS & 2) info[3] *= exp2_of((float)((double)least_t - (double)info[1] * (double)kLog2e));
+                const double rest_t = (double)least_t - (double)info[1] * (double)kLog2e;
+                if (TEMPS == 3 && a.square) info[2] *= exp2_of((float)(2.0 * (double)least_t - (double)info[0] * (double)kLog2e));
+                else if (TEMPS & 1) info[2] *= exp2_of((float)((double)least - (double)info[0] * (double)kLog2e));
+                if (TEMPS & 2) info[3] *= exp2_of((float)rest_t);
             }
+            if (TEMPS == 3 && a.square) {                      // exp(z - lse) = exp(z / 2 - lse_t)^2 exp(2 lse_t - lse)
 #pragma unroll
-            for (int i = 0; i < TA; ++i)
+                for (int i = 0; i < TA; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float z = acc[i][j][r];
-                    float g = 0.f;
-                    if constexpr (TEMPS & 1) g = info[2] * exp2_of(fmaf(z, kLog2e, -least));
-                    if constexpr (TEMPS & 2) g += info[3] * exp2_of(fmaf(z, log2e_t, -least_t));
-                    acc[i][j][r] = g;
-                }
+                    for (int r = 0; r < 16; ++r) {
+                        const float e = exp2_of(fmaf(acc[i][j][r], log2e_t, -least_t));
+                        acc[i][j][r] = e * fmaf(e, info[2], info[3]);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < TA; ++i)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float z = acc[i][j][r];
+                        float g = 0.f;
+                        if constexpr (TEMPS & 1) g = info[2] * exp2_of(fmaf(z, kLog2e, -least));
+                        if constexpr (TEMPS & 2) g += info[3] * exp2_of(fmaf(z, log2e_t, -least_t));
+                        acc[i][j][r] = g;
+                    }
+            }
             show(j);
             each_entry(row, [&](float* at, float w) { *at -= w; });
             if (a.gbias)
 #pragma unroll
-                for (int i = 0; i < TA; ++i)
+                for (int r = 0; r < 32; ++r)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const f32x4 v = *reinterpret_cast<const f32x4*>(mine + li * kRow + 32 * i + 8 * q + 4 * lh);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = v[e];
-                    }
+                    for (int e = 0; e < kOwn; ++e) column[e] += mine[r * kRow + kOwn * lane + e];
             // eight classes of a row a lane, so that a row's are next to each other
             constexpr int kLanes = 32 * TA / 8, kRows = 64 / kLanes;
             uint16_t* to = a.g + (int64_t)(m0 + wb0 + 32 * j + lane / kLanes) * width + (c0 - c_first) + wa0 + 8 * (lane % kLanes);
@@ -201,19 +215,10 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
             }
         }
         if (a.gbias) {
+            float* sums = bias;                                // [WB][256], over the bias and what follows it
             __syncthreads();
-            float* sums = reinterpret_cast<float*>(smem);      // [WB][256]
 #pragma unroll
-            for (int i = 0; i < TA; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float v = acc[i][0][r];
-#pragma unroll
-                    for (int j = 1; j < TB; ++j) v += acc[i][j][r];
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o);
-                    if (li == 0) sums[(wave / WA) * kTileC + wa0 + 32 * i + acc_row(r, lh)] = v;
-                }
+            for (int e = 0; e < kOwn; ++e) sums[(wave / WA) * kTileC + wa0 + kOwn * lane + e] = column[e];
             __syncthreads();
             for (int c = tid; c < kTileC; c += T) {
                 float v = sums[c];
@@ -240,24 +245,35 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
                                 f32x4{acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                 continue;
             }
-            const float floor = on ? a.floor[m] : 0.f;
+            const float floor = on ? a.floor[m] : INFINITY;
+            uint32_t mask[TA];                                 // bit r of a lane: accumulator r; those of lanes 32 on from bit 16 on
+            uint32_t some = 0;
 #pragma unroll
             for (int i = 0; i < TA; ++i) {
                 const int c = c0 + wa0 + 32 * i;
-                uint32_t mask = 0;
+                uint32_t bits = 0;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(acc[i][j][r] <= floor)) mask |= 1u << acc_row(r, 0);
-                if (c + 32 > l.C) mask &= c >= l.C ? 0u : (0xFFFFFFFFu >> (32 - (l.C - c))) >> (4 * lh);
-                if (!on) mask = 0;
-                if (mask) {
-#pragma unroll
+                for (int r = 15; r >= 0; --r) bits = bits + bits + !(acc[i][j][r] <= floor);
+                if (c + 32 > l.C)
                     for (int r = 0; r < 16; ++r)
-                        if (mask >> acc_row(r, 0) & 1) row[32 * i + acc_row(r, 0)] = acc[i][j][r];
-                }
-                mask <<= 4 * lh;
-                mask |= (uint32_t)__shfl_xor((int)mask, 32);
-                if (on && lh == 0) a.mask[m * (width / 32) + (c - c_first) / 32] = mask;
+                        if (c + acc_row(r, lh) >= l.C) bits &= ~(1u << r);
+                if (!on) bits = 0;
+                mask[i] = bits;
+                some |= bits;
+            }
+            if (__any(some != 0)) {
+                show(j);
+#pragma unroll
+                for (int i = 0; i < TA; ++i)
+                    for (uint32_t bits = mask[i]; bits; bits &= bits - 1) {
+                        const int at = 32 * i + acc_row(__ffs((int)bits) - 1, 0);
+                        row[at] = mine[li * kRow + 4 * lh + at];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < TA; ++i) {
+                const uint32_t other = (uint32_t)__shfl_xor((int)mask[i], 32);
+                if (on && lh == 0) a.mask[m * (width / 32) + (c0 - c_first + wa0) / 32 + i] = mask[i] | other << 16;
             }
         }
         if (!a.parts.most) return;
@@ -281,14 +297,26 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
             for (int r = 0; r < 16; ++r) most[j] = fmaxf(most[j], acc[i][j][r]);
         most[j] = fmaxf(most[j], __shfl_xor(most[j], 32));
         most[j] = fmaxf(most[j] * kLog2e, kLeastExponent);
+        if (TEMPS == 3 && a.square) {
+            const float half = 0.5f * most[j];
 #pragma unroll
-        for (int i = 0; i < TA; ++i)
+            for (int i = 0; i < TA; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float d = fmaf(acc[i][j][r], kLog2e, -most[j]);
-                sum[j] += exp2_of(d);
-                if constexpr (TEMPS & 2) sum_t[j] += exp2_of(d * a.inv_t);
-            }
+                for (int r = 0; r < 16; ++r) {
+                    const float e = exp2_of(fmaf(acc[i][j][r], 0.5f * kLog2e, -half));
+                    sum_t[j] += e;
+                    sum[j] = fmaf(e, e, sum[j]);
+                }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TA; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float d = fmaf(acc[i][j][r], kLog2e, -most[j]);
+                    sum[j] += exp2_of(d);
+                    if constexpr (TEMPS & 2) sum_t[j] += exp2_of(d * a.inv_t);
+                }
+        }
         sum[j] += __shfl_xor(sum[j], 32);
         if constexpr (TEMPS & 2) sum_t[j] += __shfl_xor(sum_t[j], 32);
     }
@@ -330,6 +358,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
 template <class P>
 constexpr int logits_lds() {
     constexpr int BB = P::kRowsB, extra = kTileC * 4 + BB * 4 + BB * kHeldEntries * 8, red = kTileC / 32 / P::TA * 4 * BB * 4;
+    static_assert(BB / 32 / P::TB * kTileC * 4 <= extra, "the sums of the gradient's columns");
     return logits_tiles_lds<P>() + (extra > red ? extra : red);
 }
 
@@ -355,10 +384,11 @@ using ManyRows = TileProduct<kTileC, 128, 2, 2, true, false>;
 constexpr int kRowsTile = 256;
 using ManyRows = TileProduct<kTileC, 256, 2, 4, true, false, 64, 2>;
 #endif
-inline int rows_of_tile(int64_t n) { return n <= 64 ? 64 : kRowsTile; }
+// Rows of a tile: 64 where there are no more rows, or where tiles of 256 would leave compute units without any.
+inline int rows_of_tile(int64_t n, int C) { return n <= 64 || round_up(n, kRowsTile) / kRowsTile * (round_up(C, kTileC) / kTileC) < 256 ? 64 : kRowsTile; }
 template <int KIND, int TEMPS, bool SPLIT = false>
-gas_status launch_logits(const LogitsArgs& a, int64_t n, int64_t tiles, hipStream_t s) {
-    if (n <= 64) return launch_logits_tile<KIND, TEMPS, SPLIT, FewRows>(a, tiles, s);
+gas_status launch_logits(const LogitsArgs& a, int tile_rows, int64_t tiles, hipStream_t s) {
+    if (tile_rows == 64) return launch_logits_tile<KIND, TEMPS, SPLIT, FewRows>(a, tiles, s);
     return launch_logits_tile<KIND, TEMPS, SPLIT, ManyRows>(a, tiles, s);
 }
 

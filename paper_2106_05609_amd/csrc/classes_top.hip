@@ -91,8 +91,8 @@ __global__ __launch_bounds__(256) void classes_select_kernel(SelectArgs a) {
     auto add = [&](uint32_t word, int at) {
         uint32_t kept = 0;
         for (uint32_t w = word; w; w &= w - 1) {
-            const int bit = __ffs((int)w) - 1;
-            if (key_of(z[at * 32 + bit], a.first + at * 32 + bit) > least) kept |= 1u << bit;
+            const int bit = __ffs((int)w) - 1, c = at * 32 + class_of_bit(bit);
+            if (key_of(z[c], a.first + c) > least) kept |= 1u << bit;
         }
         const int mine = __popc(kept);
         int before = mine;
@@ -112,8 +112,8 @@ __global__ __launch_bounds__(256) void classes_select_kernel(SelectArgs a) {
         if (n + total <= kBuffer) {
             int to = n + before;
             for (uint32_t w = kept; w; w &= w - 1) {
-                const int bit = __ffs((int)w) - 1;
-                buf[to++] = key_of(z[at * 32 + bit], a.first + at * 32 + bit);
+                const int c = at * 32 + class_of_bit(__ffs((int)w) - 1);
+                buf[to++] = key_of(z[c], a.first + c);
             }
         }
         __syncthreads();
@@ -481,7 +481,6 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
         a.floor = t.floor;
         a.z = t.z;
         a.mask = t.mask;
-        const int64_t row_tiles = (n_rows + rows_of_tile(n_rows) - 1) / rows_of_tile(n_rows);
         for (int64_t first = 0, width; first < cp; first += width) {
             width = n_rows <= kFewRows ? cp : first == 0 ? kFirstPiece : kGrowth * first;
             if (width > t.width) width = t.width;
@@ -489,7 +488,8 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
             a.first = (int32_t)first;
             a.width = (int32_t)width;
             a.all = first == 0;
-            st = launch_logits<LOGITS_TOP, 1>(a, n_rows, row_tiles * (width / 256), s);
+            const int tile = rows_of_tile(n_rows, (int)width);
+            st = launch_logits<LOGITS_TOP, 1>(a, tile, (n_rows + tile - 1) / tile * (width / 256), s);
             if (st != GAS_OK) return st;
             if (n_rows <= kFewRows) break;
             const bool last = first + width >= cp;

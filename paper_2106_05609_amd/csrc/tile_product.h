@@ -113,17 +113,25 @@ struct TileProduct {
             la.bring(a, lda, left_a, next);
             lb.bring(b, ldb, left_b, next + BA * STEP);
         }
+        // fragments are read from LDS one group of products ahead of their use
+        constexpr int N = STEP / 16;
+        bf16x8 fa[2][TA], fb[2][TB];
+        auto read = [&](int kk) {
 #pragma unroll
-        for (int kk = 0; kk < STEP / 16; ++kk) {
-            bf16x8 fa[TA], fb[TB];
+            for (int j = 0; j < TB; ++j) fb[kk & 1][j] = fragment<BB, BTURNED>(now + BA * STEP, wb0 + 32 * j, kk);
 #pragma unroll
-            for (int j = 0; j < TB; ++j) fb[j] = fragment<BB, BTURNED>(now + BA * STEP, wb0 + 32 * j, kk);
+            for (int i = 0; i < TA; ++i) fa[kk & 1][i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
+        };
+        read(0);
 #pragma unroll
-            for (int i = 0; i < TA; ++i) fa[i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
+        for (int kk = 0; kk < N; ++kk) {
+            if (kk + 1 < N) read(kk + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][i], fb[kk & 1][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
