@@ -15,9 +15,15 @@ constexpr int kTileC = 256;                       // classes of a tile
 constexpr int kMaxClasses = 1 << 22;              // a tile's 256 rows of W then lie within 4 GB
 constexpr int kMaxWidth = 1 << 16;
 constexpr int kMaxEntries = 256;                  // of a teacher's row
-constexpr int kHeldEntries = 4;                   // of a row in one tile that are fetched before the products
+constexpr int kHeldEntries = 2;                   // of a row in one tile that are fetched before the products
 
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// What follows from the number of rows that count, worked out once on the device.
+struct Shape {
+    int32_t count, width;         // classes of a piece of the gradient at the logits
+    int32_t splits_x, splits_w;   // parts of the sums of GX and GW
+};
 
 // What kernels know of the layer.
 struct Layer {
@@ -25,7 +31,7 @@ struct Layer {
     const uint16_t* w;            // [planes][F][ldw], columns up to cw readable
     int64_t ldw, w_plane, x_plane;
     const float* bias;            // [C up to 256], -inf beyond C
-    const int32_t* count;         // rows that count
+    const Shape* shape;
     int32_t F, fp, C, cw, terms, most;     // fp: F up to 64; most: rows up to 256
 };
 
@@ -85,7 +91,7 @@ struct PackArgs {
     const void *X, *W, *bias;
     int64_t ldx, ldw, n;
     const int32_t* idx;           // NULL: every row counts
-    int32_t* count;               // written where every row counts
+    Shape* shape;                 // written where every row counts
     uint16_t *x, *w;              // w NULL: read where it lies
     float* biasp;
     int64_t x_plane, w_plane;
@@ -99,8 +105,8 @@ __global__ __launch_bounds__(256) void classes_pack_kernel(PackArgs a) {
     constexpr int EB = BF ? 2 : 4;
     unsigned b = blockIdx.x;
     if (b < a.x_blocks) {
-        const int64_t count = a.idx ? *a.count : a.n;
-        if (!a.idx && b == 0 && threadIdx.x == 0) *a.count = (int32_t)a.n;
+        const int64_t count = a.idx ? a.shape->count : a.n;
+        if (!a.idx && b == 0 && threadIdx.x == 0) a.shape->count = (int32_t)a.n;
         const int64_t rows = (count + 255) / 256 * 256;
         const int pieces = a.fp / 8;
         for (int64_t q = (int64_t)b * 256 + threadIdx.x; q < rows * pieces; q += (int64_t)a.x_blocks * 256) {
@@ -136,21 +142,38 @@ __global__ __launch_bounds__(256) void classes_pack_kernel(PackArgs a) {
     a.biasp[c] = v;
 }
 
-// ---- which tile a workgroup has
-// Workgroups are dealt to the eight XCDs in turn; each XCD takes a contiguous range of the tiles, and in it eight row tiles by all
-// column tiles after one another, so that what runs there at a time reads few rows and few columns.
-__device__ __forceinline__ bool tile_of(uint32_t block, uint32_t nm, uint32_t nc, int& m, int& c) {
-    const uint32_t total = nm * nc, per = (total + 7) / 8, id = (block & 7) * per + (block >> 3);
-    if ((block >> 3) >= per || id >= total) return false;
-    const uint32_t group = id / (8 * nc), in = id - group * (8 * nc), first = group * 8;
-    if (nm - first >= 8) {
-        m = (int)(first + (in & 7));
-        c = (int)(in >> 3);
-    } else {
-        const uint32_t rows = nm - first;
-        c = (int)(in / rows);
-        m = (int)(first + in - (uint32_t)c * rows);
+// ---- which tiles a workgroup has
+// Workgroups are dealt to the eight XCDs in turn; each XCD has a contiguous range of the tiles, and in it eight row tiles by all
+// column tiles after one another, so that what runs there at a time reads few rows and few columns.  A workgroup takes every so many of its XCD's
+// tiles as there are workgroups for it.
+struct Tiles {
+    uint32_t nm, nc, per, end, id, step;
+    __device__ __forceinline__ Tiles(uint32_t nm_, uint32_t nc_) : nm(nm_), nc(nc_) {
+        const uint32_t total = nm * nc;
+        per = (total + 7) / 8;
+        end = ((blockIdx.x & 7) + 1) * per;
+        id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+        step = gridDim.x >> 3;
+        if (end > total) end = total;
     }
+    __device__ __forceinline__ bool on() const { return id < end; }
+    __device__ __forceinline__ void at(int& m, int& c) const {
+        const uint32_t group = id / (8 * nc), in = id - group * (8 * nc), first = group * 8;
+        if (nm - first >= 8) {
+            m = (int)(first + (in & 7));
+            c = (int)(in >> 3);
+        } else {
+            const uint32_t rows = nm - first;
+            c = (int)(in / rows);
+            m = (int)(first + in - (uint32_t)c * rows);
+        }
+    }
+};
+// The same where every workgroup has one tile at most.
+__device__ __forceinline__ bool tile_of(uint32_t nm, uint32_t nc, int& m, int& c) {
+    const Tiles t(nm, nc);
+    if (!t.on()) return false;
+    t.at(m, c);
     return true;
 }
 
@@ -211,7 +234,7 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     const bool in_place = dt == GAS_BF16 && C % 8 == 0 && ldw % 8 == 0 && ldw <= kMaxClasses && aligned16(W);
     const int64_t cw = in_place ? C : round_up(C, 64);
     c.layer.terms = dt == GAS_F32 ? 6 : 1;
-    int32_t* count = room.take<int32_t>(1);
+    Shape* shape = room.take<Shape>(1);
     c.idx = compact ? room.take<int32_t>(most) : nullptr;
     c.pos = compact ? room.take<int32_t>(most) : nullptr;
     c.block_counts = compact ? room.take<int32_t>(most / 256) : nullptr;
@@ -224,13 +247,13 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     c.layer.w_plane = (int64_t)F * cw;
     c.layer.x_plane = most * fp;
     c.layer.bias = biasp;
-    c.layer.count = count;
+    c.layer.shape = shape;
     c.layer.F = F;
     c.layer.fp = (int32_t)fp;
     c.layer.C = C;
     c.layer.cw = (int32_t)cw;
     c.layer.most = (int32_t)most;
-    c.pack = PackArgs{X, W, bias, ldx, ldw, n, c.idx, count, x, w, biasp, c.layer.x_plane, c.layer.w_plane, F, (int32_t)fp, C, (int32_t)cw,
+    c.pack = PackArgs{X, W, bias, ldx, ldw, n, c.idx, shape, x, w, biasp, c.layer.x_plane, c.layer.w_plane, F, (int32_t)fp, C, (int32_t)cw,
                       (int32_t)cp, c.layer.terms, blocks_for(most * fp / 8, 256, 4096), in_place ? 0u : blocks_for((int64_t)F * cw / 8, 256, 8192)};
     return c;
 }

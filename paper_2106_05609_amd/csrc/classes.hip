@@ -17,7 +17,10 @@ namespace {
 
 struct RowsArgs {
     Targets t;
-    int32_t *idx, *pos, *count;
+    int32_t *idx, *pos;
+    Shape* shape;
+    int64_t cap;                  // backward: room for the gradient at a piece's logits
+    int32_t nfx, nfw, steps_of;   // tiles of inputs of GX and GW; 64 k of one part are `steps_of` steps (of fp32's six terms)
     const float* lse;             // backward: [n] (labels alone) or [n, 2]
     const float* row_scale;       // backward: [n] or NULL
     float label_weight, temperature;
@@ -41,8 +44,36 @@ __device__ __forceinline__ void number(const RowsArgs& a, int64_t i, int r) {
     a.info[r] = f32x4{a.lse ? a.lse[i] : 0.f, 0.f, a.row_scale ? a.row_scale[i] : 1.f, 0.f};
 }
 
+// Parts of a sum whose tiles do not fill the card, each of two steps at least. A part more costs its 256 KB written and read again,
+// a fifteenth of a step's time on every unit; a round of tiles on all units some four steps beside its own.
+constexpr int kUnits = 256, kMostSplits = 32;
+__device__ __host__ inline int splits_of(int tiles, int steps, int steps_of) {
+    const int candidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, kMostSplits};
+    int best = 1;
+    int64_t least = 0;
+    for (int s : candidates) {
+        if (s > 1 && (2 * s > steps || (int64_t)s * tiles > 2 * kUnits)) break;
+        const int64_t cost = 16LL * ((tiles * s + kUnits - 1) / kUnits) * ((steps + s - 1) / s * steps_of + 4) + (s > 1 ? (int64_t)s * tiles : 0);
+        if (s == 1 || cost < least) {
+            best = s;
+            least = cost;
+        }
+    }
+    return best;
+}
+__device__ __forceinline__ Shape shape_for(const RowsArgs& a, int count) {
+    Shape s = {count, 0, 1, 1};
+    if (a.cap > 0) {
+        const int rows = count > 0 ? (count + 255) / 256 * 256 : 256;
+        s.width = piece_width(a.cap, rows, a.t.C);
+        s.splits_x = splits_of(rows / 256 * a.nfx, s.width / kStepK, a.steps_of);
+        s.splits_w = splits_of(s.width / 256 * a.nfw, rows / kStepK, a.steps_of);
+    }
+    return s;
+}
+
 // Where there are few rows one workgroup does it all.
-constexpr int kFewToNumber = 4096;
+constexpr int kFewToNumber = 4096, kFewWithEntries = 1024;
 __global__ __launch_bounds__(1024) void classes_number_few_kernel(RowsArgs a) {
     __shared__ int part[2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -60,7 +91,7 @@ __global__ __launch_bounds__(1024) void classes_number_few_kernel(RowsArgs a) {
         }
         if (i < a.t.n) number(a, i, on ? r : -1);
     }
-    if (tid == 0) *a.count = before;
+    if (tid == 0) *a.shape = shape_for(a, before);
 }
 
 // Else: rows that count in every 256, then their numbers.
@@ -90,7 +121,7 @@ __global__ __launch_bounds__(256) void classes_number_kernel(RowsArgs a, const i
     int r = before + __popcll(mask & ((1ull << lane) - 1));
     for (int w = 0; w < wave; ++w) r += part[w];
     if (i < a.t.n) number(a, i, on ? r : -1);
-    if (blockIdx.x + 1 == gridDim.x && tid == 0) *a.count = before + part[0] + part[1] + part[2] + part[3];
+    if (blockIdx.x + 1 == gridDim.x && tid == 0) *a.shape = shape_for(a, before + part[0] + part[1] + part[2] + part[3]);
 }
 
 // A wavefront a row: the teacher's distribution over the entries that are there, the label among them, put in the order of their
@@ -99,7 +130,7 @@ __global__ __launch_bounds__(64) void classes_entries_kernel(RowsArgs a) {
     constexpr int N = (kMaxEntries + 1 + 63) / 64;
     __shared__ int32_t ids[kMaxEntries + 1], sorted[kMaxEntries + 1];
     const int64_t r = blockIdx.x;
-    if (r >= *a.count) return;
+    if (r >= a.shape->count) return;
     const int64_t i = a.idx[r];
     const int lane = threadIdx.x;
     const float inv_t = 1.f / a.temperature;
@@ -284,31 +315,15 @@ struct GradArgs {
     int32_t gw_bf16;
 };
 
-// Parts of a sum, so that its tiles fill the card: two for every compute unit, of at least two steps.
-constexpr int kFill = 512, kMostSplits = 32;
-__device__ __host__ __forceinline__ int splits_of(int64_t tiles, int steps) {
-    int64_t s = kFill / (tiles > 0 ? tiles : 1);
-    if (s > kMostSplits) s = kMostSplits;
-    if (s > steps / 2) s = steps / 2;
-    return s < 1 ? 1 : (int)s;
-}
-
-// what a launch finds from the number of rows
-struct Shape {
-    int rows, width, c_first, cols;          // rows up to 256; classes of this piece
-    bool on;
+// A piece of the classes.
+struct Piece {
+    int rows, width, first, cols;            // rows up to 256; the piece's first class and how many it has
+    __device__ __forceinline__ Piece(const Shape& s, int piece, int C) : rows((s.count + 255) / 256 * 256), width(s.width) {
+        const int64_t from = (int64_t)piece * s.width;
+        first = (int)from;
+        cols = from >= C ? 0 : (int)(C - from < s.width ? C - from : s.width);
+    }
 };
-__device__ __forceinline__ Shape shape_of(const GradArgs& a) {
-    Shape s;
-    s.rows = (*a.layer.count + 255) / 256 * 256;
-    s.on = s.rows > 0;
-    s.width = piece_width(a.cap, s.on ? s.rows : 256, a.layer.C);
-    const int64_t from = (int64_t)a.piece * s.width;
-    s.on = from < a.layer.C;
-    s.c_first = (int)from;
-    s.cols = (int)(a.layer.C - from < s.width ? a.layer.C - from : s.width);
-    return s;
-}
 
 // gx += G W^T over a piece of the classes: lanes end up with four neighbouring inputs of one row
 template <class P>
@@ -316,12 +331,13 @@ __global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
     constexpr int BA = P::kRowsA, BB = P::kRowsB, WA = BA / 32 / P::TA;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
-    const Shape s = shape_of(a);
-    if (!s.on || s.rows == 0) return;
+    const Shape shape = *l.shape;
+    const Piece s(shape, a.piece, l.C);
+    if (s.cols == 0 || s.rows == 0) return;
     const int nm = s.rows / BB, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
-    const int full = (s.width + kStepK - 1) / kStepK, splits = splits_of((int64_t)nm * nf, full);
+    const int full = s.width / kStepK, splits = shape.splits_x;
     int ft, at;
-    if (!tile_of(blockIdx.x, nf, nm * splits, ft, at)) return;
+    if (!tile_of(nf, nm * splits, ft, at)) return;
     const int mt = at % nm, part = at / nm;
     const int per = (full + splits - 1) / splits;
     const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
@@ -331,7 +347,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
     const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
     f32x16 acc[P::TA][P::TB];
     P product;
-    const TileOperand oa = {l.w + (int64_t)f0 * l.ldw + s.c_first, l.ldw, l.w_plane, l.F - 1 - f0, l.cw - s.c_first};
+    const TileOperand oa = {l.w + (int64_t)f0 * l.ldw + s.first, l.ldw, l.w_plane, l.F - 1 - f0, l.cw - s.first};
     const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB - 1, s.width};
     const int end = (s.cols + P::kStepOf - 1) / P::kStepOf, from = first * (kStepK / P::kStepOf), to = last * (kStepK / P::kStepOf);
     product.run(oa, ob, from < end ? from : end, to < end ? to : end, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
@@ -374,12 +390,13 @@ __global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
     constexpr int BB = P::kRowsB, WA = P::kRowsA / 32 / P::TA;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
-    const Shape s = shape_of(a);
-    if (!s.on) return;
-    const int nc = (s.cols + 255) / 256, nf = (l.fp + BB - 1) / BB, steps = (*l.count + kStepK - 1) / kStepK;
-    const int splits = splits_of((int64_t)((s.width + 255) / 256) * nf, steps);
+    const Shape shape = *l.shape;
+    const Piece s(shape, a.piece, l.C);
+    if (s.cols == 0) return;
+    const int nc = (s.cols + 255) / 256, nf = (l.fp + BB - 1) / BB, steps = (shape.count + kStepK - 1) / kStepK;
+    const int splits = shape.splits_w;
     int ft, at;
-    if (!tile_of(blockIdx.x, nf, nc * splits, ft, at)) return;
+    if (!tile_of(nf, nc * splits, ft, at)) return;
     const int ct = at % nc, part = at / nc;
     const int per = (steps + splits - 1) / splits;
     const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
@@ -407,19 +424,19 @@ __global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
                     if (c < s.width) *reinterpret_cast<f32x4*>(a.part + ((int64_t)part * l.F + f) * s.width + c) = v;
                 } else if (c < s.cols) {
                     v *= a.scale;
-                    put4(a.gw, (int64_t)f * a.ldgw + s.c_first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+                    put4(a.gw, (int64_t)f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
                 }
             }
     }
 }
 
 // gw of a piece whose sum over the rows came in parts
-__global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a, int nf) {
+__global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a) {
     const Layer& l = a.layer;
-    const Shape s = shape_of(a);
-    if (!s.on) return;
-    const int splits = splits_of((int64_t)((s.width + 255) / 256) * nf, (*l.count + kStepK - 1) / kStepK);
-    if (splits == 1) return;
+    const Shape shape = *l.shape;
+    const Piece s(shape, a.piece, l.C);
+    const int splits = shape.splits_w;
+    if (splits == 1 || s.cols == 0) return;
     const int fours_ = (s.cols + 3) / 4;
     const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)l.F * fours_; q += (int64_t)gridDim.x * 256) {
@@ -428,15 +445,16 @@ __global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a, int nf)
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part + (p * l.F + f) * s.width + c);
         v *= a.scale;
-        put4(a.gw, f * a.ldgw + s.c_first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+        put4(a.gw, f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
     }
 }
 
 // gx of every row: the parts added up, zero for rows that don't count
-__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, int tile_rows, int nf, void* gx, int64_t ldgx, int bf) {
+__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, void* gx, int64_t ldgx, int bf) {
     const Layer& l = a.layer;
-    const Shape s = shape_of(a);
-    const int splits = splits_of((int64_t)(s.rows / tile_rows) * nf, (s.width + kStepK - 1) / kStepK);
+    const Shape shape = *l.shape;
+    const Piece s(shape, 0, l.C);
+    const int splits = shape.splits_x;
     const int fours_ = (l.F + 3) / 4;
     const bool whole = fours(gx, ldgx, bf);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n * fours_; q += (int64_t)gridDim.x * 256) {
@@ -452,10 +470,10 @@ __global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const i
 }
 
 // gbias: the row tiles' sums added up
-__global__ __launch_bounds__(256) void classes_gbias_kernel(const float* part, const int32_t* count, int tile_rows, int C, float scale, float* gbias) {
+__global__ __launch_bounds__(256) void classes_gbias_kernel(const float* part, const Shape* shape, int tile_rows, int C, float scale, float* gbias) {
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= C) return;
-    const int tiles = (*count + tile_rows - 1) / tile_rows;
+    const int tiles = (shape->count + tile_rows - 1) / tile_rows;
     const int64_t cp = ((int64_t)C + 255) / 256 * 256;
     float v = 0.f;
     for (int t = 0; t < tiles; ++t) v += part[t * cp + c];
@@ -488,7 +506,7 @@ inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bo
     r.t = c.t;
     r.idx = common.idx;
     r.pos = common.pos;
-    r.count = const_cast<int32_t*>(common.layer.count);
+    r.shape = const_cast<Shape*>(common.layer.shape);
     r.label_weight = c.label_weight;
     r.temperature = c.temperature;
     r.tiles = (int32_t)((c.C + kTileC - 1) / kTileC);
@@ -506,7 +524,7 @@ inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bo
 
 inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& r, bool distill) {
     const unsigned blocks = (unsigned)((c.n + 255) / 256);
-    if (c.n <= kFewToNumber) {
+    if (c.n <= (distill ? kFewWithEntries : kFewToNumber)) {
         hipLaunchKernelGGL(classes_number_few_kernel, dim3(1), dim3(1024), 0, c.s, r);
     } else {
         hipLaunchKernelGGL(classes_count_kernel, dim3(blocks), dim3(256), 0, c.s, c.t, common.block_counts);
@@ -542,7 +560,6 @@ inline LogitsArgs logits_args(const Call& c, const Common& common, const RowsArg
     a.inv_t = 1.f / c.temperature;
     a.info = r.info;
     a.biased = c.bias != nullptr;
-    a.square = c.temperature == 2.f;
     a.first = 0;
     a.width = r.tiles * kTileC;
     return a;
@@ -572,7 +589,8 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     const bool two = distill && c.temperature != 1.f;
     const int tile = rows_of_tile(c.n, c.C);
     const int64_t tiles = (c.n + tile - 1) / tile * rows.tiles;
-    GAS_TRY((two ? launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s) : launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s)));
+    GAS_TRY((!two ? launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s) : c.temperature == 2.f ? launch_logits<LOGITS_STATS, 4>(a, tile, tiles, c.s)
+                                                                         : launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s)));
     const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
                         c.temperature, loss, lse};
     hipLaunchKernelGGL(classes_loss_kernel, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
@@ -618,8 +636,8 @@ inline BackwardRoom lay_out_backward(Room& room, const Common& common, int64_t n
     const int64_t most = l.most;
     b.cap = piece_cap(most, l.C);
     b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
-    // parts of a sum are made only where there are at most kFill tiles of them
-    const int64_t parts = (int64_t)kFill * 256 * 256, whole_x = most * l.fp;
+    // parts of a sum are made only where there are at most two tiles of them for a compute unit
+    const int64_t parts = (int64_t)2 * kUnits * 256 * 256, whole_x = most * l.fp;
     b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
     b.gw = gw ? room.take<float>(parts) : nullptr;
     b.gbias = gbias ? room.take<float>((n + rows_of_tile(n, l.C) - 1) / rows_of_tile(n, l.C) * round_up(l.C, 256)) : nullptr;
@@ -637,14 +655,14 @@ gas_status launch_gx(const GradArgs& a, int64_t rows, int64_t fp, hipStream_t s)
     static const gas_status attr = lds_of(classes_gx_kernel<P>, P::kLdsBytes);
     if (attr != GAS_OK) return attr;
     const int64_t blocks = rows / P::kRowsB * ((fp + P::kRowsA - 1) / P::kRowsA);
-    return launch_product<P>(classes_gx_kernel<P>, a, blocks < kFill ? kFill : blocks, s);
+    return launch_product<P>(classes_gx_kernel<P>, a, blocks < 2 * kUnits ? 2 * kUnits : blocks, s);
 }
 template <class P>
 gas_status launch_gw(const GradArgs& a, int64_t cols, int64_t fp, hipStream_t s) {
     static const gas_status attr = lds_of(classes_gw_kernel<P>, P::kLdsBytes);
     if (attr != GAS_OK) return attr;
     const int64_t blocks = cols / P::kRowsA * ((fp + P::kRowsB - 1) / P::kRowsB);
-    return launch_product<P>(classes_gw_kernel<P>, a, blocks < kFill ? kFill : blocks, s);
+    return launch_product<P>(classes_gw_kernel<P>, a, blocks < 2 * kUnits ? 2 * kUnits : blocks, s);
 }
 
 template <int TEMPS>
@@ -652,7 +670,8 @@ gas_status launch_grad_of(const LogitsArgs& a, int n, int64_t tiles, gas_dtype d
     return dt == GAS_F32 ? launch_logits<LOGITS_GRAD, TEMPS, true>(a, n, tiles, s) : launch_logits<LOGITS_GRAD, TEMPS, false>(a, n, tiles, s);
 }
 gas_status launch_grad(const LogitsArgs& a, int n, int64_t tiles, int temps, gas_dtype dt, hipStream_t s) {
-    return temps == 1 ? launch_grad_of<1>(a, n, tiles, dt, s) : temps == 2 ? launch_grad_of<2>(a, n, tiles, dt, s) : launch_grad_of<3>(a, n, tiles, dt, s);
+    return temps == 1 ? launch_grad_of<1>(a, n, tiles, dt, s) : temps == 2 ? launch_grad_of<2>(a, n, tiles, dt, s)
+           : temps == 3 ? launch_grad_of<3>(a, n, tiles, dt, s) : launch_grad_of<4>(a, n, tiles, dt, s);
 }
 
 gas_status backward(const Call& c, bool distill, const Grads& g) {
@@ -662,6 +681,10 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     const BackwardRoom b = lay_out_backward(room, common, c.n, g.gx, g.gw, g.gbias);
     rows.lse = g.lse;
     rows.row_scale = g.row_scale;
+    rows.cap = b.cap;
+    const int fx = width_of_tile(common.layer.fp);
+    rows.nfx = rows.nfw = (common.layer.fp + fx - 1) / fx;
+    rows.steps_of = common.layer.terms;
     GAS_TRY(run_rows(c, common, rows, distill));
     const Layer& l = common.layer;
     LogitsArgs a = logits_args(c, common, rows, distill);
@@ -670,9 +693,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     a.gbias = b.gbias;
     a.cap = b.cap;
     GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, nullptr, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
-    const int fx = width_of_tile(l.fp), rx = 256, fw = fx;
-    const int64_t nfx = (l.fp + fx - 1) / fx, nfw = (l.fp + fw - 1) / fw;
-    // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
+        // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int tile = rows_of_tile(c.n, c.C);
     const int least = piece_width(b.cap, l.most, l.C);
     const int pieces = (c.C + least - 1) / least;
@@ -681,27 +702,27 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         a.piece = d.piece = p;
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
-        GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : (c.t.labels ? 3 : 2), c.dt, c.s));
+        GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
         if (g.gx) {
             d.part = b.gx;
             GAS_TRY((fx == 64 ? launch_gx<Gx64>(d, rows_most, l.fp, c.s) : fx == 128 ? launch_gx<Gx128>(d, rows_most, l.fp, c.s) : launch_gx<Gx256>(d, rows_most, l.fp, c.s)));
         }
         if (g.gw) {
             d.part = b.gw;
-            GAS_TRY((fw == 64 ? launch_gw<Gw64>(d, cols_most, l.fp, c.s) : fw == 128 ? launch_gw<Gw128>(d, cols_most, l.fp, c.s) : launch_gw<Gw256>(d, cols_most, l.fp, c.s)));
-            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d, (int)nfw);
+            GAS_TRY((fx == 64 ? launch_gw<Gw64>(d, cols_most, l.fp, c.s) : fx == 128 ? launch_gw<Gw128>(d, cols_most, l.fp, c.s) : launch_gw<Gw256>(d, cols_most, l.fp, c.s)));
+            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d);
             GAS_CHECK_HIP(hipGetLastError());
         }
     }
     if (g.gx) {
         d.part = b.gx;
         d.piece = 0;
-        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n, rx, (int)nfx,
+        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n,
                            g.gx, g.ldgx, c.dt == GAS_BF16);
         GAS_CHECK_HIP(hipGetLastError());
     }
     if (g.gbias) {
-        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.count, tile, c.C,
+        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.shape, tile, c.C,
                            g.scale, g.gbias);
         GAS_CHECK_HIP(hipGetLastError());
     }

@@ -412,7 +412,7 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     t.width = top_width(n, C);
     t.parts.most = room.take<float>(tiles * most);
     t.parts.sum = room.take<float>(tiles * most);
-    t.floor = room.take<float>(n);
+    t.floor = room.take<float>(most);
     const int64_t lists = n <= kFewRows ? parts_of(C) : 1;
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);

@@ -33,7 +33,7 @@ template <int BA, int BB, int WA, int WB, bool ATURNED, bool BTURNED, int STEP =
 struct TileProduct {
     static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB;
     static constexpr int kStage = (BA + BB) * STEP;                        // elements
-    static constexpr int kStepOf = STEP, kRowsA = BA, kRowsB = BB;
+    static constexpr int kStepOf = STEP, kRowsA = BA, kRowsB = BB, kStages = STAGES;
     static constexpr int kLdsBytes = STAGES * kStage * 2;
     static_assert((STEP == 32 || STEP == 64) && (STAGES == 2 || STAGES == 3), "");
     // where piece `piece` of row `row` lies, in pieces of 16 bytes
@@ -104,7 +104,7 @@ struct TileProduct {
     Loads<BA, ATURNED> la;
     Loads<BB, BTURNED> lb;
 
-    // One step: the next one's loads, then this one's products.  `now` and `next` are different halves of LDS, which the compiler has to
+    // One step: the next one's loads, then this one's products.  `now` and `next` are different parts of LDS, which the compiler has to
     // know (__restrict__): it would otherwise wait for the loads before every read of LDS.
     __device__ __forceinline__ void step(const uint16_t* __restrict__ now, uint16_t* __restrict__ next, bool more, const uint16_t* a,
                                          int64_t lda, int left_a, const uint16_t* b, int64_t ldb, int left_b, int wa0, int wb0,
@@ -113,25 +113,20 @@ struct TileProduct {
             la.bring(a, lda, left_a, next);
             lb.bring(b, ldb, left_b, next + BA * STEP);
         }
-        // fragments are read from LDS one group of products ahead of their use
-        constexpr int N = STEP / 16;
-        bf16x8 fa[2][TA], fb[2][TB];
-        auto read = [&](int kk) {
+        multiply(now, wa0, wb0, acc);
+    }
+    __device__ __forceinline__ void multiply(const uint16_t* now, int wa0, int wb0, f32x16 (&acc)[TA][TB]) const {
 #pragma unroll
-            for (int j = 0; j < TB; ++j) fb[kk & 1][j] = fragment<BB, BTURNED>(now + BA * STEP, wb0 + 32 * j, kk);
+        for (int kk = 0; kk < STEP / 16; ++kk) {
+            bf16x8 fa[TA], fb[TB];
 #pragma unroll
-            for (int i = 0; i < TA; ++i) fa[kk & 1][i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
-        };
-        read(0);
+            for (int j = 0; j < TB; ++j) fb[j] = fragment<BB, BTURNED>(now + BA * STEP, wb0 + 32 * j, kk);
 #pragma unroll
-        for (int kk = 0; kk < N; ++kk) {
-            if (kk + 1 < N) read(kk + 1);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int i = 0; i < TA; ++i) fa[i] = fragment<BA, ATURNED>(now, wa0 + 32 * i, kk);
 #pragma unroll
             for (int i = 0; i < TA; ++i)
 #pragma unroll
-                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[kk & 1][i], fb[kk & 1][j], acc[i][j], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
+                for (int j = 0; j < TB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
         }
     }
 
@@ -163,8 +158,8 @@ struct TileProduct {
         la.bring(w.a, a.ld, a.k - STEP * w.k, to);
         lb.bring(w.b, b.ld, b.k - STEP * w.k, to + BA * STEP);
     }
-    // The first steps' loads; other work may follow before run().
-    __device__ __forceinline__ Walk begin(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds) {
+    // Where the loads of a tile stand before its first step; the loads themselves are begun by bring() and advance().
+    __device__ __forceinline__ Walk start(const TileOperand& a, const TileOperand& b, int first, int last, int terms) {
         la.init(a);
         lb.init(b);
         Walk w;
@@ -176,6 +171,11 @@ struct TileProduct {
         w.terms = terms;
         w.n = last > first ? (last - first) * terms : 0;
         place(w, a, b);
+        return w;
+    }
+    // The first steps' loads; other work may follow before run().
+    __device__ __forceinline__ Walk begin(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds) {
+        Walk w = start(a, b, first, last, terms);
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s)
             if (s < w.n) {
@@ -184,29 +184,47 @@ struct TileProduct {
             }
         return w;
     }
-    // acc = the products.  Called by every thread; LDS is free for other use afterwards.
-    __device__ __forceinline__ void run(Walk& w, const TileOperand& a, const TileOperand& b, uint16_t* lds, int wa0, int wb0, f32x16 (&acc)[TA][TB]) {
+    static __device__ __forceinline__ void clear(f32x16 (&acc)[TA][TB]) {
 #pragma unroll
         for (int i = 0; i < TA; ++i)
 #pragma unroll
             for (int j = 0; j < TB; ++j)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-        int now = 0, next = STAGES - 1;
+    }
+    // Waits until at most N of this thread's memory operations, and none of LDS, are under way; then for everyone.
+    template <int N>
+    static __device__ __forceinline__ void meet() {
+        static_assert(N < 64, "the counter of memory operations under way");
+        __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | (N >> 4 << 14));
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    }
+    // The products of a tile's steps but for the last `keep` ones; ring: where in LDS its first step's operands are, and in the end the next
+    // one's.  AFTER: operations that every thread has begun since the loads of the first step.
+    template <int AFTER>
+    __device__ __forceinline__ void steps(Walk& w, const TileOperand& a, const TileOperand& b, int keep, int& ring, uint16_t* lds, int wa0, int wb0,
+                                          f32x16 (&acc)[TA][TB]) const {
 #pragma unroll 1
-        for (int s = 0; s < w.n; ++s) {
-            // this step's loads have arrived (those of the step after it may be under way), this thread is done with the step before ...
-            if (STAGES == 3 && s + 1 < w.n) __builtin_amdgcn_s_waitcnt(0x0070 | (kLoads & 15) | (kLoads >> 4 << 14));
-            else __builtin_amdgcn_s_waitcnt(0x0070);
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();                  // ... and so for everyone
-            asm volatile("" ::: "memory");
+        for (int s = 0; s < w.n - keep; ++s) {
+            // this step's loads have arrived (those of the step after it may be under way), everyone is done with the step before
+            if (STAGES == 3 && s + 1 < w.n) meet<kLoads>();
+            else if (AFTER > 0 && s == 0) meet<AFTER>();
+            else meet<0>();
             const bool more = s + STAGES - 1 < w.n;
-            step(lds + now * kStage, lds + next * kStage, more, w.a, a.ld, a.k - STEP * w.k, w.b, b.ld, b.k - STEP * w.k, wa0, wb0, acc);
+            int next = ring + STAGES - 1;
+            if (next >= STAGES) next -= STAGES;
+            step(lds + ring * kStage, lds + next * kStage, more, w.a, a.ld, a.k - STEP * w.k, w.b, b.ld, b.k - STEP * w.k, wa0, wb0, acc);
             if (more) advance(w, a, b);
-            now = now + 1 == STAGES ? 0 : now + 1;
-            next = next + 1 == STAGES ? 0 : next + 1;
+            ring = ring + 1 == STAGES ? 0 : ring + 1;
         }
+    }
+    // acc = the products.  Called by every thread; LDS is free for other use afterwards.
+    __device__ __forceinline__ void run(Walk& w, const TileOperand& a, const TileOperand& b, uint16_t* lds, int wa0, int wb0, f32x16 (&acc)[TA][TB]) {
+        clear(acc);
+        int ring = 0;
+        steps<0>(w, a, b, 0, ring, lds, wa0, wb0, acc);
         __syncthreads();
     }
     __device__ __forceinline__ void run(const TileOperand& a, const TileOperand& b, int first, int last, int terms, uint16_t* lds, int wa0, int wb0,
