@@ -65,34 +65,78 @@ __device__ __forceinline__ void sort_down(uint64_t* buf, int n) {
         }
 }
 
+// Of the workgroup's numbers, N a thread (0: none), all that can be among the k largest, put in order in buf; how many, or -1 if there is no
+// room for them. In each of the four wavefronts k / 4 threads have a largest number of at least `from`, so k numbers are no less.
+template <int N>
+__device__ __forceinline__ int keep_largest(const uint64_t (&key)[N], int k, uint64_t* buf, uint32_t* part, int* held) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t v = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v = max(v, (uint32_t)(key[i] >> 32));
+#pragma unroll
+    for (int span = 2; span <= 64; span *= 2)             // the lanes' in order, the largest first
+#pragma unroll
+        for (int step = span / 2; step > 0; step /= 2) {
+            const uint32_t o = (uint32_t)__shfl_xor((int)v, step);
+            v = ((lane & span) == 0) == ((lane & step) == 0) ? max(v, o) : min(v, o);
+        }
+    v = (uint32_t)__shfl((int)v, (k + 3) / 4 - 1);
+    __syncthreads();                                      // buf and part are free
+    if (lane == 0) part[wave] = v;
+    if (threadIdx.x == 0) *held = 0;
+    __syncthreads();
+    const uint32_t from = min(min(part[0], part[1]), min(part[2], part[3]));
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine += key[i] != 0 && (uint32_t)(key[i] >> 32) >= from;
+    int to = mine ? atomicAdd(held, mine) : 0;            // in any order: the numbers differ and are put in order below
+    __syncthreads();
+    const int n = *held;
+    if (n > kBuffer) return -1;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (key[i] != 0 && (uint32_t)(key[i] >> 32) >= from) buf[to++] = key[i];
+    __syncthreads();
+    sort_down(buf, n);
+    return n;
+}
+
 // A workgroup a row: its list joined with the logits that a piece left.
 __global__ __launch_bounds__(256) void classes_select_kernel(SelectArgs a) {
     __shared__ uint64_t buf[kBuffer];
-    __shared__ int part[4];
+    __shared__ int part[4], held;
     const int64_t r = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t* mask = a.mask + r * (a.width / 32);
     const float* z = a.z + r * a.width;
-    int n = 0;                                            // held in buf, the same in every thread
-    uint64_t least = 0;                                   // what a number has to exceed
-    if (a.first > 0) {
-        for (int i = tid; i < a.k; i += 256) buf[i] = a.best[r * a.k + i];
-        n = a.k;
-        least = a.best[r * a.k + a.k - 1];
-    }
+    int n = a.k;                                          // held in buf, the same in every thread
+    uint64_t least = 0;                                   // what a number has to exceed, once the buffer was full
+    bool shortened = false;
+    for (int i = tid; i < a.k; i += 256) buf[i] = a.best[r * a.k + i];
     __syncthreads();
     auto shorten = [&]() {                                // buf: the k largest, in order
-        sort_down(buf, n);
+        if (n <= 256) {
+            sort_down(buf, n);
+        } else {
+            uint64_t key[kBuffer / 256];
+#pragma unroll
+            for (int i = 0; i < kBuffer / 256; ++i) key[i] = tid + 256 * i < n ? buf[tid + 256 * i] : 0;
+            n = keep_largest(key, a.k, buf, reinterpret_cast<uint32_t*>(part), &held);
+        }
         if (n > a.k) n = a.k;
-        if (n == a.k) least = buf[a.k - 1];
+        least = buf[a.k - 1];                             // k are there: the first piece has more classes
+        shortened = true;
         __syncthreads();
     };
     // the candidates among the threads' words, if they fit; how many they are
     auto add = [&](uint32_t word, int at) {
-        uint32_t kept = 0;
-        for (uint32_t w = word; w; w &= w - 1) {
-            const int bit = __ffs((int)w) - 1, c = at * 32 + class_of_bit(bit);
-            if (key_of(z[c], a.first + c) > least) kept |= 1u << bit;
+        uint32_t kept = word;                             // all of them exceed the list they came against
+        if (shortened) {
+            kept = 0;
+            for (uint32_t w = word; w; w &= w - 1) {
+                const int bit = __ffs((int)w) - 1, c = at * 32 + class_of_bit(bit);
+                if (key_of(z[c], a.first + c) > least) kept |= 1u << bit;
+            }
         }
         const int mine = __popc(kept);
         int before = mine;
@@ -163,55 +207,37 @@ struct PickArgs {
     float* values;
     int64_t ld_ids, ld_values;
 };
-constexpr int kPick = 8192;
+constexpr int kPick = 8192, kPickFew = 2048;           // numbers of a part; few of them where that leaves units without any
 
-// A workgroup a part of a row, 32 numbers a thread. The k-th largest of the threads' largest is no more than the k-th largest of all, and
-// little less: what is not below it is put in order. Where that is too much (equal logits), numbers go in 256 at a time.
-template <bool KEYS>
+// A workgroup a part of a row, N numbers a thread. Where too many are left (equal logits), numbers go in 256 at a time.
+template <bool KEYS, int N>
 __global__ __launch_bounds__(256) void classes_pick_kernel(PickArgs a) {
     __shared__ uint64_t buf[kBuffer];
+    __shared__ uint32_t part_[4];
     __shared__ int held;
-    constexpr int N = kPick / 256;
     const int64_t row = blockIdx.x / a.parts;
     const int part = (int)(blockIdx.x % a.parts), first = part * a.per, tid = threadIdx.x;
     const int end = first + a.per < a.n ? first + a.per : a.n, there = end - first, k = a.k < there ? a.k : there;
-    uint64_t key[N], largest = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    auto number = [&](int i) {
         const int e = first + tid + 256 * i;
-        key[i] = 0;
-        if (e < end) {
-            if constexpr (KEYS) key[i] = a.keys[row * a.ld + e];
-            else key[i] = key_of(a.z[row * a.ld + e], e);
-        }
-        largest = key[i] > largest ? key[i] : largest;
-    }
-    buf[tid] = largest;
-    if (tid == 0) held = 0;
-    sort_down(buf, 256);
-    const uint64_t from = buf[k - 1];
-    __syncthreads();
-    int mine = 0;
+        if (e >= end) return (uint64_t)0;
+        if constexpr (KEYS) return a.keys[row * a.ld + e];
+        else return key_of(a.z[row * a.ld + e], e);
+    };
+    uint64_t key[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) mine += key[i] >= from && key[i] != 0;
-    int to = mine ? atomicAdd(&held, mine) : 0;           // in any order: the numbers differ and are put in order below
-    __syncthreads();
-    int n = held;
-    if (n <= kBuffer) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (key[i] >= from && key[i] != 0) buf[to++] = key[i];
-        __syncthreads();
-        sort_down(buf, n);
-    } else {
+    for (int i = 0; i < N; ++i) key[i] = number(i);
+    int n = keep_largest(key, k, buf, part_, &held);
+    if (n < 0) {
         uint64_t least = 0;
         n = 0;
         __syncthreads();
         if (tid == 0) held = 0;
         __syncthreads();
-#pragma unroll
+#pragma unroll 1
         for (int i = 0; i < N; ++i) {
-            if (key[i] > least) buf[atomicAdd(&held, 1)] = key[i];
+            const uint64_t one = number(i);
+            if (one > least) buf[atomicAdd(&held, 1)] = one;
             __syncthreads();
             n = held;
             if (n + 256 > kBuffer || i + 1 == N) {
@@ -393,7 +419,10 @@ inline int64_t top_width(int64_t n, int C) {
     if (w < kFirstPiece) w = kFirstPiece;
     return w < cp ? w : cp;
 }
-inline int parts_of(int64_t n) { return (int)((n + kPick - 1) / kPick); }
+inline int parts_of(int64_t n, int64_t rows) {
+    const int64_t most = rows * n < 128LL * kPick ? kPickFew : kPick;
+    return (int)((n + most - 1) / most);
+}
 
 struct TopRoom {
     Common common;
@@ -413,7 +442,7 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     t.parts.most = room.take<float>(tiles * most);
     t.parts.sum = room.take<float>(tiles * most);
     t.floor = room.take<float>(most);
-    const int64_t lists = n <= kFewRows ? parts_of(C) : 1;
+    const int64_t lists = n <= kFewRows ? parts_of(C, n) : 1;
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
@@ -499,7 +528,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
                 pick.floor = t.floor;
                 pick.ids = last ? ids : nullptr;
                 pick.values = values;
-                hipLaunchKernelGGL(classes_pick_kernel<false>, dim3((unsigned)n_rows), dim3(256), 0, s, pick);
+                hipLaunchKernelGGL((classes_pick_kernel<false, kFirstPiece / 256>), dim3((unsigned)n_rows), dim3(256), 0, s, pick);
             } else {
                 const SelectArgs sel = {t.z, t.mask, t.best, t.floor, a.first, a.width, k, last, ids, values, ld_ids, ld_values};
                 hipLaunchKernelGGL(classes_select_kernel, dim3((unsigned)n_rows), dim3(256), 0, s, sel);
@@ -511,7 +540,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
         int64_t n = n_classes;
         uint64_t *from = t.best, *to = t.best;
         for (bool keys = false;; keys = true) {
-            pick.parts = parts_of(n);
+            pick.parts = parts_of(n, n_rows);
             pick.per = (int32_t)round_up((n + pick.parts - 1) / pick.parts, 256);
             pick.parts = (int)((n + pick.per - 1) / pick.per);
             pick.n = (int32_t)n;
@@ -524,8 +553,11 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
                 pick.values = values;
             }
             const dim3 grid((unsigned)(n_rows * pick.parts));
-            if (keys) hipLaunchKernelGGL(classes_pick_kernel<true>, grid, dim3(256), 0, s, pick);
-            else hipLaunchKernelGGL(classes_pick_kernel<false>, grid, dim3(256), 0, s, pick);
+            const bool few = pick.per <= kPickFew;
+            if (keys && few) hipLaunchKernelGGL((classes_pick_kernel<true, kPickFew / 256>), grid, dim3(256), 0, s, pick);
+            else if (keys) hipLaunchKernelGGL((classes_pick_kernel<true, kPick / 256>), grid, dim3(256), 0, s, pick);
+            else if (few) hipLaunchKernelGGL((classes_pick_kernel<false, kPickFew / 256>), grid, dim3(256), 0, s, pick);
+            else hipLaunchKernelGGL((classes_pick_kernel<false, kPick / 256>), grid, dim3(256), 0, s, pick);
             GAS_CHECK_HIP(hipGetLastError());
             if (pick.parts == 1) break;
             n = (int64_t)pick.parts * k;

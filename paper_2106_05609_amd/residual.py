@@ -41,9 +41,9 @@ class ResidualModel:
         return [t for t in ts if t is not None]
 
 
-def residual_forward_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories, do_push=True, keep=None):
+def residual_forward_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories, do_push=True, keep=None, logits=True):
     """All layers for one mini-batch in the order of Algorithm 1: y [nb, C].  histories[l - 1]: table [N, F] of u_{l+1}, l = 1 .. L - 1.  keep: a
-    dict that receives what the backward pass reads."""
+    dict that receives what the backward pass reads.  logits=False: the rows that w_out is applied to, [nb, F], instead of y."""
     dev, dt, nb, nv, f = x_feat.device, x_feat.dtype, bg.nb, bg.nv, model.w_in.shape[1]
     new = lambda rows, cols=f: torch.empty((rows, cols), dtype=dt, device=dev)
     stats_of = lambda rows: None if keep is None else torch.empty((rows, 4), dtype=torch.float32, device=dev)
@@ -73,26 +73,35 @@ def residual_forward_batch(model: ResidualModel, bg: BatchGraph, x_feat, histori
             B.gas_push(u, ids, histories[l - 1])
         saved.append((x[:nb], z, a, t, h_next, stats))
         x, h = u, h_next
-    y = new(nb, model.w_out.shape[1])
-    B.gas_linear(x, model.w_out, y)
     if keep is not None:
         keep.update(x0=x0, h0=h0, stats0=stats0, layers=saved, u=x)
+    if not logits:
+        return x
+    y = new(nb, model.w_out.shape[1])
+    B.gas_linear(x, model.w_out, y)
     return y
 
 
-def residual_train_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories, grad_out, do_push=True):
+def residual_train_batch(model: ResidualModel, bg: BatchGraph, x_feat, histories, grad_out=None, do_push=True, head=None):
     """residual_forward_batch and its backward pass; bg needs the CSC copy.  grad_out: dLoss/dy [nb, C] or a function of y.  Returns (y, grads,
-    kept) with the gradients, float32, of model.tensors() in their order."""
+    kept) with the gradients, float32, of model.tensors() in their order.  head, instead of grad_out: a function of the rows u that w_out is applied to and w_out
+    that leaves the gradients at both in its last two arguments, gu as u and g_out float32 as w_out; y is None then."""
+    if (grad_out is None) == (head is None):
+        raise ValueError("residual_train_batch: either grad_out or head")
     kept = {}
-    y = residual_forward_batch(model, bg, x_feat, histories, do_push, kept)
+    y = residual_forward_batch(model, bg, x_feat, histories, do_push, kept, logits=head is None)
     dev, dt, nb, nv, f, L = x_feat.device, x_feat.dtype, bg.nb, bg.nv, model.w_in.shape[1], model.n_layers
     new = lambda rows: torch.empty((rows, f), dtype=dt, device=dev)
     like = lambda v: None if v is None else torch.empty_like(v)
     wg = _WeightGrads()
-    gy = grad_out(y) if callable(grad_out) else grad_out
-    g_out = wg.add(kept["u"], gy)
     gu, gh = new(nb), None
-    B.gas_linear_bwd_input(gy, model.w_out, gu)
+    if head is not None:
+        y, g_out = None, torch.empty(model.w_out.shape, dtype=torch.float32, device=dev)
+        head(kept["u"], model.w_out, gu, g_out)
+    else:
+        gy = grad_out(y) if callable(grad_out) else grad_out
+        g_out = wg.add(kept["u"], gy)
+        B.gas_linear_bwd_input(gy, model.w_out, gu)
     room = torch.empty(max(1, B.gas_residual_norm_bwd_workspace(nv, f, dt)), dtype=torch.uint8, device=dev)
     g_layers, g_pre = [None] * L, [None] * (L + 1)
     for l in range(L, 0, -1):
@@ -198,19 +207,53 @@ class AdamW:
         return out
 
 
-def residual_train_step(model: ResidualModel, bg: BatchGraph, x_feat, histories, labels_batch, optimizer: AdamW, n_labelled=None, do_push=True):
+def residual_train_step(model: ResidualModel, bg: BatchGraph, x_feat, histories, labels_batch, optimizer: AdamW, n_labelled=None, do_push=True,
+                        keep_logits=True):
     """One optimisation step on one mini-batch: forward with Push, softmax cross-entropy averaged over the labelled in-batch nodes
     (labels_batch int32 [nb], < 0 = unlabelled; n_labelled: their count if the caller knows it), backward, AdamW.  Returns (loss_sum as a 1-element device
-    tensor, n_labelled, y, grads)."""
+    tensor, n_labelled, y, grads).  keep_logits=False, for classes by the thousand: the logits are formed a piece at a time, for the labelled nodes alone, and y is
+    None."""
     if n_labelled is None:
         n_labelled = int((labels_batch >= 0).sum().item())
-    dev = x_feat.device
+    dev, scale = x_feat.device, 1.0 / max(1, n_labelled)
     loss_rows, loss_sum = torch.empty(bg.nb, dtype=torch.float32, device=dev), torch.empty(1, dtype=torch.float32, device=dev)
 
     def loss_grad(y):
         g = torch.empty_like(y)
-        B.gas_softmax_xent(y, labels_batch, g, loss_rows, loss_sum, scale=1.0 / max(1, n_labelled))
+        B.gas_softmax_xent(y, labels_batch, g, loss_rows, loss_sum, scale=scale)
         return g
-    y, grads, _ = residual_train_batch(model, bg, x_feat, histories, loss_grad, do_push)
+
+    def head(u, w, gu, gw):
+        lse = torch.empty_like(loss_rows)
+        B.gas_linear_xent(u, w, labels_batch, loss_rows, lse, loss_sum=loss_sum)
+        B.gas_linear_xent_bwd(u, w, labels_batch, lse, gx=gu, gw=gw, scale=scale)
+    y, grads, _ = residual_train_batch(model, bg, x_feat, histories, loss_grad if keep_logits else None, do_push, None if keep_logits else head)
     optimizer.step(grads)
     return loss_sum, n_labelled, y, grads
+
+
+def residual_top(model: ResidualModel, bg: BatchGraph, x_feat, histories, k, do_push=False):
+    """The k classes of the largest logits of every in-batch node: (ids int32, values, both [nb, k], and the logarithm of the sum of all exponentials [nb]).  Of
+    a teacher: what residual_distill_step reads."""
+    u = residual_forward_batch(model, bg, x_feat, histories, do_push, logits=False)
+    ids, values = torch.empty((bg.nb, k), dtype=torch.int32, device=u.device), torch.empty((bg.nb, k), dtype=torch.float32, device=u.device)
+    lse = torch.empty(bg.nb, dtype=torch.float32, device=u.device)
+    B.gas_linear_top(u, model.w_out, ids, values, lse=lse)
+    return ids, values, lse
+
+
+def residual_distill_step(model: ResidualModel, bg: BatchGraph, x_feat, histories, ids, values, optimizer: AdamW, temperature=1.0, labels_batch=None,
+                          label_weight=0.5, do_push=True):
+    """One optimisation step of a student on one mini-batch: distillation from a teacher's top logits (residual_top of the same batch), averaged over the in-batch
+    nodes, with labels beside it if they are given (weight label_weight).  Returns (loss_sum as a 1-element device tensor, grads)."""
+    dev = x_feat.device
+    loss_rows, loss_sum = torch.empty(bg.nb, dtype=torch.float32, device=dev), torch.empty(1, dtype=torch.float32, device=dev)
+    same = dict(labels=labels_batch, temperature=temperature, label_weight=label_weight)
+
+    def head(u, w, gu, gw):
+        lse = torch.empty((bg.nb, 2), dtype=torch.float32, device=dev)
+        B.gas_linear_distill(u, w, ids, values, loss_rows, lse, loss_sum=loss_sum, **same)
+        B.gas_linear_distill_bwd(u, w, ids, values, lse, gx=gu, gw=gw, scale=1.0 / max(1, bg.nb), **same)
+    _, grads, _ = residual_train_batch(model, bg, x_feat, histories, do_push=do_push, head=head)
+    optimizer.step(grads)
+    return loss_sum, grads
