@@ -148,12 +148,12 @@ __global__ __launch_bounds__(256) void classes_pack_kernel(PackArgs a) {
 // tiles as there are workgroups for it.
 struct Tiles {
     uint32_t nm, nc, per, end, id, step;
-    __device__ __forceinline__ Tiles(uint32_t nm_, uint32_t nc_) : nm(nm_), nc(nc_) {
+    __device__ __forceinline__ Tiles(uint32_t block, uint32_t blocks, uint32_t nm_, uint32_t nc_) : nm(nm_), nc(nc_) {
         const uint32_t total = nm * nc;
         per = (total + 7) / 8;
-        end = ((blockIdx.x & 7) + 1) * per;
-        id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-        step = gridDim.x >> 3;
+        end = ((block & 7) + 1) * per;
+        id = (block & 7) * per + (block >> 3);
+        step = blocks >> 3;
         if (end > total) end = total;
     }
     __device__ __forceinline__ bool on() const { return id < end; }
@@ -170,8 +170,8 @@ struct Tiles {
     }
 };
 // The same where every workgroup has one tile at most.
-__device__ __forceinline__ bool tile_of(uint32_t nm, uint32_t nc, int& m, int& c) {
-    const Tiles t(nm, nc);
+__device__ __forceinline__ bool tile_of(uint32_t block, uint32_t blocks, uint32_t nm, uint32_t nc, int& m, int& c) {
+    const Tiles t(block, blocks, nm, nc);
     if (!t.on()) return false;
     t.at(m, c);
     return true;

@@ -309,7 +309,8 @@ struct GradArgs {
     int64_t g_plane, cap;
     int32_t piece;
     float scale;
-    float* part;                  // gx: [split][rows][fp]; gw: [split][F][width]
+    float *part_x, *part_w;       // [split][rows][fp], [split][F][width]; NULL: that gradient is not asked for
+    uint32_t x_blocks;            // workgroups for gx, then those for gw
     void* gw;
     int64_t ldgw;
     int32_t gw_bf16;
@@ -327,9 +328,8 @@ struct Piece {
 
 // gx += G W^T over a piece of the classes: lanes end up with four neighbouring inputs of one row
 template <class P>
-__global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
+__device__ __forceinline__ void gx_tile(const GradArgs& a, uint32_t block, uint32_t blocks, char* smem) {
     constexpr int BA = P::kRowsA, BB = P::kRowsB, WA = BA / 32 / P::TA;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
     const Shape shape = *l.shape;
     const Piece s(shape, a.piece, l.C);
@@ -337,7 +337,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
     const int nm = s.rows / BB, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
     const int full = s.width / kStepK, splits = shape.splits_x;
     int ft, at;
-    if (!tile_of(nf, nm * splits, ft, at)) return;
+    if (!tile_of(block, blocks, nf, nm * splits, ft, at)) return;
     const int mt = at % nm, part = at / nm;
     const int per = (full + splits - 1) / splits;
     const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
@@ -351,7 +351,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_gx_kernel(GradArgs a) {
     const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB - 1, s.width};
     const int end = (s.cols + P::kStepOf - 1) / P::kStepOf, from = first * (kStepK / P::kStepOf), to = last * (kStepK / P::kStepOf);
     product.run(oa, ob, from < end ? from : end, to < end ? to : end, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
-    float* out = a.part + (int64_t)part * s.rows * l.fp;
+    float* out = a.part_x + (int64_t)part * s.rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
         float* row = out + (int64_t)(m0 + wb0 + 32 * j + li) * l.fp;
@@ -386,9 +386,8 @@ __device__ __host__ __forceinline__ bool fours(const void* p, int64_t ld, bool b
 
 // gw = X^T G of a piece of the classes, or a part of the sum over the rows: lanes end up with four neighbouring classes of one input
 template <class P>
-__global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
+__device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint32_t blocks, char* smem) {
     constexpr int BB = P::kRowsB, WA = P::kRowsA / 32 / P::TA;
-    extern __shared__ __attribute__((aligned(16))) char smem[];
     const Layer& l = a.layer;
     const Shape shape = *l.shape;
     const Piece s(shape, a.piece, l.C);
@@ -396,7 +395,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
     const int nc = (s.cols + 255) / 256, nf = (l.fp + BB - 1) / BB, steps = (shape.count + kStepK - 1) / kStepK;
     const int splits = shape.splits_w;
     int ft, at;
-    if (!tile_of(nf, nc * splits, ft, at)) return;
+    if (!tile_of(block, blocks, nf, nc * splits, ft, at)) return;
     const int ct = at % nc, part = at / nc;
     const int per = (steps + splits - 1) / splits;
     const int first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
@@ -421,13 +420,22 @@ __global__ __launch_bounds__(P::T, 2) void classes_gw_kernel(GradArgs a) {
                 const int c = c0 + wa0 + 32 * i + 8 * q + 4 * lh;
                 f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                 if (splits > 1) {
-                    if (c < s.width) *reinterpret_cast<f32x4*>(a.part + ((int64_t)part * l.F + f) * s.width + c) = v;
+                    if (c < s.width) *reinterpret_cast<f32x4*>(a.part_w + ((int64_t)part * l.F + f) * s.width + c) = v;
                 } else if (c < s.cols) {
                     v *= a.scale;
                     put4(a.gw, (int64_t)f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
                 }
             }
     }
+}
+
+// Both in one launch: neither fills the card alone where there are few tiles, and one's last tiles run beside the other's first.
+template <class PX, class PW>
+__global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) {
+    static_assert(PX::T == PW::T, "workgroups of one size");
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    if (blockIdx.x < a.x_blocks) gx_tile<PX>(a, blockIdx.x, a.x_blocks, smem);
+    else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
 // gw of a piece whose sum over the rows came in parts
@@ -443,7 +451,7 @@ __global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a) {
         const int64_t f = q / fours_;
         const int c = (int)(q % fours_) * 4;
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part + (p * l.F + f) * s.width + c);
+        for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part_w + (p * l.F + f) * s.width + c);
         v *= a.scale;
         put4(a.gw, f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
     }
@@ -463,7 +471,7 @@ __global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const i
         f32x4 v = {0.f, 0.f, 0.f, 0.f};
         const int64_t r = pos[i];
         if (r >= 0)
-            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part + (p * (int64_t)s.rows + r) * l.fp + f);
+            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part_x + (p * (int64_t)s.rows + r) * l.fp + f);
         v *= a.scale;
         put4(gx, i * ldgx + f, v, l.F - f < 4 ? l.F - f : 4, bf, whole && f + 4 <= l.F);
     }
@@ -605,14 +613,30 @@ inline int64_t piece_cap(int64_t most, int C) {
     const int64_t cap = all < kPieceElements ? all : kPieceElements;
     return cap > least ? cap : least;
 }
-// Tiles of the two products by inputs
+// Tiles of the two products by inputs: as many of them as leave few out; those of 64 and 128 take LDS more often for what they multiply.
 using Gx64 = TileProduct<64, 256, 1, 4, false, false, 64, 2>;
 using Gx128 = TileProduct<128, 256, 2, 4, false, false, 64, 2>;
+using Gx192 = TileProduct<192, 256, 2, 4, false, false, 64, 2>;
 using Gx256 = TileProduct<256, 256, 2, 4, false, false, 64, 2>;
+using Gx320 = TileProduct<320, 256, 2, 4, false, false, 64, 2>;
 using Gw64 = TileProduct<256, 64, 4, 1, true, true, 64, 2>;
 using Gw128 = TileProduct<256, 128, 4, 2, true, true, 64, 2>;
+using Gw192 = TileProduct<256, 192, 4, 2, true, true, 64, 2>;
 using Gw256 = TileProduct<256, 256, 2, 4, true, true, 64, 2>;
-inline int width_of_tile(int64_t fp) { return fp <= 64 ? 64 : (fp <= 128 || (round_up(fp, 256) != round_up(fp, 128)) ? 128 : 256); }
+using Gw320 = TileProduct<256, 320, 4, 2, true, true, 64, 2>;
+inline int width_of_tile(int64_t fp) {
+    const struct { int width, cost; } tiles[] = {{64, 16}, {128, 13}, {192, 11}, {256, 10}, {320, 10}};      // cost of an input, tenths
+    int best = 64;
+    int64_t least = 0;
+    for (const auto& t : tiles) {
+        const int64_t cost = (fp + t.width - 1) / t.width * t.width * t.cost;
+        if (t.width == 64 || cost <= least) {
+            best = t.width;
+            least = cost;
+        }
+    }
+    return best;
+}
 
 struct Grads {
     void* gx;
@@ -637,32 +661,28 @@ inline BackwardRoom lay_out_backward(Room& room, const Common& common, int64_t n
     b.cap = piece_cap(most, l.C);
     b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
     // parts of a sum are made only where there are at most two tiles of them for a compute unit
-    const int64_t parts = (int64_t)2 * kUnits * 256 * 256, whole_x = most * l.fp;
+    const int64_t parts = (int64_t)2 * kUnits * 256 * 320, whole_x = most * l.fp;
     b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
     b.gw = gw ? room.take<float>(parts) : nullptr;
     b.gbias = gbias ? room.take<float>((n + rows_of_tile(n, l.C) - 1) / rows_of_tile(n, l.C) * round_up(l.C, 256)) : nullptr;
     return b;
 }
 
-template <class P, class Kernel>
-gas_status launch_product(Kernel kernel, const GradArgs& a, int64_t blocks, hipStream_t s) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((blocks + 7) / 8 * 8)), dim3(P::T), P::kLdsBytes, s, a);
+template <class PX, class PW>
+gas_status launch_products(GradArgs a, int64_t rows, int64_t cols, hipStream_t s) {
+    constexpr int smem = PX::kLdsBytes > PW::kLdsBytes ? PX::kLdsBytes : PW::kLdsBytes;
+    static_assert(smem <= 160 * 1024, "LDS of a compute unit");
+    static const gas_status attr = lds_of(classes_products_kernel<PX, PW>, smem);
+    if (attr != GAS_OK) return attr;
+    const int64_t fp = a.layer.fp;
+    auto blocks_of = [](int64_t tiles) { return (tiles < 2 * kUnits ? 2 * kUnits : tiles + 7) / 8 * 8; };
+    const int64_t bx = a.part_x ? blocks_of(rows / PX::kRowsB * ((fp + PX::kRowsA - 1) / PX::kRowsA)) : 0;
+    const int64_t bw = a.part_w ? blocks_of(cols / PW::kRowsA * ((fp + PW::kRowsB - 1) / PW::kRowsB)) : 0;
+    GAS_REQUIRE(bx + bw <= 0x7FFFFFLL, "too many tiles for one launch");
+    a.x_blocks = (uint32_t)bx;
+    hipLaunchKernelGGL((classes_products_kernel<PX, PW>), dim3((unsigned)(bx + bw)), dim3(PX::T), smem, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;
-}
-template <class P>
-gas_status launch_gx(const GradArgs& a, int64_t rows, int64_t fp, hipStream_t s) {
-    static const gas_status attr = lds_of(classes_gx_kernel<P>, P::kLdsBytes);
-    if (attr != GAS_OK) return attr;
-    const int64_t blocks = rows / P::kRowsB * ((fp + P::kRowsA - 1) / P::kRowsA);
-    return launch_product<P>(classes_gx_kernel<P>, a, blocks < 2 * kUnits ? 2 * kUnits : blocks, s);
-}
-template <class P>
-gas_status launch_gw(const GradArgs& a, int64_t cols, int64_t fp, hipStream_t s) {
-    static const gas_status attr = lds_of(classes_gw_kernel<P>, P::kLdsBytes);
-    if (attr != GAS_OK) return attr;
-    const int64_t blocks = cols / P::kRowsA * ((fp + P::kRowsB - 1) / P::kRowsB);
-    return launch_product<P>(classes_gw_kernel<P>, a, blocks < 2 * kUnits ? 2 * kUnits : blocks, s);
 }
 
 template <int TEMPS>
@@ -692,7 +712,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     a.g_plane = b.cap;
     a.gbias = b.gbias;
     a.cap = b.cap;
-    GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, nullptr, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
+    GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, b.gx, b.gw, 0, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
         // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int tile = rows_of_tile(c.n, c.C);
     const int least = piece_width(b.cap, l.most, l.C);
@@ -703,19 +723,17 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
         GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
-        if (g.gx) {
-            d.part = b.gx;
-            GAS_TRY((fx == 64 ? launch_gx<Gx64>(d, rows_most, l.fp, c.s) : fx == 128 ? launch_gx<Gx128>(d, rows_most, l.fp, c.s) : launch_gx<Gx256>(d, rows_most, l.fp, c.s)));
+        if (g.gx || g.gw) {
+            const auto launch = fx == 64 ? launch_products<Gx64, Gw64> : fx == 128 ? launch_products<Gx128, Gw128> : fx == 192 ? launch_products<Gx192, Gw192>
+                              : fx == 256 ? launch_products<Gx256, Gw256> : launch_products<Gx320, Gw320>;
+            GAS_TRY(launch(d, rows_most, cols_most, c.s));
         }
         if (g.gw) {
-            d.part = b.gw;
-            GAS_TRY((fx == 64 ? launch_gw<Gw64>(d, cols_most, l.fp, c.s) : fx == 128 ? launch_gw<Gw128>(d, cols_most, l.fp, c.s) : launch_gw<Gw256>(d, cols_most, l.fp, c.s)));
             hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d);
             GAS_CHECK_HIP(hipGetLastError());
         }
     }
     if (g.gx) {
-        d.part = b.gx;
         d.piece = 0;
         hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n,
                            g.gx, g.ldgx, c.dt == GAS_BF16);

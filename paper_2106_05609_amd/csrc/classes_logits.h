@@ -92,7 +92,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
         c_end = c_first + width;
     }
     if (c_end > l.C) c_end = l.C;
-    Tiles tiles((count + BB - 1) / BB, (c_end - c_first + kTileC - 1) / kTileC);
+    Tiles tiles(blockIdx.x, gridDim.x, (count + BB - 1) / BB, (c_end - c_first + kTileC - 1) / kTileC);
     if (!tiles.on()) return;
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
