@@ -236,30 +236,35 @@ struct LossArgs {
     float *loss, *lse;
 };
 
-// sixteen rows a workgroup, sixteen threads a row: each joins every sixteenth tile, then they are joined one by one
+// ROWS rows a workgroup, 256 / ROWS threads a row: each joins every so many tiles, then they are joined in a tree
+template <int ROWS>
 __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
-    __shared__ float red[4][16][17];
-    const int row = threadIdx.x & 15, part = threadIdx.x >> 4;
-    const int64_t i = (int64_t)blockIdx.x * 16 + row;
+    constexpr int PARTS = 256 / ROWS;
+    __shared__ float red[4][PARTS][ROWS];
+    const int row = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
+    const int64_t i = (int64_t)blockIdx.x * ROWS + row;
     const int64_t r = i < a.n ? a.pos[i] : -1;
     float most = kLeastExponent, sum = 0.f, sum_t = 0.f, picked = 0.f;
     if (r >= 0) {
-        for (int t = part; t < a.tiles; t += 16) {
+        for (int t = part; t < a.tiles; t += PARTS) {
             const int64_t at = (int64_t)t * a.layer.most + r;
             join(most, sum, sum_t, a.parts.most[at], a.parts.sum[at], a.two ? a.parts.sum_t[at] : 0.f, a.inv_t);
             if (a.info) picked += a.parts.picked[at];
         }
     }
-    red[0][part][row] = most;
-    red[1][part][row] = sum;
-    red[2][part][row] = sum_t;
-    red[3][part][row] = picked;
-    __syncthreads();
-    if (part > 0 || i >= a.n) return;
-    for (int p = 1; p < 16; ++p) {
-        join(most, sum, sum_t, red[0][p][row], red[1][p][row], red[2][p][row], a.inv_t);
-        picked += red[3][p][row];
+    for (int half = PARTS / 2; half > 0; half /= 2) {
+        red[0][part][row] = most;
+        red[1][part][row] = sum;
+        red[2][part][row] = sum_t;
+        red[3][part][row] = picked;
+        __syncthreads();
+        if (part < half) {
+            join(most, sum, sum_t, red[0][part + half][row], red[1][part + half][row], red[2][part + half][row], a.inv_t);
+            picked += red[3][part + half][row];
+        }
+        __syncthreads();
     }
+    if (part > 0 || i >= a.n) return;
     const float lse = log_of(most, sum, 1.f);
     if (!a.info) {
         a.loss[i] = r < 0 ? 0.f : lse - a.parts.picked[r];
@@ -438,54 +443,86 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
     else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
-// gw of a piece whose sum over the rows came in parts
-__global__ __launch_bounds__(256) void classes_gw_sum_kernel(GradArgs a) {
-    const Layer& l = a.layer;
-    const Shape shape = *l.shape;
-    const Piece s(shape, a.piece, l.C);
-    const int splits = shape.splits_w;
-    if (splits == 1 || s.cols == 0) return;
-    const int fours_ = (s.cols + 3) / 4;
-    const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < (int64_t)l.F * fours_; q += (int64_t)gridDim.x * 256) {
-        const int64_t f = q / fours_;
-        const int c = (int)(q % fours_) * 4;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part_w + (p * l.F + f) * s.width + c);
-        v *= a.scale;
-        put4(a.gw, f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+// ---- backward: what came in parts, added up
+
+// v[0], v[step], ... n of them one after another, eight under way at a time
+template <class V>
+__device__ __forceinline__ V sum_of(const V* v, int64_t step, int n, V sum) {
+    for (int p = 0; p < n; p += 8) {
+        V part[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) part[u] = v[(p + u < n ? p + u : p) * step];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (p + u < n) sum += part[u];
     }
+    return sum;
 }
 
-// gx of every row: the parts added up, zero for rows that don't count
-__global__ __launch_bounds__(256) void classes_gx_sum_kernel(GradArgs a, const int32_t* pos, int64_t n, void* gx, int64_t ldgx, int bf) {
-    const Layer& l = a.layer;
-    const Shape shape = *l.shape;
-    const Piece s(shape, 0, l.C);
-    const int splits = shape.splits_x;
-    const int fours_ = (l.F + 3) / 4;
-    const bool whole = fours(gx, ldgx, bf);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n * fours_; q += (int64_t)gridDim.x * 256) {
-        const int64_t i = q / fours_;
-        const int f = (int)(q % fours_) * 4;
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        const int64_t r = pos[i];
-        if (r >= 0)
-            for (int p = 0; p < splits; ++p) v += *reinterpret_cast<const f32x4*>(a.part_x + (p * (int64_t)s.rows + r) * l.fp + f);
-        v *= a.scale;
-        put4(gx, i * ldgx + f, v, l.F - f < 4 ? l.F - f : 4, bf, whole && f + 4 <= l.F);
-    }
+struct SumArgs {
+    GradArgs g;
+    const int32_t* pos;
+    int64_t n, ldgx;
+    void* gx;
+    int32_t gx_bf16;
+    const float* part_b;          // [row tiles][C up to 256]
+    float* gbias;
+    int32_t tile_rows;            // of those row tiles
+    uint32_t w_blocks, x_blocks;  // workgroups for gw of this piece, for gx, then one for every 256 of gbias
+};
+
+// A row of fours: row q / fours of q.  In 32 bits where that does.
+__device__ __forceinline__ void row_of(int64_t q, int64_t total, int fours, int64_t& row, int& at) {
+    row = total <= 0xFFFFFFFFLL ? (int64_t)((uint32_t)q / (uint32_t)fours) : q / fours;
+    at = (int)(q - row * fours);
 }
 
-// gbias: the row tiles' sums added up
-__global__ __launch_bounds__(256) void classes_gbias_kernel(const float* part, const Shape* shape, int tile_rows, int C, float scale, float* gbias) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= C) return;
-    const int tiles = (shape->count + tile_rows - 1) / tile_rows;
-    const int64_t cp = ((int64_t)C + 255) / 256 * 256;
-    float v = 0.f;
-    for (int t = 0; t < tiles; ++t) v += part[t * cp + c];
-    gbias[c] = v * scale;
+// gw of a piece if its sum over the rows came in parts; after the last piece gx of every row, zero for those that don't count, and gbias
+__global__ __launch_bounds__(256) void classes_sums_kernel(SumArgs a) {
+    const Layer& l = a.g.layer;
+    const Shape shape = *l.shape;
+    uint32_t block = blockIdx.x;
+    if (block < a.w_blocks) {
+        const Piece s(shape, a.g.piece, l.C);
+        if (shape.splits_w == 1 || s.cols == 0) return;
+        const int n4 = (s.cols + 3) / 4;
+        const bool whole = fours(a.g.gw, a.g.ldgw, a.g.gw_bf16);
+        const int64_t total = (int64_t)l.F * n4, step = (int64_t)l.F * s.width / 4;
+        for (int64_t q = (int64_t)block * 256 + threadIdx.x; q < total; q += (int64_t)a.w_blocks * 256) {
+            int64_t f;
+            int c;
+            row_of(q, total, n4, f, c);
+            c *= 4;
+            f32x4 v = sum_of(reinterpret_cast<const f32x4*>(a.g.part_w + f * s.width + c), step, shape.splits_w, f32x4{0.f, 0.f, 0.f, 0.f});
+            v *= a.g.scale;
+            put4(a.g.gw, f * a.g.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.g.gw_bf16, whole && c + 4 <= s.cols);
+        }
+        return;
+    }
+    block -= a.w_blocks;
+    if (block < a.x_blocks) {
+        const Piece s(shape, 0, l.C);
+        const int n4 = (l.F + 3) / 4;
+        const bool whole = fours(a.gx, a.ldgx, a.gx_bf16);
+        const int64_t total = a.n * n4, step = (int64_t)s.rows * l.fp / 4;
+        for (int64_t q = (int64_t)block * 256 + threadIdx.x; q < total; q += (int64_t)a.x_blocks * 256) {
+            int64_t i;
+            int f;
+            row_of(q, total, n4, i, f);
+            f *= 4;
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+            const int64_t r = a.pos[i];
+            if (r >= 0) v = sum_of(reinterpret_cast<const f32x4*>(a.g.part_x + r * l.fp + f), step, shape.splits_x, v);
+            v *= a.g.scale;
+            put4(a.gx, i * a.ldgx + f, v, l.F - f < 4 ? l.F - f : 4, a.gx_bf16, whole && f + 4 <= l.F);
+        }
+        return;
+    }
+    block -= a.x_blocks;
+    const int c = (int)(block * 256 + threadIdx.x);
+    if (c >= l.C) return;
+    const int64_t cp = ((int64_t)l.C + 255) / 256 * 256;
+    a.gbias[c] = sum_of(a.part_b + c, cp, (shape.count + a.tile_rows - 1) / a.tile_rows, 0.f) * a.g.scale;
 }
 
 // ---- host
@@ -601,7 +638,9 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
                                                                          : launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s)));
     const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
                         c.temperature, loss, lse};
-    hipLaunchKernelGGL(classes_loss_kernel, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
+    // few rows: more threads for each
+    if (c.n <= 2048) hipLaunchKernelGGL(classes_loss_kernel<4>, dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, c.s, l);
+    else hipLaunchKernelGGL(classes_loss_kernel<16>, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
     GAS_CHECK_HIP(hipGetLastError());
     return run_sum(loss, c.n, sum, c.s);
 }
@@ -728,20 +767,13 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
                               : fx == 256 ? launch_products<Gx256, Gw256> : launch_products<Gx320, Gw320>;
             GAS_TRY(launch(d, rows_most, cols_most, c.s));
         }
-        if (g.gw) {
-            hipLaunchKernelGGL(classes_gw_sum_kernel, dim3(blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048)), dim3(256), 0, c.s, d);
-            GAS_CHECK_HIP(hipGetLastError());
-        }
-    }
-    if (g.gx) {
-        d.piece = 0;
-        hipLaunchKernelGGL(classes_gx_sum_kernel, dim3(blocks_for(c.n * ((c.F + 3) / 4), 256, 4096)), dim3(256), 0, c.s, d, common.pos, c.n,
-                           g.gx, g.ldgx, c.dt == GAS_BF16);
-        GAS_CHECK_HIP(hipGetLastError());
-    }
-    if (g.gbias) {
-        hipLaunchKernelGGL(classes_gbias_kernel, dim3((unsigned)((c.C + 255) / 256)), dim3(256), 0, c.s, b.gbias, l.shape, tile, c.C,
-                           g.scale, g.gbias);
+        const bool last = p + 1 == pieces;
+        SumArgs sums = {d, common.pos, c.n, g.ldgx, g.gx, c.dt == GAS_BF16, b.gbias, g.gbias, tile, 0, 0};
+        if (g.gw) sums.w_blocks = blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048);
+        if (g.gx && last) sums.x_blocks = blocks_for(c.n * ((c.F + 3) / 4), 256, 4096);
+        const unsigned blocks = sums.w_blocks + sums.x_blocks + (g.gbias && last ? (unsigned)((c.C + 255) / 256) : 0u);
+        if (blocks == 0) continue;
+        hipLaunchKernelGGL(classes_sums_kernel, dim3(blocks), dim3(256), 0, c.s, sums);
         GAS_CHECK_HIP(hipGetLastError());
     }
     return GAS_OK;
