@@ -94,8 +94,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
     if (c_end > l.C) c_end = l.C;
     Tiles tiles(blockIdx.x, gridDim.x, (count + BB - 1) / BB, (c_end - c_first + kTileC - 1) / kTileC);
     if (!tiles.on()) return;
-    const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wa0 = (wave % WA) * (32 * TA), wb0 = (wave / WA) * (32 * TB);
     const int steps = (l.F + P::kStepOf - 1) / P::kStepOf;
 
@@ -170,6 +169,10 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
             product.multiply(now, wa0, wb0, acc);
         }
         const int m0 = p.m0, c0 = p.c0, tile = c0 / kTileC;
+        // the lane's number anew: addresses made from it here would else be kept from tile to tile, in registers that the products need
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));
+        const int li = lane & 31, lh = lane >> 5;
         if (p.biased) {
 #pragma unroll
             for (int i = 0; i < TA; ++i) {
@@ -208,16 +211,19 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
                 return;
             }
             const int n = lh == 0 ? x->held[r] : 0;
-            for (int j = 0; j < n; ++j) {
-                int2 e;
-                if (j < kHeldEntries) e = x->entry[r][j];
-                else {
-                    const int64_t m = m0 + r;
-                    e = a.entries[m * a.k + a.starts[m * (a.tiles + 1) + tile] + j];
-                    e.x -= c0;
-                }
+            const int2 e0 = x->entry[r][0], e1 = x->entry[r][1];
+            auto one = [&](const int2& e, bool there) {
                 const int rel = e.x - wa0 - 64 * h;
-                if (rel >= 0 && rel < 64) use(place_of(li, rel), __int_as_float(e.y));
+                if (there && rel >= 0 && rel < 64) use(place_of(li, rel), __int_as_float(e.y));
+            };
+            one(e0, n > 0);
+            one(e1, n > 1);
+#pragma unroll 1
+            for (int j = kHeldEntries; j < n; ++j) {
+                const int64_t m = m0 + r;
+                int2 e = a.entries[m * a.k + a.starts[m * (a.tiles + 1) + tile] + j];
+                e.x -= c0;
+                one(e, true);
             }
         };
         if constexpr (KIND == LOGITS_GRAD) {
@@ -267,13 +273,14 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
                         for (int r = 0; r < 32; ++r) column[h] += *place_of(r, lane);
                     // eight classes of a row a lane, so that a row's are next to each other
                     const int r0 = lane / 8, u = 2 * (lane & 7);
-                    uint16_t* to = a.g + (int64_t)(m0 + wb0 + 32 * j + r0) * width + (c0 - c_first) + wa0 + 64 * h + 4 * u;
+                    char* tile_at = reinterpret_cast<char*>(a.g + (int64_t)m0 * width + (c0 - c_first));       // the same for all: offsets are 32 bits
+                    const uint32_t to = ((uint32_t)(wb0 + 32 * j + r0) * (uint32_t)width + wa0 + 64 * h + 4 * u) * 2;
 #pragma unroll
                     for (int r = 0; r < 32; r += 8) {
                         const float* from = mine + (r0 + r) * 64;
                         const int turn = (r0 + r) & 15;
                         const f32x4 v0 = *reinterpret_cast<const f32x4*>(from + 4 * (u ^ turn)), v1 = *reinterpret_cast<const f32x4*>(from + 4 * ((u + 1) ^ turn));
-                        uint16_t* at = to + (int64_t)r * width;
+                        uint16_t* at = reinterpret_cast<uint16_t*>(tile_at + (to + (uint32_t)r * (uint32_t)width * 2));
                         if constexpr (SPLIT) {
                             const float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
                             put8(v, 6, at, a.g_plane, 0);
