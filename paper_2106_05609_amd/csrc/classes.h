@@ -14,6 +14,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTileC = 256;                       // classes of a tile
 constexpr int kMaxClasses = 1 << 22;              // a tile's 256 rows of W then lie within 4 GB
 constexpr int kMaxWidth = 1 << 16;
+constexpr int kReadOnceRows = 64;                 // up to so many rows W is not packed
 constexpr int kMaxEntries = 256;                  // of a teacher's row
 constexpr int kHeldEntries = 2;                   // of a row in one tile that are fetched before the products
 
@@ -28,7 +29,9 @@ struct Shape {
 // What kernels know of the layer.
 struct Layer {
     const uint16_t* x;            // [planes][rows up to 256][fp], packed, zero beyond the row and beyond the last row
-    const uint16_t* w;            // [planes][F][ldw], columns up to cw readable
+    const uint16_t* w;            // [planes][F][ldw], columns up to cw readable; or NULL: it is read where and as it lies
+    const void* raw;              // W itself, rows of ld_raw
+    int64_t ld_raw;
     int64_t ldw, w_plane, x_plane;
     const float* bias;            // [C up to 256], -inf beyond C
     const Shape* shape;
@@ -232,6 +235,8 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     const int64_t most = round_up(n, 256), fp = round_up(F, 64), cp = round_up(C, kTileC);
     // W where it lies if its rows can be read in whole pieces
     const bool in_place = dt == GAS_BF16 && C % 8 == 0 && ldw % 8 == 0 && ldw <= kMaxClasses && aligned16(W);
+    // and also, by kernels of their own, where it is used for few rows: packed first, 32 x 2,048 x 131,072 of fp32 took ...
+    const bool once = !in_place && n <= kReadOnceRows;
     const int64_t cw = in_place ? C : round_up(C, 64);
     c.layer.terms = dt == GAS_F32 ? 6 : 1;
     Shape* shape = room.take<Shape>(1);
@@ -239,10 +244,12 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     c.pos = compact ? room.take<int32_t>(most) : nullptr;
     c.block_counts = compact ? room.take<int32_t>(most / 256) : nullptr;
     uint16_t* x = room.take<uint16_t>(planes * most * fp);
-    uint16_t* w = in_place ? nullptr : room.take<uint16_t>(planes * (int64_t)F * cw);
+    uint16_t* w = in_place || once ? nullptr : room.take<uint16_t>(planes * (int64_t)F * cw);
     float* biasp = room.take<float>(cp);
     c.layer.x = x;
     c.layer.w = in_place ? static_cast<const uint16_t*>(W) : w;
+    c.layer.raw = W;
+    c.layer.ld_raw = ldw;
     c.layer.ldw = in_place ? ldw : cw;
     c.layer.w_plane = (int64_t)F * cw;
     c.layer.x_plane = most * fp;
@@ -254,7 +261,7 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     c.layer.cw = (int32_t)cw;
     c.layer.most = (int32_t)most;
     c.pack = PackArgs{X, W, bias, ldx, ldw, n, c.idx, shape, x, w, biasp, c.layer.x_plane, c.layer.w_plane, F, (int32_t)fp, C, (int32_t)cw,
-                      (int32_t)cp, c.layer.terms, blocks_for(most * fp / 8, 256, 4096), in_place ? 0u : blocks_for((int64_t)F * cw / 8, 256, 8192)};
+                      (int32_t)cp, c.layer.terms, blocks_for(most * fp / 8, 256, 4096), in_place || once ? 0u : blocks_for((int64_t)F * cw / 8, 256, 8192)};
     return c;
 }
 

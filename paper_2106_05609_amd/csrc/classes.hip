@@ -20,6 +20,7 @@ struct RowsArgs {
     int32_t *idx, *pos;
     Shape* shape;
     int64_t cap;                  // backward: room for the gradient at a piece's logits
+    int32_t once;                 // GX by gx_once_tile
     int32_t nfx, nfw, steps_of;   // tiles of inputs of GX and GW; 64 k of one part are `steps_of` steps (of fp32's six terms)
     const float* lse;             // backward: [n] (labels alone) or [n, 2]
     const float* row_scale;       // backward: [n] or NULL
@@ -61,12 +62,18 @@ __device__ __host__ inline int splits_of(int tiles, int steps, int steps_of) {
     }
     return best;
 }
+// Of few rows, whose parts are short: two for every unit, of 128 classes at least.
+__device__ __host__ inline int splits_once(int tiles, int steps) {
+    int s = 2 * kUnits / tiles;
+    if (s > steps / 2) s = steps / 2;
+    return s < 1 ? 1 : s;
+}
 __device__ __forceinline__ Shape shape_for(const RowsArgs& a, int count) {
     Shape s = {count, 0, 1, 1};
     if (a.cap > 0) {
         const int rows = count > 0 ? (count + 255) / 256 * 256 : 256;
         s.width = piece_width(a.cap, rows, a.t.C);
-        s.splits_x = splits_of(rows / 256 * a.nfx, s.width / kStepK, a.steps_of);
+        s.splits_x = a.once ? splits_once(a.nfx, s.width / kStepK) : splits_of(rows / 256 * a.nfx, s.width / kStepK, a.steps_of);
         s.splits_w = splits_of(s.width / 256 * a.nfw, rows / kStepK, a.steps_of);
     }
     return s;
@@ -373,6 +380,49 @@ __device__ __forceinline__ void gx_tile(const GradArgs& a, uint32_t block, uint3
     }
 }
 
+// The same for few rows and W as it lies
+template <class P>
+__device__ __forceinline__ void gx_once_tile(const GradArgs& a, uint32_t block, uint32_t blocks, char* smem) {
+    constexpr int BA = P::kRowsA, WA = BA / 32 / P::TA;
+    const Layer& l = a.layer;
+    const Shape shape = *l.shape;
+    const Piece s(shape, a.piece, l.C);
+    if (s.cols == 0 || s.rows == 0) return;
+    const int nf = (l.fp + BA - 1) / BA, full = s.width / P::kStepOf, steps = (s.cols + P::kStepOf - 1) / P::kStepOf, splits = shape.splits_x;
+    int ft, part;
+    if (!tile_of(block, blocks, nf, splits, ft, part)) return;
+    const int per = (full + splits - 1) / splits, first = part * per < steps ? part * per : steps, last = first + per < steps ? first + per : steps;
+    const int f0 = ft * BA, lane = threadIdx.x & 63, li = lane & 31, lh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
+    constexpr int eb = P::PLANES == 1 ? 2 : 4;
+    f32x16 acc[P::TA][P::TB];
+    P product;
+    const typename P::Operand oa = {static_cast<const char*>(l.raw) + ((int64_t)f0 * l.ld_raw + s.first) * eb, l.ld_raw, l.F - f0, l.C - s.first};
+    const TileOperand ob = {a.g, s.width, a.g_plane, P::kRowsB - 1, s.width};
+    product.run(oa, ob, first, last, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    float* out = a.part_x + (int64_t)part * s.rows * l.fp;
+#pragma unroll
+    for (int j = 0; j < P::TB; ++j) {
+        float* row = out + (int64_t)(wb0 + 32 * j + li) * l.fp;
+#pragma unroll
+        for (int i = 0; i < P::TA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int f = f0 + wa0 + 32 * i + 8 * q + 4 * lh;
+                if (f >= l.fp) continue;
+                f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                if (a.piece > 0) v += *reinterpret_cast<const f32x4*>(row + f);
+                *reinterpret_cast<f32x4*>(row + f) = v;
+            }
+    }
+}
+template <class P>
+__global__ __launch_bounds__(P::T, 2) void classes_gx_once_kernel(GradArgs a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    gx_once_tile<P>(a, blockIdx.x, gridDim.x, smem);
+}
+
 __device__ __forceinline__ void put4(void* base, int64_t at, const f32x4& v, int n, bool bf, bool whole) {
     if (bf) {
         uint16_t* p = static_cast<uint16_t*>(base) + at;
@@ -658,6 +708,7 @@ using Gx128 = TileProduct<128, 256, 2, 4, false, false, 64, 2>;
 using Gx192 = TileProduct<192, 256, 2, 4, false, false, 64, 2>;
 using Gx256 = TileProduct<256, 256, 2, 4, false, false, 64, 2>;
 using Gx320 = TileProduct<320, 256, 2, 4, false, false, 64, 2>;
+template <bool BF> using GxOnce = ReadOnceProduct<256, 64, 4, 1, false, BF>;
 using Gw64 = TileProduct<256, 64, 4, 1, true, true, 64, 2>;
 using Gw128 = TileProduct<256, 128, 4, 2, true, true, 64, 2>;
 using Gw192 = TileProduct<256, 192, 4, 2, true, true, 64, 2>;
@@ -724,6 +775,17 @@ gas_status launch_products(GradArgs a, int64_t rows, int64_t cols, hipStream_t s
     return GAS_OK;
 }
 
+template <class P>
+gas_status launch_gx_once(const GradArgs& a, hipStream_t s) {
+    static const gas_status attr = lds_of(classes_gx_once_kernel<P>, P::kLdsBytes);
+    if (attr != GAS_OK) return attr;
+    const int tiles = (a.layer.fp + P::kRowsA - 1) / P::kRowsA;
+    const unsigned blocks = (unsigned)round_up(tiles > 2 * kUnits ? tiles : 2 * kUnits, 8);
+    hipLaunchKernelGGL(classes_gx_once_kernel<P>, dim3(blocks), dim3(P::T), P::kLdsBytes, s, a);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
 template <int TEMPS>
 gas_status launch_grad_of(const LogitsArgs& a, int n, int64_t tiles, gas_dtype dt, hipStream_t s) {
     return dt == GAS_F32 ? launch_logits<LOGITS_GRAD, TEMPS, true>(a, n, tiles, s) : launch_logits<LOGITS_GRAD, TEMPS, false>(a, n, tiles, s);
@@ -742,7 +804,9 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     rows.row_scale = g.row_scale;
     rows.cap = b.cap;
     const int fx = width_of_tile(common.layer.fp);
-    rows.nfx = rows.nfw = (common.layer.fp + fx - 1) / fx;
+    rows.once = common.layer.w == nullptr;
+    rows.nfw = (int32_t)((common.layer.fp + fx - 1) / fx);
+    rows.nfx = rows.once ? (int32_t)((common.layer.fp + 255) / 256) : rows.nfw;
     rows.steps_of = common.layer.terms;
     GAS_TRY(run_rows(c, common, rows, distill));
     const Layer& l = common.layer;
@@ -762,10 +826,13 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
         GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
-        if (g.gx || g.gw) {
+        if (g.gx && rows.once) GAS_TRY(c.dt == GAS_BF16 ? launch_gx_once<GxOnce<true>>(d, c.s) : launch_gx_once<GxOnce<false>>(d, c.s));
+        if ((g.gx && !rows.once) || g.gw) {
             const auto launch = fx == 64 ? launch_products<Gx64, Gw64> : fx == 128 ? launch_products<Gx128, Gw128> : fx == 192 ? launch_products<Gx192, Gw192>
                               : fx == 256 ? launch_products<Gx256, Gw256> : launch_products<Gx320, Gw320>;
-            GAS_TRY(launch(d, rows_most, cols_most, c.s));
+            GradArgs both = d;
+            if (rows.once) both.part_x = nullptr;
+            GAS_TRY(launch(both, rows_most, cols_most, c.s));
         }
         const bool last = p + 1 == pieces;
         SumArgs sums = {d, common.pos, c.n, g.ldgx, g.gx, c.dt == GAS_BF16, b.gbias, g.gbias, tile, 0, 0};

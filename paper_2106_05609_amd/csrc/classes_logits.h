@@ -160,7 +160,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
     // next: where the next tile's first step goes.
     auto finish = [&](uint16_t* __restrict__ now, uint16_t* __restrict__ next, const Extras<BB>* __restrict__ x, Extras<BB>* __restrict__ nx, const P& product, const Place& p,
                       f32x16 (&acc)[TA][TB], bool more, const Place& np, typename P::Walk& walk) {
-        if (STREAM) {
+        if constexpr (STREAM) {
             if (more) {
                 product.bring(walk, np.a, np.b, next);
                 product.advance(walk, np.a, np.b);
@@ -435,6 +435,17 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
     int ring = 0, turn = 0;
     typename P::Walk walk;
     f32x16 acc[TA][TB];
+    if constexpr (P::kReadOnce) {
+        bring_extras(p.m0, p.c0, p.biased, extras);
+        fetch(p.m0, p.c0);
+        fetch_entries(p.m0, p.c0);
+        put(extras[0]);
+        constexpr int eb = P::PLANES == 1 ? 2 : 4;
+        const typename P::Operand oa = {static_cast<const char*>(l.raw) + (int64_t)p.c0 * eb, l.ld_raw, l.C - p.c0, l.F};
+        product.run(oa, p.b, 0, steps, lds, wa0, wb0, acc);
+        finish(lds, lds, extras, extras, product, p, acc, false, p, walk);
+        return;
+    } else {
     if constexpr (STREAM) {
         walk = product.start(p.a, p.b, 0, steps, l.terms);
         product.bring(walk, p.a, p.b, lds);
@@ -472,6 +483,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
         p = np;
         ring ^= 1;
     }
+    }
 }
 
 template <bool STREAM, class P>
@@ -494,12 +506,21 @@ gas_status launch_logits_tile(const LogitsArgs& a, int64_t tiles, hipStream_t s)
 
 // tiles: of rows by classes, at most, for tiles of rows_of_tile() rows
 using FewRows = TileProduct<kTileC, 64, 4, 1, true, false>;
+template <bool BF> using FewRowsOnce = ReadOnceProduct<kTileC, 64, 4, 1, true, BF>;
 constexpr int kRowsTile = 256;
 using ManyRows = TileProduct<kTileC, kRowsTile, 2, 4, true, false, 64, 2>;
 // Rows of a tile: 64 where there are no more rows, or where tiles of 256 would leave compute units without any.
 inline int rows_of_tile(int64_t n, int C) { return n <= 64 || round_up(n, kRowsTile) / kRowsTile * (round_up(C, kTileC) / kTileC) < 256 ? 64 : kRowsTile; }
 template <int KIND, int TEMPS, bool SPLIT = false>
 gas_status launch_logits(const LogitsArgs& a, int tile_rows, int64_t tiles, hipStream_t s) {
+    if (!a.layer.w) {
+        // SPLIT goes with fp32
+        if (a.layer.terms == 1) {
+            if constexpr (!SPLIT) return launch_logits_tile<KIND, TEMPS, SPLIT, false, FewRowsOnce<true>>(a, tiles, s);
+        } else if constexpr (SPLIT || KIND != LOGITS_GRAD) {
+            return launch_logits_tile<KIND, TEMPS, SPLIT, false, FewRowsOnce<false>>(a, tiles, s);
+        }
+    }
     if (tile_rows == 64) return launch_logits_tile<KIND, TEMPS, SPLIT, false, FewRows>(a, tiles, s);
     return launch_logits_tile<KIND, TEMPS, SPLIT, true, ManyRows>(a, tiles, s);
 }

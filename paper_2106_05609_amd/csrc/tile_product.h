@@ -34,6 +34,7 @@ struct TileProduct {
     static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB;
     static constexpr int kStage = (BA + BB) * STEP;                        // elements
     static constexpr int kStepOf = STEP, kRowsA = BA, kRowsB = BB, kStages = STAGES;
+    static constexpr bool kReadOnce = false;
     static constexpr int kLdsBytes = STAGES * kStage * 2;
     static_assert((STEP == 32 || STEP == 64) && (STAGES == 2 || STAGES == 3), "");
     // where piece `piece` of row `row` lies, in pieces of 16 bytes
@@ -231,6 +232,145 @@ struct TileProduct {
                                         f32x16 (&acc)[TA][TB]) {
         Walk w = begin(a, b, first, last, terms, lds);
         run(w, a, b, lds, wa0, wb0, acc);
+    }
+};
+
+// The same sums where the first operand is read once and used by few rows of the second: packing it beforehand (16 bytes a value
+// of fp32 and more, 4 of bf16) would take several times what reading it takes. It is read as it lies, any alignment and width, into
+// registers, a step ahead, and goes to LDS in its parts; the second operand's planes are packed.  32 k a step, all terms of a step at once.
+template <int BA, int BB, int WA, int WB, bool ATURNED, bool BF>
+struct ReadOnceProduct {
+    static constexpr int T = 64 * WA * WB, TA = BA / 32 / WA, TB = BB / 32 / WB, STEP = 32, PLANES = BF ? 1 : 3;
+    static constexpr int kStepOf = STEP, kRowsA = BA, kRowsB = BB, kStages = 1;
+    static constexpr int kA = BA * STEP, kB = BB * STEP;                   // elements of a plane
+    static constexpr int kStage = PLANES * (kA + kB), kLdsBytes = kStage * 2 > T * 128 ? kStage * 2 : T * 128;      // room for 8 KB a wavefront afterwards
+    static constexpr bool kReadOnce = true;
+    using Same = TileProduct<BA, BB, WA, WB, ATURNED, false, STEP, 2>;     // where pieces lie in LDS, and how they are read
+    static constexpr int NA = kA / 8 / T, NB = PLANES * kB / 8 / T;
+    static_assert(kA / 8 % T == 0 && PLANES * kB / 8 % T == 0, "every thread brings as many pieces");
+    typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+    struct Operand {              // element (r, k) of the tile at p[r ld + k], turned at p[k ld + r]; rows and k that are there
+        const void* p;
+        int64_t ld;
+        int rows, k;
+    };
+    struct Walk {
+        int first, last;
+    };
+    union Piece {
+        float f[8];
+        u32x4 h;
+    };
+    Piece va[NA];
+    u32x4 vb[NB];
+
+    __device__ __forceinline__ void fetch(const Operand& a, const TileOperand& b, int k0) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int q = i * T + (int)threadIdx.x;
+            const int major = ATURNED ? q / (BA / 8) : q / (STEP / 8), minor = 8 * (ATURNED ? q % (BA / 8) : q % (STEP / 8));
+            // turned: major a k, minor rows; else major a row, minor k
+            const int majors = ATURNED ? a.k - k0 : a.rows, minors = ATURNED ? a.rows : a.k - k0;
+            const int64_t at = ATURNED ? (int64_t)(k0 + major) * a.ld + minor : (int64_t)major * a.ld + k0 + minor;
+            if constexpr (BF) va[i].h = u32x4{0u, 0u, 0u, 0u};
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) va[i].f[e] = 0.f;
+            if (major >= majors || minor >= minors) continue;
+            if (minor + 8 <= minors) {
+                if constexpr (BF) {
+                    va[i].h = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(a.p) + at);
+                } else {
+                    const f32x4 x = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(a.p) + at);
+                    const f32x4 y = *reinterpret_cast<const f32x4_any*>(static_cast<const float*>(a.p) + at + 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        va[i].f[e] = x[e];
+                        va[i].f[4 + e] = y[e];
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (minor + e < minors) {
+                        if constexpr (BF) va[i].h[e / 2] |= (uint32_t)static_cast<const uint16_t*>(a.p)[at + e] << (16 * (e & 1));
+                        else va[i].f[e] = static_cast<const float*>(a.p)[at + e];
+                    }
+            }
+        }
+        // the second operand: rows and k beyond what is there repeat the last ones, whose products nothing takes or which the first one's zeros meet
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int q = i * T + (int)threadIdx.x, plane = q / (kB / 8), row = q % (kB / 8) / (STEP / 8), k = k0 + 8 * (q % (STEP / 8));
+            vb[i] = *reinterpret_cast<const u32x4*>(b.p + plane * b.plane + (int64_t)(row < b.last ? row : b.last) * b.ld + (k < b.k - 8 ? k : b.k - 8));
+        }
+    }
+    __device__ __forceinline__ void stage(uint16_t* lds) const {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) {
+            const int q = i * T + (int)threadIdx.x;
+            int to;                                                        // in pieces
+            if constexpr (ATURNED) {
+                const int k = q / (BA / 8);
+                to = k * (BA / 8) + ((q % (BA / 8)) ^ (4 * (k & 3) & (BA / 8 - 1)));
+            } else {
+                const int row = q / (STEP / 8);
+                to = row * (STEP / 8) + ((q % (STEP / 8)) ^ Same::swap(row));
+            }
+            if constexpr (BF) {
+                *reinterpret_cast<u32x4*>(lds + 8 * to) = va[i].h;
+            } else {
+                u32x4 h, m, l;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t x, y, z;
+                    split_pair(va[i].f[2 * e], va[i].f[2 * e + 1], x, y, z);
+                    h[e] = x; m[e] = y; l[e] = z;
+                }
+                *reinterpret_cast<u32x4*>(lds + 8 * to) = h;
+                *reinterpret_cast<u32x4*>(lds + 8 * to + kA) = m;
+                *reinterpret_cast<u32x4*>(lds + 8 * to + 2 * kA) = l;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const int q = i * T + (int)threadIdx.x, plane = q / (kB / 8), row = q % (kB / 8) / (STEP / 8), piece = q % (STEP / 8);
+            *reinterpret_cast<u32x4*>(lds + PLANES * kA + plane * kB + 8 * (row * (STEP / 8) + (piece ^ Same::swap(row)))) = vb[i];
+        }
+    }
+    // acc = the products over steps [first, last) of 32 k.  Called by every thread; LDS is free for other use afterwards.
+    __device__ __forceinline__ void run(const Operand& a, const TileOperand& b, int first, int last, uint16_t* lds, int wa0, int wb0,
+                                        f32x16 (&acc)[TA][TB]) {
+        Same::clear(acc);
+        if (first < last) fetch(a, b, STEP * first);
+#pragma unroll 1
+        for (int s = first; s < last; ++s) {
+            __syncthreads();                                               // everyone is done with the step before
+            stage(lds);
+            __syncthreads();
+            if (s + 1 < last) fetch(a, b, STEP * (s + 1));
+            constexpr int PA[6] = {1, 2, 0, 1, 0, 0}, PB[6] = {1, 0, 2, 0, 1, 0};      // the smallest product first
+#pragma unroll
+            for (int kk = 0; kk < STEP / 16; ++kk) {
+                bf16x8 fa[PLANES][TA], fb[PLANES][TB];
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p) {
+#pragma unroll
+                    for (int i = 0; i < TA; ++i) fa[p][i] = Same::template fragment<BA, ATURNED>(lds + p * kA, wa0 + 32 * i, kk);
+#pragma unroll
+                    for (int j = 0; j < TB; ++j) fb[p][j] = Same::template fragment<BB, false>(lds + PLANES * kA + p * kB, wb0 + 32 * j, kk);
+                }
+#pragma unroll
+                for (int t = BF ? 5 : 0; t < 6; ++t)
+#pragma unroll
+                    for (int i = 0; i < TA; ++i)
+#pragma unroll
+                        for (int j = 0; j < TB; ++j)
+                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[PA[t]][i], fb[PB[t]][j], acc[i][j], 0, 0, 0);
+            }
+        }
+        __syncthreads();
     }
 };
 
