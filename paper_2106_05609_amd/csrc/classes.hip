@@ -400,7 +400,7 @@ __device__ __forceinline__ void gx_once_tile(const GradArgs& a, uint32_t block, 
     P product;
     const typename P::Operand oa = {static_cast<const char*>(l.raw) + ((int64_t)f0 * l.ld_raw + s.first) * eb, l.ld_raw, l.F - f0, l.C - s.first};
     const TileOperand ob = {a.g, s.width, a.g_plane, P::kRowsB - 1, s.width};
-    product.run(oa, ob, first, last, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
+    product.run(oa, ob, shape.count, first, last, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     float* out = a.part_x + (int64_t)part * s.rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
@@ -463,25 +463,46 @@ __device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint3
     const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, l.most};
     const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
     product.run(oa, ob, first * (kStepK / P::kStepOf), last * (kStepK / P::kStepOf), l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
-    const bool whole = fours(a.gw, a.ldgw, a.gw_bf16);
+    // A lane has classes of 32 inputs' rows, memory wants a row's next to each other: through 32 rows of 64 classes of LDS that belong to the
+    // wavefront (stored as they came, rows of no whole pieces took two bytes from every lane to a row of its own: ...).
+    const bool whole = fours(a.gw, a.ldgw, a.gw_bf16) && s.first + c0 + 256 <= s.first + s.cols;
+    float* mine = reinterpret_cast<float*>(smem) + wave * (32 * 64);
+    static_assert(P::T / 64 * 32 * 64 * 4 <= P::kLdsBytes && P::TA % 2 == 0, "the wavefronts' pieces fit where operands were");
 #pragma unroll
-    for (int j = 0; j < P::TB; ++j) {
-        const int f = f0 + wb0 + 32 * j + li;
-        if (f >= l.F) continue;
+    for (int j = 0; j < P::TB; ++j)
 #pragma unroll
-        for (int i = 0; i < P::TA; ++i)
+        for (int h = 0; h < P::TA / 2; ++h) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = c0 + wa0 + 32 * i + 8 * q + 4 * lh;
-                f32x4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                if (splits > 1) {
-                    if (c < s.width) *reinterpret_cast<f32x4*>(a.part_w + ((int64_t)part * l.F + f) * s.width + c) = v;
-                } else if (c < s.cols) {
-                    v *= a.scale;
-                    put4(a.gw, (int64_t)f * a.ldgw + s.first + c, v, s.cols - c < 4 ? s.cols - c : 4, a.gw_bf16, whole && c + 4 <= s.cols);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16& v = acc[2 * h + i][j];
+                    *reinterpret_cast<f32x4*>(mine + li * 64 + 4 * ((8 * i + 2 * q + lh) ^ (li & 15))) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                }
+            const int f_first = f0 + wb0 + 32 * j, c_first = c0 + wa0 + 64 * h;
+            if (splits > 1 || whole) {                         // four classes a lane, sixteen lanes a row
+                const int u = lane & 15;
+#pragma unroll
+                for (int r = lane >> 4; r < 32; r += 4) {
+                    f32x4 v = *reinterpret_cast<const f32x4*>(mine + r * 64 + 4 * (u ^ (r & 15)));
+                    const int f = f_first + r, c = c_first + 4 * u;
+                    if (f >= l.F) continue;
+                    if (splits > 1) *reinterpret_cast<f32x4*>(a.part_w + ((int64_t)part * l.F + f) * s.width + c) = v;
+                    else put4(a.gw, (int64_t)f * a.ldgw + s.first + c, v * a.scale, 4, a.gw_bf16, true);
+                }
+            } else {                                           // a class a lane
+                const int c = c_first + lane;
+#pragma unroll 8
+                for (int r = 0; r < 32; ++r) {
+                    const float v = mine[r * 64 + 4 * ((lane >> 2) ^ (r & 15)) + (lane & 3)] * a.scale;
+                    const int f = f_first + r;
+                    if (f >= l.F || c >= s.cols) continue;
+                    const int64_t at = (int64_t)f * a.ldgw + s.first + c;
+                    if (a.gw_bf16) static_cast<uint16_t*>(a.gw)[at] = (uint16_t)f32_to_bf16(v);
+                    else static_cast<float*>(a.gw)[at] = v;
                 }
             }
-    }
+        }
 }
 
 // Both in one launch: neither fills the card alone where there are few tiles, and one's last tiles run beside the other's first.

@@ -442,7 +442,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
         put(extras[0]);
         constexpr int eb = P::PLANES == 1 ? 2 : 4;
         const typename P::Operand oa = {static_cast<const char*>(l.raw) + (int64_t)p.c0 * eb, l.ld_raw, l.C - p.c0, l.F};
-        product.run(oa, p.b, 0, steps, lds, wa0, wb0, acc);
+        product.run(oa, p.b, count, 0, steps, lds, wa0, wb0, acc);
         finish(lds, lds, extras, extras, product, p, acc, false, p, walk);
         return;
     } else {

@@ -264,6 +264,7 @@ struct ReadOnceProduct {
     };
     Piece va[NA];
     u32x4 vb[NB];
+    int blocks;                   // of 32 rows of the second operand that are wanted; the others' products are left out
 
     __device__ __forceinline__ void fetch(const Operand& a, const TileOperand& b, int k0) {
 #pragma unroll
@@ -339,9 +340,11 @@ struct ReadOnceProduct {
             *reinterpret_cast<u32x4*>(lds + PLANES * kA + plane * kB + 8 * (row * (STEP / 8) + (piece ^ Same::swap(row)))) = vb[i];
         }
     }
-    // acc = the products over steps [first, last) of 32 k.  Called by every thread; LDS is free for other use afterwards.
-    __device__ __forceinline__ void run(const Operand& a, const TileOperand& b, int first, int last, uint16_t* lds, int wa0, int wb0,
+    // acc = the products over steps [first, last) of 32 k, with b's first `rows` rows.  Called by every thread; LDS is free for other use afterwards.
+    __device__ __forceinline__ void run(const Operand& a, const TileOperand& b, int rows, int first, int last, uint16_t* lds, int wa0, int wb0,
                                         f32x16 (&acc)[TA][TB]) {
+        static_assert(WB == 1, "a wavefront's blocks are the tile's");
+        blocks = (rows + 31) / 32;
         Same::clear(acc);
         if (first < last) fetch(a, b, STEP * first);
 #pragma unroll 1
@@ -359,14 +362,16 @@ struct ReadOnceProduct {
 #pragma unroll
                     for (int i = 0; i < TA; ++i) fa[p][i] = Same::template fragment<BA, ATURNED>(lds + p * kA, wa0 + 32 * i, kk);
 #pragma unroll
-                    for (int j = 0; j < TB; ++j) fb[p][j] = Same::template fragment<BB, false>(lds + PLANES * kA + p * kB, wb0 + 32 * j, kk);
+                    for (int j = 0; j < TB; ++j)
+                        if (j == 0 || j < blocks) fb[p][j] = Same::template fragment<BB, false>(lds + PLANES * kA + p * kB, wb0 + 32 * j, kk);
                 }
+#pragma unroll
+                for (int j = 0; j < TB; ++j)
+                    if (j == 0 || j < blocks)
 #pragma unroll
                 for (int t = BF ? 5 : 0; t < 6; ++t)
 #pragma unroll
                     for (int i = 0; i < TA; ++i)
-#pragma unroll
-                        for (int j = 0; j < TB; ++j)
                             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[PA[t]][i], fb[PB[t]][j], acc[i][j], 0, 0, 0);
             }
         }
