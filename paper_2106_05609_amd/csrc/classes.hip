@@ -9,6 +9,7 @@
 // products' type and multiplied by W and X.
 
 #include "classes_logits.h"
+#include "classes_vector.h"
 
 namespace gas {
 namespace {
@@ -241,6 +242,12 @@ struct LossArgs {
     int32_t tiles, two;
     float inv_t, temperature;
     float *loss, *lse;
+    // few rows, whose logits are there: where the targets are
+    const float* z;
+    int64_t ldz;
+    const int32_t* labels;        // [rows], or
+    const int2* entries;          // [rows][k]
+    int32_t k;
 };
 
 // ROWS rows a workgroup, 256 / ROWS threads a row: each joins every so many tiles, then they are joined in a tree
@@ -256,7 +263,16 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
         for (int t = part; t < a.tiles; t += PARTS) {
             const int64_t at = (int64_t)t * a.layer.most + r;
             join(most, sum, sum_t, a.parts.most[at], a.parts.sum[at], a.two ? a.parts.sum_t[at] : 0.f, a.inv_t);
-            if (a.info) picked += a.parts.picked[at];
+            if (a.info && !a.z) picked += a.parts.picked[at];
+        }
+        if (a.z) {
+            const float* z = a.z + r * a.ldz;
+            if (!a.info) picked = part == 0 ? z[a.labels[r]] : 0.f;
+            else
+                for (int e = part; e < a.k; e += PARTS) {
+                    const int2 one = a.entries[r * a.k + e];
+                    if (one.x < a.layer.C) picked = fmaf(__int_as_float(one.y), z[one.x], picked);
+                }
         }
     }
     for (int half = PARTS / 2; half > 0; half /= 2) {
@@ -274,7 +290,7 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
     if (part > 0 || i >= a.n) return;
     const float lse = log_of(most, sum, 1.f);
     if (!a.info) {
-        a.loss[i] = r < 0 ? 0.f : lse - a.parts.picked[r];
+        a.loss[i] = r < 0 ? 0.f : lse - (a.z ? picked : a.parts.picked[r]);
         a.lse[i] = r < 0 ? 0.f : lse;
         return;
     }
@@ -514,6 +530,65 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
     else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
+// ---- backward: the gradient at the logits of few rows, 256 classes of the piece a workgroup, two of every other row a thread
+__global__ __launch_bounds__(256) void classes_grad_few_kernel(LogitsArgs a, const float* z, int64_t ldz) {
+    __shared__ float sums[256];
+    const Layer& l = a.layer;
+    const int count = l.shape->count, width = l.shape->width, tid = threadIdx.x, c0 = (int)(blockIdx.x * 256);
+    if (c0 >= width || (int64_t)a.piece * width + c0 >= ldz) return;
+    const int pair = 2 * (tid & 127), half = tid >> 7, planes = l.terms > 1 ? 3 : 1;
+    const int64_t c = (int64_t)a.piece * width + c0 + pair;
+    float sum[2] = {0.f, 0.f};
+    for (int r = half; r < count; r += 2) {
+        const f32x4 info = a.info[r];
+        const int label = a.labels ? a.labels[r] : -1;
+        int from = 0, to = 0;
+        if (!a.labels) {
+            const uint16_t* s = a.starts + (int64_t)r * (a.tiles + 1) + c / 256;
+            from = s[0];
+            to = s[1];
+        }
+        float g[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            g[j] = 0.f;
+            if (c + j >= l.C) continue;
+            const float v = z[r * ldz + c + j];
+            if (a.labels || info[2] != 0.f) g[j] = info[2] * exp2_of((v - info[0]) * kLog2e);
+            if (!a.labels && info[3] != 0.f) g[j] = fmaf(info[3], exp2_of((v * a.inv_t - info[1]) * kLog2e), g[j]);
+            if (c + j == label) g[j] -= info[2];
+        }
+        for (int e = from; e < to; ++e) {
+            const int2 one = a.entries[(int64_t)r * a.k + e];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                if (one.x == c + j) g[j] -= __int_as_float(one.y);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) sum[j] += g[j];
+        uint32_t part[3];
+        split_pair(g[0], g[1], part[0], part[1], part[2]);
+        uint16_t* at = a.g + (int64_t)r * width + c0 + pair;
+        *reinterpret_cast<uint32_t*>(at) = part[0];
+        if (planes > 1) {
+            *reinterpret_cast<uint32_t*>(at + a.g_plane) = part[1];
+            *reinterpret_cast<uint32_t*>(at + 2 * a.g_plane) = part[2];
+        }
+    }
+    // rows up to 64 are read later on
+    for (int r = count + (tid >> 5); r < 64; r += 8)
+        for (int p = 0; p < planes; ++p) *reinterpret_cast<u32x4*>(a.g + p * a.g_plane + (int64_t)r * width + c0 + 8 * (tid & 31)) = u32x4{0, 0, 0, 0};
+    if (!a.gbias) return;
+    if (half) {
+        sums[pair] = sum[0];
+        sums[pair + 1] = sum[1];
+    }
+    __syncthreads();
+    if (half) return;
+    a.gbias[c] = sum[0] + sums[pair];
+    a.gbias[c + 1] = sum[1] + sums[pair + 1];
+}
+
 // ---- backward: what came in parts, added up
 
 // v[0], v[step], ... n of them one after another, eight under way at a time
@@ -638,7 +713,7 @@ inline RowsArgs lay_out_rows(Room& room, const Call& c, const Common& common, bo
     return r;
 }
 
-inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& r, bool distill) {
+inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& r, bool distill, bool pack) {
     const unsigned blocks = (unsigned)((c.n + 255) / 256);
     if (c.n <= (distill ? kFewWithEntries : kFewToNumber)) {
         hipLaunchKernelGGL(classes_number_few_kernel, dim3(1), dim3(1024), 0, c.s, r);
@@ -651,7 +726,7 @@ inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& 
         hipLaunchKernelGGL(classes_entries_kernel, dim3((unsigned)c.n), dim3(64), 0, c.s, r);
         GAS_CHECK_HIP(hipGetLastError());
     }
-    return run_pack(common, c.dt, c.s);
+    return pack ? run_pack(common, c.dt, c.s) : GAS_OK;
 }
 
 // What the forward call needs beside: the tiles' statistics
@@ -694,21 +769,31 @@ inline gas_status run_sum(const float* loss, int64_t n, float* out, hipStream_t 
         if (st_ != GAS_OK) return st_;      \
     } while (0)
 
+// Logits of few rows, all of them
+gas_status launch_few(const Call& c, const Common& common, float inv_t, float* z, const Parts* parts) {
+    const VectorArgs v = {c.X, c.W, c.bias, c.ldx, c.ldw, round_up(c.C, 256), common.layer.most, common.idx, common.layer.shape, (int32_t)c.n, c.F, c.C, inv_t, z,
+                          parts ? *parts : Parts{}};
+    return c.dt == GAS_BF16 ? launch_vector<true>(v, c.s) : launch_vector<false>(v, c.s);
+}
+
 gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* lse) {
     Room room{static_cast<char*>(c.workspace)};
     const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
     const RowsArgs rows = lay_out_rows(room, c, common, distill);
     const Parts parts = lay_out_parts(room, common, distill);
-    GAS_TRY(run_rows(c, common, rows, distill));
+    const bool few = c.n <= kRowsByVector;
+    float* z = few ? room.take<float>(kRowsByVector * (int64_t)round_up(c.C, 256)) : nullptr;
+    GAS_TRY(run_rows(c, common, rows, distill, !few));
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.parts = parts;
     const bool two = distill && c.temperature != 1.f;
     const int tile = rows_of_tile(c.n, c.C);
     const int64_t tiles = (c.n + tile - 1) / tile * rows.tiles;
-    GAS_TRY((!two ? launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s) : c.temperature == 2.f ? launch_logits<LOGITS_STATS, 4>(a, tile, tiles, c.s)
+    if (few) GAS_TRY(launch_few(c, common, two ? a.inv_t : 0.f, z, &parts));
+    else GAS_TRY((!two ? launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s) : c.temperature == 2.f ? launch_logits<LOGITS_STATS, 4>(a, tile, tiles, c.s)
                                                                          : launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s)));
     const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
-                        c.temperature, loss, lse};
+                        c.temperature, loss, lse, z, round_up(c.C, 256), rows.labels, rows.entries, rows.k};
     // few rows: more threads for each
     if (c.n <= 2048) hipLaunchKernelGGL(classes_loss_kernel<4>, dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, c.s, l);
     else hipLaunchKernelGGL(classes_loss_kernel<16>, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
@@ -829,7 +914,10 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     rows.nfw = (int32_t)((common.layer.fp + fx - 1) / fx);
     rows.nfx = rows.once ? (int32_t)((common.layer.fp + 255) / 256) : rows.nfw;
     rows.steps_of = common.layer.terms;
-    GAS_TRY(run_rows(c, common, rows, distill));
+    const bool few = c.n <= kRowsByVector;
+    float* z = few ? room.take<float>(kRowsByVector * (int64_t)round_up(c.C, 256)) : nullptr;
+    GAS_TRY(run_rows(c, common, rows, distill, true));
+    if (few) GAS_TRY(launch_few(c, common, 0.f, z, nullptr));
     const Layer& l = common.layer;
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.g = b.g;
@@ -846,7 +934,12 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         a.piece = d.piece = p;
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
-        GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
+        if (few) {
+            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 256)), dim3(256), 0, c.s, a, z, cols_most);
+            GAS_CHECK_HIP(hipGetLastError());
+        } else {
+            GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
+        }
         if (g.gx && rows.once) GAS_TRY(c.dt == GAS_BF16 ? launch_gx_once<GxOnce<true>>(d, c.s) : launch_gx_once<GxOnce<false>>(d, c.s));
         if ((g.gx && !rows.once) || g.gw) {
             const auto launch = fx == 64 ? launch_products<Gx64, Gw64> : fx == 128 ? launch_products<Gx128, Gw128> : fx == 192 ? launch_products<Gx192, Gw192>
@@ -892,6 +985,7 @@ int64_t workspace_of(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k, b
     lay_out_rows(room, c, common, k > 0);
     if (bwd) lay_out_backward(room, common, n, true, true, true);
     else lay_out_parts(room, common, k > 0);
+    if (n <= kRowsByVector) room.take<float>(kRowsByVector * round_up(C, 256));
     return room.used;
 }
 

@@ -12,6 +12,7 @@
 // A logit and its class make one whole number, larger for larger logits and, of equal ones, for lower classes, so the numbers of a
 // row differ and any order of work finds the same k. A NaN counts as less than every number.
 #include "classes_logits.h"
+#include "classes_vector.h"
 
 namespace gas {
 namespace {
@@ -21,7 +22,7 @@ constexpr int kBuffer = 2048;                     // numbers that a workgroup ho
 constexpr int kFirstPiece = 4096;                 // classes
 constexpr int kGrowth = 7;                        // of a piece, to all before
 constexpr int64_t kTopElements = 1LL << 29;       // of a piece
-constexpr int kFewRows = 64, kRowsByVector = 8;
+constexpr int kFewRows = 64;
 
 __device__ __forceinline__ uint64_t key_of(float z, int c) {
     const uint32_t b = __float_as_uint(z == 0.f ? 0.f : z);
@@ -261,137 +262,6 @@ __global__ __launch_bounds__(256) void classes_pick_kernel(PickArgs a) {
     if (a.floor && tid == 0) a.floor[row] = logit_of(buf[a.k - 1]);
 }
 
-// ---- logits of up to R rows by the vector units
-
-struct VectorArgs {
-    const void *X, *W, *bias;
-    int64_t ldx, ldw, ldz, most;
-    int32_t n, F, C;
-    float* z;                     // [n][ldz]
-    Parts parts;                  // `most` NULL: not asked for
-};
-
-// A workgroup 256 classes, four a lane; its eight wavefronts take every eighth row of W, sixteen rows of it under way at a time, and their sums
-// are added up through LDS. Rows of W need no alignment beyond their elements'.
-template <bool BF, int R>
-__global__ __launch_bounds__(512) void classes_vector_kernel(VectorArgs a) {
-    typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-    typedef float f32x4_here __attribute__((ext_vector_type(4), aligned(4)));
-    constexpr int kChunk = 512, U = 16;
-    __shared__ __attribute__((aligned(16))) float xs[kChunk * R];
-    __shared__ __attribute__((aligned(16))) float sums[2][8][256];
-    __shared__ float stats[2][2][4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int c0 = blockIdx.x * 256 + 4 * lane, at = c0 + 4 <= a.C ? c0 : (a.C >= 4 ? a.C - 4 : 0);    // the last whole four where these are not
-    float acc[R][4];
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[r][e] = 0.f;
-    struct Four { float v[4]; };
-    auto load = [&](int f) {
-        Four w;
-        if (a.C < 4) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t i = (int64_t)f * a.ldw + (e < a.C ? e : 0);
-                w.v[e] = BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.W)[i] << 16) : static_cast<const float*>(a.W)[i];
-            }
-        } else if constexpr (BF) {
-            const u32x2_any v = *reinterpret_cast<const u32x2_any*>(static_cast<const uint16_t*>(a.W) + (int64_t)f * a.ldw + at);
-            w = Four{bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1])};
-        } else {
-            const f32x4_here v = *reinterpret_cast<const f32x4_here*>(static_cast<const float*>(a.W) + (int64_t)f * a.ldw + at);
-            w = Four{v[0], v[1], v[2], v[3]};
-        }
-        return w;
-    };
-    auto use = [&](const Four& w, int i) {                // i: of the row of W in the chunk
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float x = xs[i * R + r];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(x, w.v[e], acc[r][e]);
-        }
-    };
-    for (int f0 = 0; f0 < a.F; f0 += kChunk) {
-        const int fs = a.F - f0 < kChunk ? a.F - f0 : kChunk;
-        __syncthreads();
-        for (int i = tid; i < fs * R; i += 512) {
-            const int r = i / fs, f = i % fs;
-            float x = 0.f;
-            if (r < a.n) {
-                const int64_t j = r * a.ldx + f0 + f;
-                x = BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.X)[j] << 16) : static_cast<const float*>(a.X)[j];
-            }
-            xs[f * R + r] = x;
-        }
-        __syncthreads();
-        int f = wave;
-        for (; f + 8 * (U - 1) < fs; f += 8 * U) {
-            Four w[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) w[u] = load(f0 + f + 8 * u);
-#pragma unroll
-            for (int u = 0; u < U; ++u) use(w[u], f + 8 * u);
-        }
-        for (; f < fs; f += 8) use(load(f0 + f), f);
-    }
-#pragma unroll
-    for (int r0 = 0; r0 < R; r0 += 2) {                   // two rows at a time: 256 threads each
-        if (r0 >= a.n) break;
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (r0 + h < R) {
-                if (at == c0) *reinterpret_cast<f32x4*>(&sums[h][wave][4 * lane]) = f32x4{acc[(r0 + h) % R][0], acc[(r0 + h) % R][1], acc[(r0 + h) % R][2], acc[(r0 + h) % R][3]};
-                else
-                    for (int e = 0; e < 4; ++e)
-                        if (at + e >= c0 && at + e < a.C) sums[h][wave][at + e - blockIdx.x * 256] = acc[(r0 + h) % R][e];
-            }
-        __syncthreads();
-        const int h = tid >> 8, t = tid & 255, r = r0 + h, c = blockIdx.x * 256 + t;
-        const bool on = r < a.n && r < R && c < a.C;
-        float z = -INFINITY;
-        if (on) {
-            z = 0.f;
-#pragma unroll
-            for (int w = 0; w < 8; ++w) z += sums[h][w][t];
-            if (a.bias) z += BF ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.bias)[c] << 16) : static_cast<const float*>(a.bias)[c];
-            a.z[r * a.ldz + c] = z;
-        }
-        if (a.parts.most) {
-            float most = z;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
-            if (lane == 0) stats[0][h][wave & 3] = most;
-            __syncthreads();
-            most = fmaxf(fmaxf(stats[0][h][0], stats[0][h][1]), fmaxf(stats[0][h][2], stats[0][h][3]));
-            most = fmaxf(most * kLog2e, kLeastExponent);
-            float sum = exp2_of(fmaf(z, kLog2e, -most));
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-            if (lane == 0) stats[1][h][wave & 3] = sum;
-            __syncthreads();
-            if (t == 0 && r < a.n && r < R) {
-                a.parts.most[blockIdx.x * a.most + r] = most;
-                a.parts.sum[blockIdx.x * a.most + r] = stats[1][h][0] + stats[1][h][1] + stats[1][h][2] + stats[1][h][3];
-            }
-        }
-    }
-}
-
-template <bool BF>
-gas_status launch_vector(const VectorArgs& a, hipStream_t s) {
-    const dim3 grid((unsigned)((a.C + 255) / 256)), block(512);
-    if (a.n == 1) hipLaunchKernelGGL((classes_vector_kernel<BF, 1>), grid, block, 0, s, a);
-    else if (a.n == 2) hipLaunchKernelGGL((classes_vector_kernel<BF, 2>), grid, block, 0, s, a);
-    else if (a.n <= 4) hipLaunchKernelGGL((classes_vector_kernel<BF, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((classes_vector_kernel<BF, 8>), grid, block, 0, s, a);
-    GAS_CHECK_HIP(hipGetLastError());
-    return GAS_OK;
-}
-
 // ---- lse of every row: its tiles' statistics joined, by 256 / ROWS threads a row, in a fixed tree
 template <int ROWS>
 __global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t most_rows, int64_t n, int tiles, float* lse) {
@@ -494,7 +364,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     const int tiles = (int)(cp / kTileC);
     PickArgs pick = {t.z, nullptr, t.width, n_classes, n_classes, 1, k, t.best, nullptr, nullptr, nullptr, ld_ids, ld_values};
     if (n_rows <= kRowsByVector) {
-        VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.most, (int32_t)n_rows, F, n_classes, t.z, {}};
+        VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.most, nullptr, nullptr, (int32_t)n_rows, F, n_classes, 0.f, t.z, {}};
         if (lse) v.parts = t.parts;
         st = dt == GAS_BF16 ? launch_vector<true>(v, s) : launch_vector<false>(v, s);
         if (st != GAS_OK) return st;

@@ -133,6 +133,31 @@ def test_strides_and_alignments(dtype, ld, off):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("n", [1, 2, 4, 7])
+@pytest.mark.parametrize("ld, off", [((40, 304), (0, 0)), ((41, 301), (1, 3)), ((200, 1000), (5, 8))])
+def test_few_rows_of_any_alignment(dtype, n, ld, off):
+    s, _ = make(n, 37, 296, dtype, ld=ld, off=off, labelled=1.0)
+    plain, _ = make(n, 37, 296, dtype, labelled=1.0)
+    got, want = forward(s), forward(plain)
+    assert all(torch.equal(got[k], want[k]) for k in got)
+    got, want = (backward(v, want["lse"], dtype) for v in (s, plain))
+    assert all(torch.equal(got[k], want[k]) for k in got)
+
+
+@pytest.mark.parametrize("n", [8, 40])
+@pytest.mark.parametrize("dtype, gw", [("f32", "f32"), ("bf16", "bf16")])
+def test_few_rows_of_more_classes_than_a_piece_has(dtype, gw, n):
+    """2^21 of them are a piece where the rows are at most 256."""
+    s, _ = make(n, 2, 2 ** 21 + 300, dtype)
+    lse = forward(s)["lse"]
+    got = backward(s, lse, dtype, gw)
+    x, w = wide(s["x"]), wide(s["w"])
+    g, off = R.grad_at_logits(x, w, wide(s["bias"]), wide(lse), wide(s["labels"]), None)
+    for name, want in R.gradients(x, w, g, off, 0.37, dtype == "bf16", gw == "bf16").items():
+        check(got[name], want, name)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 def test_any_gradient_alone(dtype):
     s, _ = make(150, 70, 600, dtype)
     lse = forward(s)["lse"]
@@ -144,7 +169,7 @@ def test_any_gradient_alone(dtype):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
-@pytest.mark.parametrize("n", [50, 270])
+@pytest.mark.parametrize("n", [6, 50, 270])
 def test_rows_without_a_label(dtype, n):
     """NaN and infinities in them reach nothing; none labelled at all gives zeros."""
     s, _ = make(n, 70, 600, dtype, labelled=0.5)
