@@ -614,6 +614,7 @@ struct SumArgs {
     const float* part_b;          // [row tiles][C up to 256]
     float* gbias;
     int32_t tile_rows;            // of those row tiles
+    int32_t lanes;                // a wavefront's lanes that share a sum of gx: few rows come in up to 512 parts
     uint32_t w_blocks, x_blocks;  // workgroups for gw of this piece, for gx, then one for every 256 of gbias
 };
 
@@ -651,14 +652,20 @@ __global__ __launch_bounds__(256) void classes_sums_kernel(SumArgs a) {
         const int n4 = (l.F + 3) / 4;
         const bool whole = fours(a.gx, a.ldgx, a.gx_bf16);
         const int64_t total = a.n * n4, step = (int64_t)s.rows * l.fp / 4;
-        for (int64_t q = (int64_t)block * 256 + threadIdx.x; q < total; q += (int64_t)a.x_blocks * 256) {
+        const int part = (int)threadIdx.x & (a.lanes - 1);
+        for (int64_t q = ((int64_t)block * 256 + threadIdx.x) / a.lanes; q < total; q += (int64_t)a.x_blocks * 256 / a.lanes) {
             int64_t i;
             int f;
             row_of(q, total, n4, i, f);
             f *= 4;
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
             const int64_t r = a.pos[i];
-            if (r >= 0) v = sum_of(reinterpret_cast<const f32x4*>(a.g.part_x + r * l.fp + f), step, shape.splits_x, v);
+            if (r >= 0 && part < shape.splits_x)
+                v = sum_of(reinterpret_cast<const f32x4*>(a.g.part_x + r * l.fp + f) + part * step, step * a.lanes, (shape.splits_x - 1 - part) / a.lanes + 1, v);
+            for (int o = a.lanes / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] += __shfl_xor(v[e], o);
+            if (part > 0) continue;
             v *= a.g.scale;
             put4(a.gx, i * a.ldgx + f, v, l.F - f < 4 ? l.F - f : 4, a.gx_bf16, whole && f + 4 <= l.F);
         }
@@ -949,9 +956,9 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
             GAS_TRY(launch(both, rows_most, cols_most, c.s));
         }
         const bool last = p + 1 == pieces;
-        SumArgs sums = {d, common.pos, c.n, g.ldgx, g.gx, c.dt == GAS_BF16, b.gbias, g.gbias, tile, 0, 0};
+        SumArgs sums = {d, common.pos, c.n, g.ldgx, g.gx, c.dt == GAS_BF16, b.gbias, g.gbias, tile, rows.once ? 32 : 1, 0, 0};
         if (g.gw) sums.w_blocks = blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048);
-        if (g.gx && last) sums.x_blocks = blocks_for(c.n * ((c.F + 3) / 4), 256, 4096);
+        if (g.gx && last) sums.x_blocks = blocks_for(c.n * ((c.F + 3) / 4), 256 / sums.lanes, 4096);
         const unsigned blocks = sums.w_blocks + sums.x_blocks + (g.gbias && last ? (unsigned)((c.C + 255) / 256) : 0u);
         if (blocks == 0) continue;
         hipLaunchKernelGGL(classes_sums_kernel, dim3(blocks), dim3(256), 0, c.s, sums);
