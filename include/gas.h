@@ -476,9 +476,10 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * The output layer over many classes, without its logits: with X [n_rows, F], W [F, n_classes] and bias [n_classes] (or NULL) of type dt,
  *     z_i = X[i] W + bias
  * is formed a tile at a time on the matrix cores, used, and dropped.  Products are summed in fp32 (fp32 operands by three bf16 parts each,
- * as in gas_linear), statistics of a row and sums over rows are fp32.  F up to 65536, n_classes up to 4194304; the calls are meant for
+ * as in gas_linear), statistics of a row and sums over rows are fp32.  F up to 65536, n_classes up to 4194304, n_rows up to 2^25 (gas_linear_top 2^23); the calls are meant for
  * classes by the thousand (for a few dozen gas_linear and gas_softmax_xent take less).  A bias of -infinity takes a class out: its
- * probability is 0.  An infinity or NaN of X stays in its row, one of W makes its class's logits NaN.
+ * probability is 0.  An infinity or NaN of X stays in its row, one of W makes its class's logits
+ * infinite or NaN, and what sums over them NaN or, where they are -infinity, without that class.
  *
  * gas_linear_xent: cross-entropy of the rows with a label, 0 <= labels[i] < n_classes:
  *     lse[i] = log sum_c exp z_ic,   loss_rows[i] = lse[i] - z_{i, labels[i]};   rows without one: 0 and 0, at no cost.
@@ -505,9 +506,10 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
  *
  * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
- * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X and, unless W
- * is bf16 with 16-byte aligned rows of whole 16-byte pieces, W as the products take them; statistics of every 256 classes;
- * backward a piece of G, 1 GB (fp32: 3.2 GB) or 256 classes of it if they are more.
+ * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X and, for more than
+ * 64 rows, W as the products take them (not W where it is bf16 with 16-byte aligned rows of whole 16-byte pieces: that is read as it lies, as
+ * for up to 64 rows every W is); statistics of every 256 classes; backward a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it,
+ * or 256 classes of it if they are more; gas_linear_top the logits of up to 64 rows, of more rows those of a piece, 2 GB or 4,096 classes.
  */
 GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
 GAS_API gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,

@@ -14,6 +14,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kTileC = 256;                       // classes of a tile
 constexpr int kMaxClasses = 1 << 22;              // a tile's 256 rows of W then lie within 4 GB
 constexpr int kMaxWidth = 1 << 16;
+constexpr int64_t kMaxRows = 1 << 25;             // a launch of 64 threads a row
 constexpr int kReadOnceRows = 64;                 // up to so many rows W is not packed
 constexpr int kMaxEntries = 256;                  // of a teacher's row
 constexpr int kHeldEntries = 2;                   // of a row in one tile that are fetched before the products
@@ -235,7 +236,8 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     const int64_t most = round_up(n, 256), fp = round_up(F, 64), cp = round_up(C, kTileC);
     // W where it lies if its rows can be read in whole pieces
     const bool in_place = dt == GAS_BF16 && C % 8 == 0 && ldw % 8 == 0 && ldw <= kMaxClasses && aligned16(W);
-    // and also, by kernels of their own, where it is used for few rows: packed first, 32 x 2,048 x 131,072 of fp32 took ...
+    // and also, by kernels of their own, where it is used for few rows: gradients of
+    // 5 x 64 x 125,838 of fp32 took 121 us, W packed first 382
     const bool once = !in_place && n <= kReadOnceRows;
     const int64_t cw = in_place ? C : round_up(C, 64);
     c.layer.terms = dt == GAS_F32 ? 6 : 1;
@@ -277,7 +279,7 @@ inline gas_status run_pack(const Common& c, gas_dtype dt, hipStream_t s) {
 inline gas_status check_layer(const char* who, const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t C,
                               gas_dtype dt) {
     if (!valid_dtype(dt)) return fail(GAS_ERR_DTYPE, "%s: unknown dtype %d", who, (int)dt);
-    GAS_REQUIRE(n_rows >= 0 && n_rows <= (1 << 28), "%s: n_rows=%lld, at most 2^28 are taken", who, (long long)n_rows);
+    GAS_REQUIRE(n_rows >= 0 && n_rows <= kMaxRows, "%s: n_rows=%lld, at most 2^25 are taken", who, (long long)n_rows);
     GAS_REQUIRE(F > 0 && F <= kMaxWidth, "%s: F=%d, 1 to 65536 are taken", who, F);
     GAS_REQUIRE(C > 0 && C <= kMaxClasses, "%s: n_classes=%d, 1 to 4194304 are taken", who, C);
     if (n_rows == 0) return GAS_OK;

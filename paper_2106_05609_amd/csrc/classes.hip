@@ -480,7 +480,7 @@ __device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint3
     const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
     product.run(oa, ob, first * (kStepK / P::kStepOf), last * (kStepK / P::kStepOf), l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     // A lane has classes of 32 inputs' rows, memory wants a row's next to each other: through 32 rows of 64 classes of LDS that belong to the
-    // wavefront (stored as they came, rows of no whole pieces took two bytes from every lane to a row of its own: ...).
+    // wavefront (stored as they came, rows of no whole pieces took two bytes from every lane to a row of its own).
     const bool whole = fours(a.gw, a.ldgw, a.gw_bf16) && s.first + c0 + 256 <= s.first + s.cols;
     float* mine = reinterpret_cast<float*>(smem) + wave * (32 * 64);
     static_assert(P::T / 64 * 32 * 64 * 4 <= P::kLdsBytes && P::TA % 2 == 0, "the wavefronts' pieces fit where operands were");
@@ -983,7 +983,7 @@ gas_status zero(void* p, int64_t ld, int64_t rows, int64_t cols, int bytes, hipS
 
 // bytes of a call, for the widest that its arguments allow
 int64_t workspace_of(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k, bool bwd) {
-    if (n < 0 || n > (1 << 28) || F <= 0 || F > kMaxWidth || C <= 0 || C > kMaxClasses || k < 0 || k > kMaxEntries || !valid_dtype(dt)) return -1;
+    if (n < 0 || n > kMaxRows || F <= 0 || F > kMaxWidth || C <= 0 || C > kMaxClasses || k < 0 || k > kMaxEntries || !valid_dtype(dt)) return -1;
     if (n == 0) return 0;
     Room room{nullptr};
     Call c = {};

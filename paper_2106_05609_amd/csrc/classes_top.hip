@@ -23,6 +23,7 @@ constexpr int kFirstPiece = 4096;                 // classes
 constexpr int kGrowth = 7;                        // of a piece, to all before
 constexpr int64_t kTopElements = 1LL << 29;       // of a piece
 constexpr int kFewRows = 64;
+constexpr int64_t kMostRows = 1 << 23;            // a launch of 256 threads a row
 
 __device__ __forceinline__ uint64_t key_of(float z, int c) {
     const uint32_t b = __float_as_uint(z == 0.f ? 0.f : z);
@@ -321,7 +322,7 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
 }
 
 int64_t top_workspace(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k) {
-    if (n < 0 || n > (1 << 28) || F <= 0 || F > kMaxWidth || C <= 0 || C > kMaxClasses || k <= 0 || k > kMostTop || k > C || !valid_dtype(dt)) return -1;
+    if (n < 0 || n > kMostRows || F <= 0 || F > kMaxWidth || C <= 0 || C > kMaxClasses || k <= 0 || k > kMostTop || k > C || !valid_dtype(dt)) return -1;
     if (n == 0) return 0;
     Room room{nullptr};
     lay_out_top(room, nullptr, F, n, F, reinterpret_cast<const void*>(2), C, C, nullptr, dt, k);
@@ -345,6 +346,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     const char* who = "gas_linear_top";
     gas_status st = check_layer(who, X, ldx, n_rows, F, W, ldw, n_classes, dt);
     if (st != GAS_OK) return st;
+    GAS_REQUIRE(n_rows <= kMostRows, "%s: n_rows=%lld, at most 2^23 are taken", who, (long long)n_rows);
     GAS_REQUIRE(k > 0 && k <= kMostTop && k <= n_classes, "%s: k=%d of %d classes, 1 to 128 are taken", who, k, n_classes);
     if (n_rows == 0) return GAS_OK;
     GAS_REQUIRE(ids && values, "%s: null pointer", who);

@@ -149,6 +149,9 @@ def test_workspaces_are_known_for_what_calls_take():
         assert gas.gas_linear_distill_workspace(N, F, C, torch.float32, k) == -1
     for k in (0, 129, C + 1):
         assert gas.gas_linear_top_workspace(N, F, C, torch.float32, k) == -1
+    # a launch's threads are counted in 32 bits
+    assert gas.gas_linear_xent_workspace(2 ** 25, 1, 2, torch.float32) > 0 > gas.gas_linear_xent_workspace(2 ** 25 + 1, 1, 2, torch.float32)
+    assert gas.gas_linear_top_workspace(2 ** 23, 1, 2, torch.float32, 1) > 0 > gas.gas_linear_top_workspace(2 ** 23 + 1, 1, 2, torch.float32, 1)
     # the logits are not in it: less than they take, from a few thousand classes and rows on
     for dt, eb in ((torch.float32, 4), (torch.bfloat16, 2)):
         n, c = 100_000, 500_000
