@@ -206,6 +206,20 @@ __device__ __forceinline__ float log_of(float most, float sum, float inv_t) {
     return (float)((double)most * (double)inv_t / (double)kLog2e + (double)logf(sum));
 }
 
+// v[0], v[step], ... n of them one after another, eight under way at a time
+template <class V>
+__device__ __forceinline__ V sum_of(const V* v, int64_t step, int n, V sum) {
+    for (int p = 0; p < n; p += 8) {
+        V part[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) part[u] = v[(p + u < n ? p + u : p) * step];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (p + u < n) sum += part[u];
+    }
+    return sum;
+}
+
 inline unsigned blocks_for(int64_t items, int64_t per, int64_t most) {
     const int64_t b = (items + per - 1) / per;
     return (unsigned)(b < 1 ? 1 : (b < most ? b : most));

@@ -8,8 +8,7 @@
 // joins.  Backward: a piece of the classes at a time, the gradient at its logits (formed again from the products) is stored in the
 // products' type and multiplied by W and X.
 
-#include "classes_logits.h"
-#include "classes_vector.h"
+#include "classes_split.h"
 
 namespace gas {
 namespace {
@@ -530,80 +529,76 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
     else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
-// ---- backward: the gradient at the logits of few rows, 256 classes of the piece a workgroup, two of every other row a thread
-__global__ __launch_bounds__(256) void classes_grad_few_kernel(LogitsArgs a, const float* z, int64_t ldz) {
-    __shared__ float sums[256];
+// ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two of every eighth row a thread
+__global__ __launch_bounds__(256) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
+    __shared__ float sums[8][64];
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
     const Layer& l = a.layer;
-    const int count = l.shape->count, width = l.shape->width, tid = threadIdx.x, c0 = (int)(blockIdx.x * 256);
-    if (c0 >= width || (int64_t)a.piece * width + c0 >= ldz) return;
-    const int pair = 2 * (tid & 127), half = tid >> 7, planes = l.terms > 1 ? 3 : 1;
-    const int64_t c = (int64_t)a.piece * width + c0 + pair;
-    float sum[2] = {0.f, 0.f};
-    for (int r = half; r < count; r += 2) {
-        const f32x4 info = a.info[r];
-        const int label = a.labels ? a.labels[r] : -1;
-        int from = 0, to = 0;
-        if (!a.labels) {
-            const uint16_t* s = a.starts + (int64_t)r * (a.tiles + 1) + c / 256;
-            from = s[0];
-            to = s[1];
-        }
-        float g[2];
+    const int count = l.shape->count, width = l.shape->width, tid = threadIdx.x, in = (int)(blockIdx.x * 64) + 2 * (tid & 31), group = tid >> 5;
+    const int64_t c = (int64_t)a.piece * width + in;
+    const int r0 = (int)blockIdx.y * 64;
+    if ((int)(blockIdx.x * 64) >= width || c >= from.ld || r0 >= count) return;       // whole workgroups: widths are of whole tiles
+    f32x2 z[8], sum = {0.f, 0.f}, bias = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            g[j] = 0.f;
-            if (c + j >= l.C) continue;
-            const float v = z[r * ldz + c + j];
-            if (a.labels || info[2] != 0.f) g[j] = info[2] * exp2_of((v - info[0]) * kLog2e);
-            if (!a.labels && info[3] != 0.f) g[j] = fmaf(info[3], exp2_of((v * a.inv_t - info[1]) * kLog2e), g[j]);
-            if (c + j == label) g[j] -= info[2];
-        }
-        for (int e = from; e < to; ++e) {
-            const int2 one = a.entries[(int64_t)r * a.k + e];
+    for (int j = 0; j < 8; ++j) z[j] = f32x2{0.f, 0.f};
+    for (int s = 0; s < from.splits; ++s)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                if (one.x == c + j) g[j] -= __int_as_float(one.y);
+        for (int j = 0; j < 8; ++j) {
+            const int r = r0 + group + 8 * j;
+            if (r < count) z[j] += *reinterpret_cast<const f32x2*>(from.p + s * from.step + r * from.ld + c);
+        }
+    if (from.bias) bias = *reinterpret_cast<const f32x2*>(from.bias + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int r = r0 + group + 8 * j;
+        float g[2] = {0.f, 0.f};                               // rows up to 64 are read later on: zero beyond those that count
+        if (r < count) {
+            const f32x4 info = a.info[r];
+            const int label = a.labels ? a.labels[r] : -1;
+            int e = 0, end = 0;
+            if (!a.labels) {
+                const uint16_t* s = a.starts + (int64_t)r * (a.tiles + 1) + c / kTileC;
+                e = s[0];
+                end = s[1];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (c + i >= l.C) continue;
+                const float v = z[j][i] + bias[i];
+                if (a.labels || info[2] != 0.f) g[i] = info[2] * exp2_of((v - info[0]) * kLog2e);
+                if (!a.labels && info[3] != 0.f) g[i] = fmaf(info[3], exp2_of((v * a.inv_t - info[1]) * kLog2e), g[i]);
+                if (c + i == label) g[i] -= info[2];
+            }
+            for (; e < end; ++e) {
+                const int2 one = a.entries[(int64_t)r * a.k + e];
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    if (one.x == c + i) g[i] -= __int_as_float(one.y);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 2; ++j) sum[j] += g[j];
+        for (int i = 0; i < 2; ++i) sum[i] += g[i];
         uint32_t part[3];
         split_pair(g[0], g[1], part[0], part[1], part[2]);
-        uint16_t* at = a.g + (int64_t)r * width + c0 + pair;
+        uint16_t* at = a.g + (int64_t)r * width + in;
         *reinterpret_cast<uint32_t*>(at) = part[0];
-        if (planes > 1) {
+        if (l.terms > 1) {
             *reinterpret_cast<uint32_t*>(at + a.g_plane) = part[1];
             *reinterpret_cast<uint32_t*>(at + 2 * a.g_plane) = part[2];
         }
     }
-    // rows up to 64 are read later on
-    for (int r = count + (tid >> 5); r < 64; r += 8)
-        for (int p = 0; p < planes; ++p) *reinterpret_cast<u32x4*>(a.g + p * a.g_plane + (int64_t)r * width + c0 + 8 * (tid & 31)) = u32x4{0, 0, 0, 0};
     if (!a.gbias) return;
-    if (half) {
-        sums[pair] = sum[0];
-        sums[pair + 1] = sum[1];
-    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sums[group][2 * (tid & 31) + i] = sum[i];
     __syncthreads();
-    if (half) return;
-    a.gbias[c] = sum[0] + sums[pair];
-    a.gbias[c + 1] = sum[1] + sums[pair + 1];
+    if (tid >= 64) return;
+    float v = 0.f;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) v += sums[g][tid];
+    a.gbias[blockIdx.y * from.ld + (int64_t)a.piece * width + blockIdx.x * 64 + tid] = v;
 }
 
 // ---- backward: what came in parts, added up
-
-// v[0], v[step], ... n of them one after another, eight under way at a time
-template <class V>
-__device__ __forceinline__ V sum_of(const V* v, int64_t step, int n, V sum) {
-    for (int p = 0; p < n; p += 8) {
-        V part[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) part[u] = v[(p + u < n ? p + u : p) * step];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-            if (p + u < n) sum += part[u];
-    }
-    return sum;
-}
 
 struct SumArgs {
     GradArgs g;
@@ -789,18 +784,21 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     const RowsArgs rows = lay_out_rows(room, c, common, distill);
     const Parts parts = lay_out_parts(room, common, distill);
     const bool few = c.n <= kRowsByVector;
-    float* z = few ? room.take<float>(kRowsByVector * (int64_t)round_up(c.C, 256)) : nullptr;
+    const FewRoom f = lay_out_few(room, c.n, c.F, c.C, c.dt, true);
     GAS_TRY(run_rows(c, common, rows, distill, !few));
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.parts = parts;
     const bool two = distill && c.temperature != 1.f;
     const int tile = rows_of_tile(c.n, c.C);
     const int64_t tiles = (c.n + tile - 1) / tile * rows.tiles;
-    if (few) GAS_TRY(launch_few(c, common, two ? a.inv_t : 0.f, z, &parts));
-    else GAS_TRY((!two ? launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s) : c.temperature == 2.f ? launch_logits<LOGITS_STATS, 4>(a, tile, tiles, c.s)
+    if (few) GAS_TRY(launch_few(c, common, two ? a.inv_t : 0.f, f.z, &parts));
+    else if (f.splits > 1) {
+        GAS_TRY(launch_split(common.layer, f, c.n, c.s));
+        GAS_TRY(launch_join(common.layer, f, c.n, two ? a.inv_t : 0.f, &parts, c.s));
+    } else GAS_TRY((!two ? launch_logits<LOGITS_STATS, 1>(a, tile, tiles, c.s) : c.temperature == 2.f ? launch_logits<LOGITS_STATS, 4>(a, tile, tiles, c.s)
                                                                          : launch_logits<LOGITS_STATS, 3>(a, tile, tiles, c.s)));
     const LossArgs l = {common.layer, parts, common.pos, distill ? rows.info : nullptr, rows.entropy, c.n, rows.tiles, two, a.inv_t,
-                        c.temperature, loss, lse, z, round_up(c.C, 256), rows.labels, rows.entries, rows.k};
+                        c.temperature, loss, lse, f.z, f.ld, rows.labels, rows.entries, rows.k};
     // few rows: more threads for each
     if (c.n <= 2048) hipLaunchKernelGGL(classes_loss_kernel<4>, dim3((unsigned)((c.n + 3) / 4)), dim3(256), 0, c.s, l);
     else hipLaunchKernelGGL(classes_loss_kernel<16>, dim3((unsigned)((c.n + 15) / 16)), dim3(256), 0, c.s, l);
@@ -921,10 +919,15 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     rows.nfw = (int32_t)((common.layer.fp + fx - 1) / fx);
     rows.nfx = rows.once ? (int32_t)((common.layer.fp + 255) / 256) : rows.nfw;
     rows.steps_of = common.layer.terms;
-    const bool few = c.n <= kRowsByVector;
-    float* z = few ? room.take<float>(kRowsByVector * (int64_t)round_up(c.C, 256)) : nullptr;
+    const FewRoom f = lay_out_few(room, c.n, c.F, c.C, c.dt, false);
+    PartsOfZ z = {f.parts, f.ld, f.step, f.splits, common.layer.bias};
     GAS_TRY(run_rows(c, common, rows, distill, true));
-    if (few) GAS_TRY(launch_few(c, common, 0.f, z, nullptr));
+    if (f.z) {
+        GAS_TRY(launch_few(c, common, 0.f, f.z, nullptr));
+        z = PartsOfZ{f.z, f.ld, 0, 1, nullptr};
+    } else if (f.parts) {
+        GAS_TRY(launch_split(common.layer, f, c.n, c.s));
+    }
     const Layer& l = common.layer;
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.g = b.g;
@@ -941,8 +944,8 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         a.piece = d.piece = p;
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
-        if (few) {
-            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 256)), dim3(256), 0, c.s, a, z, cols_most);
+        if (z.p) {
+            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 64), (unsigned)((c.n + 63) / 64)), dim3(256), 0, c.s, a, z);
             GAS_CHECK_HIP(hipGetLastError());
         } else {
             GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
@@ -992,7 +995,7 @@ int64_t workspace_of(int64_t n, int32_t F, int32_t C, gas_dtype dt, int32_t k, b
     lay_out_rows(room, c, common, k > 0);
     if (bwd) lay_out_backward(room, common, n, true, true, true);
     else lay_out_parts(room, common, k > 0);
-    if (n <= kRowsByVector) room.take<float>(kRowsByVector * round_up(C, 256));
+    lay_out_few(room, n, F, C, dt, !bwd);
     return room.used;
 }
 

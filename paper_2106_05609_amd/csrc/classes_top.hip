@@ -11,8 +11,7 @@
 //
 // A logit and its class make one whole number, larger for larger logits and, of equal ones, for lower classes, so the numbers of a
 // row differ and any order of work finds the same k. A NaN counts as less than every number.
-#include "classes_logits.h"
-#include "classes_vector.h"
+#include "classes_split.h"
 
 namespace gas {
 namespace {
@@ -302,6 +301,7 @@ struct TopRoom {
     uint32_t* mask;
     uint64_t *best, *other;
     int64_t width;
+    FewRoom few;                  // parts of the first piece's sums
 };
 TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, const void* W, int64_t ldw, int C, const void* bias, gas_dtype dt,
                     int k) {
@@ -317,6 +317,8 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
+    t.few = lay_out_few(room, n, F, (int)(n <= kFewRows || t.width < kFirstPiece ? t.width : kFirstPiece), dt, false);
+    t.few.z = t.z;
     t.mask = room.take<uint32_t>(n * (t.width / 32));
     return t;
 }
@@ -390,7 +392,12 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
             a.width = (int32_t)width;
             a.all = first == 0;
             const int tile = rows_of_tile(n_rows, (int)width);
-            st = launch_logits<LOGITS_TOP, 1>(a, tile, (n_rows + tile - 1) / tile * (width / 256), s);
+            if (first == 0 && t.few.splits > 1) {
+                st = launch_split(a.layer, t.few, n_rows, s);
+                if (st == GAS_OK) st = launch_join(a.layer, t.few, n_rows, 0.f, lse ? &t.parts : nullptr, s);
+            } else {
+                st = launch_logits<LOGITS_TOP, 1>(a, tile, (n_rows + tile - 1) / tile * (width / 256), s);
+            }
             if (st != GAS_OK) return st;
             if (n_rows <= kFewRows) break;
             const bool last = first + width >= cp;

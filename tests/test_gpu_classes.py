@@ -12,7 +12,8 @@ pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 # rows, width, classes: one of everything, below and above a tile's sides, steps' and pieces' ends
 SIZES = [(1, 1, 1), (1, 1, 2), (2, 3, 5), (3, 64, 255), (5, 17, 256), (64, 8, 257), (65, 33, 511), (63, 64, 512), (64, 65, 1000), (130, 100, 777),
-         (255, 128, 264), (256, 129, 300), (257, 300, 513), (300, 1433, 264), (31, 2050, 97), (700, 40, 4001), (513, 256, 2056)]
+         (255, 128, 264), (256, 129, 300), (257, 300, 513), (300, 1433, 264), (31, 2050, 97), (700, 40, 4001), (513, 256, 2056),
+         (9, 1030, 600), (64, 2048, 263), (65, 700, 1000), (200, 1500, 2000)]
 
 
 def mat(values, dtype, ld=None, off=0):
@@ -345,7 +346,7 @@ def distill_forward(s, t, label_weight, labels=True):
 
 
 CASES = [(1, 4, 6, 1, 1.0, 0.5), (3, 5, 9, 4, 2.0, 0.3), (40, 33, 300, 7, 0.5, 0.0), (64, 64, 513, 64, 1.0, 1.0), (70, 20, 1000, 65, 3.0, 0.25),
-         (300, 65, 700, 100, 2.0, 0.5), (257, 128, 2600, 256, 1.0, 0.4), (20, 300, 4001, 255, 4.0, 0.9)]
+         (300, 65, 700, 100, 2.0, 0.5), (257, 128, 2600, 256, 1.0, 0.4), (20, 300, 4001, 255, 4.0, 0.9), (50, 900, 700, 30, 2.0, 0.5), (130, 1100, 520, 40, 1.5, 0.5)]
 
 
 @pytest.mark.parametrize("n, f, c, k, t, label_weight", CASES)
@@ -422,7 +423,8 @@ def top(s, k, lse=True):
 
 @pytest.mark.parametrize("n, f, c, k", [(1, 1, 1, 1), (1, 3, 7, 7), (2, 8, 128, 128), (5, 2, 256, 10), (1, 64, 5000, 50), (9, 30, 4096, 128), (64, 40, 4097, 1),
                                         (65, 16, 9000, 64), (300, 2, 20_000, 100), (31, 1, 30_001, 128), (8, 300, 12_289, 17), (16, 100, 4100, 33),
-                                        (17, 100, 4100, 33), (2, 512, 100_003, 10), (700, 33, 6001, 20)])
+                                        (17, 100, 4100, 33), (2, 512, 100_003, 10), (700, 33, 6001, 20), (20, 2048, 2000, 40), (100, 1000, 700, 64),
+                                        (100, 800, 9000, 64)])
 @pytest.mark.parametrize("dtype", list(DT))
 def test_top_logits(n, f, c, k, dtype):
     s = exact_layer(n, f, c, dtype)
