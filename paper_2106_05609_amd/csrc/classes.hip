@@ -48,13 +48,13 @@ __device__ __forceinline__ void number(const RowsArgs& a, int64_t i, int r) {
 // Parts of a sum whose tiles do not fill the card, each of two steps at least. A part more costs its 256 KB written and read again,
 // a fifteenth of a step's time on every unit; a round of tiles on all units some four steps beside its own.
 constexpr int kUnits = 256, kMostSplits = 32;
-__device__ __host__ inline int splits_of(int tiles, int steps, int steps_of) {
+__device__ __host__ inline int splits_of(int tiles, int steps, int steps_of, int units) {
     const int candidates[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, kMostSplits};
     int best = 1;
     int64_t least = 0;
     for (int s : candidates) {
-        if (s > 1 && (2 * s > steps || (int64_t)s * tiles > 2 * kUnits)) break;
-        const int64_t cost = 16LL * ((tiles * s + kUnits - 1) / kUnits) * ((steps + s - 1) / s * steps_of + 4) + (s > 1 ? (int64_t)s * tiles : 0);
+        if (s > 1 && (2 * s > steps || (int64_t)s * tiles > 2 * units)) break;
+        const int64_t cost = 16LL * ((tiles * s + units - 1) / units) * ((steps + s - 1) / s * steps_of + 4) + (s > 1 ? (int64_t)s * tiles : 0);
         if (s == 1 || cost < least) {
             best = s;
             least = cost;
@@ -73,8 +73,11 @@ __device__ __forceinline__ Shape shape_for(const RowsArgs& a, int count) {
     if (a.cap > 0) {
         const int rows = count > 0 ? (count + 255) / 256 * 256 : 256;
         s.width = piece_width(a.cap, rows, a.t.C);
-        s.splits_x = a.once ? splits_once(a.nfx, s.width / kStepK) : splits_of(rows / 256 * a.nfx, s.width / kStepK, a.steps_of);
-        s.splits_w = splits_of(s.width / 256 * a.nfw, rows / kStepK, a.steps_of);
+        // they run beside each other: half of the units for each where both could have a round of their own together
+        const int64_t tiles_x = (int64_t)rows / 256 * a.nfx, tiles_w = (int64_t)s.width / 256 * a.nfw;
+        const int units = !a.once && tiles_x + tiles_w <= kUnits / 2 ? kUnits / 2 : kUnits;
+        s.splits_x = a.once ? splits_once(a.nfx, s.width / kStepK) : splits_of((int)tiles_x, s.width / kStepK, a.steps_of, units);
+        s.splits_w = splits_of((int)tiles_w, rows / kStepK, a.steps_of, units);
     }
     return s;
 }
@@ -529,28 +532,25 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
     else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
-// ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two of every eighth row a thread
-__global__ __launch_bounds__(256) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
-    __shared__ float sums[8][64];
+// ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two classes of two rows a thread
+__global__ __launch_bounds__(1024) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
+    __shared__ float sums[32][64];
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     const Layer& l = a.layer;
     const int count = l.shape->count, width = l.shape->width, tid = threadIdx.x, in = (int)(blockIdx.x * 64) + 2 * (tid & 31), group = tid >> 5;
     const int64_t c = (int64_t)a.piece * width + in;
     const int r0 = (int)blockIdx.y * 64;
     if ((int)(blockIdx.x * 64) >= width || c >= from.ld || r0 >= count) return;       // whole workgroups: widths are of whole tiles
-    f32x2 z[8], sum = {0.f, 0.f}, bias = {0.f, 0.f};
+    f32x2 z[2], sum = {0.f, 0.f}, bias = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) z[j] = f32x2{0.f, 0.f};
-    for (int s = 0; s < from.splits; ++s)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int r = r0 + group + 8 * j;
-            if (r < count) z[j] += *reinterpret_cast<const f32x2*>(from.p + s * from.step + r * from.ld + c);
-        }
+    for (int j = 0; j < 2; ++j) {
+        const int r = r0 + group + 32 * j < count ? r0 + group + 32 * j : count - 1;
+        z[j] = sum_of(reinterpret_cast<const f32x2*>(from.p + r * from.ld + c), from.step / 2, from.splits, f32x2{0.f, 0.f});
+    }
     if (from.bias) bias = *reinterpret_cast<const f32x2*>(from.bias + c);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int r = r0 + group + 8 * j;
+    for (int j = 0; j < 2; ++j) {
+        const int r = r0 + group + 32 * j;
         float g[2] = {0.f, 0.f};                               // rows up to 64 are read later on: zero beyond those that count
         if (r < count) {
             const f32x4 info = a.info[r];
@@ -594,7 +594,7 @@ __global__ __launch_bounds__(256) void classes_grad_few_kernel(LogitsArgs a, Par
     if (tid >= 64) return;
     float v = 0.f;
 #pragma unroll
-    for (int g = 0; g < 8; ++g) v += sums[g][tid];
+    for (int g = 0; g < 32; ++g) v += sums[g][tid];
     a.gbias[blockIdx.y * from.ld + (int64_t)a.piece * width + blockIdx.x * 64 + tid] = v;
 }
 
@@ -783,8 +783,8 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     const Common common = lay_out(room, c.X, c.ldx, c.n, c.F, c.W, c.ldw, c.C, c.bias, c.dt, true);
     const RowsArgs rows = lay_out_rows(room, c, common, distill);
     const Parts parts = lay_out_parts(room, common, distill);
-    const bool few = c.n <= kRowsByVector;
     const FewRoom f = lay_out_few(room, c.n, c.F, c.C, c.dt, true);
+    const bool few = f.by_vector;
     GAS_TRY(run_rows(c, common, rows, distill, !few));
     LogitsArgs a = logits_args(c, common, rows, distill);
     a.parts = parts;
@@ -945,7 +945,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
         if (z.p) {
-            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 64), (unsigned)((c.n + 63) / 64)), dim3(256), 0, c.s, a, z);
+            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 64), (unsigned)((c.n + 63) / 64)), dim3(1024), 0, c.s, a, z);
             GAS_CHECK_HIP(hipGetLastError());
         } else {
             GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));

@@ -101,7 +101,9 @@ __global__ __launch_bounds__(256) void classes_join_kernel(JoinArgs a) {
 
 // Parts of the sums for which a tile's are worth it: two workgroups for every unit, of a few steps each. A step of fp32 takes as long as several.
 inline int splits_of_few(int64_t n, int F, int C, gas_dtype dt) {
-    if (n <= kRowsByVector || rows_of_tile(n, C) != 64) return 1;
+    if (rows_of_tile(n, C) != 64) return 1;
+    // the vector units are as fast for rows of W that are not so long, and there are enough classes: 3 x 2,048 x 600 of fp32 took them 34 us
+    if (n <= kRowsByVector && (F < 1024 || C > 32 * kTileC)) return 1;
     const int64_t tiles = (n + 63) / 64 * (round_up(C, kTileC) / kTileC), steps = round_up(F, FewRows::kStepOf) / FewRows::kStepOf / (dt == GAS_F32 ? 4 : 8);
     int64_t s = 512 / tiles;
     if (s > steps) s = steps;
@@ -109,16 +111,18 @@ inline int splits_of_few(int64_t n, int F, int C, gas_dtype dt) {
     return s < 2 ? 1 : (int)s;
 }
 
-// Room for the logits of few rows, or of parts of them: none if `z` is NULL.
+// Room for the logits of few rows, or for parts of them; neither if they are formed in tiles.
 struct FewRoom {
     float *z, *parts;
     int64_t ld, step;
     int32_t splits;
+    bool by_vector;               // up to eight rows, by the vector units
 };
 inline FewRoom lay_out_few(Room& room, int64_t n, int F, int C, gas_dtype dt, bool whole) {
-    FewRoom f = {nullptr, nullptr, round_up(C, kTileC), round_up(n, 64) * round_up(C, kTileC), splits_of_few(n, F, C, dt)};
+    FewRoom f = {nullptr, nullptr, round_up(C, kTileC), round_up(n, 64) * round_up(C, kTileC), splits_of_few(n, F, C, dt), false};
+    f.by_vector = n <= kRowsByVector && f.splits == 1;
     if (f.splits > 1) f.parts = room.take<float>(f.splits * f.step);
-    if (n <= kRowsByVector || (whole && f.splits > 1)) f.z = room.take<float>((n <= kRowsByVector ? kRowsByVector : round_up(n, 64)) * f.ld);
+    if (f.by_vector || (whole && f.splits > 1)) f.z = room.take<float>((f.by_vector ? kRowsByVector : round_up(n, 64)) * f.ld);
     return f;
 }
 

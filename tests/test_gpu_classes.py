@@ -13,7 +13,7 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 # rows, width, classes: one of everything, below and above a tile's sides, steps' and pieces' ends
 SIZES = [(1, 1, 1), (1, 1, 2), (2, 3, 5), (3, 64, 255), (5, 17, 256), (64, 8, 257), (65, 33, 511), (63, 64, 512), (64, 65, 1000), (130, 100, 777),
          (255, 128, 264), (256, 129, 300), (257, 300, 513), (300, 1433, 264), (31, 2050, 97), (700, 40, 4001), (513, 256, 2056),
-         (9, 1030, 600), (64, 2048, 263), (65, 700, 1000), (200, 1500, 2000)]
+         (9, 1030, 600), (7, 1100, 700), (64, 2048, 263), (65, 700, 1000), (200, 1500, 2000)]
 
 
 def mat(values, dtype, ld=None, off=0):
