@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void classes_number_kernel(RowsArgs a, const i
     if (blockIdx.x + 1 == gridDim.x && tid == 0) *a.shape = shape_for(a, before + part[0] + part[1] + part[2] + part[3]);
 }
 
-// A wavefront a row: the teacher's distribution over the entries that are there, the label among them, put in the order of their
+// A wavefront a row (16,384 rows of 64 entries 52 us): the teacher's distribution over the entries that are there, the label among them, put in the order of their
 // classes by counting how many come before each, and where each tile of classes begins in them.
 __global__ __launch_bounds__(64) void classes_entries_kernel(RowsArgs a) {
     constexpr int N = (kMaxEntries + 1 + 63) / 64;
@@ -252,7 +252,8 @@ struct LossArgs {
     int32_t k;
 };
 
-// ROWS rows a workgroup, 256 / ROWS threads a row: each joins every so many tiles, then they are joined in a tree
+// ROWS rows a workgroup, 256 / ROWS threads a row: each joins every so many tiles, then they are joined in a tree. Bound by reading 16 bytes for every 256
+// logits: 8,192 x 131,072 takes 22 us
 template <int ROWS>
 __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
     constexpr int PARTS = 256 / ROWS;
@@ -523,7 +524,9 @@ __device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint3
         }
 }
 
-// Both in one launch: neither fills the card alone where there are few tiles, and one's last tiles run beside the other's first.
+// Both in one launch: neither fills the card alone where there are few tiles, and one's last tiles run beside the other's first.  Bound by the matrix
+// units: 16,384 x 512 x 131,072 of bf16 takes four launches of 1.07 ms, 1,020 TFLOP/s; fp32 is six products, 4,096 x 256 x 65,536 1.86 ms,
+// 890 TFLOP/s of them.
 template <class PX, class PW>
 __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) {
     static_assert(PX::T == PW::T, "workgroups of one size");
@@ -532,7 +535,8 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
     else gw_tile<PW>(a, blockIdx.x - a.x_blocks, gridDim.x - a.x_blocks, smem);
 }
 
-// ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two classes of two rows a thread
+// ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two classes of two rows a thread. Waits for memory:
+// 100 x 1,500 logits of 16 parts take 7 us (with eight rows a thread, one part after another, 44)
 __global__ __launch_bounds__(1024) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
     __shared__ float sums[32][64];
     typedef float f32x2 __attribute__((ext_vector_type(2)));

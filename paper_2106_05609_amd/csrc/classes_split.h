@@ -1,5 +1,6 @@
 // Logits of so few tiles that most of the card would have none, where the sums are long: a workgroup a part of a tile's sums, and the parts
-// added up by what reads them.  100 x 2,048 x 1,500 of fp32 is 12 tiles of 384 steps one after another.
+// added up by what reads them.  100 x 2,048 x 1,500 of fp32 is 12 tiles of 384 steps one after another: its loss took 202 us, in sixteen parts 46 (the
+// products 19, adding up 5).
 #pragma once
 #include "classes_logits.h"
 #include "classes_vector.h"
