@@ -303,9 +303,10 @@ def test_pieces_of_the_classes(dtype):
             assert close(grads[name], want) <= R.U32 * (12 + math.sqrt(k)) + (half if dtype == "bf16" else 0), (name, few)
 
 
-def test_the_same_bits_again():
+@pytest.mark.parametrize("n, f, c", [(400, 100, 3000), (6, 100, 3000), (30, 100, 3000), (100, 1100, 700)])
+def test_the_same_bits_again(n, f, c):
     for dtype in DT:
-        s, _ = make(400, 100, 3000, dtype)
+        s, _ = make(n, f, c, dtype)
         first = forward(s)
         grads = backward(s, first["lse"], dtype)
         for _ in range(2):
@@ -484,16 +485,16 @@ def test_top_of_strided_outputs():
 
 # ---- together
 
-def test_on_another_stream_and_in_graphs():
+@pytest.mark.parametrize("n, f, c", [(200, 64, 3000), (5, 64, 3000), (30, 64, 3000), (100, 1100, 700)])
+def test_on_another_stream_and_in_graphs(n, f, c):
     """A forward and a backward call in one graph, the top logits in another, replayed in turn with eager work between, on inputs that change."""
     for dtype in DT:
-        s, _ = with_teacher(200, 64, 3000, 12, dtype, 0.5)
-        n, c = 200, 3000
+        s, _ = with_teacher(n, f, c, 12, dtype, 0.5)
         out = dict(loss=torch.empty(n, device="cuda"), lse=torch.empty(n, 2, device="cuda"))
-        grads = dict(gx=torch.empty_like(s["x"]), gw=torch.empty(64, c, device="cuda"), gbias=torch.empty(c, device="cuda"))
+        grads = dict(gx=torch.empty_like(s["x"]), gw=torch.empty(f, c, device="cuda"), gbias=torch.empty(c, device="cuda"))
         ids, values, lse = torch.empty(n, 5, dtype=torch.int32, device="cuda"), torch.empty(n, 5, device="cuda"), torch.empty(n, device="cuda")
-        work = torch.empty(max(gas.gas_linear_distill_workspace(n, 64, c, DT[dtype], 12), gas.gas_linear_distill_bwd_workspace(n, 64, c, DT[dtype], 12),
-                               gas.gas_linear_top_workspace(n, 64, c, DT[dtype], 5)), dtype=torch.uint8, device="cuda")
+        work = torch.empty(max(gas.gas_linear_distill_workspace(n, f, c, DT[dtype], 12), gas.gas_linear_distill_bwd_workspace(n, f, c, DT[dtype], 12),
+                               gas.gas_linear_top_workspace(n, f, c, DT[dtype], 5)), dtype=torch.uint8, device="cuda")
         same = dict(bias=s["bias"], labels=s["labels"], temperature=2.0, label_weight=0.3, workspace=work)
 
         def train():
@@ -506,11 +507,11 @@ def test_on_another_stream_and_in_graphs():
         side.wait_stream(torch.cuda.current_stream())
         graphs = []
         with torch.cuda.stream(side):
-            for f in (train, answer):
-                f()
+            for call in (train, answer):
+                call()
                 g = torch.cuda.CUDAGraph()
                 with torch.cuda.graph(g, stream=side):
-                    f()
+                    call()
                 graphs.append(g)
         torch.cuda.current_stream().wait_stream(side)
         every = (*out.values(), *grads.values(), ids, values, lse)
