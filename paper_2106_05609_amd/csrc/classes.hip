@@ -536,26 +536,29 @@ __global__ __launch_bounds__(PX::T, 2) void classes_products_kernel(GradArgs a) 
 }
 
 // ---- backward: the gradient at logits that are there, 64 rows by 64 classes of the piece a workgroup, two classes of two rows a thread. Waits for memory:
-// 100 x 1,500 logits of 16 parts take 7 us (with eight rows a thread, one part after another, 44)
-__global__ __launch_bounds__(1024) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
-    __shared__ float sums[32][64];
+// 100 x 1,500 logits of 16 parts take 7 us (with eight rows a thread, one part after another, 44), 1 x 200,003 6
+// GROUPS of 32 threads, ROWS rows for each: 64 rows, or the eight of a call that has no more.
+template <int GROUPS, int ROWS>
+__global__ __launch_bounds__(32 * GROUPS) void classes_grad_few_kernel(LogitsArgs a, PartsOfZ from) {
+    constexpr bool kFew = GROUPS * ROWS < 64;
+    __shared__ float sums[GROUPS][64];
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     const Layer& l = a.layer;
     const int count = l.shape->count, width = l.shape->width, tid = threadIdx.x, in = (int)(blockIdx.x * 64) + 2 * (tid & 31), group = tid >> 5;
     const int64_t c = (int64_t)a.piece * width + in;
     const int r0 = (int)blockIdx.y * 64;
     if ((int)(blockIdx.x * 64) >= width || c >= from.ld || r0 >= count) return;       // whole workgroups: widths are of whole tiles
-    f32x2 z[2], sum = {0.f, 0.f}, bias = {0.f, 0.f};
+    f32x2 z[ROWS], sum = {0.f, 0.f}, bias = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int r = r0 + group + 32 * j < count ? r0 + group + 32 * j : count - 1;
+    for (int j = 0; j < ROWS; ++j) {
+        const int r = r0 + group + GROUPS * j < count ? r0 + group + GROUPS * j : count - 1;
         z[j] = sum_of(reinterpret_cast<const f32x2*>(from.p + r * from.ld + c), from.step / 2, from.splits, f32x2{0.f, 0.f});
     }
     if (from.bias) bias = *reinterpret_cast<const f32x2*>(from.bias + c);
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int r = r0 + group + 32 * j;
-        float g[2] = {0.f, 0.f};                               // rows up to 64 are read later on: zero beyond those that count
+    for (int j = 0; j < ROWS; ++j) {
+        const int r = r0 + group + GROUPS * j;
+        float g[2] = {0.f, 0.f};                               // zero beyond the rows that count: the sums of gw go on to 64
         if (r < count) {
             const f32x4 info = a.info[r];
             const int label = a.labels ? a.labels[r] : -1;
@@ -582,6 +585,7 @@ __global__ __launch_bounds__(1024) void classes_grad_few_kernel(LogitsArgs a, Pa
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) sum[i] += g[i];
+        if (kFew && r >= count) continue;                      // of few rows they end before
         uint32_t part[3];
         split_pair(g[0], g[1], part[0], part[1], part[2]);
         uint16_t* at = a.g + (int64_t)r * width + in;
@@ -598,8 +602,59 @@ __global__ __launch_bounds__(1024) void classes_grad_few_kernel(LogitsArgs a, Pa
     if (tid >= 64) return;
     float v = 0.f;
 #pragma unroll
-    for (int g = 0; g < 32; ++g) v += sums[g][tid];
+    for (int g = 0; g < GROUPS; ++g) v += sums[g][tid];
     a.gbias[blockIdx.y * from.ld + (int64_t)a.piece * width + blockIdx.x * 64 + tid] = v;
+}
+
+// ---- backward: gw of up to eight rows by the vector units, 1,024 classes of the piece by 16 inputs a workgroup, four classes a thread.
+// Bound by writing it: 1,024 x 200,003 of fp32 takes 147 us (5.6 TB/s); as tiles of matrix products, most of whose rows are none, it took 252
+template <int R>
+__global__ __launch_bounds__(256) void classes_gw_few_kernel(GradArgs a) {
+    typedef float f32x4_here __attribute__((ext_vector_type(4), aligned(4)));
+    constexpr int kInputs = 16;
+    __shared__ __attribute__((aligned(16))) float xs[kInputs][R];
+    const Layer& l = a.layer;
+    const Shape shape = *l.shape;
+    const Piece s(shape, a.piece, l.C);
+    const int planes = l.terms > 1 ? 3 : 1, f0 = (int)blockIdx.y * kInputs, fs = l.F - f0 < kInputs ? l.F - f0 : kInputs;
+    // a value is the sum of its parts
+    auto whole = [&](const uint16_t* p, int64_t plane) {
+        float v = __uint_as_float((uint32_t)p[0] << 16);
+        if (planes > 1) v += __uint_as_float((uint32_t)p[plane] << 16) + __uint_as_float((uint32_t)p[2 * plane] << 16);
+        return v;
+    };
+    auto four = [&](const uint16_t* p) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+        return f32x4{bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1])};
+    };
+    for (int i = threadIdx.x; i < fs * R; i += 256) {
+        const int r = i / fs, f = i % fs;
+        xs[f][r] = r < shape.count ? whole(l.x + (int64_t)r * l.fp + f0 + f, l.x_plane) * a.scale : 0.f;
+    }
+    __syncthreads();
+    const int c = (int)(blockIdx.x * 256 + threadIdx.x) * 4, n = s.cols - c < 4 ? s.cols - c : 4;
+    if (n <= 0) return;
+    f32x4 g[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        g[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (r >= shape.count) continue;
+        const uint16_t* at = a.g + (int64_t)r * s.width + c;
+        g[r] = four(at);
+        if (planes > 1) g[r] += four(at + a.g_plane) + four(at + 2 * a.g_plane);
+    }
+    const bool fours_of_bf16 = a.gw_bf16 && n == 4 && fours(a.gw, a.ldgw, true) && s.first % 4 == 0;
+#pragma unroll 4
+    for (int f = 0; f < fs; ++f) {
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = fmaf(xs[f][r], g[r][e], v[e]);
+        const int64_t at = (int64_t)(f0 + f) * a.ldgw + s.first + c;
+        if (!a.gw_bf16 && n == 4) *reinterpret_cast<f32x4_here*>(static_cast<float*>(a.gw) + at) = v;
+        else put4(a.gw, at, v, n, a.gw_bf16, fours_of_bf16);
+    }
 }
 
 // ---- backward: what came in parts, added up
@@ -890,6 +945,16 @@ gas_status launch_products(GradArgs a, int64_t rows, int64_t cols, hipStream_t s
     return GAS_OK;
 }
 
+gas_status launch_gw_few(const GradArgs& a, int64_t n, int64_t cols, hipStream_t s) {
+    const dim3 grid((unsigned)((cols + 1023) / 1024), (unsigned)((a.layer.F + 15) / 16)), block(256);
+    if (n == 1) hipLaunchKernelGGL(classes_gw_few_kernel<1>, grid, block, 0, s, a);
+    else if (n == 2) hipLaunchKernelGGL(classes_gw_few_kernel<2>, grid, block, 0, s, a);
+    else if (n <= 4) hipLaunchKernelGGL(classes_gw_few_kernel<4>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(classes_gw_few_kernel<8>, grid, block, 0, s, a);
+    GAS_CHECK_HIP(hipGetLastError());
+    return GAS_OK;
+}
+
 template <class P>
 gas_status launch_gx_once(const GradArgs& a, hipStream_t s) {
     static const gas_status attr = lds_of(classes_gx_once_kernel<P>, P::kLdsBytes);
@@ -949,22 +1014,27 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
         const int64_t rows_most = l.most, cols_most = round_up(c.C, 256);
         const int64_t all = (c.n + tile - 1) / tile * (cols_most / 256), fit = b.cap / (tile * 256);
         if (z.p) {
-            hipLaunchKernelGGL(classes_grad_few_kernel, dim3((unsigned)(cols_most / 64), (unsigned)((c.n + 63) / 64)), dim3(1024), 0, c.s, a, z);
+            const dim3 grid((unsigned)(cols_most / 64), (unsigned)((c.n + 63) / 64));
+            if (c.n <= kRowsByVector) hipLaunchKernelGGL((classes_grad_few_kernel<8, 1>), grid, dim3(256), 0, c.s, a, z);
+            else hipLaunchKernelGGL((classes_grad_few_kernel<32, 2>), grid, dim3(1024), 0, c.s, a, z);
             GAS_CHECK_HIP(hipGetLastError());
         } else {
             GAS_TRY(launch_grad(a, tile, all < fit ? all : fit, !distill ? 1 : !c.t.labels ? 2 : c.temperature == 2.f ? 4 : 3, c.dt, c.s));
         }
         if (g.gx && rows.once) GAS_TRY(c.dt == GAS_BF16 ? launch_gx_once<GxOnce<true>>(d, c.s) : launch_gx_once<GxOnce<false>>(d, c.s));
-        if ((g.gx && !rows.once) || g.gw) {
+        const bool gw_few = g.gw && c.n <= kRowsByVector;
+        if (gw_few) GAS_TRY(launch_gw_few(d, c.n, cols_most, c.s));
+        if ((g.gx && !rows.once) || (g.gw && !gw_few)) {
             const auto launch = fx == 64 ? launch_products<Gx64, Gw64> : fx == 128 ? launch_products<Gx128, Gw128> : fx == 192 ? launch_products<Gx192, Gw192>
                               : fx == 256 ? launch_products<Gx256, Gw256> : launch_products<Gx320, Gw320>;
             GradArgs both = d;
             if (rows.once) both.part_x = nullptr;
+            if (gw_few) both.part_w = nullptr;
             GAS_TRY(launch(both, rows_most, cols_most, c.s));
         }
         const bool last = p + 1 == pieces;
         SumArgs sums = {d, common.pos, c.n, g.ldgx, g.gx, c.dt == GAS_BF16, b.gbias, g.gbias, tile, rows.once ? 32 : 1, 0, 0};
-        if (g.gw) sums.w_blocks = blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048);
+        if (g.gw && !gw_few) sums.w_blocks = blocks_for((int64_t)c.F * ((cols_most + 3) / 4), 256, 2048);
         if (g.gx && last) sums.x_blocks = blocks_for(c.n * ((c.F + 3) / 4), 256 / sums.lanes, 4096);
         const unsigned blocks = sums.w_blocks + sums.x_blocks + (g.gbias && last ? (unsigned)((c.C + 255) / 256) : 0u);
         if (blocks == 0) continue;
