@@ -192,10 +192,11 @@ def test_rows_without_a_label(dtype, n):
 
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("low", [-math.inf, "least"])
-def test_classes_taken_out_by_the_bias(dtype, low):
+@pytest.mark.parametrize("n, f", [(90, 20), (6, 20), (90, 1100)])
+def test_classes_taken_out_by_the_bias(dtype, low, n, f):
     """-infinity, or the type's least value: probability 0, and a label on one an infinite (a very large) loss with a finite gradient.  A whole
     tile of them, and all but one."""
-    n, f, c = 90, 20, 700
+    c = 700
     low = torch.finfo(DT[dtype]).min if low == "least" else low
     for out in (slice(3, 9), slice(256, 512), slice(1, c)):
         s, _ = make(n, f, c, dtype, labelled=1.0)
@@ -217,9 +218,10 @@ def test_classes_taken_out_by_the_bias(dtype, low):
 
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("shift", [0.0, 80.0, -3000.0])
-def test_large_logits(dtype, shift):
+@pytest.mark.parametrize("n, f", [(70, 64), (7, 64), (70, 1100)])
+def test_large_logits(dtype, shift, n, f):
     """Logits of some thousand, differences of some hundred: exponentials from the largest on."""
-    n, f, c = 70, 64, 520
+    c = 520
     s, _ = make(n, f, c, dtype, spread=60.0)
     s["bias"].add_(shift)
     got = forward(s)
@@ -228,13 +230,14 @@ def test_large_logits(dtype, shift):
     check(got["loss"], want["loss"], "loss")
 
 
-def test_a_nan_in_a_row_stays_there():
+@pytest.mark.parametrize("n, f", [(80, 40), (8, 40), (80, 1100)])
+def test_a_nan_in_a_row_stays_there(n, f):
     for dtype in DT:
-        s, _ = make(80, 40, 300, dtype, labelled=1.0)
+        s, _ = make(n, f, 300, dtype, labelled=1.0)
         clean = forward(s)
         s["x"][7, 3] = math.nan
         got = forward(s)
-        rows = torch.arange(80, device="cuda") != 7
+        rows = torch.arange(n, device="cuda") != 7
         assert got["loss"][7].isnan() and got["lse"][7].isnan() and got["sum"].isnan().all()
         assert torch.equal(got["loss"][rows], clean["loss"][rows])
         grads = backward(s, got["lse"], dtype)
