@@ -158,6 +158,32 @@ def test_few_rows_of_more_classes_than_a_piece_has(dtype, gw, n):
         check(got[name], want, name)
 
 
+@pytest.mark.parametrize("c", [2_100_000, 2_100_001])
+@pytest.mark.parametrize("n", [3, 40, 300])
+def test_offsets_beyond_32_bits(n, c):
+    """W and its gradient of 2.3 G elements, zero but for nine classes: what those nine have to be follows from them alone."""
+    f, gen = 1100, torch.Generator().manual_seed(n)
+    at = torch.tensor([0, 5, 256, 70_001, 1_048_577, 2_000_000, 2_097_152, c - 2, c - 1])
+    w = torch.zeros((f, c), dtype=torch.bfloat16, device="cuda")
+    w[:, at.cuda()] = (torch.randn(f, 9, generator=gen) * 3 / math.sqrt(f)).bfloat16().cuda()
+    pick = torch.randint(0, 9, (n,), generator=gen)
+    s = dict(x=torch.randn(n, f, generator=gen).bfloat16().cuda(), w=w, bias=None, labels=at[pick].int().cuda())
+    got = forward(s)
+    x, few = wide(s["x"]), wide(w[:, at.cuda()])
+    z, off = R.logits(x, few, None)
+    lse = torch.log(torch.exp(z).sum(1) + (c - 9))
+    off_lse = off.amax(1) + R.U32 * (120 + c / 256 / 16 + 8 * lse.abs() + 8 * z.abs().amax(1))
+    check(got["lse"], (lse, off_lse), "lse")
+    loss = lse - z.gather(1, pick[:, None])[:, 0]
+    check(got["loss"], (loss, off_lse + off.amax(1) + 2 * R.U32 * loss.abs()), "loss")
+    grads = dict(gx=torch.full_like(s["x"], math.nan), gw=torch.full_like(w, math.nan), gbias=torch.full((c,), math.nan, device="cuda"))
+    gas.gas_linear_xent_bwd(s["x"], w, s["labels"], got["lse"], scale=0.37, **grads)
+    g, off = R.grad_at_logits(x, few, None, wide(got["lse"]), pick.int(), None)
+    for name, want in R.gradients(x, few, g, off, 0.37, True, True).items():
+        check(grads[name] if name == "gx" else grads[name][..., at.cuda()], want, name)
+    assert not any(v.isnan().any() for v in grads.values())
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 def test_any_gradient_alone(dtype):
     s, _ = make(150, 70, 600, dtype)
