@@ -502,7 +502,7 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * lse: fp32[n_rows, 2], log sum exp z and log sum exp (z / T).  gas_linear_distill_bwd: the gradient as above, with
  *     G[i, c] = r_i (a (p_c - [c == labels[i]]) + b T (p^T_c - q_c)).
  *
- * gas_linear_top: the k largest logits of every row, the largest first, of equal ones those of lower classes first: ids int32
+ * gas_linear_top: the k largest logits of every row, the largest first, of equal ones (fp32, as they are summed; a class's sums are formed as every other's) those of lower classes first: ids int32
  * [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
  *
  * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
@@ -510,7 +510,8 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * 64 rows, W as the products take them (not W where it is bf16 with 16-byte aligned rows of whole 16-byte pieces: that is read as it lies, as
  * for up to 64 rows every W is); statistics of every 256 classes; the logits of up to eight rows,
  * and up to 34 MB of parts of their sums where there are few tiles of long ones; backward a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it,
- * or 256 classes of it if they are more; gas_linear_top the logits of up to 64 rows, of more rows those of a piece, 2 GB or 4,096 classes.
+ * or 256 classes of it if they are more; gas_linear_top the logits of up to 64 rows, and of more where there are few tiles (16 MB), else
+ * those of a piece, 2 GB or 4,096 classes.
  */
 GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
 GAS_API gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,

@@ -1,8 +1,8 @@
 // The k largest logits of an output layer over many classes, and the logarithm of the sum of all their exponentials, without its logits
 // (gas_linear_top).
 //
-// Few rows (64): all logits of them are stored, 4 bytes beside the 2 F or 4 F of W's column, and searched. Up to eight rows have a kernel
-// of their own that reads W as it lies and multiplies by the vector units, bound by reading it.
+// Few rows (64), and more of so few tiles that their sums are split: all logits of them are stored, 4 bytes beside the 2 F or 4 F of W's column, and
+// searched. Up to eight rows have a kernel of their own that reads W as it lies and multiplies by the vector units, bound by reading it.
 //
 // Many rows: the classes are taken in pieces. Of the first, 4,096 classes, all logits are stored; of a later one only those above the row's k-th largest
 // of the pieces before (a later class never replaces an equal earlier one), with a bit for each, and a row's list is joined with them. A piece seven
@@ -284,9 +284,14 @@ __global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t m
     if (part == 0 && r < n) lse[r] = log_of(most, sum, 1.f);
 }
 
-inline int64_t top_width(int64_t n, int C) {
+// Whether all logits are stored: of few rows, and where their sums are split. Pieces whose sums were split in different ways would leave
+// equal logits with different last bits, and the higher class could come first. 100 x 1,000 x 9,000 of fp32 takes 79 us, of bf16 44; in pieces, the
+// first one's sums split, 162 and 60, no sums split 235 and 66.  Pieces whose own tiles would be split and all classes' would not (100 x 2,000
+// x 100,000 of fp32, 1,390 us with a split first piece) take a tenth longer.
+inline bool top_whole(int64_t n, int F, int C, gas_dtype dt) { return n <= kFewRows || splits_of_few(n, F, C, dt) > 1; }
+inline int64_t top_width(int64_t n, int C, bool whole) {
     const int64_t cp = round_up(C, 256);
-    if (n <= kFewRows) return cp;
+    if (whole) return cp;
     int64_t w = kTopElements / n / 256 * 256;
     if (w < kFirstPiece) w = kFirstPiece;
     return w < cp ? w : cp;
@@ -303,7 +308,8 @@ struct TopRoom {
     uint32_t* mask;
     uint64_t *best, *other;
     int64_t width;
-    FewRoom few;                  // parts of the first piece's sums
+    bool whole;
+    FewRoom few;                  // parts of the sums
 };
 TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, const void* W, int64_t ldw, int C, const void* bias, gas_dtype dt,
                     int k) {
@@ -311,15 +317,16 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     if (n > kRowsByVector) t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
     else t.common.layer.most = kRowsByVector;
     const int64_t most = t.common.layer.most, tiles = (C + kTileC - 1) / kTileC;
-    t.width = top_width(n, C);
+    t.whole = top_whole(n, F, C, dt);
+    t.width = top_width(n, C, t.whole);
     t.parts.most = room.take<float>(tiles * most);
     t.parts.sum = room.take<float>(tiles * most);
     t.floor = room.take<float>(most);
-    const int64_t lists = n <= kFewRows ? parts_of(C, n) : 1;
+    const int64_t lists = t.whole ? parts_of(C, n) : 1;
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
-    t.few = lay_out_few(room, n, F, (int)(n <= kFewRows || t.width < kFirstPiece ? t.width : kFirstPiece), dt, false);
+    if (t.whole) t.few = lay_out_few(room, n, F, C, dt, false);
     t.few.z = t.z;
     t.mask = room.take<uint32_t>(n * (t.width / 32));
     return t;
@@ -387,21 +394,21 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
         a.z = t.z;
         a.mask = t.mask;
         for (int64_t first = 0, width; first < cp; first += width) {
-            width = n_rows <= kFewRows ? cp : first == 0 ? kFirstPiece : kGrowth * first;
+            width = t.whole ? cp : first == 0 ? kFirstPiece : kGrowth * first;
             if (width > t.width) width = t.width;
             if (first + width > cp) width = cp - first;
             a.first = (int32_t)first;
             a.width = (int32_t)width;
             a.all = first == 0;
             const int tile = rows_of_tile(n_rows, (int)width);
-            if (first == 0 && t.few.splits > 1) {
+            if (t.few.splits > 1) {
                 st = launch_split(a.layer, t.few, n_rows, s);
                 if (st == GAS_OK) st = launch_join(a.layer, t.few, n_rows, 0.f, lse ? &t.parts : nullptr, s);
             } else {
                 st = launch_logits<LOGITS_TOP, 1>(a, tile, (n_rows + tile - 1) / tile * (width / 256), s);
             }
             if (st != GAS_OK) return st;
-            if (n_rows <= kFewRows) break;
+            if (t.whole) break;
             const bool last = first + width >= cp;
             if (first == 0) {
                 pick.ld = width;
@@ -417,7 +424,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
             GAS_CHECK_HIP(hipGetLastError());
         }
     }
-    if (n_rows <= kFewRows) {                             // parts of 8,192, and what is left of them, until one is left
+    if (t.whole) {                                        // parts of 8,192, and what is left of them, until one is left
         int64_t n = n_classes;
         uint64_t *from = t.best, *to = t.best;
         for (bool keys = false;; keys = true) {
