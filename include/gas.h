@@ -506,11 +506,14 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
  *
  * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
- * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X and, for more than
+ * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X, its rows up to a multiple of
+ * 256, and, for more than
  * 64 rows, W as the products take them (not W where it is bf16 with 16-byte aligned rows of whole 16-byte pieces: that is read as it lies, as
  * for up to 64 rows every W is); statistics of every 256 classes; the logits of up to eight rows,
- * and up to 34 MB of parts of their sums where there are few tiles of long ones; backward a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it,
- * or 256 classes of it if they are more; gas_linear_top the logits of up to 64 rows, and of more where there are few tiles (16 MB), else
+ * and up to 34 MB of parts of their sums where there are few tiles of long ones; backward a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it
+ * (its rows up to a multiple of 256, where there are few tiles of 64, up to eight rows as they are),
+ * or 256 classes of it if they are more, and parts of the sums of GX and GW, for either as much as GX or GW in fp32 takes times the parts that its sums can be
+ * split into, at most 168 MB beyond one GX; gas_linear_top the logits of up to 64 rows, and of more where there are few tiles (16 MB), else
  * those of a piece, 2 GB or 4,096 classes.
  */
 GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);

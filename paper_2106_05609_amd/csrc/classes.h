@@ -24,6 +24,7 @@ inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; 
 // What follows from the number of rows that count, worked out once on the device.
 struct Shape {
     int32_t count, width;         // classes of a piece of the gradient at the logits
+    int32_t rows;                 // of it that are stored: `count` up to whole tiles
     int32_t splits_x, splits_w;   // parts of the sums of GX and GW
 };
 
@@ -37,6 +38,7 @@ struct Layer {
     const float* bias;            // [C up to 256], -inf beyond C
     const Shape* shape;
     int32_t F, fp, C, cw, terms, most;     // fp: F up to 64; most: rows up to 256
+    int32_t stats;                // rows of the tiles' statistics: up to 16
 };
 
 // ---- rows that count
@@ -190,7 +192,7 @@ __device__ __forceinline__ int acc_row(int r, int lh) { return 8 * (r / 4) + 4 *
 // The largest one times log2 e, rounded, and the sum of 2 to the logits times log2 e less that: one fused multiply-add each, whose rounding is of
 // the difference.  A logit that leaves fp32's range by that factor, below -2.3e38, is as one of -infinity.
 struct Parts {
-    float *most, *sum, *sum_t, *picked;      // [class tiles][most rows]; sum_t: at the temperature; picked: sum of weighted target logits
+    float *most, *sum, *sum_t, *picked;      // [class tiles][stats rows]; sum_t: at the temperature; picked: sum of weighted target logits
 };
 constexpr float kLeastExponent = -3.4028234e38f;
 
@@ -237,6 +239,18 @@ struct Room {
     }
 };
 
+#define GAS_TRY(expr)                       \
+    do {                                    \
+        const gas_status st_ = (expr);      \
+        if (st_ != GAS_OK) return st_;      \
+    } while (0)
+
+// The size that a call was told may not depend on where W lies; what is laid out may.
+inline gas_status check_room(const char* who, const Room& room, int64_t bytes) {
+    GAS_REQUIRE(room.used <= bytes, "%s: the workspace is laid out over %lld bytes, %lld are there", who, (long long)room.used, (long long)bytes);
+    return GAS_OK;
+}
+
 // The parts of the workspace that every call has, and the layer as its kernels take it.
 struct Common {
     Layer layer;
@@ -276,6 +290,7 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     c.layer.C = C;
     c.layer.cw = (int32_t)cw;
     c.layer.most = (int32_t)most;
+    c.layer.stats = (int32_t)round_up(n, 16);
     c.pack = PackArgs{X, W, bias, ldx, ldw, n, c.idx, shape, x, w, biasp, c.layer.x_plane, c.layer.w_plane, F, (int32_t)fp, C, (int32_t)cw,
                       (int32_t)cp, c.layer.terms, blocks_for(most * fp / 8, 256, 4096), in_place || once ? 0u : blocks_for((int64_t)F * cw / 8, 256, 8192)};
     return c;

@@ -20,6 +20,7 @@ struct RowsArgs {
     int32_t *idx, *pos;
     Shape* shape;
     int64_t cap;                  // backward: room for the gradient at a piece's logits
+    int32_t row_step;             // its rows are a multiple of it
     int32_t once;                 // GX by gx_once_tile
     int32_t nfx, nfw, steps_of;   // tiles of inputs of GX and GW; 64 k of one part are `steps_of` steps (of fp32's six terms)
     const float* lse;             // backward: [n] (labels alone) or [n, 2]
@@ -69,10 +70,11 @@ __device__ __host__ inline int splits_once(int tiles, int steps) {
     return s < 1 ? 1 : s;
 }
 __device__ __forceinline__ Shape shape_for(const RowsArgs& a, int count) {
-    Shape s = {count, 0, 1, 1};
+    Shape s = {count, 0, 0, 1, 1};
     if (a.cap > 0) {
         const int rows = count > 0 ? (count + 255) / 256 * 256 : 256;
-        s.width = piece_width(a.cap, rows, a.t.C);
+        s.rows = (count + a.row_step - 1) / a.row_step * a.row_step;
+        s.width = piece_width(a.cap, s.rows > 0 ? s.rows : a.row_step, a.t.C);
         // they run beside each other: half of the units for each where both could have a round of their own together
         const int64_t tiles_x = (int64_t)rows / 256 * a.nfx, tiles_w = (int64_t)s.width / 256 * a.nfw;
         const int units = !a.once && tiles_x + tiles_w <= kUnits / 2 ? kUnits / 2 : kUnits;
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(256) void classes_loss_kernel(LossArgs a) {
     float most = kLeastExponent, sum = 0.f, sum_t = 0.f, picked = 0.f;
     if (r >= 0) {
         for (int t = part; t < a.tiles; t += PARTS) {
-            const int64_t at = (int64_t)t * a.layer.most + r;
+            const int64_t at = (int64_t)t * a.layer.stats + r;
             join(most, sum, sum_t, a.parts.most[at], a.parts.sum[at], a.two ? a.parts.sum_t[at] : 0.f, a.inv_t);
             if (a.info && !a.z) picked += a.parts.picked[at];
         }
@@ -349,8 +351,8 @@ struct GradArgs {
 
 // A piece of the classes.
 struct Piece {
-    int rows, width, first, cols;            // rows up to 256; the piece's first class and how many it has
-    __device__ __forceinline__ Piece(const Shape& s, int piece, int C) : rows((s.count + 255) / 256 * 256), width(s.width) {
+    int rows, width, first, cols;            // the piece's first class and how many it has
+    __device__ __forceinline__ Piece(const Shape& s, int piece, int C) : rows(s.rows), width(s.width) {
         const int64_t from = (int64_t)piece * s.width;
         first = (int)from;
         cols = from >= C ? 0 : (int)(C - from < s.width ? C - from : s.width);
@@ -365,7 +367,7 @@ __device__ __forceinline__ void gx_tile(const GradArgs& a, uint32_t block, uint3
     const Shape shape = *l.shape;
     const Piece s(shape, a.piece, l.C);
     if (s.cols == 0 || s.rows == 0) return;
-    const int nm = s.rows / BB, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
+    const int nm = (s.rows + BB - 1) / BB, nf = (l.fp + BA - 1) / BA, steps = (s.cols + kStepK - 1) / kStepK;
     const int full = s.width / kStepK, splits = shape.splits_x;
     int ft, at;
     if (!tile_of(block, blocks, nf, nm * splits, ft, at)) return;
@@ -379,13 +381,15 @@ __device__ __forceinline__ void gx_tile(const GradArgs& a, uint32_t block, uint3
     f32x16 acc[P::TA][P::TB];
     P product;
     const TileOperand oa = {l.w + (int64_t)f0 * l.ldw + s.first, l.ldw, l.w_plane, l.F - 1 - f0, l.cw - s.first};
-    const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB - 1, s.width};
+    const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB < s.rows - m0 ? BB - 1 : s.rows - m0 - 1, s.width};
     const int end = (s.cols + P::kStepOf - 1) / P::kStepOf, from = first * (kStepK / P::kStepOf), to = last * (kStepK / P::kStepOf);
     product.run(oa, ob, from < end ? from : end, to < end ? to : end, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     float* out = a.part_x + (int64_t)part * s.rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
-        float* row = out + (int64_t)(m0 + wb0 + 32 * j + li) * l.fp;
+        const int m = m0 + wb0 + 32 * j + li;
+        if (m >= s.rows) continue;
+        float* row = out + (int64_t)m * l.fp;
 #pragma unroll
         for (int i = 0; i < P::TA; ++i)
 #pragma unroll
@@ -418,12 +422,14 @@ __device__ __forceinline__ void gx_once_tile(const GradArgs& a, uint32_t block, 
     f32x16 acc[P::TA][P::TB];
     P product;
     const typename P::Operand oa = {static_cast<const char*>(l.raw) + ((int64_t)f0 * l.ld_raw + s.first) * eb, l.ld_raw, l.F - f0, l.C - s.first};
-    const TileOperand ob = {a.g, s.width, a.g_plane, P::kRowsB - 1, s.width};
+    const TileOperand ob = {a.g, s.width, a.g_plane, s.rows - 1, s.width};
     product.run(oa, ob, shape.count, first, last, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     float* out = a.part_x + (int64_t)part * s.rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
-        float* row = out + (int64_t)(wb0 + 32 * j + li) * l.fp;
+        const int m = wb0 + 32 * j + li;
+        if (m >= s.rows) continue;
+        float* row = out + (int64_t)m * l.fp;
 #pragma unroll
         for (int i = 0; i < P::TA; ++i)
 #pragma unroll
@@ -479,7 +485,7 @@ __device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint3
     const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
     f32x16 acc[P::TA][P::TB];
     P product;
-    const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, l.most};
+    const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, s.rows};
     const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
     product.run(oa, ob, first * (kStepK / P::kStepOf), last * (kStepK / P::kStepOf), l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     // A lane has classes of 32 inputs' rows, memory wants a row's next to each other: through 32 rows of 64 classes of LDS that belong to the
@@ -792,7 +798,7 @@ inline gas_status run_rows(const Call& c, const Common& common, const RowsArgs& 
 
 // What the forward call needs beside: the tiles' statistics
 inline Parts lay_out_parts(Room& room, const Common& common, bool distill) {
-    const int64_t tiles = (common.layer.C + kTileC - 1) / kTileC, n = tiles * common.layer.most;
+    const int64_t tiles = (common.layer.C + kTileC - 1) / kTileC, n = tiles * common.layer.stats;
     Parts p = {};
     p.most = room.take<float>(n);
     p.sum = room.take<float>(n);
@@ -824,15 +830,9 @@ inline gas_status run_sum(const float* loss, int64_t n, float* out, hipStream_t 
     return GAS_OK;
 }
 
-#define GAS_TRY(expr)                       \
-    do {                                    \
-        const gas_status st_ = (expr);      \
-        if (st_ != GAS_OK) return st_;      \
-    } while (0)
-
 // Logits of few rows, all of them
 gas_status launch_few(const Call& c, const Common& common, float inv_t, float* z, const Parts* parts) {
-    const VectorArgs v = {c.X, c.W, c.bias, c.ldx, c.ldw, round_up(c.C, 256), common.layer.most, common.idx, common.layer.shape, (int32_t)c.n, c.F, c.C, inv_t, z,
+    const VectorArgs v = {c.X, c.W, c.bias, c.ldx, c.ldw, round_up(c.C, 256), common.layer.stats, common.idx, common.layer.shape, (int32_t)c.n, c.F, c.C, inv_t, z,
                           parts ? *parts : Parts{}};
     return c.dt == GAS_BF16 ? launch_vector<true>(v, c.s) : launch_vector<false>(v, c.s);
 }
@@ -843,6 +843,7 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     const RowsArgs rows = lay_out_rows(room, c, common, distill);
     const Parts parts = lay_out_parts(room, common, distill);
     const FewRoom f = lay_out_few(room, c.n, c.F, c.C, c.dt, true);
+    GAS_TRY(check_room(c.who, room, c.workspace_bytes));
     const bool few = f.by_vector;
     GAS_TRY(run_rows(c, common, rows, distill, !few));
     LogitsArgs a = logits_args(c, common, rows, distill);
@@ -865,10 +866,12 @@ gas_status forward(const Call& c, bool distill, float* loss, float* sum, float* 
     return run_sum(loss, c.n, sum, c.s);
 }
 
+// Rows of the gradient at the logits are stored in tiles as they are formed, of up to eight one by one.
+inline int row_step_of(int64_t n, int C) { return n <= kRowsByVector ? 1 : rows_of_tile(n, C); }
 // Room for the gradient at the logits of a piece, in elements.
 constexpr int64_t kPieceElements = 1LL << 29;
-inline int64_t piece_cap(int64_t most, int C) {
-    const int64_t all = most * round_up(C, 256), least = most * 256;
+inline int64_t piece_cap(int64_t rows, int C) {
+    const int64_t all = rows * round_up(C, 256), least = rows * 256;
     const int64_t cap = all < kPieceElements ? all : kPieceElements;
     return cap > least ? cap : least;
 }
@@ -917,13 +920,24 @@ struct BackwardRoom {
 inline BackwardRoom lay_out_backward(Room& room, const Common& common, int64_t n, bool gx, bool gw, bool gbias) {
     BackwardRoom b = {};
     const Layer& l = common.layer;
-    const int64_t most = l.most;
-    b.cap = piece_cap(most, l.C);
+    const int64_t rows = round_up(n, row_step_of(n, l.C)), cp = round_up(l.C, 256);
+    b.cap = piece_cap(rows, l.C);
     b.g = room.take<uint16_t>(b.cap * (l.terms > 1 ? 3 : 1));
-    // parts of a sum are made only where there are at most two tiles of them for a compute unit
-    const int64_t parts = (int64_t)2 * kUnits * 256 * 320, whole_x = most * l.fp;
-    b.gx = gx ? room.take<float>(whole_x > parts ? whole_x : parts) : nullptr;
-    b.gw = gw ? room.take<float>(parts) : nullptr;
+    // The most parts that the sums of any number of rows up to n can have (splits_of, splits_once): no more than two tiles of them for a unit, and two steps
+    // at least for each.  For few rows, whether W is read by gx_once_tile or lies in whole pieces, which the workspace's size is to do for.
+    const int fx = width_of_tile(l.fp);
+    auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    const int64_t tiles = (l.fp + fx - 1) / fx, steps = cp / kStepK, splits = least(2 * kUnits / tiles, least(kMostSplits, steps / 2));
+    int64_t parts_x = least(2 * kUnits / tiles * 256, splits * rows);
+    if (parts_x < rows) parts_x = rows;
+    if (n <= kReadOnceRows) {
+        const int64_t parts_once = splits_once((l.fp + 255) / 256, (int)steps) * rows;
+        if (parts_x < parts_once) parts_x = parts_once;
+    }
+    b.gx = gx ? room.take<float>(parts_x * l.fp) : nullptr;
+    // of up to eight rows GW is formed as a whole
+    const int64_t parts_w = n <= kRowsByVector ? 0 : least(2 * kUnits / tiles, least(kMostSplits, l.most / kStepK / 2) * (cp / 256)) * 256;
+    b.gw = gw ? room.take<float>(parts_w > 0 ? parts_w * l.F : 1) : nullptr;
     b.gbias = gbias ? room.take<float>((n + rows_of_tile(n, l.C) - 1) / rows_of_tile(n, l.C) * round_up(l.C, 256)) : nullptr;
     return b;
 }
@@ -983,12 +997,14 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     rows.lse = g.lse;
     rows.row_scale = g.row_scale;
     rows.cap = b.cap;
+    rows.row_step = row_step_of(c.n, c.C);
     const int fx = width_of_tile(common.layer.fp);
     rows.once = common.layer.w == nullptr;
     rows.nfw = (int32_t)((common.layer.fp + fx - 1) / fx);
     rows.nfx = rows.once ? (int32_t)((common.layer.fp + 255) / 256) : rows.nfw;
     rows.steps_of = common.layer.terms;
     const FewRoom f = lay_out_few(room, c.n, c.F, c.C, c.dt, false);
+    GAS_TRY(check_room(c.who, room, c.workspace_bytes));
     PartsOfZ z = {f.parts, f.ld, f.step, f.splits, common.layer.bias};
     GAS_TRY(run_rows(c, common, rows, distill, true));
     if (f.z) {
@@ -1006,7 +1022,7 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, b.gx, b.gw, 0, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
         // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int tile = rows_of_tile(c.n, c.C);
-    const int least = piece_width(b.cap, l.most, l.C);
+    const int least = piece_width(b.cap, round_up(c.n, rows.row_step), l.C);
     const int pieces = (c.C + least - 1) / least;
     for (int p = 0; p < pieces; ++p) {
         // the widest that piece p can be, and the most tiles that it can have: width * rows <= cap, or 256 classes

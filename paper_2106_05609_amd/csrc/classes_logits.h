@@ -425,7 +425,7 @@ __global__ __launch_bounds__(P::T, 2) void classes_logits_kernel(LogitsArgs a) {
                 join(top, s, st, v[0], v[1], v[2], a.inv_t);
                 z += v[3];
             }
-            const int64_t at = (int64_t)tile * l.most + m;
+            const int64_t at = (int64_t)tile * l.stats + m;
             a.parts.most[at] = top;
             a.parts.sum[at] = s;
             if constexpr (KIND == LOGITS_STATS) {

@@ -65,7 +65,7 @@ struct PartsOfZ {
 struct JoinArgs {
     PartsOfZ from;
     const Shape* shape;
-    int64_t most;
+    int64_t stats;
     float inv_t;                  // 0: one temperature
     float* z;                     // [rows][ld]
     Parts parts;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(256) void classes_join_kernel(JoinArgs a) {
         sum_t += __shfl_xor(sum_t, o);
     }
     if (lane > 0) return;
-    const int64_t to = blockIdx.x * a.most + r;
+    const int64_t to = blockIdx.x * a.stats + r;
     a.parts.most[to] = most;
     a.parts.sum[to] = sum;
     if (a.inv_t != 0.f) a.parts.sum_t[to] = sum_t;
@@ -123,7 +123,7 @@ inline FewRoom lay_out_few(Room& room, int64_t n, int F, int C, gas_dtype dt, bo
     FewRoom f = {nullptr, nullptr, round_up(C, kTileC), round_up(n, 64) * round_up(C, kTileC), splits_of_few(n, F, C, dt), false};
     f.by_vector = n <= kRowsByVector && f.splits == 1;
     if (f.splits > 1) f.parts = room.take<float>(f.splits * f.step);
-    if (f.by_vector || (whole && f.splits > 1)) f.z = room.take<float>((f.by_vector ? kRowsByVector : round_up(n, 64)) * f.ld);
+    if (f.by_vector || (whole && f.splits > 1)) f.z = room.take<float>((f.by_vector ? n : round_up(n, 64)) * f.ld);
     return f;
 }
 
@@ -141,7 +141,7 @@ inline gas_status launch_split(const Layer& l, const FewRoom& f, int64_t n, hipS
     return l.w ? launch_split_of<FewRows>(a, n, s) : l.terms == 1 ? launch_split_of<FewRowsOnce<true>>(a, n, s) : launch_split_of<FewRowsOnce<false>>(a, n, s);
 }
 inline gas_status launch_join(const Layer& l, const FewRoom& f, int64_t n, float inv_t, const Parts* parts, hipStream_t s) {
-    const JoinArgs a = {{f.parts, f.ld, f.step, f.splits, l.bias}, l.shape, l.most, inv_t, f.z, parts ? *parts : Parts{}};
+    const JoinArgs a = {{f.parts, f.ld, f.step, f.splits, l.bias}, l.shape, l.stats, inv_t, f.z, parts ? *parts : Parts{}};
     hipLaunchKernelGGL(classes_join_kernel, dim3((unsigned)(f.ld / kTileC), (unsigned)((n + 3) / 4)), dim3(256), 0, s, a);
     GAS_CHECK_HIP(hipGetLastError());
     return GAS_OK;

@@ -266,14 +266,14 @@ __global__ __launch_bounds__(256) void classes_pick_kernel(PickArgs a) {
 
 // ---- lse of every row: its tiles' statistics joined, by 256 / ROWS threads a row, in a fixed tree
 template <int ROWS>
-__global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t most_rows, int64_t n, int tiles, float* lse) {
+__global__ __launch_bounds__(256) void classes_lse_kernel(Parts parts, int64_t stats, int64_t n, int tiles, float* lse) {
     constexpr int PARTS = 256 / ROWS;
     __shared__ float red[2][PARTS][ROWS];
     const int row = threadIdx.x % ROWS, part = threadIdx.x / ROWS;
     const int64_t r = (int64_t)blockIdx.x * ROWS + row;
     float most = kLeastExponent, sum = 0.f, none = 0.f;
     if (r < n)
-        for (int t = part; t < tiles; t += PARTS) join(most, sum, none, parts.most[t * most_rows + r], parts.sum[t * most_rows + r], 0.f, 1.f);
+        for (int t = part; t < tiles; t += PARTS) join(most, sum, none, parts.most[t * stats + r], parts.sum[t * stats + r], 0.f, 1.f);
     for (int half = PARTS / 2; half > 0; half /= 2) {
         red[0][part][row] = most;
         red[1][part][row] = sum;
@@ -315,12 +315,12 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
                     int k) {
     TopRoom t = {};
     if (n > kRowsByVector) t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
-    else t.common.layer.most = kRowsByVector;
-    const int64_t most = t.common.layer.most, tiles = (C + kTileC - 1) / kTileC;
+    else t.common.layer.most = t.common.layer.stats = kRowsByVector;
+    const int64_t most = t.common.layer.most, stats = t.common.layer.stats, tiles = (C + kTileC - 1) / kTileC;
     t.whole = top_whole(n, F, C, dt);
     t.width = top_width(n, C, t.whole);
-    t.parts.most = room.take<float>(tiles * most);
-    t.parts.sum = room.take<float>(tiles * most);
+    t.parts.most = room.take<float>(tiles * stats);
+    t.parts.sum = room.take<float>(tiles * stats);
     t.floor = room.take<float>(most);
     const int64_t lists = t.whole ? parts_of(C, n) : 1;
     t.best = room.take<uint64_t>(n * lists * k);
@@ -373,11 +373,12 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     hipStream_t s = (hipStream_t)stream;
     Room room{static_cast<char*>(workspace)};
     const TopRoom t = lay_out_top(room, X, ldx, n_rows, F, W, ldw, n_classes, bias, dt, k);
+    GAS_TRY(check_room(who, room, workspace_bytes));
     const int64_t cp = round_up(n_classes, 256);
     const int tiles = (int)(cp / kTileC);
     PickArgs pick = {t.z, nullptr, t.width, n_classes, n_classes, 1, k, t.best, nullptr, nullptr, nullptr, ld_ids, ld_values};
     if (n_rows <= kRowsByVector) {
-        VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.most, nullptr, nullptr, (int32_t)n_rows, F, n_classes, 0.f, t.z, {}};
+        VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.stats, nullptr, nullptr, (int32_t)n_rows, F, n_classes, 0.f, t.z, {}};
         if (lse) v.parts = t.parts;
         st = dt == GAS_BF16 ? launch_vector<true>(v, s) : launch_vector<false>(v, s);
         if (st != GAS_OK) return st;
@@ -454,9 +455,9 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
         }
     }
     if (lse) {
-        const int64_t most = t.common.layer.most;
-        if (n_rows <= 1024) hipLaunchKernelGGL(classes_lse_kernel<1>, dim3((unsigned)n_rows), dim3(256), 0, s, t.parts, most, n_rows, tiles, lse);
-        else hipLaunchKernelGGL(classes_lse_kernel<16>, dim3((unsigned)((n_rows + 15) / 16)), dim3(256), 0, s, t.parts, most, n_rows, tiles, lse);
+        const int64_t stats = t.common.layer.stats;
+        if (n_rows <= 1024) hipLaunchKernelGGL(classes_lse_kernel<1>, dim3((unsigned)n_rows), dim3(256), 0, s, t.parts, stats, n_rows, tiles, lse);
+        else hipLaunchKernelGGL(classes_lse_kernel<16>, dim3((unsigned)((n_rows + 15) / 16)), dim3(256), 0, s, t.parts, stats, n_rows, tiles, lse);
         GAS_CHECK_HIP(hipGetLastError());
     }
     return GAS_OK;

@@ -9,7 +9,7 @@ constexpr int kRowsByVector = 8;
 
 struct VectorArgs {
     const void *X, *W, *bias;
-    int64_t ldx, ldw, ldz, most;
+    int64_t ldx, ldw, ldz, stats;
     const int32_t* idx;           // the rows that count, shape->count of them; NULL: all n
     const Shape* shape;
     int32_t n, F, C;
@@ -130,9 +130,9 @@ __global__ __launch_bounds__(512) void classes_vector_kernel(VectorArgs a) {
             }
             __syncthreads();
             if (t == 0 && r < n && r < R) {
-                a.parts.most[blockIdx.x * a.most + r] = most;
-                a.parts.sum[blockIdx.x * a.most + r] = stats[1][h][0] + stats[1][h][1] + stats[1][h][2] + stats[1][h][3];
-                if (a.inv_t != 0.f) a.parts.sum_t[blockIdx.x * a.most + r] = stats[2][h][0] + stats[2][h][1] + stats[2][h][2] + stats[2][h][3];
+                a.parts.most[blockIdx.x * a.stats + r] = most;
+                a.parts.sum[blockIdx.x * a.stats + r] = stats[1][h][0] + stats[1][h][1] + stats[1][h][2] + stats[1][h][3];
+                if (a.inv_t != 0.f) a.parts.sum_t[blockIdx.x * a.stats + r] = stats[2][h][0] + stats[2][h][1] + stats[2][h][2] + stats[2][h][3];
             }
         }
     }
