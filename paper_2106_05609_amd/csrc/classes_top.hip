@@ -326,7 +326,7 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
-    if (t.whole) t.few = lay_out_few(room, n, F, C, dt, false);
+    if (t.whole && n > kRowsByVector) t.few = lay_out_few(room, n, F, C, dt, false);
     t.few.z = t.z;
     t.mask = room.take<uint32_t>(n * (t.width / 32));
     return t;
