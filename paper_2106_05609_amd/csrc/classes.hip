@@ -339,7 +339,7 @@ __global__ __launch_bounds__(1024) void classes_sum_kernel(const float* x, int64
 struct GradArgs {
     Layer layer;
     const uint16_t* g;
-    int64_t g_plane, cap;
+    int64_t g_plane;
     int32_t piece;
     float scale;
     float *part_x, *part_w;       // [split][rows][fp], [split][F][width]; NULL: that gradient is not asked for
@@ -1018,9 +1018,8 @@ gas_status backward(const Call& c, bool distill, const Grads& g) {
     a.g = b.g;
     a.g_plane = b.cap;
     a.gbias = b.gbias;
-    a.cap = b.cap;
-    GradArgs d = {l, b.g, b.cap, b.cap, 0, g.scale, b.gx, b.gw, 0, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
-        // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
+    GradArgs d = {l, b.g, b.cap, 0, g.scale, b.gx, b.gw, 0, g.gw, g.ldgw, g.dt_gw == GAS_BF16};
+    // pieces if every row counts; with fewer of them the pieces are wider and fewer, and launches beyond the last one end at once
     const int tile = rows_of_tile(c.n, c.C);
     const int least = piece_width(b.cap, round_up(c.n, rows.row_step), l.C);
     const int pieces = (c.C + least - 1) / least;

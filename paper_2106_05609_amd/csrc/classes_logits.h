@@ -22,7 +22,6 @@ struct LogitsArgs {
     uint16_t* g;                  // [planes][rows][width of a piece]
     int64_t g_plane;
     float* gbias;                 // [row tiles][C up to 256], or NULL
-    int64_t cap;                  // elements of a plane of g
     int32_t piece;
     // top
     const float* floor;           // [rows]: the value that a logit has to exceed
