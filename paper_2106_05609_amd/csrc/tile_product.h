@@ -1,7 +1,7 @@
 // Products of bf16 matrices by tiles, for the output layer over many classes (classes.hip): the main loop shared by its logits,
 // its input gradient and its weight gradient.
 //
-// A workgroup of WA x WB wavefronts owns BA rows of the first operand by BB rows of the second, sum over k, k in steps of 64.  An
+// A workgroup of WA x WB wavefronts owns BA rows of the first operand by BB rows of the second, sum over k, k in steps of 64 or 32.  An
 // operand lies in memory with k contiguous (element (r, k) at p[r ld + k]) or with r contiguous (TURNED: at p[k ld + r]); a turned one is
 // put right on its way out of LDS (ds_read_b64_tr_b16: sixteen lanes read four k of sixteen rows, and a lane receives four k of
 // one row), so nothing is transposed in memory: the logits read W [F, C] turned and X as it lies, the input gradient W and G as they lie, the
@@ -12,7 +12,8 @@
 // neighbouring rows, and the 32 bytes of each of four k, then fall on banks of their own.
 //
 // fp32 operands come as three bf16 planes (split.h says how and what is dropped): `terms` = 6 products of planes follow one
-// another over the same accumulators, the smallest first, so that only the last one's sums round at the result's size.
+// another over the same accumulators, the smallest first, so that only the last one's sums round at the result's size.  ReadOnceProduct, which takes all
+// six at every step, has accumulators of their own for the small ones.
 #pragma once
 #include "split.h"
 
@@ -20,7 +21,6 @@ namespace gas {
 namespace {
 
 constexpr int kStepK = 64;                        // k are a multiple of it, padded or split
-
 
 struct TileOperand {
     const uint16_t* p;        // the tile's first row and first k
@@ -347,7 +347,11 @@ struct ReadOnceProduct {
                                         f32x16 (&acc)[TA][TB]) {
         static_assert(WB == 1, "a wavefront's blocks are the tile's");
         blocks = (rows + 31) / 32;
+        // The small products have accumulators of their own, as in linear.hip: with one for all six, each step rounded six times at the sum's size (sums of
+        // 2,048 terms were 5.9e-7 off, 2-norm, now 2.3e-7; 32 x 2,048 x 131,072 takes as long, 2 workgroups to a unit either way).
+        f32x16 small[TA][TB];
         Same::clear(acc);
+        if constexpr (!BF) Same::clear(small);
         if (first < last) fetch(a, b, STEP * first);
 #pragma unroll 1
         for (int s = first; s < last; ++s) {
@@ -371,11 +375,19 @@ struct ReadOnceProduct {
                 for (int j = 0; j < TB; ++j)
                     if (j == 0 || j < blocks)
 #pragma unroll
-                for (int t = BF ? 5 : 0; t < 6; ++t)
+                        for (int t = BF ? 5 : 0; t < 6; ++t)
 #pragma unroll
-                    for (int i = 0; i < TA; ++i)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[PA[t]][i], fb[PB[t]][j], acc[i][j], 0, 0, 0);
+                            for (int i = 0; i < TA; ++i) {
+                                f32x16& sum = t < 5 ? small[i][j] : acc[i][j];
+                                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[PA[t]][i], fb[PB[t]][j], sum, 0, 0, 0);
+                            }
             }
+        }
+        if constexpr (!BF) {
+#pragma unroll
+            for (int i = 0; i < TA; ++i)
+#pragma unroll
+                for (int j = 0; j < TB; ++j) acc[i][j] += small[i][j];
         }
         __syncthreads();
     }

@@ -30,3 +30,50 @@ def test_equal_logits_of_classes_far_apart(n, f, half, dtype, bias):
     whole = values > values[:, -1:]
     pair = (ids % half)[:, :, None] == (ids % half)[:, None, :]
     assert (pair.sum(2)[whole] == 2).all() and not (pair & (values[:, :, None] != values[:, None, :])).any()
+
+
+def most_off(k, own=1.0):
+    """Of a sum of k fp32 products, relative and as a root mean square over many sums: the last rounding and `own` units beside; k / 16 roundings to half a step at most, evenly
+    spread (a third of its square), of a sum that grows to its size as its terms' squares do (half of that), of which half as much again is allowed."""
+    return R.U32 * (own + 1.5 * math.sqrt(k / 16 / 6))
+
+
+def two_parts(a):
+    """What is left of fp32 values without the third of their bf16 parts."""
+    high = a.float().bfloat16().float()
+    return (high + (a.float() - high).bfloat16().float()).double()
+
+
+# the vector units; W read as it lies, in whole sums and in split ones; small tiles, whole and split; many tiles
+PATHS = [(5, 250, 2900), (40, 200, 2900), (40, 250, 2900), (200, 200, 2900), (200, 300, 2900), (300, 200, 40_000)]
+
+
+@pytest.mark.parametrize("n, f, c", PATHS + [(5, 2048, 66_000), (40, 2048, 66_000), (100, 2048, 66_000), (40, 2048, 9000)])
+def test_digits_of_fp32_logits(n, f, c):
+    s, _ = make(n, f, c, "f32", bias=False)
+    got = top(s, 64)
+    x, w = s["x"].double(), s["w"].double()
+    z = x @ w
+    want = z.gather(1, got["ids"].long())
+    assert close(got["values"], want) <= most_off(f)
+    assert close(got["lse"], torch.logsumexp(z, 1)) <= most_off(f, 3.0)
+    if f <= 300:                                          # or the bound would let it pass
+        lost = (two_parts(x) @ two_parts(w)).gather(1, got["ids"].long())
+        assert close(lost, want) > 2 * most_off(f)
+
+
+@pytest.mark.parametrize("n, f, c", PATHS)
+def test_digits_of_fp32_gradients(n, f, c):
+    """The gradient at the logits is off by the logits' error, the exponent's and the exponential's rounding: eight units at most, most of them of small probabilities."""
+    s, _ = make(n, f, c, "f32", bias=False, labelled=1.0)
+    got = forward(s)
+    grads = backward(s, got["lse"], "f32", scale=1.0)
+    x, w = s["x"].double(), s["w"].double()
+    g = torch.exp(x @ w - got["lse"].double()[:, None])
+    g.scatter_add_(1, s["labels"].long()[:, None], torch.full((n, 1), -1.0, dtype=torch.float64, device="cuda"))
+    for name, a, b, k in (("gx", g, w.t(), c), ("gw", x.t(), g, n)):
+        want = a @ b
+        assert close(grads[name], want) <= most_off(k, 8.0), name
+        if k < 10_000:
+            assert close(two_parts(a) @ two_parts(b), want) > most_off(k, 8.0), name
+    assert close(grads["gbias"], g.sum(0)) <= most_off(n, 8.0)
