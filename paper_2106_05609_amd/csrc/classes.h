@@ -25,6 +25,7 @@ inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; 
 struct Shape {
     int32_t count, width;         // classes of a piece of the gradient at the logits
     int32_t rows;                 // of it that are stored: `count` up to whole tiles
+    int32_t part_rows;            // of a part of GX
     int32_t splits_x, splits_w;   // parts of the sums of GX and GW
 };
 

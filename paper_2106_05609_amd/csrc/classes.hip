@@ -69,11 +69,14 @@ __device__ __host__ inline int splits_once(int tiles, int steps) {
     if (s > steps / 2) s = steps / 2;
     return s < 1 ? 1 : s;
 }
+// Rows of a part of GX: gx_tile stores 32 at a time, gx_once_tile those that are there.
+__device__ __host__ inline int64_t part_rows_of(int64_t rows, bool once) { return once ? rows : (rows + 31) / 32 * 32; }
 __device__ __forceinline__ Shape shape_for(const RowsArgs& a, int count) {
-    Shape s = {count, 0, 0, 1, 1};
+    Shape s = {count, 0, 0, 0, 1, 1};
     if (a.cap > 0) {
         const int rows = count > 0 ? (count + 255) / 256 * 256 : 256;
         s.rows = (count + a.row_step - 1) / a.row_step * a.row_step;
+        s.part_rows = part_rows_of(s.rows, a.once);
         s.width = piece_width(a.cap, s.rows > 0 ? s.rows : a.row_step, a.t.C);
         // they run beside each other: half of the units for each where both could have a round of their own together
         const int64_t tiles_x = (int64_t)rows / 256 * a.nfx, tiles_w = (int64_t)s.width / 256 * a.nfw;
@@ -384,12 +387,11 @@ __device__ __forceinline__ void gx_tile(const GradArgs& a, uint32_t block, uint3
     const TileOperand ob = {a.g + (int64_t)m0 * s.width, s.width, a.g_plane, BB < s.rows - m0 ? BB - 1 : s.rows - m0 - 1, s.width};
     const int end = (s.cols + P::kStepOf - 1) / P::kStepOf, from = first * (kStepK / P::kStepOf), to = last * (kStepK / P::kStepOf);
     product.run(oa, ob, from < end ? from : end, to < end ? to : end, l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
-    float* out = a.part_x + (int64_t)part * s.rows * l.fp;
+    float* out = a.part_x + (int64_t)part * shape.part_rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
-        const int m = m0 + wb0 + 32 * j + li;
-        if (m >= s.rows) continue;
-        float* row = out + (int64_t)m * l.fp;
+        if (m0 + wb0 + 32 * j >= s.rows) continue;
+        float* row = out + (int64_t)(m0 + wb0 + 32 * j + li) * l.fp;
 #pragma unroll
         for (int i = 0; i < P::TA; ++i)
 #pragma unroll
@@ -424,7 +426,7 @@ __device__ __forceinline__ void gx_once_tile(const GradArgs& a, uint32_t block, 
     const typename P::Operand oa = {static_cast<const char*>(l.raw) + ((int64_t)f0 * l.ld_raw + s.first) * eb, l.ld_raw, l.F - f0, l.C - s.first};
     const TileOperand ob = {a.g, s.width, a.g_plane, s.rows - 1, s.width};
     product.run(oa, ob, shape.count, first, last, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
-    float* out = a.part_x + (int64_t)part * s.rows * l.fp;
+    float* out = a.part_x + (int64_t)part * shape.part_rows * l.fp;
 #pragma unroll
     for (int j = 0; j < P::TB; ++j) {
         const int m = wb0 + 32 * j + li;
@@ -708,10 +710,9 @@ __global__ __launch_bounds__(256) void classes_sums_kernel(SumArgs a) {
     }
     block -= a.w_blocks;
     if (block < a.x_blocks) {
-        const Piece s(shape, 0, l.C);
         const int n4 = (l.F + 3) / 4;
         const bool whole = fours(a.gx, a.ldgx, a.gx_bf16);
-        const int64_t total = a.n * n4, step = (int64_t)s.rows * l.fp / 4;
+        const int64_t total = a.n * n4, step = (int64_t)shape.part_rows * l.fp / 4;
         const int part = (int)threadIdx.x & (a.lanes - 1);
         for (int64_t q = ((int64_t)block * 256 + threadIdx.x) / a.lanes; q < total; q += (int64_t)a.x_blocks * 256 / a.lanes) {
             int64_t i;
@@ -928,8 +929,8 @@ inline BackwardRoom lay_out_backward(Room& room, const Common& common, int64_t n
     const int fx = width_of_tile(l.fp);
     auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
     const int64_t tiles = (l.fp + fx - 1) / fx, steps = cp / kStepK, splits = least(2 * kUnits / tiles, least(kMostSplits, steps / 2));
-    int64_t parts_x = least(2 * kUnits / tiles * 256, splits * rows);
-    if (parts_x < rows) parts_x = rows;
+    int64_t parts_x = least(2 * kUnits / tiles * 256, splits * part_rows_of(rows, false));
+    if (parts_x < part_rows_of(rows, false)) parts_x = part_rows_of(rows, false);
     if (n <= kReadOnceRows) {
         const int64_t parts_once = splits_once((l.fp + 255) / 256, (int)steps) * rows;
         if (parts_x < parts_once) parts_x = parts_once;
