@@ -17,13 +17,13 @@ def up(v, to):
 @pytest.mark.parametrize("dtype", list(DT))
 def test_gradients_of_few_rows_or_classes(n, f, c, dtype):
     """X's planes for 256 rows at a time, W's for more than 64; the bias; G's planes and logits, up to 64 rows more; targets and statistics; parts of the sums: up to
-    32 times GX and GW in fp32, of up to 64 rows' GX two for every unit or one for 128 classes, of up to eight rows' GW none."""
+    32 times GX, 32 rows at a time, and GW in fp32; of up to 64 rows' GX two for every unit or one for 128 classes; of up to eight rows' GW none."""
     planes, cp, fp = (3 if dtype == "f32" else 1), up(c, 256), up(f, 64)
     rows = n if n <= 8 else up(n, 64)
     need = 2 * planes * (up(n, 256) * fp + rows * cp + (f * up(c, 64) if n > 64 else 0)) + 4 * cp * (1 + up(n, 64) // 64) + 4 * rows * cp + 48 * up(n, 256)
     need += 16 * up(n, 16) * (cp // 256)
     need += 34 * MB if f >= 256 and n > 8 or f >= 1024 else 0
-    gx = 4 * rows * fp * max(min(32, cp // 128), min(512, cp // 128) if n <= 64 else 0)
+    gx = 4 * fp * max(up(rows, 32) * min(32, cp // 128), rows * min(512, cp // 128) if n <= 64 else 0)
     gw = 4 * f * cp * min(32, up(n, 256) // 128) if n > 8 else 0
     got = gas.gas_linear_xent_bwd_workspace(n, f, c, DT[dtype])
     assert got <= need + gx + gw + 8192
