@@ -100,11 +100,25 @@ __global__ __launch_bounds__(256) void classes_join_kernel(JoinArgs a) {
     if (a.inv_t != 0.f) a.parts.sum_t[to] = sum_t;
 }
 
+// Whether up to eight rows are better off in split sums than with the vector units, whose time grows with the rows and F until there are classes enough
+// to hide it; forward / backward in us, the vector units first:
+//     fp32   1 x 1,024 x 4,000     19 / 44      22 / 39        bf16   1 x 512 x 1,001       19 / 38      24 / 40
+//            1 x 2,560 x 4,000     39 / 70      29 / 52               1 x 512 x 1,000       19 / 35      17 / 29
+//            1 x 2,560 x 24,000    48 / 174     52 / 166              1 x 2,048 x 4,001     81 / 120     26 / 51
+//            4 x 512 x 4,000       19 / 43      22 / 41               4 x 512 x 4,001       24 / 45      25 / 42
+//            4 x 1,024 x 4,000     27 / 56      23 / 42               8 x 512 x 64,000      43 / 114     27 / 93
+//            8 x 512 x 4,000       24 / 49      23 / 44               8 x 2,048 x 50,000   127 / 243     48 / 158
+//            8 x 2,560 x 40,000   104 / 292     96 / 286              8 x 4,096 x 16,000   226 / 292     35 / 99
+//            8 x 2,560 x 64,000   139 / 435    133 / 432
+// bf16 whose rows are no whole pieces is read once as fp32 is, and so as long in coming.
+inline bool few_by_split(int64_t n, int F, int C, gas_dtype dt) {
+    const int64_t work = (int64_t)F * (n + 5);
+    return dt == GAS_F32 ? work >= 6656 && C <= 4096 * (n + 3) : C % 8 == 0 || work >= 4608;
+}
 // Parts of the sums for which a tile's are worth it: two workgroups for every unit, of a few steps each. A step of fp32 takes as long as several.
 inline int splits_of_few(int64_t n, int F, int C, gas_dtype dt) {
     if (rows_of_tile(n, C) != 64) return 1;
-    // the vector units are as fast for rows of W that are not so long, and there are enough classes: 3 x 2,048 x 600 of fp32 took them 34 us
-    if (n <= kRowsByVector && (F < 1024 || C > 32 * kTileC)) return 1;
+    if (n <= kRowsByVector && !few_by_split(n, F, C, dt)) return 1;
     const int64_t tiles = (n + 63) / 64 * (round_up(C, kTileC) / kTileC), steps = round_up(F, FewRows::kStepOf) / FewRows::kStepOf / (dt == GAS_F32 ? 4 : 8);
     int64_t s = 512 / tiles;
     if (s > steps) s = steps;

@@ -2,7 +2,7 @@
 // (gas_linear_top).
 //
 // Few rows (64), and more of so few tiles that their sums are split: all logits of them are stored, 4 bytes beside the 2 F or 4 F of W's column, and
-// searched. Up to eight rows have a kernel of their own that reads W as it lies and multiplies by the vector units, bound by reading it.
+// searched. Up to eight rows that are not better off so have a kernel of their own that reads W as it lies and multiplies by the vector units.
 //
 // Many rows: the classes are taken in pieces. Of the first, 4,096 classes, all logits are stored; of a later one only those above the row's k-th largest
 // of the pieces before (a later class never replaces an equal earlier one), with a bit for each, and a row's list is joined with them. A piece seven
@@ -308,13 +308,14 @@ struct TopRoom {
     uint32_t* mask;
     uint64_t *best, *other;
     int64_t width;
-    bool whole;
+    bool whole, by_vector;
     FewRoom few;                  // parts of the sums
 };
 TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, const void* W, int64_t ldw, int C, const void* bias, gas_dtype dt,
                     int k) {
     TopRoom t = {};
-    if (n > kRowsByVector) t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
+    t.by_vector = n <= kRowsByVector && splits_of_few(n, F, C, dt) == 1;
+    if (!t.by_vector) t.common = lay_out(room, X, ldx, n, F, W, ldw, C, bias, dt, false);
     else t.common.layer.most = t.common.layer.stats = kRowsByVector;
     const int64_t most = t.common.layer.most, stats = t.common.layer.stats, tiles = (C + kTileC - 1) / kTileC;
     t.whole = top_whole(n, F, C, dt);
@@ -326,7 +327,7 @@ TopRoom lay_out_top(Room& room, const void* X, int64_t ldx, int64_t n, int F, co
     t.best = room.take<uint64_t>(n * lists * k);
     t.other = room.take<uint64_t>(n * lists * k);
     t.z = room.take<float>(n * t.width);
-    if (t.whole && n > kRowsByVector) t.few = lay_out_few(room, n, F, C, dt, false);
+    if (t.whole && !t.by_vector) t.few = lay_out_few(room, n, F, C, dt, false);
     t.few.z = t.z;
     t.mask = room.take<uint32_t>(n * (t.width / 32));
     return t;
@@ -377,7 +378,7 @@ gas_status gas_linear_top(const void* X, int64_t ldx, int64_t n_rows, int32_t F,
     const int64_t cp = round_up(n_classes, 256);
     const int tiles = (int)(cp / kTileC);
     PickArgs pick = {t.z, nullptr, t.width, n_classes, n_classes, 1, k, t.best, nullptr, nullptr, nullptr, ld_ids, ld_values};
-    if (n_rows <= kRowsByVector) {
+    if (t.by_vector) {
         VectorArgs v = {X, W, bias, ldx, ldw, t.width, t.common.layer.stats, nullptr, nullptr, (int32_t)n_rows, F, n_classes, 0.f, t.z, {}};
         if (lse) v.parts = t.parts;
         st = dt == GAS_BF16 ? launch_vector<true>(v, s) : launch_vector<false>(v, s);

@@ -6,7 +6,7 @@ import torch
 
 import paper_2106_05609_amd as gas
 from tests import classes_reference as R
-from tests.test_gpu_classes import DT, backward, close, forward, make, top
+from tests.test_gpu_classes import DT, backward, check, close, exact_layer, forward, make, top
 
 pytestmark = pytest.mark.gpu
 
@@ -44,8 +44,8 @@ def two_parts(a):
     return (high + (a.float() - high).bfloat16().float()).double()
 
 
-# the vector units; W read as it lies, in whole sums and in split ones; small tiles, whole and split; many tiles
-PATHS = [(5, 250, 2900), (40, 200, 2900), (40, 250, 2900), (200, 200, 2900), (200, 300, 2900), (300, 200, 40_000)]
+# the vector units; few rows in split sums; W read as it lies, in whole sums and in split ones; small tiles, whole and split; many tiles
+PATHS = [(5, 250, 2900), (6, 1100, 2900), (40, 200, 2900), (40, 250, 2900), (200, 200, 2900), (200, 300, 2900), (300, 200, 40_000)]
 
 
 @pytest.mark.parametrize("n, f, c", PATHS + [(5, 2048, 66_000), (40, 2048, 66_000), (100, 2048, 66_000), (40, 2048, 9000)])
@@ -77,3 +77,15 @@ def test_digits_of_fp32_gradients(n, f, c):
         if k < 10_000:
             assert close(two_parts(a) @ two_parts(b), want) > most_off(k, 8.0), name
     assert close(grads["gbias"], g.sum(0)) <= most_off(n, 8.0)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("n, f, c", [(1, 2048, 4001), (1, 1500, 16_000), (3, 1100, 20_001), (8, 512, 40_000), (8, 600, 40_003), (5, 1600, 300)])
+def test_top_logits_of_few_rows_in_split_sums(n, f, c, dtype):
+    s = exact_layer(n, f, c, dtype)
+    got = top(s, 33)
+    z = s["x"].double() @ s["w"].double() + s["bias"].double()
+    ids, values = R.top(z, 33)
+    assert torch.equal(got["ids"].long(), ids) and torch.equal(got["values"].double(), values)
+    lse, off = R.log_sum_exp(z, torch.zeros_like(z))
+    check(got["lse"], (lse.cpu(), off.cpu()), "lse")
