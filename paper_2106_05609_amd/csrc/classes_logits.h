@@ -514,8 +514,12 @@ using FewRows = TileProduct<kTileC, 64, 4, 1, true, false>;
 template <bool BF> using FewRowsOnce = ReadOnceProduct<kTileC, 64, 4, 1, true, BF>;
 constexpr int kRowsTile = 256;
 using ManyRows = TileProduct<kTileC, kRowsTile, 2, 4, true, false, 64, 2>;
-// Rows of a tile: 64 where there are no more rows, or where tiles of 256 would leave compute units without any.
-inline int rows_of_tile(int64_t n, int C) { return n <= 64 || round_up(n, kRowsTile) / kRowsTile * (round_up(C, kTileC) / kTileC) < 256 ? 64 : kRowsTile; }
+// Rows of a tile: 64 where there are no more rows, or where tiles of 64 are all under way at once, two on a unit; tiles of 256 take less where there would be
+// a second round. Forward in us, 64 rows and 256:
+//     512 tiles of 64     512 x 1,024 x 16,384 fp32    158   184        512 x 256 x 16,384 bf16    19   22
+//     516                 256 x 1,024 x 33,000         286   235        256 x 256 x 33,000         24   22
+//     752                 512 x 256 x 24,000            80    66        512 x 1,024 x 24,000       49   41
+inline int rows_of_tile(int64_t n, int C) { return n <= 64 || (n + 63) / 64 * (round_up(C, kTileC) / kTileC) <= 512 ? 64 : kRowsTile; }
 template <int KIND, int TEMPS, bool SPLIT = false>
 gas_status launch_logits(const LogitsArgs& a, int tile_rows, int64_t tiles, hipStream_t s) {
     if (!a.layer.w) {
