@@ -16,6 +16,9 @@ constexpr int kMaxClasses = 1 << 22;              // a tile's 256 rows of W then
 constexpr int kMaxWidth = 1 << 16;
 constexpr int64_t kMaxRows = 1 << 25;             // a launch of 64 threads a row
 constexpr int kReadOnceRows = 64;                 // up to so many rows W is not packed
+constexpr int kCopiedClasses = 1 << 15;           // but for bf16 of no more classes
+constexpr int64_t kCopiedElements = 1 << 22;      // and elements
+constexpr int kRowsByVector = 8;                  // up to so many rows may be multiplied by the vector units
 constexpr int kMaxEntries = 256;                  // of a teacher's row
 constexpr int kHeldEntries = 2;                   // of a row in one tile that are fetched before the products
 
@@ -265,9 +268,15 @@ inline Common lay_out(Room& room, const void* X, int64_t ldx, int64_t n, int F, 
     const int64_t most = round_up(n, 256), fp = round_up(F, 64), cp = round_up(C, kTileC);
     // W where it lies if its rows can be read in whole pieces
     const bool in_place = dt == GAS_BF16 && C % 8 == 0 && ldw % 8 == 0 && ldw <= kMaxClasses && aligned16(W);
-    // and also, by kernels of their own, where it is used for few rows: gradients of
-    // 5 x 64 x 125,838 of fp32 took 121 us, W packed first 382
-    const bool once = !in_place && n <= kReadOnceRows;
+    // and also, by kernels of their own with one tile of rows, where it is used for no more rows than that tile has; of bf16 a copy of a few MB costs less than
+    // reading W through registers. Forward / backward in us, read once and packed:
+    //     fp32   9 x 512 x 100,001     75 / 306     237 / 716      bf16   9 x 512 x 100,001     51 / 161     82 / 195
+    //            64 x 2,048 x 20,001   76 / 248     195 / 387             64 x 512 x 20,001     37 / 81      41 / 69
+    //            64 x 512 x 2,001      30 / 72       34 / 66              64 x 2,048 x 2,001    30 / 79      31 / 56
+    //            9 x 128 x 2,001       23 / 46       25 / 43              9 x 512 x 2,001       26 / 55      20 / 43
+    //                                                                     9 x 64 x 64,001       16 / 37      21 / 51
+    const bool small_copy = dt == GAS_BF16 && n > kRowsByVector && C <= kCopiedClasses && (int64_t)F * C <= kCopiedElements;
+    const bool once = !in_place && n <= kReadOnceRows && !small_copy;
     const int64_t cw = in_place ? C : round_up(C, 64);
     c.layer.terms = dt == GAS_F32 ? 6 : 1;
     Shape* shape = room.take<Shape>(1);

@@ -5,8 +5,6 @@
 namespace gas {
 namespace {
 
-constexpr int kRowsByVector = 8;
-
 struct VectorArgs {
     const void *X, *W, *bias;
     int64_t ldx, ldw, ldz, stats;
