@@ -479,7 +479,8 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * as in gas_linear), statistics of a row and sums over rows are fp32.  F up to 65536, n_classes up to 4194304, n_rows up to 2^25 (gas_linear_top 2^23); the calls are meant for
  * classes by the thousand (for a few dozen gas_linear and gas_softmax_xent take less).  A bias of -infinity takes a class out: its
  * probability is 0.  An infinity or NaN of X stays in its row, one of W makes its class's logits
- * infinite or NaN, and what sums over them NaN or, where they are -infinity, without that class.
+ * infinite or NaN, and what sums over them NaN or, where they are -infinity, without that class.  Of logits beyond 2.3e38 the sums are NaN, those below
+ * -2.3e38 are as -infinity in them.
  *
  * gas_linear_xent: cross-entropy of the rows with a label, 0 <= labels[i] < n_classes:
  *     lse[i] = log sum_c exp z_ic,   loss_rows[i] = lse[i] - z_{i, labels[i]};   rows without one: 0 and 0, at no cost.
@@ -490,7 +491,8 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  *     G[i, c] = r_i (exp(z_ic - lse_i) - [c == labels[i]]),   GX = scale G W^T,   GW = scale X^T G,   gbias = scale sum_i G[i]
  * GX [n_rows, F] of type dt; GW [F, n_classes] of dt_gw, fp32 or W's type; gbias fp32[n_classes]; each may be NULL, not all of them.  Rows
  * without a label get zeros in GX.  The logits are formed again, a piece of the classes at a time, and G of the piece is rounded to
- * bf16 for its products where dt is GAS_BF16 (before scale; gbias sums it unrounded).  n_rows = 0 writes zeros to GW and gbias.
+ * bf16 for its products where dt is GAS_BF16 (before scale; gbias sums it unrounded), whatever GW's type: GW of a distillation is 1.6e-3 off by that
+ * (2-norm), as much as by one rounding to bf16, of labels alone 6e-5.  n_rows = 0 writes zeros to GW and gbias.
  *
  * gas_linear_distill: a student's loss against a teacher's k top logits, with labels beside it (labels not NULL) or without.  ids int32
  * [n_rows, k], values fp32 [n_rows, k]: classes and logits in any order, as gas_linear_top writes them; an entry whose id is
@@ -502,19 +504,18 @@ GAS_API gas_status gas_sgd_steps(int32_t count, void* const* W, const int64_t* n
  * lse: fp32[n_rows, 2], log sum exp z and log sum exp (z / T).  gas_linear_distill_bwd: the gradient as above, with
  *     G[i, c] = r_i (a (p_c - [c == labels[i]]) + b T (p^T_c - q_c)).
  *
- * gas_linear_top: the k largest logits of every row, the largest first, of equal ones (fp32, as they are summed; a class's sums are formed as every other's) those of lower classes first: ids int32
- * [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
+ * gas_linear_top: the k largest logits of every row, the largest first, of equal ones those of lower classes first (a
+ * class's logit does not depend on where it is: the sums of all are formed alike): ids int32 [n_rows, k], values fp32 [n_rows, k]; lse optional, fp32[n_rows].  k up to 128 and n_classes.  A NaN counts as less than any number.
  *
  * No two outputs of a call may overlap, nor an output anything that the call reads.  workspace: 16-byte aligned device memory of
- * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds X, its rows up to a multiple of
- * 256, and, for more than
- * 64 rows, W as the products take them (not W where it is bf16 with 16-byte aligned rows of whole 16-byte pieces: that is read as it lies, as
- * for up to 64 rows every W is); statistics of every 256 classes; the logits of up to eight rows,
- * and up to 34 MB of parts of their sums where there are few tiles of long ones; backward a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it
- * (its rows up to a multiple of 256, where there are few tiles of 64, up to eight rows as they are),
- * or 256 classes of it if they are more, and parts of the sums of GX and GW, for either as much as GX or GW in fp32 takes times the parts that its sums can be
- * split into, at most 168 MB beyond one GX; gas_linear_top the logits of up to 64 rows, and of more where there are few tiles (16 MB), else
- * those of a piece, 2 GB or 4,096 classes.
+ * gas_linear_*_workspace(...) bytes, caller-owned, contents undefined afterwards (-1: no call takes these sizes).  It holds
+ *   - X as the products take it, its rows up to a multiple of 256, and W for more than 64 rows (of bf16 for more than 8 where it has up to 32,768 classes and
+ *     4 M elements).  W is read as it lies for fewer rows, and always where it is bf16 with 16-byte aligned rows of whole 16-byte pieces;
+ *   - statistics of every 256 classes; the logits of up to eight rows, or up to 34 MB of parts of their sums where there are few tiles of long ones;
+ *   - backward: a piece of G of 2^29 elements (bf16 1 GB, fp32 3.2 GB), or all of it if that is less, or 256 classes of it if they are more, its rows up to a
+ *     multiple of 256, 64 where there are few tiles, 1 for up to eight rows; parts of the sums of GX and GW, each of them GX or GW in fp32
+ *     as many times over as its sums are split, up to 168 MB, or GX once;
+ *   - gas_linear_top: the logits of up to 64 rows, and of more where there are few tiles (16 MB), else those of a piece, 2 GB or 4,096 classes.
  */
 GAS_API int64_t gas_linear_xent_workspace(int64_t n_rows, int32_t F, int32_t n_classes, gas_dtype dt);
 GAS_API gas_status gas_linear_xent(const void* X, int64_t ldx, int64_t n_rows, int32_t F, const void* W, int64_t ldw, int32_t n_classes,
