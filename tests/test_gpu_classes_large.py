@@ -1,5 +1,5 @@
 """Output layers over many classes at sizes with at least 256 tiles of 256 rows by 256 classes, which workgroups take one after another: the loads of the next
-tile begin, and its entries are fetched, while this one's logits are used. Against the definitions in 64 bits (tests/classes_reference.py), formed on the GPU."""
+tile begin, and its entries are fetched, while this one's logits are used; and at few rows of a large W. Against the definitions in 64 bits (tests/classes_reference.py), formed on the GPU."""
 import math
 
 import pytest
@@ -116,3 +116,20 @@ def test_top_of_logits_in_hard_orders(dtype):
     got = top(dict(s, bias=bias), k, lse=False)
     ids, values = R.top(wide(s["w"]) + wide(bias), k)
     assert (got["ids"] == ids).all() and torch.equal(got["values"].double(), values.expand(n, k))
+
+
+@pytest.mark.parametrize("n, f, c", [(40, 600, 33_001), (64, 1100, 8001), (12, 64, 40_003), (33, 2048, 2047), (9, 300, 13_000), (64, 64, 32_769), (6, 600, 33_001)])
+@pytest.mark.parametrize("dtype, gw", [("f32", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+def test_few_rows_and_a_large_w(n, f, c, dtype, gw):
+    """W read once, in whole and in split sums, in place and copied: on both sides of where it is."""
+    s, _ = make(n, f, c, dtype)
+    got = twice(lambda: forward(s))
+    with torch.device("cuda"):
+        x, w, b = wide(s["x"]), wide(s["w"]), wide(s["bias"])
+        want = R.xent(x, w, b, s["labels"])
+        for name in ("loss", "lse"):
+            check(got[name], here(want[name]), name)
+        grads = twice(lambda: backward(s, got["lse"], dtype, gw))
+        g, off = R.grad_at_logits(x, w, b, wide(got["lse"]), s["labels"], None)
+        for name, v in R.gradients(x, w, g, off, 0.37, dtype == "bf16", gw == "bf16").items():
+            check(grads[name], here(v), name)

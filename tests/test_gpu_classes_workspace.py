@@ -7,7 +7,7 @@ from tests.test_gpu_classes import DT, exact_layer, with_teacher
 
 pytestmark = pytest.mark.gpu
 SIZES = [(1, 64, 500), (3, 1100, 700), (8, 256, 29_360), (8, 40, 5001), (9, 1030, 600), (40, 200, 9000), (64, 2048, 264), (65, 33, 511), (100, 2048, 1500),
-         (200, 5000, 520), (300, 1433, 264), (520, 70, 40_000), (30, 8200, 300)]
+         (200, 5000, 520), (300, 1433, 264), (520, 70, 40_000), (30, 8200, 300), (40, 600, 33_001)]
 
 
 def room(need):
