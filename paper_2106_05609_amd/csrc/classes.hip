@@ -491,7 +491,8 @@ __device__ __forceinline__ void gw_tile(const GradArgs& a, uint32_t block, uint3
     const int wa0 = (wave % WA) * (32 * P::TA), wb0 = (wave / WA) * (32 * P::TB);
     f32x16 acc[P::TA][P::TB];
     P product;
-    const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, s.rows};
+    // the steps end within the rows of G that are stored
+    const TileOperand oa = {a.g + c0, s.width, a.g_plane, s.width - 8 - c0, l.most};
     const TileOperand ob = {l.x + f0, l.fp, l.x_plane, l.fp - 8 - f0, l.most};
     product.run(oa, ob, first * (kStepK / P::kStepOf), last * (kStepK / P::kStepOf), l.terms, reinterpret_cast<uint16_t*>(smem), wa0, wb0, acc);
     // A lane has classes of 32 inputs' rows, memory wants a row's next to each other: through 32 rows of 64 classes of LDS that belong to the
